@@ -376,6 +376,106 @@ int oscar_bf16_decode_attn(const void *q, const void *k, const void *v, const in
                            int32_t max_seq_len_hint, int32_t num_splits, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* ---- a decoding step with drafted tokens ---------------------------------------------------
+ * A server that drafts tokens runs the target model on the last token and its drafts at once, T
+ * tokens a sequence: oscar_rope puts positions on their queries and keys, oscar_draft_attn attends
+ * over the cache and over themselves, and when the model has answered, oscar_verify_drafts counts
+ * the drafts that stand; the counts are the new_lens with which oscar_quantize_append takes the
+ * keys and values of those tokens, layer by layer, into the cache.  (A token cannot be taken back
+ * out of a packed block, so nothing is appended before it is accepted.)  oscar_cache_read is the
+ * way back out of the cache. */
+
+/* Rotary positions, with up to four position axes (time, height, width of images and video), on
+ * queries and keys.  Pair i of a vector, i < rotary_dim / 2, turns by the angle
+ *     a = positions[pair_axis[i]][token] * inv_freq[i]
+ *     y1 = x1 cos a - x2 sin a,  y2 = x2 cos a + x1 sin a
+ * where x1, x2 are channels i and i + rotary_dim / 2, or 2i and 2i + 1 with OSCAR_ROPE_ADJACENT.
+ * Channels from rotary_dim on are copied.  The angle is the exact product, reduced in 64 bits, so
+ * far positions lose nothing; the turn is fp32 and rounded once.
+ *   q, k    : device, io_dtype, n_tokens rows of n_q_heads (n_kv_heads) vectors of 128 channels; a
+ *             row's heads are contiguous, rows are q_stride (k_stride) elements apart, so q and k
+ *             may lie side by side in one projection's output.  0 heads: that side is left out.
+ *   q_out, k_out : the same with their own strides; may be q, k with the same stride (in place)
+ *             and must not overlap them otherwise
+ *   positions : device int32 [n_axes][n_tokens], any value
+ *   inv_freq  : device fp32 [rotary_dim / 2]
+ *   pair_axis : HOST uint8 [rotary_dim / 2], the axis of every pair; NULL with one axis
+ *   flags   : OSCAR_ROPE_INVERSE takes the turn back: the inverse, and the gradient's way
+ * Pointers are 16-byte aligned, strides multiples of 16 bytes; rotary_dim is even, 2 .. 128.
+ * One launch. */
+enum { OSCAR_ROPE_ADJACENT = 1u, OSCAR_ROPE_INVERSE = 2u };
+int oscar_rope(const void *q, const void *k, void *q_out, void *k_out, int64_t n_tokens,
+               int32_t n_q_heads, int32_t n_kv_heads, int64_t q_stride, int64_t k_stride,
+               int64_t q_out_stride, int64_t k_out_stride, const int32_t *positions,
+               const float *inv_freq, const uint8_t *pair_axis, int32_t n_axes, int32_t rotary_dim,
+               int32_t io_dtype, uint32_t flags, void *stream);
+
+/* Keys and values of T tokens of every sequence, from its token starts[b] on, as
+ * oscar_quantize_append took them (keys after RoPE: rotated back and multiplied by their norm), up
+ * to the quantization; tokens of the window come from their 16-bit form.
+ *   starts : device int32[batch] or NULL = 0; may be negative
+ *   k, v   : device, [batch][T][n_kv_heads][head_dim] of out_dtype (any of the three), 16-byte
+ *            aligned; either may be NULL
+ * Rows of tokens that a sequence does not hold (before 0, from seq_lens[b] on, or in a page whose
+ * block_table entry is no page) are left as they were.  The cache is not changed.  One launch. */
+int oscar_cache_read(const oscar_cache *cache, const int32_t *starts, int32_t T, void *k, void *v,
+                     int32_t out_dtype, void *stream);
+
+/* Attention of T new tokens of every sequence over its cache and, causally, over each other:
+ *   out[b][t][h] = softmax( logits of all seq_lens[b] cached tokens,
+ *                           scale * <q[b][t][h], k_new[b][j]>, j <= t ) . values
+ * with the cached tokens' logits and values as in oscar_decode_attn.  The new tokens are not in the
+ * cache and the call does not put them there.  T is the last token and its drafts, or a piece of a
+ * prompt.
+ *   q            : device, [batch][T][n_q_heads][head_dim], io_dtype, un-rotated
+ *   k_new, v_new : device, [batch][T][n_kv_heads][head_dim], io_dtype (keys after RoPE)
+ *   new_lens     : device int32[batch] or NULL; sequence b has new_lens[b] (0..T) new tokens, the
+ *                  rows behind them are zeros; NULL = T for all
+ *   out          : device, [batch][T][n_q_heads][head_dim], io_dtype
+ *   softmax_scale, max_seq_len_hint, num_splits (<= 512, 0 = oscar_draft_auto_splits): as in
+ *                  oscar_decode_attn
+ *   workspace    : at least oscar_draft_workspace_bytes(...), 8-byte aligned; NULL where that is 0
+ *                  (one split).  Calls that share one must be ordered.
+ * io_dtype BF16 or F16 (OSCAR_ERR_UNSUPPORTED for F32); every other field of the configuration as
+ * for oscar_decode_attn.  Operands of the matrix products are fp16 (steps, zero terms,
+ * probabilities; values and zero terms beyond its range, infinities and NaNs among the values of
+ * new tokens, count as +-65504), sums are fp32.  The same call gives the same bits every time.
+ * q, k_new, v_new, out: 16-byte aligned.  One launch, two with several splits. */
+int32_t oscar_draft_auto_splits(const oscar_config *cfg, int32_t batch, int32_t T, int32_t max_seq_len);
+size_t oscar_draft_workspace_bytes(const oscar_config *cfg, int32_t batch, int32_t T, int32_t num_splits);
+int oscar_draft_attn(const void *q, const void *k_new, const void *v_new, int32_t T,
+                     const int32_t *new_lens, const oscar_cache *cache, void *out,
+                     float softmax_scale, int32_t max_seq_len_hint, int32_t num_splits,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* Verification of drafted tokens against the target's probabilities, from given random numbers
+ * (speculative sampling: what comes out is distributed as the target's own samples).  Sequence b
+ * has n = draft_lens[b] drafts (0..T; NULL = T for all):
+ *   draft t stands  iff  u[b][t] * draft[b][t][x] < target[b][t][x],  x = drafts[b][t],  and all
+ *                   drafts before it do; an x outside the vocabulary does not stand
+ *   a             = the number of drafts that stand
+ *   next token    = the smallest i whose running sum w_0 + .. + w_i exceeds u[b][T] * (sum of w),
+ *                   w = max(target[b][a] - draft[b][a], 0) if a < n and that is not all zero, else
+ *                   target[b][a]; a row without a positive number gives token 0
+ *   target : device, [batch][T+1][vocab] of dtype (F32|BF16|F16); rows need not add up to 1
+ *   draft  : device, [batch][T][vocab] of dtype, what the drafts were drawn from
+ *   drafts : device int32 [batch][T];   u : device fp32 [batch][T+1], in [0, 1)
+ *   n_new  : device int32 [batch]: a + 1, the tokens the step yields, which is also the new_lens of
+ *            oscar_quantize_append for the keys and values of the last token and the drafts
+ *   tokens : device int32 [batch][T+1]: the drafts that stand, the next token, then -1
+ *   workspace : at least oscar_verify_workspace_bytes(...), 16-byte aligned; its contents do not
+ *            matter.  Calls that share one must be ordered.
+ * Numbers that are not above zero, NaNs among them, count as 0, infinities as the largest fp32.
+ * Sums and comparisons are in 64 bits.  draft and drafts may be NULL with T == 0.
+ * batch <= 65535. */
+#define OSCAR_VERIFY_MAX_DRAFTS 4096
+#define OSCAR_VERIFY_MAX_VOCAB (1 << 24)
+size_t oscar_verify_workspace_bytes(int32_t batch, int32_t vocab);
+int oscar_verify_drafts(const void *target, const void *draft, const int32_t *drafts,
+                        const int32_t *draft_lens, const float *u, int32_t batch, int32_t T,
+                        int32_t vocab, int32_t dtype, int32_t *n_new, int32_t *tokens,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
 /* Test/debug: copy sequence b, kv head h back to the HOST in a layout-free
  * form (one code per byte). Synchronizes `stream`. Host outputs, each may be
  * NULL; `cap_tokens` is the token capacity of the caller's arrays.

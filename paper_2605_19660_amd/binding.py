@@ -31,7 +31,9 @@ EXPORTS = ("oscar_version", "oscar_status_string", "oscar_cache_sizes",
            "oscar_timer_destroy", "oscar_timer_elapsed_us", "oscar_decode_attn_partial_timed",
            "oscar_probe_stream_read", "oscar_rotate", "oscar_rotate_columns",
            "oscar_debug_force_generic_decode", "oscar_decode_attn_noalloc",
-           "oscar_decode_step", "oscar_cache_layer")
+           "oscar_decode_step", "oscar_cache_layer", "oscar_rope", "oscar_cache_read",
+           "oscar_draft_auto_splits", "oscar_draft_workspace_bytes", "oscar_draft_attn",
+           "oscar_verify_workspace_bytes", "oscar_verify_drafts")
 
 
 class OscarError(RuntimeError):
@@ -119,6 +121,20 @@ def lib():
     L.oscar_debug_force_generic_decode.argtypes = [i32]
     L.oscar_debug_dump.restype = C.c_int
     L.oscar_debug_dump.argtypes = [C.POINTER(CCache), i32, i32, i32] + [vp] * 11 + [vp]
+    L.oscar_rope.restype = C.c_int
+    L.oscar_rope.argtypes = [vp, vp, vp, vp, C.c_int64, i32, i32] + [C.c_int64] * 4 + [vp, vp, C.c_char_p, i32, i32, i32, u32, vp]
+    L.oscar_cache_read.restype = C.c_int
+    L.oscar_cache_read.argtypes = [C.POINTER(CCache), vp, i32, vp, vp, i32, vp]
+    L.oscar_draft_auto_splits.restype = i32
+    L.oscar_draft_auto_splits.argtypes = [C.POINTER(CConfig), i32, i32, i32]
+    L.oscar_draft_workspace_bytes.restype = sz
+    L.oscar_draft_workspace_bytes.argtypes = [C.POINTER(CConfig), i32, i32, i32]
+    L.oscar_draft_attn.restype = C.c_int
+    L.oscar_draft_attn.argtypes = [vp, vp, vp, i32, vp, C.POINTER(CCache), vp, f32, i32, i32, vp, sz, vp]
+    L.oscar_verify_workspace_bytes.restype = sz
+    L.oscar_verify_workspace_bytes.argtypes = [i32, i32]
+    L.oscar_verify_drafts.restype = C.c_int
+    L.oscar_verify_drafts.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -505,6 +521,157 @@ def bf16_decode_attn(q, k, v, seq_lens, out=None, scale: float = 0.0, max_seq_le
                                       workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     _check(rc, "oscar_bf16_decode_attn")
     return out
+
+
+ROPE_ADJACENT, ROPE_INVERSE = 1, 2
+
+
+def rope_axes(sections, interleaved: bool = False) -> bytes:
+    """The axis of every pair, for `rope`: sections[a] pairs turn with axis a, in that order or
+    (interleaved) dealt out one after the other, an axis leaving the round when its share is used up."""
+    if interleaved:
+        left, order = list(sections), []
+        while any(left):
+            for a, n in enumerate(left):
+                if n:
+                    order.append(a)
+                    left[a] -= 1
+        return bytes(order)
+    return bytes(a for a, n in enumerate(sections) for _ in range(n))
+
+
+def _token_rows(x):
+    """Heads and elements between tokens of a [..., heads, 128] tensor whose tokens lie evenly apart."""
+    assert x.is_cuda and x.dim() >= 2 and x.shape[-1] == 128 and x.stride(-1) == 1
+    heads = x.shape[-2]
+    assert heads == 1 or x.stride(-2) == 128
+    step = None
+    for size, stride in zip(reversed(x.shape[:-2]), reversed(x.stride()[:-2])):
+        if size == 1:
+            continue
+        assert step is None or stride == step * inner, "tokens do not lie evenly apart"
+        if step is None:
+            step, inner = stride, size
+        else:
+            inner *= size
+    return heads, heads * 128 if step is None else step
+
+
+def rope(q, k, positions, inv_freq, axes: bytes | None = None, adjacent: bool = False, inverse: bool = False,
+         out_q=None, out_k=None, stream=None):
+    """oscar_rope: q [..., n_q_heads, 128], k [..., n_kv_heads, 128] (one of them may be None) of any even
+    distance between tokens; positions int32 [n_tokens] or [n_axes, n_tokens]; inv_freq fp32
+    [rotary_dim / 2]; axes: see rope_axes.  Returns (q, k) turned, in new tensors unless out_q, out_k
+    say where (q and k themselves for in place)."""
+    import torch
+    lead = (q if q is not None else k).shape[:-2]
+    n = lead.numel()
+    n_axes = positions.shape[0] if positions.dim() == 2 else 1
+    assert positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32
+    assert positions.numel() == n_axes * n and inv_freq.is_cuda and inv_freq.is_contiguous() and inv_freq.dtype == torch.float32
+    pairs = inv_freq.numel()
+    assert axes is None or len(axes) == pairs
+    ptr, heads, strides, outs = [None] * 4, [0, 0], [0] * 4, [None, None]
+    dtype = (q if q is not None else k).dtype
+    for i, (x, o) in enumerate(((q, out_q), (k, out_k))):
+        if x is None:
+            continue
+        assert x.dtype == dtype and x.shape[:-2] == lead
+        if o is None:
+            o = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        assert o.shape == x.shape and o.dtype == dtype
+        heads[i], strides[i] = _token_rows(x)
+        strides[2 + i] = _token_rows(o)[1]
+        ptr[i], ptr[2 + i], outs[i] = x.data_ptr(), o.data_ptr(), o
+    rc = lib().oscar_rope(*ptr, n, *heads, *strides, positions.data_ptr(), inv_freq.data_ptr(), axes, n_axes, 2 * pairs,
+                          dtype_code(dtype), (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0),
+                          _stream_ptr(stream))
+    _check(rc, "oscar_rope")
+    return tuple(outs)
+
+
+def cache_read(cache: Cache, starts=None, k=None, v=None, stream=None):
+    """oscar_cache_read: fills k and v ([batch, T, n_kv_heads, 128], one type of the three, either may be
+    None) with the tokens from starts[b] on (int32 [batch]; None = 0) and returns them; rows of tokens that
+    a sequence does not hold stay as they are."""
+    import torch
+    shape, dtype = (k if k is not None else v).shape, (k if k is not None else v).dtype
+    assert shape[0] == cache.batch and tuple(shape[2:]) == (cache.cfg.n_kv_heads, cache.cfg.head_dim)
+    for x in (k, v):
+        assert x is None or (x.is_cuda and x.is_contiguous() and x.shape == shape and x.dtype == dtype)
+    assert starts is None or (starts.is_cuda and starts.is_contiguous() and starts.dtype == torch.int32 and starts.numel() == cache.batch)
+    rc = lib().oscar_cache_read(C.byref(cache.c), None if starts is None else starts.data_ptr(), shape[1],
+                                None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
+                                dtype_code(dtype), _stream_ptr(stream))
+    _check(rc, "oscar_cache_read")
+    return k, v
+
+
+def draft_auto_splits(cfg: Config, batch: int, tokens: int, max_seq_len: int) -> int:
+    cc = cfg.c()
+    return int(lib().oscar_draft_auto_splits(C.byref(cc), batch, tokens, max_seq_len))
+
+
+def draft_workspace_bytes(cfg: Config, batch: int, tokens: int, num_splits: int) -> int:
+    cc = cfg.c()
+    return int(lib().oscar_draft_workspace_bytes(C.byref(cc), batch, tokens, num_splits))
+
+
+def draft_attn(cache: Cache, q, k_new, v_new, new_lens=None, out=None, scale: float = 0.0, max_seq_len_hint: int = 0,
+               num_splits: int = 0, workspace=None, stream=None):
+    """oscar_draft_attn: q [batch, T, n_q_heads, 128], k_new and v_new [batch, T, n_kv_heads, 128], all of the io
+    dtype; returns `out` (of q's shape and type)."""
+    import torch
+    cfg, shape = cache.cfg, q.shape
+    assert q.is_cuda and q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous()
+    assert q.dtype == k_new.dtype == v_new.dtype == torch_dtype(cfg.io_dtype)
+    assert shape[0] == cache.batch and tuple(shape[2:]) == (cfg.n_q_heads, cfg.head_dim)
+    assert k_new.shape == v_new.shape == (shape[0], shape[1], cfg.n_kv_heads, cfg.head_dim)
+    assert new_lens is None or (new_lens.is_cuda and new_lens.is_contiguous() and new_lens.dtype == torch.int32 and new_lens.numel() == cache.batch)
+    if out is None:
+        out = torch.empty_like(q)
+    assert out.is_contiguous() and out.shape == shape and out.dtype == q.dtype
+    L, cc = lib(), C.byref(cache.c.cfg)
+    if num_splits == 0:
+        num_splits = L.oscar_draft_auto_splits(cc, shape[0], shape[1], max_seq_len_hint)
+    if workspace is None and num_splits > 1:
+        workspace = torch.empty(L.oscar_draft_workspace_bytes(cc, shape[0], shape[1], num_splits),
+                                dtype=torch.uint8, device=q.device)
+    rc = L.oscar_draft_attn(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), shape[1],
+                            None if new_lens is None else new_lens.data_ptr(), C.byref(cache.c), out.data_ptr(), scale,
+                            max_seq_len_hint, num_splits, None if workspace is None else workspace.data_ptr(),
+                            0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    _check(rc, "oscar_draft_attn")
+    return out
+
+
+def verify_workspace_bytes(batch: int, vocab: int) -> int:
+    return int(lib().oscar_verify_workspace_bytes(batch, vocab))
+
+
+def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=None, workspace=None, stream=None):
+    """oscar_verify_drafts: target [batch, T + 1, vocab] and draft [batch, T, vocab] of one type, drafts int32
+    [batch, T], u fp32 [batch, T + 1]; returns (n_new int32 [batch], tokens int32 [batch, T + 1])."""
+    import torch
+    batch, T, vocab = target.shape[0], target.shape[1] - 1, target.shape[2]
+    assert target.is_cuda and target.is_contiguous() and draft.is_contiguous() and target.dtype == draft.dtype
+    assert tuple(draft.shape) == (batch, T, vocab) and tuple(drafts.shape) == (batch, T) and tuple(u.shape) == (batch, T + 1)
+    assert drafts.is_contiguous() and drafts.dtype == torch.int32 and u.is_contiguous() and u.dtype == torch.float32
+    assert draft_lens is None or (draft_lens.is_cuda and draft_lens.is_contiguous() and draft_lens.dtype == torch.int32 and draft_lens.numel() == batch)
+    if n_new is None:
+        n_new = torch.empty(batch, dtype=torch.int32, device=target.device)
+    if tokens is None:
+        tokens = torch.empty(batch, T + 1, dtype=torch.int32, device=target.device)
+    assert n_new.is_contiguous() and n_new.dtype == torch.int32 and n_new.numel() == batch
+    assert tokens.is_contiguous() and tokens.dtype == torch.int32 and tuple(tokens.shape) == (batch, T + 1)
+    if workspace is None:
+        workspace = torch.empty(verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=target.device)
+    rc = lib().oscar_verify_drafts(target.data_ptr(), draft.data_ptr(), drafts.data_ptr(),
+                                   None if draft_lens is None else draft_lens.data_ptr(), u.data_ptr(), batch, T, vocab,
+                                   dtype_code(target.dtype), n_new.data_ptr(), tokens.data_ptr(), workspace.data_ptr(),
+                                   workspace.numel(), _stream_ptr(stream))
+    _check(rc, "oscar_verify_drafts")
+    return n_new, tokens
 
 
 def debug_dump(cache: Cache, b: int, h: int, cap_tokens: int | None = None, stream=None) -> dict:

@@ -32,6 +32,10 @@ SOURCES = {
     "oscar_decode_step_zpmin.hip": [],
     "oscar_bf16_decode.hip": [],
     "oscar_probe.hip": [],
+    "oscar_rope.hip": [],
+    "oscar_cache_read.hip": [],
+    "oscar_draft.hip": [],
+    "oscar_verify.hip": [],
 }
 
 

@@ -1,0 +1,243 @@
+// oscar_cache_read: keys and values of a range of tokens, out of the packed cache.
+//
+//   k_t = H(n_t K_u,t) / sqrt(128),  K_u,tj = Delta_gj (c_tj - z_gj)      (H is its own inverse)
+//   v_tj = Delta_tg (c_tj - z_tg)
+// and from the window K_u and V as they stand (float zero-points: Delta c + zero).
+//
+// What bounds it: 86 bytes a token and kv head are read (2-bit codes) and 512 written (16-bit), so it is a
+// stream of writes.  One workgroup takes one page of one kv head: wave w the token tiles 2w and 2w + 1 of
+// the keys, whose two chunks a lane loads with one access (1 KB a wave), and the channels 32w .. 32w + 31 of
+// the values.  A lane holds 32 channels of a token: five Hadamard stages are in its registers, two are
+// exchanges inside a quad of lanes.  Both go through LDS so that a wave writes whole rows.
+#include "oscar_decode_common.h"
+#include "oscar_rowops.h"
+
+namespace {
+
+struct ReadParams {
+  void *k, *v;
+  const int32_t* starts;
+  oscar_cache c;
+  PageGeom g;
+  int64_t T;
+};
+
+// the 32 codes of a lane's chunk as floats, in their natural order
+template <int BITS> __device__ __forceinline__ void unpack_chunk(const uint32_t* w, float (&x)[32]) {
+#pragma unroll
+  for (int u = 0; u < 32; ++u) x[u] = (float)((w[u * BITS / 32] >> (u * BITS % 32)) & ((1u << BITS) - 1u));
+}
+
+// 8 metadata numbers from 16-byte aligned storage
+template <bool M32> __device__ __forceinline__ void load_meta8(const uint8_t* base, int idx, float (&x)[8]) {
+  if (M32) {
+    const float4* p = reinterpret_cast<const float4*>(base + (size_t)idx * 4);
+    const float4 a = p[0], b = p[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  } else {
+    const uint4 w = *reinterpret_cast<const uint4*>(base + (size_t)idx * 2);
+    const __half* h = reinterpret_cast<const __half*>(&w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __half2float(h[i]);
+  }
+}
+
+__device__ __forceinline__ float dequant(float c, float step, float zero, bool zp_min) {
+  return zp_min ? fmaf(c, step, zero) : (c - zero) * step;
+}
+
+// H over 128 channels, 32 consecutive ones in each lane of a quad (lane % 4 = which), times mul
+__device__ __forceinline__ void rotate_quad(float (&x)[32], float mul) {
+#pragma unroll
+  for (int h = 1; h < 32; h <<= 1) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if ((i & h) == 0) {
+        const float a = x[i], b = x[i | h];
+        x[i] = a + b;
+        x[i | h] = a - b;
+      }
+    }
+  }
+  const int q4 = threadIdx.x & 3;
+  const float s0 = q4 & 1 ? -1.0f : 1.0f, s1 = q4 & 2 ? -1.0f : 1.0f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], s0, partner<0>(x[i]));
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], s1, partner<1>(x[i])) * mul;
+}
+
+constexpr int PAD = 32;   // bytes: rows of four tokens that a wave writes at once fall on other banks
+
+template <int BITS, typename OUT, bool M32>
+__global__ __launch_bounds__(256) void oscar_cache_read_kernel(ReadParams P) {
+  constexpr int ROW = D * sizeof(OUT) + PAD;
+  __shared__ __align__(16) uint8_t s_row[R * ROW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int h = blockIdx.y, b = blockIdx.z, Hkv = P.c.cfg.n_kv_heads;
+  const int seq_len = max(P.c.seq_lens[b], 0);
+  const int res = min(max(P.c.res_lens[b], 0), min(R, seq_len));
+  const int pages = min((seq_len - res) / R, P.c.max_pages_per_seq);
+  const int64_t start = P.starts ? P.starts[b] : 0;
+  const int64_t t_begin = max(start, (int64_t)0), t_end = min(start + P.T, (int64_t)pages * R + res);
+  const int64_t page = t_begin / R + blockIdx.x;
+  const int64_t lo = max(t_begin, page * R), hi = min(t_end, (page + 1) * R);
+  if (lo >= hi) return;
+  const int t_lo = (int)(lo - page * R), t_hi = (int)(hi - page * R);   // of this page's tokens
+  const bool window = page == pages;
+  int64_t phys = 0;
+  if (!window) {
+    phys = P.c.block_table[(int64_t)b * P.c.max_pages_per_seq + page];
+    if (phys < 0 || phys >= P.c.num_pages) return;
+  }
+  const int64_t unit = window ? (int64_t)b * Hkv + h : phys * Hkv + h;
+  const int n = lane >> 2, q4 = lane & 3;
+  const bool zp_min = P.c.cfg.zp_mode == OSCAR_ZP_MIN, rotated = P.c.cfg.rotation == OSCAR_ROTATION_ON;
+  // row `page * R + t` of the outputs
+  const int64_t out_row = (((int64_t)b * P.T + page * R - start) * Hkv + h) * D;
+
+  // rows t_lo .. t_hi of the LDS image to the output, 16 bytes a lane
+  auto write_rows = [&](void* out) {
+    constexpr int LANES = D * sizeof(OUT) / 16;
+    OUT* o = reinterpret_cast<OUT*>(out) + out_row;
+#pragma unroll 4
+    for (int t = t_lo + tid / LANES; t < t_hi; t += 256 / LANES) {
+      const int c = tid % LANES;
+      *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(o + (int64_t)t * Hkv * D) + c * 16) =
+          *reinterpret_cast<const uint4*>(s_row + t * ROW + c * 16);
+    }
+  };
+
+  if (P.k) {
+    uint32_t w[2 * BITS];
+    float step[32], zero[32];
+    if (!window) {
+      const uint8_t* codes = reinterpret_cast<const uint8_t*>(P.c.k_codes) + unit * P.g.k_codes_bytes;
+      const uint4* src = reinterpret_cast<const uint4*>(codes + chunk_offset(BITS, 2 * wave, n, q4));
+#pragma unroll
+      for (int i = 0; i < BITS / 2; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = src[i];
+      // the two tiles lie in one group of 32, 64 or 128 tokens
+      const uint8_t* meta = reinterpret_cast<const uint8_t*>(P.c.k_meta) + unit * P.g.k_meta_bytes;
+      const int group = wave * 32 / P.g.k_group;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        float a[8], z[8];
+        load_meta8<M32>(meta, group * D + 32 * q4 + 8 * kk, a);
+        load_meta8<M32>(meta, (P.g.ngk + group) * D + 32 * q4 + 8 * kk, z);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) step[slot_index(BITS, kk, e)] = a[e], zero[slot_index(BITS, kk, e)] = z[e];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = (2 * wave + i) * 16 + n;
+      if ((2 * wave + i) * 16 >= t_hi || (2 * wave + i) * 16 + 16 <= t_lo) continue;
+      float x[32], norm;
+      if (!window) {
+        unpack_chunk<BITS>(w + i * BITS, x);
+#pragma unroll
+        for (int u = 0; u < 32; ++u) x[u] = dequant(x[u], step[u], zero[u], zp_min);
+        norm = load_meta(reinterpret_cast<const uint8_t*>(P.c.k_norms) + unit * P.g.k_norms_bytes, tok_meta_pos(t),
+                         M32 ? 4 : 2);
+      } else {
+        const __half* src = reinterpret_cast<const __half*>(P.c.res_k) + (unit * R + t) * D + 32 * q4;
+#pragma unroll
+        for (int u = 0; u < 32; ++u) x[u] = __half2float(src[u]);
+        norm = load_meta(P.c.res_norm, unit * R + t, M32 ? 4 : 2);
+      }
+      if (rotated) {
+        rotate_quad(x, norm * 0.08838834764831845f);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 32; ++u) x[u] *= norm;
+      }
+      OUT* row = reinterpret_cast<OUT*>(s_row + t * ROW) + 32 * q4;
+#pragma unroll
+      for (int u = 0; u < 32; ++u) row[u] = from_f32<OUT>(x[u]);
+    }
+    __syncthreads();
+    write_rows(P.k);
+    if (P.v) __syncthreads();
+  }
+  if (P.v) {
+    if (!window) {
+      const uint8_t* codes = reinterpret_cast<const uint8_t*>(P.c.v_codes) + unit * P.g.v_codes_bytes;
+      const uint4* src = reinterpret_cast<const uint4*>(codes + chunk_offset(BITS, 2 * wave, n, q4));
+      uint32_t w[2 * BITS];
+#pragma unroll
+      for (int i = 0; i < BITS / 2; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = src[i];
+      const uint8_t* meta = reinterpret_cast<const uint8_t*>(P.c.v_meta) + unit * P.g.v_meta_bytes;
+      const int group = wave * 32 / P.g.v_group;
+      float x[2][32];
+      unpack_chunk<BITS>(w, x[0]);
+      unpack_chunk<BITS>(w + BITS, x[1]);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        float a[8], z[8];
+        load_meta8<M32>(meta, group * R + (4 * kk + q4) * 8, a);
+        load_meta8<M32>(meta, (P.g.ngv + group) * R + (4 * kk + q4) * 8, z);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int t = 16 * e + 4 * kk + q4;
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            reinterpret_cast<OUT*>(s_row + t * ROW)[16 * (2 * wave + i) + n] =
+                from_f32<OUT>(dequant(x[i][slot_index(BITS, kk, e)], a[e], z[e], zp_min));
+        }
+      }
+    } else {
+      for (int i = t_lo * D + tid; i < t_hi * D; i += 256)
+        reinterpret_cast<OUT*>(s_row + (i / D) * ROW)[i % D] =
+            from_f32<OUT>(load_io(P.c.res_v, unit * R * D + i, P.c.cfg.io_dtype));
+    }
+    __syncthreads();
+    write_rows(P.v);
+  }
+}
+
+template <int BITS, typename OUT> void launch(const ReadParams& P, dim3 grid, hipStream_t st) {
+  if (P.g.meta_bytes == 4)
+    hipLaunchKernelGGL((oscar_cache_read_kernel<BITS, OUT, true>), grid, dim3(256), 0, st, P);
+  else
+    hipLaunchKernelGGL((oscar_cache_read_kernel<BITS, OUT, false>), grid, dim3(256), 0, st, P);
+}
+template <typename OUT> void launch(const ReadParams& P, dim3 grid, hipStream_t st) {
+  if (P.g.bits == 2)
+    launch<2, OUT>(P, grid, st);
+  else
+    launch<4, OUT>(P, grid, st);
+}
+
+}  // namespace
+
+extern "C" int oscar_cache_read(const oscar_cache* cache, const int32_t* starts, int32_t T, void* k, void* v,
+                                int32_t out_dtype, void* stream) {
+  const int rc = oscar_check_cache(cache);
+  if (rc != OSCAR_OK) return rc;
+  if (T < 0 || cache->num_pages <= 0) return OSCAR_ERR_INVALID_ARG;
+  if (out_dtype != OSCAR_F32 && out_dtype != OSCAR_BF16 && out_dtype != OSCAR_F16) return OSCAR_ERR_INVALID_ARG;
+  if (((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15) != 0) return OSCAR_ERR_INVALID_ARG;
+  if (cache->cfg.n_kv_heads > 65535 || cache->batch > 65535) return OSCAR_ERR_INVALID_ARG;
+  if (T == 0) return OSCAR_OK;
+  if (!k && !v) return OSCAR_ERR_INVALID_ARG;
+  ReadParams P;
+  P.k = k;
+  P.v = v;
+  P.starts = starts;
+  P.c = *cache;
+  P.g = make_geom(cache->cfg.bits, cache->cfg.k_group, cache->cfg.v_group, cache->cfg.meta_dtype);
+  P.T = T;
+  // pages that T tokens from anywhere can touch, and no more than a sequence has with its window
+  int64_t blocks = starts ? ((int64_t)T - 1) / R + 2 : ((int64_t)T - 1) / R + 1;
+  if (blocks > (int64_t)cache->max_pages_per_seq + 1) blocks = (int64_t)cache->max_pages_per_seq + 1;
+  const dim3 grid((unsigned)blocks, cache->cfg.n_kv_heads, cache->batch);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (out_dtype == OSCAR_F32)
+    launch<float>(P, grid, st);
+  else if (out_dtype == OSCAR_BF16)
+    launch<__hip_bfloat16>(P, grid, st);
+  else
+    launch<__half>(P, grid, st);
+  if (hipGetLastError() != hipSuccess) return OSCAR_ERR_HIP;
+  return OSCAR_OK;
+}

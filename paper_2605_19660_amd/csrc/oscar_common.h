@@ -158,6 +158,8 @@ __device__ __forceinline__ int ticket_answer(int ticket) {   // thread 0's, in i
 
 // Host-side validation shared by the entry points.
 int oscar_validate_config(const oscar_config* cfg);
+// The checks of a cache that an attention or a read makes: configuration, sizes, pointers.
+int oscar_check_cache(const oscar_cache* cache);
 // Compute units of the current device (asked for once a device).
 int oscar_compute_units();
 

@@ -468,7 +468,7 @@ int launch_gq(const DecodeParams& P, int gq, dim3 grid, hipStream_t st, hipEvent
 
 }  // namespace
 
-static int check_decode_cache(const oscar_cache* cache) {
+int oscar_check_cache(const oscar_cache* cache) {
   if (!cache) return OSCAR_ERR_INVALID_ARG;
   int rc = oscar_validate_config(&cache->cfg);
   if (rc != OSCAR_OK) return rc;
@@ -487,7 +487,7 @@ static int launch_partial(const void* q, const oscar_cache* cache, void* out, in
                           size_t workspace_bytes, void* stream, oscar_timer* timer,
                           int* wrote_out = nullptr, const void* k_new = nullptr,
                           const void* v_new = nullptr) {
-  int rc = check_decode_cache(cache);
+  int rc = oscar_check_cache(cache);
   if (rc != OSCAR_OK) return rc;
   if (!q || num_splits <= 0 || num_splits > 512) return OSCAR_ERR_INVALID_ARG;
   hipEvent_t e0 = timer ? timer->start : nullptr, e1 = timer ? timer->stop : nullptr;
@@ -580,7 +580,7 @@ extern "C" int oscar_decode_attn_partial(const void* q, const oscar_cache* cache
 extern "C" int oscar_decode_attn_reduce(const oscar_cache* cache, void* out, int32_t out_dtype,
                                         int32_t num_splits, const void* workspace,
                                         size_t workspace_bytes, void* stream) {
-  int rc = check_decode_cache(cache);
+  int rc = oscar_check_cache(cache);
   if (rc != OSCAR_OK) return rc;
   if (!out || num_splits <= 0 || num_splits > 512) return OSCAR_ERR_INVALID_ARG;
   if (out_dtype != OSCAR_F32 && out_dtype != cache->cfg.io_dtype) return OSCAR_ERR_INVALID_ARG;
@@ -597,7 +597,7 @@ extern "C" int oscar_decode_attn(const void* q, const oscar_cache* cache, void* 
                                  int32_t out_dtype, float softmax_scale,
                                  int32_t max_seq_len_hint, int32_t num_splits, void* workspace,
                                  size_t workspace_bytes, void* stream) {
-  int rc = check_decode_cache(cache);
+  int rc = oscar_check_cache(cache);
   if (rc != OSCAR_OK) return rc;
   if (!q || !out || max_seq_len_hint < 0 || num_splits < 0) return OSCAR_ERR_INVALID_ARG;
   if (out_dtype != OSCAR_F32 && out_dtype != cache->cfg.io_dtype) return OSCAR_ERR_INVALID_ARG;
@@ -619,7 +619,7 @@ extern "C" int oscar_decode_step(const void* k_new, const void* v_new, const voi
                                  float softmax_scale, int32_t max_seq_len_hint, int32_t num_splits,
                                  void* workspace, size_t workspace_bytes, void* stream,
                                  oscar_timer* partial_timer) {
-  int rc = check_decode_cache(cache);
+  int rc = oscar_check_cache(cache);
   if (rc != OSCAR_OK) return rc;
   if (!k_new || !v_new || !q || !out || max_seq_len_hint < 1 || num_splits < 0 || num_splits > 512)
     return OSCAR_ERR_INVALID_ARG;
@@ -687,7 +687,7 @@ extern "C" int oscar_decode_attn_noalloc(const void* q, const oscar_cache* cache
                                          int32_t out_dtype, float softmax_scale,
                                          int32_t max_seq_len_hint, int32_t num_splits,
                                          void* stream) {
-  int rc = check_decode_cache(cache);
+  int rc = oscar_check_cache(cache);
   if (rc != OSCAR_OK) return rc;
   if (!q || !out || max_seq_len_hint < 0 || num_splits < 0 || num_splits > 512)
     return OSCAR_ERR_INVALID_ARG;
