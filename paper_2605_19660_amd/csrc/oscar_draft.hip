@@ -1,29 +1,33 @@
 // oscar_draft_attn: attention of several new tokens of every sequence over its packed cache and, causally,
 // over each other.
 //
-//   logit[t][h][i] = scale n_i sum_j Q_j (Delta_k c_k + b_k)_ij      cached token i, Q = H(q_th)/sqrt(128),
-//                                                                    b = -Delta z (integer zero-points) or zero
-//   logit[t][h][j] = scale <q_th, k_j>                               new token j <= t
+//   logit[t][h][i] = scale n_i sum_j Q_j (Delta_k c_k - Delta_k z_k)_ij   cached token i, Q = H(q_th)/sqrt(128)
+//                                                                        (float zero-points: Delta_k c_k + zero)
+//   logit[t][h][j] = scale <q_th, k_j>                                   new token j <= t
 //   out[t][h]      = softmax over both, times the values
 //
-// The T tokens' g query heads of a kv head are T g rows that read the same keys and values.  A wave holds
-// 16 or 32 of them (16 a matrix tile) and takes whole pages of 128 tokens on its own, with its own running
-// maximum and sum; four waves and the splits of the sequence are joined at the end.
+// The T tokens' g query heads of a kv head are T g rows that read the same keys and values.  A workgroup
+// takes 16 .. 64 of them (16 a matrix tile) through a share of the sequence, page by page:
+//   wave w: S^T = K Q^T for tokens 32 w .. + 31   v_mfma_f32_16x16x32_f16, rows = tokens, columns = query rows
+//   the rows' maxima through LDS, barrier; probabilities to LDS, barrier
+//   wave w: O^T = V^T P^T for channels 32 w .. + 31, over all 128 tokens
+// so that each code is loaded and unpacked once a workgroup, a wave's share of the keys lies in one group of
+// tokens and that of the values in one group of channels, and the state of a row (16 registers a tile in all)
+// leaves room for several workgroups a CU, which cover each other's barriers and loads.
 //
-//   S^T = K Q^T : v_mfma_f32_16x16x32_f16, rows = 16 tokens, columns = 16 query rows, over 128 channels
-//   O^T = V^T P^T: rows = 16 channels, columns = query rows, over 128 tokens
-// Row n of a token tile is token 4 (n % 4) + n / 4 of it, so that a lane's four results of tile T are its
-// tokens 16 T + 4 r + lane / 16: exactly the tokens whose value codes the lane's chunk of the page holds for
-// step r.  The probabilities are packed where they are and nothing is exchanged between lanes but the row
-// maxima.
+// Row n of a token tile is token 4 (n % 4) + n / 4 of it: a lane's four results of tile T are then its tokens
+// 16 T + 4 r + lane / 16, exactly those whose value codes the lane's chunk of the page holds for k-step r, and a
+// lane reads the probabilities it multiplies with as 16 consecutive bytes.
 //
 // Codes become fp16 operands with a mask (a code parked in the mantissa of a subnormal: c 2^(s - 24)); the
-// steps go to the other operand, Q Delta_k once a group of tokens and P Delta_v once a group of channels, and
-// 2^-s with them.  Q Delta and P Delta are rounded to fp16: half a step of 2^-11, a fourth of the output's
-// own in bf16.  The zero terms (b) are products of their own on the matrix cores: for the keys they are
-// what a tile's sums start from, for the values they and the row sums are rows of one extra tile.
-// The probabilities are scaled by 2^15 (less where a value step of 2 or more would carry P Delta past the
-// fp16 range): a token counts down to 2^-39 of the largest.  Sums, maxima and outputs are fp32.
+// steps go to the other operand, Q Delta_k and P Delta_v, and 2^-s with them.  Codes count from their middle:
+// the term that takes it off again is a product of the same rounded operands with a constant, what is left of
+// the zero-points is of the size of a group's mean, and both are products on the matrix cores too: for the keys
+// what a tile's sums start from, for the values one extra tile, whose other rows are the rows' sums.  Seen from
+// code 0 the same roundings moved the logits three times as far.  Roundings: Q, Q Delta, P, P Delta and the
+// mean terms to fp16, half a step (2^-11) each.  The probabilities are scaled by 2^15 (less where a value step
+// of 2 or more would carry P Delta past the fp16 range): a token counts down to 2^-39 of the largest.  Sums,
+// maxima and outputs are fp32.
 #include "oscar_decode_common.h"
 
 namespace {
@@ -37,7 +41,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kHalfMax = 65504.0f;
 constexpr int kQShift = 2;           // the queries carry 2^2
-constexpr int TAIL = 32;             // tokens of a 16-bit piece (window, new tokens)
 
 struct DraftParams {
   const void *q, *k_new, *v_new;
@@ -52,7 +55,7 @@ struct DraftParams {
 
 template <int BITS> struct Codes {
   static constexpr int BPMIN = BITS == 2 ? 4 : 2, BPMAX = BITS == 2 ? 8 : 6;
-  static constexpr int WORDS = BITS;   // dwords of a chunk
+  static constexpr float MID = 0.5f * (float)((1 << BITS) - 1);
   // the operand of k-step kk from a chunk
   __device__ static __forceinline__ half8 operand(const uint32_t* w, int kk) {
     u32x4 r;
@@ -72,8 +75,8 @@ template <int BITS> struct Codes {
     return __builtin_bit_cast(half8, r);
   }
   // what an element's bit position is above the lowest
-  __device__ static constexpr int above(int kk, int e) { return slot_bitpos(BITS, kk, e) - BPMIN; }
-  // 2^(above - (BPMAX - BPMIN)), the other operand's counterweight for what is no code
+  __host__ __device__ static constexpr int above(int kk, int e) { return slot_bitpos(BITS, kk, e) - BPMIN; }
+  // 2^(above - (BPMAX - BPMIN)), the other operand's counterweight for what is no code (kk counts modulo 2)
   __device__ static __forceinline__ half8 counterweight(int kk) {
     half8 r;
 #pragma unroll
@@ -82,57 +85,74 @@ template <int BITS> struct Codes {
   }
 };
 
-// 8 numbers of a page's metadata, as fp16 (fp32 metadata: rounded, and kept inside the range)
-template <bool M32> __device__ __forceinline__ half8 load_step(const uint8_t* base, int idx) {
-  if (!M32) return *reinterpret_cast<const half8*>(base + (size_t)idx * 2);
-  half8 r;
+// A page's metadata as the waves read it: steps and mean terms (with their counterweights) as fp16 in operand
+// order, norms as fp32 with the codes' unit taken out.
+struct Staged {
+  half8 k_step[64], k_base[64];   // [group][quarter][k-step]
+  half8 v_step[64], v_base[64];   // [group][k-step][quarter]
+  float norm[R];                  // position (token % 16) * 8 + token / 16
+  int off;                        // exponent the probabilities can carry
+};
+// What a lane holds of the metadata of a page to come: 8 steps and 8 zeros (wave 0 of the keys, wave 1 of the
+// values) or 8 norms (the others).  All waves make the same loads, so that how many are in flight is known
+// wherever one is waited for.
+template <bool M32> struct Fetched {
+  u32x4 a[M32 ? 2 : 1], b[M32 ? 2 : 1];
+  __device__ __forceinline__ void load(const uint8_t* src, const uint8_t* zsrc, uint32_t at) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = (_Float16)fminf(reinterpret_cast<const float*>(base)[idx + e], kHalfMax);
-  return r;
-}
-// and the zero term b that belongs to steps `idx` and zeros `zidx`
-template <bool M32> __device__ __forceinline__ half8 load_b(const uint8_t* base, int idx, int zidx, bool zp_min) {
-  half8 r;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float s, z;
-    if (M32) {
-      s = reinterpret_cast<const float*>(base)[idx + e];
-      z = reinterpret_cast<const float*>(base)[zidx + e];
-    } else {
-      s = (float)reinterpret_cast<const _Float16*>(base)[idx + e];
-      z = (float)reinterpret_cast<const _Float16*>(base)[zidx + e];
+    for (int i = 0; i < (M32 ? 2 : 1); ++i) {
+      a[i] = *reinterpret_cast<const u32x4*>(src + at + 16 * i);
+      b[i] = *reinterpret_cast<const u32x4*>(zsrc + at + 16 * i);
     }
-    r[e] = (_Float16)__builtin_amdgcn_fmed3f(zp_min ? z : -z * s, -kHalfMax, kHalfMax);
   }
-  return r;
-}
+  __device__ __forceinline__ static float number(const u32x4* x, int e) {
+    if (M32) return __uint_as_float(x[e / 4][e % 4]);
+    return (float)__builtin_bit_cast(half8, x[0])[e];
+  }
+  // step and mean term: x = step (c - mid) + base
+  __device__ __forceinline__ void step_and_base(bool zp_min, float mid, half8& step, half8& base) const {
+    if (M32) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float s = number(a, e), z = number(b, e);
+        step[e] = (_Float16)fminf(s, kHalfMax);
+        base[e] = (_Float16)__builtin_amdgcn_fmed3f(zp_min ? fmaf(s, mid, z) : (mid - z) * s, -kHalfMax, kHalfMax);
+      }
+    } else {
+      step = __builtin_bit_cast(half8, a[0]);
+      const half8 z = __builtin_bit_cast(half8, b[0]), m = (_Float16)mid, most = (_Float16)kHalfMax;
+      const half8 t = m - z;
+      base = zp_min ? __builtin_elementwise_fma(step, m, z) : t * step;
+      base = __builtin_elementwise_min(__builtin_elementwise_max(base, -most), most);
+    }
+  }
+};
 
 __device__ __forceinline__ float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ half2v pack2(float a, float b) {
-  return __builtin_convertvector((float2v){a, b}, half2v);
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v){a, b}, half2v));
 }
 __device__ __forceinline__ float max_of_row(float v) {   // over the four lanes that hold a query row
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
-// The running state of one tile of 16 query rows: lane's row = lane % 16.
-struct RowTile {
-  float4v o[8];   // channels 16 ct + 4 (lane / 16) + r, in units of the codes once pages have begun
-  float4v x;      // of rows 4 (lane / 16) + r of the extra tile: zero terms of the value groups, then the row sum
-  float m;        // running maximum, log2 units
-};
+// Workgroups a CU that a variant's registers are held to.
+__host__ __device__ constexpr int wgs_per_cu(int nr) { return nr == 1 ? 4 : nr == 2 ? 3 : 2; }
 
 template <int BITS, bool M32, int NR>
-__global__ __launch_bounds__(256, 2) void oscar_draft_kernel(DraftParams P) {
+__global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftParams P) {
   using C = Codes<BITS>;
   constexpr int ROWS = NR * 16;
-  constexpr int OROW = D + 4;
-  __shared__ __align__(16) float s_o[4][ROWS][OROW];
-  __shared__ float s_m[4][ROWS], s_l[4][ROWS];
+  constexpr int UNITS = C::BPMAX - C::BPMIN;         // log2 of what the counterweights leave in the extra tile
+  __shared__ __align__(16) half8 s_qh[NR][4][64], s_qc[NR][4][64];   // queries as operands: natural order, codes' order
+  __shared__ __align__(16) uint32_t s_p[NR][4][64][4];               // probabilities as operands
+  __shared__ __align__(16) float s_max[ROWS][4];
+  __shared__ __align__(16) Staged s_meta[3];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, q4 = lane >> 4;
@@ -148,38 +168,124 @@ __global__ __launch_bounds__(256, 2) void oscar_draft_kernel(DraftParams P) {
   const int rows = min(max(n_new * g - row0, 0), ROWS);         // of this block that are there
   const bool zp_min = P.c.cfg.zp_mode == OSCAR_ZP_MIN;
   const bool bf16 = P.c.cfg.io_dtype == OSCAR_BF16;
+  const int row_of_tile = 4 * (n % 4) + n / 4;                  // token of a tile that this lane's row is
 
-  RowTile tile[NR];
+  float4v o[NR][2];   // channels 32 wave + 16 j + 4 q4 + r of row n, in units of the codes once pages have begun
+  float4v x[NR];      // [0]: zero terms of the wave's value group, [1]: the row's sum
+  float m[NR];        // running maximum, log2 units
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
-#pragma unroll
-    for (int ct = 0; ct < 8; ++ct) tile[i].o[ct] = (float4v){0, 0, 0, 0};
-    tile[i].x = (float4v){0, 0, 0, 0};
-    tile[i].m = -INFINITY;
+    o[i][0] = o[i][1] = x[i] = (float4v){0, 0, 0, 0};
+    m[i] = -INFINITY;
   }
   int eoff = 15;
 
   if (rows > 0) {
-    // ---- queries: lane's row, channels 32 q4 .. + 31 ----
-    half8 qh[NR][4];
-    const uint16_t* q = reinterpret_cast<const uint16_t*>(P.q);
-    int row_t[NR];
+    // what the pages are: tail units (window, then new tokens, 128 each) and packed pages, dealt to the splits
+    const int last_t = (row0 + rows - 1) / g;                            // last new token any row here sees
+    const int n_win = res > 0 ? 1 : 0;
+    const int n_tail = n_win + (min(n_new, last_t + 1) + R - 1) / R;
+    const int step = P.num_splits;
+    int page = split < n_tail ? split + (n_tail - split + step - 1) / step * step - n_tail : split - n_tail;
+    const int32_t* table = P.c.block_table + (size_t)b * P.c.max_pages_per_seq;
+    // Physical page of page p; what is none is marked (its metadata is staged as zeros and its tokens are left
+    // out), and loads past the end take a page again: every iteration then makes the same loads.
+    struct Page {
+      int phys;
+      bool held;
+    };
+    auto page_at = [&](int p) {
+      const int phys = table[min(max(p, 0), max(pages - 1, 0))];
+      const bool ok = phys >= 0 && phys < P.c.num_pages;
+      return Page{ok ? phys : 0, ok && p < pages};
+    };
+
+    // ---- loads ahead ----
+    uint32_t kc[2 * BITS], vc[2 * BITS];
+    const size_t k_stride = (size_t)Hkv * P.g.k_codes_bytes, v_stride = (size_t)Hkv * P.g.v_codes_bytes;
+    const uint8_t* k_pool = reinterpret_cast<const uint8_t*>(P.c.k_codes) + (size_t)kvh * P.g.k_codes_bytes;
+    const uint8_t* v_pool = reinterpret_cast<const uint8_t*>(P.c.v_codes) + (size_t)kvh * P.g.v_codes_bytes;
+    const uint32_t k_at = chunk_offset(BITS, 2 * wave, row_of_tile, q4), v_at = chunk_offset(BITS, 2 * wave, n, q4);
+    auto load_codes = [&](const uint8_t* page, uint32_t at, uint32_t* w) {
+#pragma unroll
+      for (int j = 0; j < BITS / 2; ++j) *reinterpret_cast<u32x4*>(w + 4 * j) = *reinterpret_cast<const u32x4*>(page + at + 16 * j);
+    };
+    constexpr int MB = M32 ? 4 : 2;
+    const int m_bytes = wave == 0 ? P.g.k_meta_bytes : wave == 1 ? P.g.v_meta_bytes : P.g.k_norms_bytes;
+    const int m_groups = wave == 0 ? P.g.ngk : wave == 1 ? P.g.ngv : 1;
+    const uint8_t* m_pool = reinterpret_cast<const uint8_t*>(wave == 0 ? P.c.k_meta : wave == 1 ? P.c.v_meta : P.c.k_norms) +
+                            (size_t)kvh * m_bytes;
+    const size_t m_stride = (size_t)Hkv * m_bytes;
+    const uint32_t m_zero = wave < 2 ? (uint32_t)m_groups * 128 * MB : 0, m_at = (uint32_t)min(lane, 16 * m_groups - 1) * 8 * MB;
+    Fetched<M32> f;
+    auto fetch_meta = [&](const Page& pg) {
+      const uint8_t* src = m_pool + pg.phys * m_stride;
+      f.load(src, src + m_zero, m_at);
+    };
+    auto stage_meta = [&](Staged& s, bool held) {
+      if (wave >= 2) {
+        if (wave == 2 && lane < 16) {
+          constexpr float unit_of_codes = (float)(1 << (24 - C::BPMIN - kQShift));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s.norm[8 * lane + e] = held ? f.number(f.a, e) * unit_of_codes : 0.0f;
+        }
+        return;
+      }
+      half8 st, base;
+      f.step_and_base(zp_min, C::MID, st, base);
+      const int kk = wave == 0 ? lane : lane / 4;
+      base *= kk % 2 == 0 ? C::counterweight(0) : C::counterweight(1);
+      if (!held) st = base = (half8)(_Float16)0.0f;
+      if (wave == 0) {
+        s.k_step[lane] = st;
+        s.k_base[lane] = base;
+        return;
+      }
+      s.v_step[lane] = st;
+      s.v_base[lane] = base;
+      // the exponent of the largest step (fp16 bits; steps are not negative), bit by bit over the wave
+      uint32_t big = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t two = __builtin_bit_cast(u32x4, st)[e];
+        big = max(big, max(two & 0xffffu, two >> 16));
+      }
+      uint64_t among = ~0ull;
+      int exponent = 0;
+#pragma unroll
+      for (int bit = 14; bit >= 10; --bit) {
+        const uint64_t have = __ballot(big >> bit & 1) & among;
+        if (have) among = have, exponent |= 1 << (bit - 10);
+      }
+      if (lane == 0) s.off = 15 - max(exponent - 14, 0);
+    };
+
+    // page, page + 1 step, page + 2 steps: the codes of the first two and the metadata of all are on their way
+    Page pg0 = page_at(page), pg1 = page_at(page + step), pg2 = page_at(page + 2 * step);
+    fetch_meta(pg0);
+    load_codes(k_pool + pg0.phys * k_stride, k_at, kc);
+    load_codes(v_pool + pg0.phys * v_stride, v_at, vc);
+
+    // ---- queries: lane's row, channels 32 q4 .. + 31; wave i rotates tile i ----
     const uint16_t* q_row[NR];
+    int row_t[NR];
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       const int row = row0 + 16 * i + n;
       row_t[i] = row / g;
       const bool there = row < n_new * g;
-      q_row[i] = q + (((size_t)b * P.T + (there ? row_t[i] : 0)) * Hq + (size_t)kvh * g + (there ? row % g : 0)) * D + 32 * q4;
-      float x[32];
+      q_row[i] = reinterpret_cast<const uint16_t*>(P.q) +
+                 (((size_t)b * P.T + (there ? row_t[i] : 0)) * Hq + (size_t)kvh * g + (there ? row % g : 0)) * D + 32 * q4;
+      if (wave != i) continue;
+      float y[32];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(q_row[i] + 8 * u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint16_t v = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
-          const float f = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
-          x[8 * u + e] = there ? f : 0.0f;
+          const float t = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
+          y[8 * u + e] = there ? t : 0.0f;
         }
       }
       float mul = P.scale_log2 * (float)(1 << kQShift);
@@ -189,9 +295,9 @@ __global__ __launch_bounds__(256, 2) void oscar_draft_kernel(DraftParams P) {
 #pragma unroll
           for (int u = 0; u < 32; ++u) {
             if ((u & h) == 0) {
-              const float a = x[u], c = x[u | h];
-              x[u] = a + c;
-              x[u | h] = a - c;
+              const float a = y[u], c = y[u | h];
+              y[u] = a + c;
+              y[u | h] = a - c;
             }
           }
         }
@@ -199,25 +305,76 @@ __global__ __launch_bounds__(256, 2) void oscar_draft_kernel(DraftParams P) {
         for (int s = 0; s < 2; ++s) {
           const float sg = (q4 >> s) & 1 ? -1.0f : 1.0f;
 #pragma unroll
-          for (int u = 0; u < 32; ++u) x[u] = fmaf(x[u], sg, __shfl_xor(x[u], 16 << s, 64));
+          for (int u = 0; u < 32; ++u) {
+            // (each call leaves the two lanes' numbers side by side in both)
+            const uint32_t v = __float_as_uint(y[u]);
+            const auto two = s == 0 ? __builtin_amdgcn_permlane16_swap(v, v, false, false)
+                                    : __builtin_amdgcn_permlane32_swap(v, v, false, false);
+            y[u] = fmaf(__uint_as_float(two[1]), sg, __uint_as_float(two[0]));
+          }
         }
         mul *= 0.08838834764831845f;
       }
+      half8 qh[4];
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          qh[i][kk][e] = (_Float16)(x[8 * kk + e] * mul);
+        for (int e = 0; e < 8; ++e) qh[kk][e] = (_Float16)(y[8 * kk + e] * mul);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        half8 qc;   // in the codes' order, with the counterweights of their bit positions
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int u = slot_index(BITS, kk, e);
+          qc[e] = qh[u / 8][u % 8] * (_Float16)(1.0f / (float)(1 << C::above(kk, e)));
+        }
+        s_qh[i][kk][lane] = qh[kk];
+        s_qc[i][kk][lane] = qc;
+      }
     }
+    stage_meta(s_meta[0], pg0.held);
+    fetch_meta(pg1);
+    stage_meta(s_meta[1], pg1.held);
+    fetch_meta(pg2);
+    __syncthreads();
 
-    // ---- 16-bit tokens: the window's pieces, then the new tokens', dealt to the waves of all splits ----
-    const int waves = P.num_splits * 4, own = split * 4 + wave;
-    const int n_win = (res + TAIL - 1) / TAIL;
-    const int last_t = (row0 + rows - 1) / g;                            // last new token any row here sees
-    const int n_tail = n_win + (min(n_new, last_t + 1) + TAIL - 1) / TAIL;
-    for (int u = own; u < n_tail; u += waves) {
+    // Rows' maxima joined, state rescaled, probabilities to LDS; s[i][j][r]: logit (log2 units) of the wave's
+    // token 16 (2 wave + j) + 4 r + q4.  even, odd: weights' exponents of the k-steps.  Two barriers.
+    auto softmax = [&](float4v (&s)[NR][2], int off, int even, int odd) {
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        float mx = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
+                         fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3])));
+        mx = max_of_row(mx);
+        if (q4 == 0) s_max[16 * i + n][wave] = mx;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const float4v mw = *reinterpret_cast<const float4v*>(s_max[16 * i + n]);
+        const float mn = fmaxf(m[i], fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3])));
+        if (__any(mn > m[i]) || off != eoff) {
+          const float alpha = m[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[i] - mn + (float)(off - eoff));
+          o[i][0] *= alpha;
+          o[i][1] *= alpha;
+          x[i] *= alpha;
+          m[i] = mn;
+        }
+        const float M = mn == -INFINITY ? 0.0f : mn - (float)off;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float Mk = M + (float)(r % 2 == 0 ? even : odd);
+          s_p[i][r][lane][wave] = pack2(__builtin_amdgcn_exp2f(s[i][0][r] - Mk), __builtin_amdgcn_exp2f(s[i][1][r] - Mk));
+        }
+      }
+      eoff = off;
+      __syncthreads();
+    };
+
+    // ---- 16-bit tokens ----
+    for (int u = split; u < n_tail; u += step) {
       const bool win = u < n_win;
-      const int t0 = (win ? u : u - n_win) * TAIL, count = win ? res : n_new;
+      const int t0 = win ? 0 : (u - n_win) * R, count = win ? res : n_new;
       const size_t head = (size_t)b * Hkv + kvh;
       const uint16_t *kb, *vb;
       size_t stride;
@@ -230,326 +387,213 @@ __global__ __launch_bounds__(256, 2) void oscar_draft_kernel(DraftParams P) {
         vb = reinterpret_cast<const uint16_t*>(P.v_new) + ((size_t)b * P.T * Hkv + kvh) * D;
         stride = (size_t)Hkv * D;
       }
-      // logits: tile s holds tokens t0 + 16 s + .., row n of the tile = token n of it
-      float4v S[NR][2];
+      float4v s[NR][2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int t = min(t0 + 16 * s + n, count - 1);
-        u32x4 a[4];
+      for (int j = 0; j < 2; ++j) {
+        const int tile0 = t0 + 16 * (2 * wave + j);
+        if (tile0 < count) {
+          const int t = min(tile0 + row_of_tile, count - 1);
+          u32x4 a[4];
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) a[kk] = *reinterpret_cast<const u32x4*>(kb + (size_t)t * stride + 32 * q4 + 8 * kk);
+          for (int kk = 0; kk < 4; ++kk) a[kk] = *reinterpret_cast<const u32x4*>(kb + (size_t)t * stride + 32 * q4 + 8 * kk);
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          float4v acc = {0, 0, 0, 0};
+          for (int i = 0; i < NR; ++i) {
+            float4v acc = {0, 0, 0, 0};
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            if (win) {
-              acc = mfma(__builtin_bit_cast(half8, a[kk]), qh[i][kk], acc);
-            } else {
-              const u32x4 r = *reinterpret_cast<const u32x4*>(q_row[i] + 8 * kk);
-              if (bf16)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[kk]),
-                                                              __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
-              else
-                acc = mfma(__builtin_bit_cast(half8, a[kk]), __builtin_bit_cast(half8, r), acc);
+            for (int kk = 0; kk < 4; ++kk) {
+              if (win) {
+                acc = mfma(__builtin_bit_cast(half8, a[kk]), s_qh[i][kk][lane], acc);
+              } else {
+                const u32x4 r = *reinterpret_cast<const u32x4*>(q_row[i] + 8 * kk);
+                if (bf16)
+                  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[kk]),
+                                                                __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
+                else
+                  acc = mfma(__builtin_bit_cast(half8, a[kk]), __builtin_bit_cast(half8, r), acc);
+              }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int tok = tile0 + 4 * r + q4;
+              const float fac = win ? load_meta(P.c.res_norm, head * R + min(tok, R - 1), M32 ? 4 : 2) * (1.0f / (1 << kQShift))
+                                    : P.scale_log2;
+              s[i][j][r] = tok < count && (win || tok <= row_t[i]) ? acc[r] * fac : -INFINITY;
             }
           }
-          S[i][s] = acc;
+        } else {
+#pragma unroll
+          for (int i = 0; i < NR; ++i) s[i][j] = (float4v){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
         }
       }
-      float f[2][4];
+      softmax(s, eoff, 0, 0);
+      // values: channel 32 wave + 16 j + n of tokens t0 + 16 e + 4 kk + q4
+      const half8 one = (_Float16)(n % 4 == 1 ? 1.0f / (1 << UNITS) : 0.0f);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int kk = 0; kk < 4; ++kk) {
+        half8 a[2];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = t0 + 16 * s + 4 * q4 + r;
-          f[s][r] = win ? load_meta(P.c.res_norm, head * R + min(t, R - 1), M32 ? 4 : 2) * (1.0f / (1 << kQShift)) : P.scale_log2;
+        for (int e = 0; e < 8; ++e) {
+          const int t = t0 + 16 * e + 4 * kk + q4;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float y = 0.0f;
+            if (t0 + 16 * e < count) {
+              const uint16_t v = vb[(size_t)min(t, count - 1) * stride + 32 * wave + 16 * j + n];
+              y = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
+              y = t < count ? __builtin_amdgcn_fmed3f(y, -kHalfMax, kHalfMax) : 0.0f;
+            }
+            a[j][e] = (_Float16)y;
+          }
         }
-      half8 pr[NR];
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = t0 + 16 * s + 4 * q4 + r;
-            const bool seen = t < count && (win || t <= row_t[i]);
-            const float v = seen ? S[i][s][r] * f[s][r] : -INFINITY;
-            S[i][s][r] = v;
-            mx = fmaxf(mx, v);
-          }
-        const float m = fmaxf(tile[i].m, max_of_row(mx));
-        const float M = m == -INFINITY ? 0.0f : m - eoff;
-        const float alpha = tile[i].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(tile[i].m - m);
-        tile[i].m = m;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) pr[i][4 * s + r] = (_Float16)__builtin_amdgcn_exp2f(S[i][s][r] - M);
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct) tile[i].o[ct] *= alpha;
-        tile[i].x *= alpha;
-        half8 one;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) one[e] = (_Float16)(n == 4 ? 1.0f / (1 << (C::BPMAX - C::BPMIN)) : 0.0f);
-        tile[i].x = mfma(one, pr[i], tile[i].x);
-      }
-      // values: channel 16 ct + n of tokens t0 + 16 s + 4 q4 + r
-#pragma unroll
-      for (int ct = 0; ct < 8; ++ct) {
-        half8 a;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = t0 + 16 * s + 4 * q4 + r;
-            const uint16_t v = vb[(size_t)min(t, count - 1) * stride + 16 * ct + n];
-            const float x = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
-            a[4 * s + r] = (_Float16)(t < count ? __builtin_amdgcn_fmed3f(x, -kHalfMax, kHalfMax) : 0.0f);
-          }
-#pragma unroll
-        for (int i = 0; i < NR; ++i) tile[i].o[ct] = mfma(a, pr[i], tile[i].o[ct]);
+        for (int i = 0; i < NR; ++i) {
+          const half8 p = *reinterpret_cast<const half8*>(s_p[i][kk][lane]);
+          o[i][0] = mfma(a[0], p, o[i][0]);
+          o[i][1] = mfma(a[1], p, o[i][1]);
+          x[i] = mfma(one, p, x[i]);
+        }
       }
     }
 
     // ---- pages ----
-    // queries in the codes' order, with the counterweights of their bit positions
-    half8 qc[NR][4];
-#pragma unroll
-    for (int i = 0; i < NR; ++i)
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int u = slot_index(BITS, kk, e);
-          qc[i][kk][e] = qh[i][u / 8][u % 8] * (_Float16)(1.0f / (float)(1 << C::above(kk, e)));
-        }
     constexpr float kCodeUnit = 1.0f / (float)(1 << (24 - C::BPMIN));     // of a code in the sums
 #pragma unroll
-    for (int i = 0; i < NR; ++i)
-#pragma unroll
-      for (int ct = 0; ct < 8; ++ct) tile[i].o[ct] *= kCodeUnit;
-    const int row_of_tile = 4 * (n % 4) + n / 4;                          // token of a tile that this lane's row is
-
-    for (int u = own < n_tail ? own + (n_tail - own + waves - 1) / waves * waves : own; u - n_tail < pages; u += waves) {
-      const int phys = P.c.block_table[(size_t)b * P.c.max_pages_per_seq + (u - n_tail)];
-      if (phys < 0 || phys >= P.c.num_pages) continue;
-      const size_t pg = (size_t)phys * Hkv + kvh;
-      const uint8_t* kcodes = reinterpret_cast<const uint8_t*>(P.c.k_codes) + pg * P.g.k_codes_bytes;
-      const uint8_t* kmeta = reinterpret_cast<const uint8_t*>(P.c.k_meta) + pg * P.g.k_meta_bytes;
-      const uint8_t* knorm = reinterpret_cast<const uint8_t*>(P.c.k_norms) + pg * P.g.k_norms_bytes;
-      const uint8_t* vcodes = reinterpret_cast<const uint8_t*>(P.c.v_codes) + pg * P.g.v_codes_bytes;
-      const uint8_t* vmeta = reinterpret_cast<const uint8_t*>(P.c.v_meta) + pg * P.g.v_meta_bytes;
-      uint32_t kc[4][2 * BITS], vc[4][2 * BITS];
-#pragma unroll
-      for (int w = 0; w < 4; ++w)
-#pragma unroll
-        for (int j = 0; j < BITS / 2; ++j) {
-          *reinterpret_cast<u32x4*>(&kc[w][4 * j]) =
-              *reinterpret_cast<const u32x4*>(kcodes + chunk_offset(BITS, 2 * w, row_of_tile, q4) + 16 * j);
-          *reinterpret_cast<u32x4*>(&vc[w][4 * j]) =
-              *reinterpret_cast<const u32x4*>(vcodes + chunk_offset(BITS, 2 * w, n, q4) + 16 * j);
-        }
-
-      // logits of 128 tokens
-      float4v S[NR][8];
+    for (int i = 0; i < NR; ++i) {
+      o[i][0] *= kCodeUnit;
+      o[i][1] *= kCodeUnit;
+    }
+    // the wave's groups in the staged metadata, its probabilities' weights, constants of the middle
+    const int gk = wave * 32 / P.g.k_group * 16, gv = wave * 32 / P.g.v_group * 16;
+    const int even = BITS == 2 ? 2 * (wave % 2) : 4 * (wave % 2);
+    const int odd = BITS == 2 ? (wave == 0 || wave == 3 ? 4 : 2 * (wave - 1)) : 4 * (wave % 2);
+    for (int buf = 0; page < pages; page += step) {
+      const Staged& meta = s_meta[buf];
+      // logits
+      float4v s[NR][2], start[NR];
       half8 qd[NR][4];
-      float4v start[NR];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        if (w * 32 % P.g.k_group == 0) {
-          const int gk = w * 32 / P.g.k_group;
-#pragma unroll
-          for (int i = 0; i < NR; ++i) start[i] = (float4v){0, 0, 0, 0};
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            const int at = gk * D + 32 * q4 + 8 * kk;
-            const half8 step = load_step<M32>(kmeta, at);
-            const half8 zb = load_b<M32>(kmeta, at, P.g.ngk * D + at, zp_min) * C::counterweight(kk);
-#pragma unroll
-            for (int i = 0; i < NR; ++i) {
-              qd[i][kk] = qc[i][kk] * step;
-              start[i] = mfma(zb, qc[i][kk], start[i]);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < NR; ++i) start[i] *= 1.0f / (float)(1 << (24 - C::BPMAX));
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-          for (int i = 0; i < NR; ++i) S[i][2 * w + j] = start[i];
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            const half8 a = C::operand(kc[w] + j * BITS, kk);
-#pragma unroll
-            for (int i = 0; i < NR; ++i) S[i][2 * w + j] = mfma(a, qd[i][kk], S[i][2 * w + j]);
-          }
-        }
-      }
-
-      // the extra tile's rows: zero terms of the value groups (0 .. 3), row sum (4)
-      half8 extra[4];
-      uint32_t big = 0;   // largest value step (fp16 bits) of this lane's group
+      for (int i = 0; i < NR; ++i) start[i] = (float4v){0, 0, 0, 0};
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        const int at = min(n, P.g.ngv - 1) * R + (4 * kk + q4) * 8;
-        const half8 step = load_step<M32>(vmeta, at);
-        const half8 zb = load_b<M32>(vmeta, at, P.g.ngv * R + at, zp_min);
-        const half8 cw = C::counterweight(kk);
+        const half8 st = meta.k_step[gk + 4 * q4 + kk], base = meta.k_base[gk + 4 * q4 + kk];
+        const half8 mid = C::counterweight(kk) * (_Float16)-C::MID;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          extra[kk][e] = n == 4 ? cw[e] : zb[e] * cw[e];
-          big = max(big, (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)step[e]));
+        for (int i = 0; i < NR; ++i) {
+          const half8 qc = s_qc[i][kk][lane];
+          qd[i][kk] = qc * st;
+          start[i] = mfma(base, qc, start[i]);
+          start[i] = mfma(mid, qd[i][kk], start[i]);
         }
       }
-      int page_off = 15;
-      if (__any(big >= 0x4000u)) {
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, s, 64));
-        page_off = __builtin_amdgcn_readfirstlane(15 - max((int)(big >> 10) - 14, 0));
-      }
-      const int off = min(eoff, page_off);
-
-      // probabilities
-      float nrm[4][8];
+      for (int i = 0; i < NR; ++i) s[i][0] = s[i][1] = start[i] * (1.0f / (float)(1 << (24 - C::BPMAX)));
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int t = 0; t < 8; ++t)
-          nrm[r][t] = load_meta(knorm, (4 * r + q4) * 8 + t, M32 ? 4 : 2) * (float)(1 << (24 - C::BPMIN - kQShift));
-      half8 pr[NR][4];
+        for (int kk = 0; kk < 4; ++kk) {
+          const half8 a = C::operand(kc + j * BITS, kk);
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            S[i][t][r] *= nrm[r][t];
-            mx = fmaxf(mx, S[i][t][r]);
-          }
-        const float m = fmaxf(tile[i].m, max_of_row(mx));
-        if (__any(m > tile[i].m) || off != eoff) {
-          const float alpha = tile[i].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(tile[i].m - m + (float)(off - eoff));
-#pragma unroll
-          for (int ct = 0; ct < 8; ++ct) tile[i].o[ct] *= alpha;
-          tile[i].x *= alpha;
-          tile[i].m = m;
+          for (int i = 0; i < NR; ++i) s[i][j] = mfma(a, qd[i][kk], s[i][j]);
         }
-        const float M = m - (float)off;
+      load_codes(k_pool + pg1.phys * k_stride, k_at, kc);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < 4; ++r) {
+        const float2v nm = *reinterpret_cast<const float2v*>(&meta.norm[(4 * r + q4) * 8 + 2 * wave]);
 #pragma unroll
-          for (int t = 0; t < 8; t += 2) {
-            const float Mk = M + (float)C::above(r, t);
-            const half2v p = pack2(__builtin_amdgcn_exp2f(S[i][t][r] - Mk), __builtin_amdgcn_exp2f(S[i][t + 1][r] - Mk));
-            pr[i][r][t] = p[0];
-            pr[i][r][t + 1] = p[1];
-          }
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) tile[i].x = mfma(extra[kk], pr[i][kk], tile[i].x);
+        for (int i = 0; i < NR; ++i) {
+          s[i][0][r] *= nm[0];
+          s[i][1][r] *= nm[1];
+        }
       }
-      eoff = off;
-
+      if (!pg0.held) {   // no page: its tokens are left out
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+          s[i][0] = s[i][1] = (float4v){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+      softmax(s, min(eoff, __builtin_amdgcn_readfirstlane(meta.off)), even, odd);
       // values
-      half8 pd[NR][4];
+      half8 st[4], base[4];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        if (w * 32 % P.g.v_group == 0) {
-          const int gv = w * 32 / P.g.v_group;
+      for (int kk = 0; kk < 4; ++kk) {
+        st[kk] = meta.v_step[gv + 4 * kk + q4];
+        base[kk] = meta.v_base[gv + 4 * kk + q4];
+        const half8 cw = C::counterweight(kk);
+        base[kk] = n % 4 == 1 ? cw : base[kk];
+      }
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            const half8 step = load_step<M32>(vmeta, gv * R + (4 * kk + q4) * 8);
+      for (int kk = 0; kk < 4; ++kk) {
+        const half8 mid = C::counterweight(kk) * (_Float16)(n % 4 == 0 ? -C::MID : 0.0f);
+        const half8 a0 = C::operand(vc, kk), a1 = C::operand(vc + BITS, kk);
 #pragma unroll
-            for (int i = 0; i < NR; ++i) pd[i][kk] = pr[i][kk] * step;
-          }
+        for (int i = 0; i < NR; ++i) {
+          const half8 p = *reinterpret_cast<const half8*>(s_p[i][kk][lane]);
+          const half8 pd = p * st[kk];
+          x[i] = mfma(base[kk], p, x[i]);
+          x[i] = mfma(mid, pd, x[i]);
+          o[i][0] = mfma(a0, pd, o[i][0]);
+          o[i][1] = mfma(a1, pd, o[i][1]);
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            const half8 a = C::operand(vc[w] + j * BITS, kk);
-#pragma unroll
-            for (int i = 0; i < NR; ++i) tile[i].o[2 * w + j] = mfma(a, pd[i][kk], tile[i].o[2 * w + j]);
-          }
       }
-    }
-    // back to numbers: codes' unit, zero terms of each channel's value group
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      tile[i].x *= (float)(1 << (C::BPMAX - C::BPMIN));
-      float zb[4];
-#pragma unroll
-      for (int gv = 0; gv < 4; ++gv) zb[gv] = __shfl(tile[i].x[gv], n, 64);
-#pragma unroll
-      for (int ct = 0; ct < 8; ++ct) {
-        const int gv = ct * 16 / P.g.v_group;
-        const float z = gv == 0 ? zb[0] : gv == 1 ? zb[1] : gv == 2 ? zb[2] : zb[3];
-        tile[i].o[ct] = tile[i].o[ct] * (float)(1 << (24 - C::BPMIN)) + z;
-      }
+      load_codes(v_pool + pg1.phys * v_stride, v_at, vc);
+      // every wave has left the page before this one: its buffer takes the page after next
+      const int into = buf == 0 ? 2 : buf - 1;
+      stage_meta(s_meta[into], pg2.held);
+      pg0 = pg1;
+      pg1 = pg2;
+      pg2 = page_at(page + 3 * step);
+      fetch_meta(pg2);
+      buf = buf == 2 ? 0 : buf + 1;
     }
   }
 
-  // ---- the four waves joined ----
+  // ---- back to numbers, and out ----
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
-    const float l = __shfl(tile[i].x[0], 16 + n, 64);
-    if (q4 == 0) {
-      s_m[wave][16 * i + n] = tile[i].m == -INFINITY ? -INFINITY : tile[i].m - (float)eoff;
-      s_l[wave][16 * i + n] = l;
-    }
+    const int row = row0 + 16 * i + n;
+    if (row >= P.T * g) continue;
+    const bool there = 16 * i + n < rows;
+    const float zero = x[i][0] * (float)(1 << UNITS), l = x[i][1] * (float)(1 << UNITS);
+    const size_t out_row = ((size_t)b * P.T + row / g) * Hq + kvh * g + row % g;
+    const float inv = there && l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-    for (int ct = 0; ct < 8; ++ct) *reinterpret_cast<float4v*>(&s_o[wave][16 * i + n][16 * ct + 4 * q4]) = tile[i].o[ct];
-  }
-  __syncthreads();
-  const int c4 = (tid & 31) * 4;
-  for (int row = tid >> 5; row < ROWS; row += 8) {
-    if (row0 + row >= P.T * g) break;
-    float M = -INFINITY;
+    for (int j = 0; j < 2; ++j) {
+      const int c = 32 * wave + 16 * j + 4 * q4;
+      float4v y = o[i][j] * (float)(1 << (24 - C::BPMIN)) + zero;
+      if (!there) y = (float4v){0, 0, 0, 0};
+      if (P.num_splits > 1) {
+        float* rec = P.ws + (out_row * P.num_splits + split) * WS_STRIDE + c;
+        *reinterpret_cast<float2v*>(rec) = (float2v){y[0], y[1]};
+        *reinterpret_cast<float2v*>(rec + 2) = (float2v){y[2], y[3]};
+      } else {
+        uint16_t v[4];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, s_m[w][row]);
-    float4v o = {0, 0, 0, 0};
-    float l = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if (s_m[w][row] == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(s_m[w][row] - M);
-      o += *reinterpret_cast<const float4v*>(&s_o[w][row][c4]) * f;
-      l = fmaf(s_l[w][row], f, l);
-    }
-    const bool there = row < rows;
-    const int t = (row0 + row) / g, h = kvh * g + (row0 + row) % g;
-    const size_t out_row = ((size_t)b * P.T + t) * Hq + h;
-    if (P.num_splits > 1) {
-      float* rec = P.ws + (out_row * P.num_splits + split) * WS_STRIDE;
-      *reinterpret_cast<float2v*>(rec + c4) = there ? (float2v){o[0], o[1]} : (float2v){0, 0};
-      *reinterpret_cast<float2v*>(rec + c4 + 2) = there ? (float2v){o[2], o[3]} : (float2v){0, 0};
-      if (c4 == 0) *reinterpret_cast<float2v*>(rec + D) = there ? (float2v){M, l} : (float2v){-INFINITY, 0};
-    } else {
-      const float inv = there && l > 0.0f ? 1.0f / l : 0.0f;
-      uint16_t* dst = reinterpret_cast<uint16_t*>(P.out) + out_row * D + c4;
-      uint16_t v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = there ? o[e] * inv : 0.0f;
-        v[e] = bf16 ? __builtin_bit_cast(uint16_t, __float2bfloat16(x)) : __builtin_bit_cast(uint16_t, __float2half_rn(x));
+        for (int e = 0; e < 4; ++e)
+          v[e] = bf16 ? __builtin_bit_cast(uint16_t, __float2bfloat16(y[e] * inv))
+                      : __builtin_bit_cast(uint16_t, __float2half_rn(y[e] * inv));
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(P.out) + out_row * D + c) =
+            make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
       }
-      *reinterpret_cast<uint2*>(dst) = make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
     }
+    if (P.num_splits > 1 && wave == 0 && q4 == 0)
+      *reinterpret_cast<float2v*>(P.ws + (out_row * P.num_splits + split) * WS_STRIDE + D) =
+          there && m[i] > -INFINITY ? (float2v){m[i] - (float)eoff, l} : (float2v){-INFINITY, 0};
   }
 }
 
 template <int BITS, bool M32> void launch(const DraftParams& P, int nr, dim3 grid, hipStream_t st) {
-  if (nr == 1)
-    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 1>), grid, dim3(256), 0, st, P);
-  else
-    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 2>), grid, dim3(256), 0, st, P);
+  switch (nr) {
+    case 1: hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 1>), grid, dim3(256), 0, st, P); break;
+    case 2: hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 2>), grid, dim3(256), 0, st, P); break;
+    case 3: hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 3>), grid, dim3(256), 0, st, P); break;
+    default: hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 4>), grid, dim3(256), 0, st, P); break;
+  }
 }
 
-// tiles of 16 query rows a wave holds
-int row_tiles(const oscar_config& cfg, int T) { return (int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) <= 16 ? 1 : 2; }
+// tiles of 16 query rows a workgroup takes
+int row_tiles(const oscar_config& cfg, int T) {
+  const int64_t tiles = ((int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) + 15) / 16;
+  return tiles < 4 ? (int)tiles : 4;
+}
 int64_t row_blocks(const oscar_config& cfg, int T) {
   const int rows = 16 * row_tiles(cfg, T);
   return ((int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) + rows - 1) / rows;
@@ -567,8 +611,8 @@ extern "C" int32_t oscar_draft_auto_splits(const oscar_config* cfg, int32_t batc
   if (check_draft_config(cfg) != OSCAR_OK || batch <= 0 || T <= 0) return 1;
   const int64_t units = (int64_t)batch * cfg->n_kv_heads * row_blocks(*cfg, T);
   const int64_t pages = max_seq_len > 0 ? ((int64_t)max_seq_len + R - 1) / R : 1;
-  int64_t splits = 2 * (int64_t)oscar_compute_units() / units;
-  if (splits > (pages + 3) / 4) splits = (pages + 3) / 4;
+  int64_t splits = wgs_per_cu(row_tiles(*cfg, T)) * (int64_t)oscar_compute_units() / units;
+  if (splits > pages) splits = pages;
   if (splits > 512) splits = 512;
   return splits < 1 ? 1 : (int32_t)splits;
 }
