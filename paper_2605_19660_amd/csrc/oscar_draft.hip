@@ -25,8 +25,8 @@
 // the zero-points is of the size of a group's mean, and both are products on the matrix cores too: for the keys
 // what a tile's sums start from, for the values one extra tile, whose other rows are the rows' sums.  Seen from
 // code 0 the same roundings moved the logits three times as far.  Roundings: Q, Q Delta, P, P Delta and the
-// mean terms to fp16, half a step (2^-11) each.  The probabilities are scaled by 2^15 (less where a value step
-// of 2 or more would carry P Delta past the fp16 range): a token counts down to 2^-39 of the largest.  Sums,
+// mean terms to fp16, half a step (2^-11) each.  The probabilities are scaled by 2^9 .. 2^15 (less where a value
+// step of 2 or more would carry P Delta past the fp16 range): a token counts down to 2^-33 of the largest.  Sums,
 // maxima and outputs are fp32.
 #include "oscar_decode_common.h"
 
@@ -89,10 +89,15 @@ template <int BITS> struct Codes {
 // order, norms as fp32 with the codes' unit taken out.
 struct Staged {
   half8 k_step[64], k_base[64];   // [group][quarter][k-step]
-  half8 v_step[64], v_base[64];   // [group][k-step][quarter]
+  half8 v_step[64], v_base[80];   // [group][k-step][quarter]; behind the four groups the counterweights alone
   float norm[R];                  // position (token % 16) * 8 + token / 16
   int off;                        // exponent the probabilities can carry
 };
+// A row's probabilities are taken against a reference that follows its maximum only when that has passed it by
+// 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs the workgroup a
+// barrier and a rescaling.
+constexpr float kSlack = 6.0f, kNone = -3e38f;
+constexpr int kOff = 9;          // exponent of a probability at its reference: kOff + kSlack stay inside fp16
 // What a lane holds of the metadata of a page to come: 8 steps and 8 zeros (wave 0 of the keys, wave 1 of the
 // values) or 8 norms (the others).  All waves make the same loads, so that how many are in flight is known
 // wherever one is waited for.
@@ -120,9 +125,12 @@ template <bool M32> struct Fetched {
       }
     } else {
       step = __builtin_bit_cast(half8, a[0]);
-      const half8 z = __builtin_bit_cast(half8, b[0]), m = (_Float16)mid, most = (_Float16)kHalfMax;
-      const half8 t = m - z;
-      base = zp_min ? __builtin_elementwise_fma(step, m, z) : t * step;
+      const half8 z = __builtin_bit_cast(half8, b[0]), most = (_Float16)kHalfMax;
+      const uint32_t two = __builtin_bit_cast(uint32_t, (half2v)(_Float16)mid);
+      u32x4 w = {two, two, two, two};
+      asm("" : "+v"(w));   // (as a constant it is taken apart into single halves)
+      const half8 m = __builtin_bit_cast(half8, w);
+      base = zp_min ? __builtin_elementwise_fma(step, m, z) : (m - z) * step;
       base = __builtin_elementwise_min(__builtin_elementwise_max(base, -most), most);
     }
   }
@@ -150,7 +158,8 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
   constexpr int ROWS = NR * 16;
   constexpr int UNITS = C::BPMAX - C::BPMIN;         // log2 of what the counterweights leave in the extra tile
   __shared__ __align__(16) half8 s_qh[NR][4][64], s_qc[NR][4][64];   // queries as operands: natural order, codes' order
-  __shared__ __align__(16) uint32_t s_p[NR][4][64][4];               // probabilities as operands
+  __shared__ __align__(16) uint32_t s_p[2][NR][4][64][4];            // probabilities as operands
+  __shared__ __align__(16) int s_flag[2][4];
   __shared__ __align__(16) float s_max[ROWS][4];
   __shared__ __align__(16) Staged s_meta[3];
 
@@ -172,13 +181,13 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
 
   float4v o[NR][2];   // channels 32 wave + 16 j + 4 q4 + r of row n, in units of the codes once pages have begun
   float4v x[NR];      // [0]: zero terms of the wave's value group, [1]: the row's sum
-  float m[NR];        // running maximum, log2 units
+  float ref[NR];      // what the row's probabilities are taken against, log2 units
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
     o[i][0] = o[i][1] = x[i] = (float4v){0, 0, 0, 0};
-    m[i] = -INFINITY;
+    ref[i] = kNone;
   }
-  int eoff = 15;
+  int off = kOff;
 
   if (rows > 0) {
     // what the pages are: tail units (window, then new tokens, 128 each) and packed pages, dealt to the splits
@@ -187,15 +196,17 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
     const int n_tail = n_win + (min(n_new, last_t + 1) + R - 1) / R;
     const int step = P.num_splits;
     int page = split < n_tail ? split + (n_tail - split + step - 1) / step * step - n_tail : split - n_tail;
-    const int32_t* table = P.c.block_table + (size_t)b * P.c.max_pages_per_seq;
+    // (read as constant memory, by the scalar unit: a vector load's wait would be one for every load ahead)
+    const auto table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+        reinterpret_cast<uintptr_t>(P.c.block_table + (size_t)b * P.c.max_pages_per_seq));
     // Physical page of page p; what is none is marked (its metadata is staged as zeros and its tokens are left
     // out), and loads past the end take a page again: every iteration then makes the same loads.
     struct Page {
       int phys;
       bool held;
     };
-    auto page_at = [&](int p) {
-      const int phys = table[min(max(p, 0), max(pages - 1, 0))];
+    auto entry_of = [&](int p) { return table[min(max(p, 0), max(pages - 1, 0))]; };
+    auto page_of = [&](int p, int phys) {
       const bool ok = phys >= 0 && phys < P.c.num_pages;
       return Page{ok ? phys : 0, ok && p < pages};
     };
@@ -257,11 +268,12 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
         const uint64_t have = __ballot(big >> bit & 1) & among;
         if (have) among = have, exponent |= 1 << (bit - 10);
       }
-      if (lane == 0) s.off = 15 - max(exponent - 14, 0);
+      if (lane == 0) s.off = kOff - max(exponent - 14, 0);
     };
 
     // page, page + 1 step, page + 2 steps: the codes of the first two and the metadata of all are on their way
-    Page pg0 = page_at(page), pg1 = page_at(page + step), pg2 = page_at(page + 2 * step);
+    Page pg0 = page_of(page, entry_of(page)), pg1 = page_of(page + step, entry_of(page + step)),
+         pg2 = page_of(page + 2 * step, entry_of(page + 2 * step));
     fetch_meta(pg0);
     load_codes(k_pool + pg0.phys * k_stride, k_at, kc);
     load_codes(v_pool + pg0.phys * v_stride, v_at, vc);
@@ -332,42 +344,68 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
         s_qc[i][kk][lane] = qc;
       }
     }
+    if (wave == 3 && lane < 16) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) s_meta[i].v_base[64 + lane] = lane / 4 % 2 == 0 ? C::counterweight(0) : C::counterweight(1);
+    }
     stage_meta(s_meta[0], pg0.held);
     fetch_meta(pg1);
     stage_meta(s_meta[1], pg1.held);
     fetch_meta(pg2);
     __syncthreads();
 
-    // Rows' maxima joined, state rescaled, probabilities to LDS; s[i][j][r]: logit (log2 units) of the wave's
-    // token 16 (2 wave + j) + 4 r + q4.  even, odd: weights' exponents of the k-steps.  Two barriers.
-    auto softmax = [&](float4v (&s)[NR][2], int off, int even, int odd) {
+    // Probabilities to LDS, as operands; s[i][j][r]: logit (log2 units) of the wave's token 16 (2 wave + j) + 4 r + q4.
+    // even, odd: weights' exponents of the k-steps; gone: infinite for what is no page (its numbers are finite),
+    // whose probabilities are zeros.  They are written against the references as they stand; if a
+    // wave finds a row past its reference, all join the rows' maxima, rescale and write them again.  What was
+    // written two calls ago is free: between lies a barrier that everyone reaches behind its reads.
+    int turn = 0;
+    auto softmax = [&](const float4v (&s)[NR][2], int most_off, float even, float odd, float gone) {
+      auto write = [&] {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          const float M = ref[i] - (float)off;
+          const float Mk[2] = {M + (even + gone), M + (odd + gone)};
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            s_p[turn][i][r][lane][wave] = pack2(__builtin_amdgcn_exp2f(s[i][0][r] - Mk[r % 2]),
+                                                __builtin_amdgcn_exp2f(s[i][1][r] - Mk[r % 2]));
+        }
+      };
+      turn ^= 1;
+      float mx[NR];
+      bool past = most_off < off;
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        float mx = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
-                         fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3])));
-        mx = max_of_row(mx);
-        if (q4 == 0) s_max[16 * i + n][wave] = mx;
+        mx[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
+                      fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3])));
+        past |= mx[i] > ref[i] + (kSlack + gone);
+      }
+      write();
+      const int flag = __any(past);
+      if (lane == 0) s_flag[turn][wave] = flag;
+      __syncthreads();
+      const u32x4 flags = *reinterpret_cast<const u32x4*>(s_flag[turn]);
+      if (__builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) == 0) return;
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        mx[i] = max_of_row(mx[i]);
+        if (q4 == 0) s_max[16 * i + n][wave] = mx[i];
       }
       __syncthreads();
+      const int now = min(off, most_off);
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
         const float4v mw = *reinterpret_cast<const float4v*>(s_max[16 * i + n]);
-        const float mn = fmaxf(m[i], fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3])));
-        if (__any(mn > m[i]) || off != eoff) {
-          const float alpha = m[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[i] - mn + (float)(off - eoff));
-          o[i][0] *= alpha;
-          o[i][1] *= alpha;
-          x[i] *= alpha;
-          m[i] = mn;
-        }
-        const float M = mn == -INFINITY ? 0.0f : mn - (float)off;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float Mk = M + (float)(r % 2 == 0 ? even : odd);
-          s_p[i][r][lane][wave] = pack2(__builtin_amdgcn_exp2f(s[i][0][r] - Mk), __builtin_amdgcn_exp2f(s[i][1][r] - Mk));
-        }
+        const float to = fmaxf(ref[i], fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3])));
+        const float alpha = __builtin_amdgcn_exp2f(ref[i] - to + (float)(now - off));
+        o[i][0] *= alpha;
+        o[i][1] *= alpha;
+        x[i] *= alpha;
+        ref[i] = to;
       }
-      eoff = off;
+      off = now;
+      write();
       __syncthreads();
     };
 
@@ -425,7 +463,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
           for (int i = 0; i < NR; ++i) s[i][j] = (float4v){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
         }
       }
-      softmax(s, eoff, 0, 0);
+      softmax(s, off, 0.0f, 0.0f, 0.0f);
       // values: channel 32 wave + 16 j + n of tokens t0 + 16 e + 4 kk + q4
       const half8 one = (_Float16)(n % 4 == 1 ? 1.0f / (1 << UNITS) : 0.0f);
 #pragma unroll
@@ -447,7 +485,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
         }
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          const half8 p = *reinterpret_cast<const half8*>(s_p[i][kk][lane]);
+          const half8 p = *reinterpret_cast<const half8*>(s_p[turn][i][kk][lane]);
           o[i][0] = mfma(a[0], p, o[i][0]);
           o[i][1] = mfma(a[1], p, o[i][1]);
           x[i] = mfma(one, p, x[i]);
@@ -464,10 +502,12 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
     }
     // the wave's groups in the staged metadata, its probabilities' weights, constants of the middle
     const int gk = wave * 32 / P.g.k_group * 16, gv = wave * 32 / P.g.v_group * 16;
-    const int even = BITS == 2 ? 2 * (wave % 2) : 4 * (wave % 2);
-    const int odd = BITS == 2 ? (wave == 0 || wave == 3 ? 4 : 2 * (wave - 1)) : 4 * (wave % 2);
+    const int gb = n % 4 == 1 ? 64 : gv;     // the extra tile's second row: the rows' sums
+    const float even = (float)(BITS == 2 ? 2 * (wave % 2) : 4 * (wave % 2));
+    const float odd = (float)(BITS == 2 ? (wave == 0 || wave == 3 ? 4 : 2 * (wave - 1)) : 4 * (wave % 2));
     for (int buf = 0; page < pages; page += step) {
       const Staged& meta = s_meta[buf];
+      const int entry = entry_of(page + 3 * step);
       // logits
       float4v s[NR][2], start[NR];
       half8 qd[NR][4];
@@ -505,30 +545,18 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
           s[i][1][r] *= nm[1];
         }
       }
-      if (!pg0.held) {   // no page: its tokens are left out
-#pragma unroll
-        for (int i = 0; i < NR; ++i)
-          s[i][0] = s[i][1] = (float4v){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      }
-      softmax(s, min(eoff, __builtin_amdgcn_readfirstlane(meta.off)), even, odd);
+      softmax(s, __builtin_amdgcn_readfirstlane(meta.off), even, odd, pg0.held ? 0.0f : INFINITY);
       // values
-      half8 st[4], base[4];
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        st[kk] = meta.v_step[gv + 4 * kk + q4];
-        base[kk] = meta.v_base[gv + 4 * kk + q4];
-        const half8 cw = C::counterweight(kk);
-        base[kk] = n % 4 == 1 ? cw : base[kk];
-      }
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
+        const half8 st = meta.v_step[gv + 4 * kk + q4], base = meta.v_base[gb + 4 * kk + q4];
         const half8 mid = C::counterweight(kk) * (_Float16)(n % 4 == 0 ? -C::MID : 0.0f);
         const half8 a0 = C::operand(vc, kk), a1 = C::operand(vc + BITS, kk);
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          const half8 p = *reinterpret_cast<const half8*>(s_p[i][kk][lane]);
-          const half8 pd = p * st[kk];
-          x[i] = mfma(base[kk], p, x[i]);
+          const half8 p = *reinterpret_cast<const half8*>(s_p[turn][i][kk][lane]);
+          const half8 pd = p * st;
+          x[i] = mfma(base, p, x[i]);
           x[i] = mfma(mid, pd, x[i]);
           o[i][0] = mfma(a0, pd, o[i][0]);
           o[i][1] = mfma(a1, pd, o[i][1]);
@@ -540,7 +568,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
       stage_meta(s_meta[into], pg2.held);
       pg0 = pg1;
       pg1 = pg2;
-      pg2 = page_at(page + 3 * step);
+      pg2 = page_of(page + 3 * step, entry);
       fetch_meta(pg2);
       buf = buf == 2 ? 0 : buf + 1;
     }
@@ -576,7 +604,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
     }
     if (P.num_splits > 1 && wave == 0 && q4 == 0)
       *reinterpret_cast<float2v*>(P.ws + (out_row * P.num_splits + split) * WS_STRIDE + D) =
-          there && m[i] > -INFINITY ? (float2v){m[i] - (float)eoff, l} : (float2v){-INFINITY, 0};
+          there && ref[i] > kNone ? (float2v){ref[i] - (float)off, l} : (float2v){-INFINITY, 0};
   }
 }
 
