@@ -6,18 +6,17 @@
 //   logit[t][h][j] = scale <q_th, k_j>                                   new token j <= t
 //   out[t][h]      = softmax over both, times the values
 //
-// The T tokens' g query heads of a kv head are T g rows that read the same keys and values.  A workgroup
-// takes 16 .. 64 of them (16 a matrix tile) through a share of the sequence, page by page:
-//   wave w: S^T = K Q^T for tokens 32 w .. + 31   v_mfma_f32_16x16x32_f16, rows = tokens, columns = query rows
-//   the rows' maxima through LDS, barrier; probabilities to LDS, barrier
-//   wave w: O^T = V^T P^T for channels 32 w .. + 31, over all 128 tokens
-// so that each code is loaded and unpacked once a workgroup, a wave's share of the keys lies in one group of
-// tokens and that of the values in one group of channels, and the state of a row (16 registers a tile in all)
-// leaves room for several workgroups a CU, which cover each other's barriers and loads.
-//
+// The T tokens' g query heads of a kv head are T g rows that read the same keys and values.  A wave holds 16 or
+// 32 of them (16 a matrix tile) and takes whole pages of 128 tokens on its own, with its own running state, so
+// that nothing in the page loop waits for another wave; the four waves of a workgroup and the splits of the
+// sequence are joined at the end.
+//   S^T = K Q^T  : v_mfma_f32_16x16x32_f16, rows = 16 tokens, columns = 16 query rows, over 128 channels
+//   O^T = V^T P^T: rows = 16 channels, columns = query rows, over 128 tokens
 // Row n of a token tile is token 4 (n % 4) + n / 4 of it: a lane's four results of tile T are then its tokens
-// 16 T + 4 r + lane / 16, exactly those whose value codes the lane's chunk of the page holds for k-step r, and a
-// lane reads the probabilities it multiplies with as 16 consecutive bytes.
+// 16 T + 4 r + lane / 16, exactly those whose value codes the lane's chunk of the page holds for k-step r: the
+// probabilities are packed where they are and become operands without an exchange.
+// (Four waves on one page, a quarter of its tokens and of its channels each, probabilities through LDS: 2.3 times
+// the LDS traffic, 1.4 times the matrix products and a barrier a page; 8 new tokens over 8 x 32K took 99 us.)
 //
 // Codes become fp16 operands with a mask (a code parked in the mantissa of a subnormal: c 2^(s - 24)); the
 // steps go to the other operand, Q Delta_k and P Delta_v, and 2^-s with them.  Codes count from their middle:
@@ -91,16 +90,13 @@ struct Staged {
   half8 k_step[64], k_base[64];   // [group][quarter][k-step]
   half8 v_step[64], v_base[80];   // [group][k-step][quarter]; behind the four groups the counterweights alone
   float norm[R];                  // position (token % 16) * 8 + token / 16
-  int off;                        // exponent the probabilities can carry
 };
 // A row's probabilities are taken against a reference that follows its maximum only when that has passed it by
-// 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs the workgroup a
-// barrier and a rescaling.
+// 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs a rescaling of the
+// whole state.
 constexpr float kSlack = 6.0f, kNone = -3e38f;
 constexpr int kOff = 9;          // exponent of a probability at its reference: kOff + kSlack stay inside fp16
-// What a lane holds of the metadata of a page to come: 8 steps and 8 zeros (wave 0 of the keys, wave 1 of the
-// values) or 8 norms (the others).  All waves make the same loads, so that how many are in flight is known
-// wherever one is waited for.
+// What a lane holds of the metadata of a page to come: 8 steps and 8 zeros of the keys or of the values.
 template <bool M32> struct Fetched {
   u32x4 a[M32 ? 2 : 1], b[M32 ? 2 : 1];
   __device__ __forceinline__ void load(const uint8_t* src, const uint8_t* zsrc, uint32_t at) {
@@ -139,9 +135,7 @@ template <bool M32> struct Fetched {
 __device__ __forceinline__ float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v){a, b}, half2v));
-}
+__device__ __forceinline__ half2v pack2(float a, float b) { return __builtin_convertvector((float2v){a, b}, half2v); }
 __device__ __forceinline__ float max_of_row(float v) {   // over the four lanes that hold a query row
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
@@ -149,19 +143,31 @@ __device__ __forceinline__ float max_of_row(float v) {   // over the four lanes 
   return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
-// Workgroups a CU that a variant's registers are held to.
-__host__ __device__ constexpr int wgs_per_cu(int nr) { return nr == 1 ? 4 : nr == 2 ? 3 : 2; }
+constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens)
 
-template <int BITS, bool M32, int NR>
+// Workgroups a CU that a variant's registers are held to.
+__host__ __device__ constexpr int wgs_per_cu(int nr) { return nr == 1 ? 3 : 2; }
+
+// ONE: k_group is the whole page.
+template <int BITS, bool M32, bool ONE, int NR>
 __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftParams P) {
   using C = Codes<BITS>;
   constexpr int ROWS = NR * 16;
   constexpr int UNITS = C::BPMAX - C::BPMIN;         // log2 of what the counterweights leave in the extra tile
-  __shared__ __align__(16) half8 s_qh[NR][4][64], s_qc[NR][4][64];   // queries as operands: natural order, codes' order
-  __shared__ __align__(16) uint32_t s_p[2][NR][4][64][4];            // probabilities as operands
-  __shared__ __align__(16) int s_flag[2][4];
-  __shared__ __align__(16) float s_max[ROWS][4];
-  __shared__ __align__(16) Staged s_meta[3];
+  constexpr int OROW = D + 4;
+  struct Loop {
+    half8 qh[NR][4][64], qc[NR][4][64];              // queries as operands: natural order, codes' order
+    Staged meta[4];                                  // of each wave's page
+    half8 cw[2], mid[2], none[2];                    // counterweights of even and odd k-steps, times -MID, zeros
+  };
+  struct Join {
+    float o[4][ROWS][OROW], m[4][ROWS], l[4][ROWS];
+  };
+  __shared__ __align__(16) union Lds {
+    Loop loop;
+    Join join;
+    __device__ Lds() {}
+  } lds;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, q4 = lane >> 4;
@@ -177,25 +183,26 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
   const int rows = min(max(n_new * g - row0, 0), ROWS);         // of this block that are there
   const bool zp_min = P.c.cfg.zp_mode == OSCAR_ZP_MIN;
   const bool bf16 = P.c.cfg.io_dtype == OSCAR_BF16;
-  const int row_of_tile = 4 * (n % 4) + n / 4;                  // token of a tile that this lane's row is
 
-  float4v o[NR][2];   // channels 32 wave + 16 j + 4 q4 + r of row n, in units of the codes once pages have begun
-  float4v x[NR];      // [0]: zero terms of the wave's value group, [1]: the row's sum
+  float4v o[NR][8];   // channels 16 ct + 4 q4 + r of row n, in units of the codes once pages have begun
+  float4v x[NR];      // row 4 q4 + r of the extra tile: 0 .. 3 the value groups' mean terms, 4 the row's sum
   float ref[NR];      // what the row's probabilities are taken against, log2 units
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
-    o[i][0] = o[i][1] = x[i] = (float4v){0, 0, 0, 0};
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) o[i][ct] = (float4v){0, 0, 0, 0};
+    x[i] = (float4v){0, 0, 0, 0};
     ref[i] = kNone;
   }
   int off = kOff;
 
   if (rows > 0) {
-    // what the pages are: tail units (window, then new tokens, 128 each) and packed pages, dealt to the splits
+    // ---- what this wave takes: 16-bit pieces (window, then new tokens) and pages, dealt to the waves of all splits ----
     const int last_t = (row0 + rows - 1) / g;                            // last new token any row here sees
-    const int n_win = res > 0 ? 1 : 0;
-    const int n_tail = n_win + (min(n_new, last_t + 1) + R - 1) / R;
-    const int step = P.num_splits;
-    int page = split < n_tail ? split + (n_tail - split + step - 1) / step * step - n_tail : split - n_tail;
+    const int n_win = (res + TAIL - 1) / TAIL;
+    const int n_tail = n_win + (min(n_new, last_t + 1) + TAIL - 1) / TAIL;
+    const int step = P.num_splits * 4, own = split * 4 + wave;
+    int page = own < n_tail ? own + (n_tail - own + step - 1) / step * step - n_tail : own - n_tail;
     // (read as constant memory, by the scalar unit: a vector load's wait would be one for every load ahead)
     const auto table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
         reinterpret_cast<uintptr_t>(P.c.block_table + (size_t)b * P.c.max_pages_per_seq));
@@ -212,48 +219,62 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
     };
 
     // ---- loads ahead ----
-    uint32_t kc[2 * BITS], vc[2 * BITS];
-    const size_t k_stride = (size_t)Hkv * P.g.k_codes_bytes, v_stride = (size_t)Hkv * P.g.v_codes_bytes;
-    const uint8_t* k_pool = reinterpret_cast<const uint8_t*>(P.c.k_codes) + (size_t)kvh * P.g.k_codes_bytes;
-    const uint8_t* v_pool = reinterpret_cast<const uint8_t*>(P.c.v_codes) + (size_t)kvh * P.g.v_codes_bytes;
-    const uint32_t k_at = chunk_offset(BITS, 2 * wave, row_of_tile, q4), v_at = chunk_offset(BITS, 2 * wave, n, q4);
-    auto load_codes = [&](const uint8_t* page, uint32_t at, uint32_t* w) {
+    uint32_t kc[4][2 * BITS], vc[4][2 * BITS];
+    auto pool_of = [&](const void* pool, int bytes, int phys) {
+      return reinterpret_cast<const uint8_t*>(pool) + ((size_t)phys * Hkv + kvh) * bytes;
+    };
+    const uint32_t k_at = chunk_offset(BITS, 0, 4 * (n % 4) + n / 4, q4), v_at = chunk_offset(BITS, 0, n, q4);
+    auto load_codes = [&](const uint8_t* page, uint32_t at, uint32_t (&w)[4][2 * BITS]) {
 #pragma unroll
-      for (int j = 0; j < BITS / 2; ++j) *reinterpret_cast<u32x4*>(w + 4 * j) = *reinterpret_cast<const u32x4*>(page + at + 16 * j);
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < BITS / 2; ++j)
+          *reinterpret_cast<u32x4*>(&w[c][4 * j]) = *reinterpret_cast<const u32x4*>(page + at + chunk_offset(BITS, 2 * c, 0, 0) + 16 * j);
     };
     constexpr int MB = M32 ? 4 : 2;
-    const int m_bytes = wave == 0 ? P.g.k_meta_bytes : wave == 1 ? P.g.v_meta_bytes : P.g.k_norms_bytes;
-    const int m_groups = wave == 0 ? P.g.ngk : wave == 1 ? P.g.ngv : 1;
-    const uint8_t* m_pool = reinterpret_cast<const uint8_t*>(wave == 0 ? P.c.k_meta : wave == 1 ? P.c.v_meta : P.c.k_norms) +
-                            (size_t)kvh * m_bytes;
-    const size_t m_stride = (size_t)Hkv * m_bytes;
-    const uint32_t m_zero = wave < 2 ? (uint32_t)m_groups * 128 * MB : 0, m_at = (uint32_t)min(lane, 16 * m_groups - 1) * 8 * MB;
-    Fetched<M32> f;
+    const uint32_t km_at = (uint32_t)min(lane, 16 * P.g.ngk - 1) * 8 * MB, vm_at = (uint32_t)min(lane, 16 * P.g.ngv - 1) * 8 * MB;
+    Fetched<M32> fk, fv;
+    u32x4 fn;
     auto fetch_meta = [&](const Page& pg) {
-      const uint8_t* src = m_pool + pg.phys * m_stride;
-      f.load(src, src + m_zero, m_at);
+      const uint8_t* km = pool_of(P.c.k_meta, P.g.k_meta_bytes, pg.phys);
+      const uint8_t* vm = pool_of(P.c.v_meta, P.g.v_meta_bytes, pg.phys);
+      fk.load(km, km + P.g.k_meta_bytes / 2, km_at);
+      fv.load(vm, vm + P.g.v_meta_bytes / 2, vm_at);
+      const uint8_t* kn = pool_of(P.c.k_norms, P.g.k_norms_bytes, pg.phys);
+      if (M32) {
+        const uint2 v = *reinterpret_cast<const uint2*>(kn + lane * 8);
+        fn[0] = v.x, fn[1] = v.y;
+      } else {
+        fn[0] = *reinterpret_cast<const uint32_t*>(kn + lane * 4);
+      }
     };
-    auto stage_meta = [&](Staged& s, bool held) {
-      if (wave >= 2) {
-        if (wave == 2 && lane < 16) {
-          constexpr float unit_of_codes = (float)(1 << (24 - C::BPMIN - kQShift));
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s.norm[8 * lane + e] = held ? f.number(f.a, e) * unit_of_codes : 0.0f;
-        }
-        return;
-      }
+    Staged& meta = lds.loop.meta[wave];
+    auto stage_keys = [&](bool held) {
       half8 st, base;
-      f.step_and_base(zp_min, C::MID, st, base);
-      const int kk = wave == 0 ? lane : lane / 4;
-      base *= kk % 2 == 0 ? C::counterweight(0) : C::counterweight(1);
+      fk.step_and_base(zp_min, C::MID, st, base);
+      base *= lds.loop.cw[lane % 2];
       if (!held) st = base = (half8)(_Float16)0.0f;
-      if (wave == 0) {
-        s.k_step[lane] = st;
-        s.k_base[lane] = base;
-        return;
+      meta.k_step[lane] = st;
+      meta.k_base[lane] = base;
+      float v[2];
+      if (M32) {
+        v[0] = __uint_as_float(fn[0]), v[1] = __uint_as_float(fn[1]);
+      } else {
+        const half2v h = __builtin_bit_cast(half2v, fn[0]);
+        v[0] = (float)h[0], v[1] = (float)h[1];
       }
-      s.v_step[lane] = st;
-      s.v_base[lane] = base;
+      constexpr float unit_of_codes = (float)(1 << (24 - C::BPMIN - kQShift));
+      *reinterpret_cast<float2v*>(&meta.norm[2 * lane]) =
+          held ? (float2v){v[0] * unit_of_codes, v[1] * unit_of_codes} : (float2v){0.0f, 0.0f};
+    };
+    // returns the exponent that the probabilities can carry
+    auto stage_values = [&](bool held) {
+      half8 st, base;
+      fv.step_and_base(zp_min, C::MID, st, base);
+      base *= lds.loop.cw[lane / 4 % 2];
+      if (!held) st = base = (half8)(_Float16)0.0f;
+      meta.v_step[lane] = st;
+      meta.v_base[lane] = base;
       // the exponent of the largest step (fp16 bits; steps are not negative), bit by bit over the wave
       uint32_t big = 0;
 #pragma unroll
@@ -268,15 +289,13 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
         const uint64_t have = __ballot(big >> bit & 1) & among;
         if (have) among = have, exponent |= 1 << (bit - 10);
       }
-      if (lane == 0) s.off = kOff - max(exponent - 14, 0);
+      return kOff - max(exponent - 14, 0);
     };
 
-    // page, page + 1 step, page + 2 steps: the codes of the first two and the metadata of all are on their way
-    Page pg0 = page_of(page, entry_of(page)), pg1 = page_of(page + step, entry_of(page + step)),
-         pg2 = page_of(page + 2 * step, entry_of(page + 2 * step));
+    Page pg0 = page_of(page, entry_of(page)), pg1 = page_of(page + step, entry_of(page + step));
     fetch_meta(pg0);
-    load_codes(k_pool + pg0.phys * k_stride, k_at, kc);
-    load_codes(v_pool + pg0.phys * v_stride, v_at, vc);
+    load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg0.phys), k_at, kc);
+    load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0.phys), v_at, vc);
 
     // ---- queries: lane's row, channels 32 q4 .. + 31; wave i rotates tile i ----
     const uint16_t* q_row[NR];
@@ -340,79 +359,44 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
           const int u = slot_index(BITS, kk, e);
           qc[e] = qh[u / 8][u % 8] * (_Float16)(1.0f / (float)(1 << C::above(kk, e)));
         }
-        s_qh[i][kk][lane] = qh[kk];
-        s_qc[i][kk][lane] = qc;
+        lds.loop.qh[i][kk][lane] = qh[kk];
+        lds.loop.qc[i][kk][lane] = qc;
       }
     }
-    if (wave == 3 && lane < 16) {
-#pragma unroll
-      for (int i = 0; i < 3; ++i) s_meta[i].v_base[64 + lane] = lane / 4 % 2 == 0 ? C::counterweight(0) : C::counterweight(1);
+    // (constants of the page loop wait in LDS: the registers are spoken for)
+    if (lane < 16) meta.v_base[64 + lane] = lane / 4 % 2 == 0 ? C::counterweight(0) : C::counterweight(1);
+    if (lane < 2) {
+      const half8 cw = lane == 0 ? C::counterweight(0) : C::counterweight(1);
+      lds.loop.cw[lane] = cw;   // (the same from every wave)
+      lds.loop.mid[lane] = cw * (_Float16)-C::MID;
+      lds.loop.none[lane] = (half8)(_Float16)0.0f;
     }
-    stage_meta(s_meta[0], pg0.held);
+    __syncthreads();
+    stage_keys(pg0.held);
+    int page_off = stage_values(pg0.held);
     fetch_meta(pg1);
-    stage_meta(s_meta[1], pg1.held);
-    fetch_meta(pg2);
     __syncthreads();
 
-    // Probabilities to LDS, as operands; s[i][j][r]: logit (log2 units) of the wave's token 16 (2 wave + j) + 4 r + q4.
-    // even, odd: weights' exponents of the k-steps; gone: infinite for what is no page (its numbers are finite),
-    // whose probabilities are zeros.  They are written against the references as they stand; if a
-    // wave finds a row past its reference, all join the rows' maxima, rescale and write them again.  What was
-    // written two calls ago is free: between lies a barrier that everyone reaches behind its reads.
-    int turn = 0;
-    auto softmax = [&](const float4v (&s)[NR][2], int most_off, float even, float odd, float gone) {
-      auto write = [&] {
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          const float M = ref[i] - (float)off;
-          const float Mk[2] = {M + (even + gone), M + (odd + gone)};
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            s_p[turn][i][r][lane][wave] = pack2(__builtin_amdgcn_exp2f(s[i][0][r] - Mk[r % 2]),
-                                                __builtin_amdgcn_exp2f(s[i][1][r] - Mk[r % 2]));
-        }
-      };
-      turn ^= 1;
-      float mx[NR];
-      bool past = most_off < off;
+    // New references where a row has passed its own (or the exponent has to give way), and the state against them;
+    // in whole powers of two, so that probabilities already packed only change their exponents.
+    auto move_to = [&](const float (&mx)[NR], int now, auto&& packed) {
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        mx[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
-                      fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3])));
-        past |= mx[i] > ref[i] + (kSlack + gone);
-      }
-      write();
-      const int flag = __any(past);
-      if (lane == 0) s_flag[turn][wave] = flag;
-      __syncthreads();
-      const u32x4 flags = *reinterpret_cast<const u32x4*>(s_flag[turn]);
-      if (__builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) == 0) return;
+        const float to = fmaxf(ref[i], ceilf(max_of_row(mx[i])));
+        const float alpha = __builtin_amdgcn_exp2f(fmaxf(ref[i] - to, -200.0f) + (float)(now - off));
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
-        mx[i] = max_of_row(mx[i]);
-        if (q4 == 0) s_max[16 * i + n][wave] = mx[i];
-      }
-      __syncthreads();
-      const int now = min(off, most_off);
-#pragma unroll
-      for (int i = 0; i < NR; ++i) {
-        const float4v mw = *reinterpret_cast<const float4v*>(s_max[16 * i + n]);
-        const float to = fmaxf(ref[i], fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3])));
-        const float alpha = __builtin_amdgcn_exp2f(ref[i] - to + (float)(now - off));
-        o[i][0] *= alpha;
-        o[i][1] *= alpha;
+        for (int ct = 0; ct < 8; ++ct) o[i][ct] *= alpha;
         x[i] *= alpha;
+        packed(i, alpha);
         ref[i] = to;
       }
       off = now;
-      write();
-      __syncthreads();
     };
 
     // ---- 16-bit tokens ----
-    for (int u = split; u < n_tail; u += step) {
+    for (int u = own; u < n_tail; u += step) {
       const bool win = u < n_win;
-      const int t0 = win ? 0 : (u - n_win) * R, count = win ? res : n_new;
+      const int t0 = (win ? u : u - n_win) * TAIL, count = win ? res : n_new;
       const size_t head = (size_t)b * Hkv + kvh;
       const uint16_t *kb, *vb;
       size_t stride;
@@ -425,203 +409,288 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
         vb = reinterpret_cast<const uint16_t*>(P.v_new) + ((size_t)b * P.T * Hkv + kvh) * D;
         stride = (size_t)Hkv * D;
       }
+      // logits: tile j holds tokens t0 + 16 j .., row n of the tile = token n of it
       float4v s[NR][2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int tile0 = t0 + 16 * (2 * wave + j);
-        if (tile0 < count) {
-          const int t = min(tile0 + row_of_tile, count - 1);
-          u32x4 a[4];
+        const int t = min(t0 + 16 * j + n, count - 1);
+        u32x4 a[4];
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) a[kk] = *reinterpret_cast<const u32x4*>(kb + (size_t)t * stride + 32 * q4 + 8 * kk);
+        for (int kk = 0; kk < 4; ++kk) a[kk] = *reinterpret_cast<const u32x4*>(kb + (size_t)t * stride + 32 * q4 + 8 * kk);
+        float f[4];
 #pragma unroll
-          for (int i = 0; i < NR; ++i) {
-            float4v acc = {0, 0, 0, 0};
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              if (win) {
-                acc = mfma(__builtin_bit_cast(half8, a[kk]), s_qh[i][kk][lane], acc);
-              } else {
-                const u32x4 r = *reinterpret_cast<const u32x4*>(q_row[i] + 8 * kk);
-                if (bf16)
-                  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[kk]),
-                                                                __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
-                else
-                  acc = mfma(__builtin_bit_cast(half8, a[kk]), __builtin_bit_cast(half8, r), acc);
-              }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int tok = tile0 + 4 * r + q4;
-              const float fac = win ? load_meta(P.c.res_norm, head * R + min(tok, R - 1), M32 ? 4 : 2) * (1.0f / (1 << kQShift))
-                                    : P.scale_log2;
-              s[i][j][r] = tok < count && (win || tok <= row_t[i]) ? acc[r] * fac : -INFINITY;
-            }
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < NR; ++i) s[i][j] = (float4v){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        }
-      }
-      softmax(s, off, 0.0f, 0.0f, 0.0f);
-      // values: channel 32 wave + 16 j + n of tokens t0 + 16 e + 4 kk + q4
-      const half8 one = (_Float16)(n % 4 == 1 ? 1.0f / (1 << UNITS) : 0.0f);
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        half8 a[2];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int t = t0 + 16 * e + 4 * kk + q4;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            float y = 0.0f;
-            if (t0 + 16 * e < count) {
-              const uint16_t v = vb[(size_t)min(t, count - 1) * stride + 32 * wave + 16 * j + n];
-              y = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
-              y = t < count ? __builtin_amdgcn_fmed3f(y, -kHalfMax, kHalfMax) : 0.0f;
-            }
-            a[j][e] = (_Float16)y;
-          }
-        }
+        for (int r = 0; r < 4; ++r)
+          f[r] = win ? load_meta(P.c.res_norm, head * R + min(t0 + 16 * j + 4 * q4 + r, R - 1), MB) * (1.0f / (1 << kQShift))
+                     : P.scale_log2;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          const half8 p = *reinterpret_cast<const half8*>(s_p[turn][i][kk][lane]);
-          o[i][0] = mfma(a[0], p, o[i][0]);
-          o[i][1] = mfma(a[1], p, o[i][1]);
-          x[i] = mfma(one, p, x[i]);
+          float4v acc = {0, 0, 0, 0};
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            if (win) {
+              acc = mfma(__builtin_bit_cast(half8, a[kk]), lds.loop.qh[i][kk][lane], acc);
+            } else {
+              const u32x4 r = *reinterpret_cast<const u32x4*>(q_row[i] + 8 * kk);
+              if (bf16)
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[kk]),
+                                                              __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
+              else
+                acc = mfma(__builtin_bit_cast(half8, a[kk]), __builtin_bit_cast(half8, r), acc);
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int tok = t0 + 16 * j + 4 * q4 + r;
+            s[i][j][r] = tok < count && (win || tok <= row_t[i]) ? acc[r] * f[r] : -INFINITY;
+          }
         }
+      }
+      float mx[NR];
+      bool past = false;
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        mx[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
+                      fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3])));
+        past |= mx[i] > ref[i] + kSlack;
+      }
+      if (__any(past)) move_to(mx, off, [](int, float) {});
+      half8 pr[NR];
+      const half8 one = (_Float16)(n == 4 ? 1.0f / (1 << UNITS) : 0.0f);
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const float M = ref[i] - (float)off;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) pr[i][4 * j + r] = (_Float16)__builtin_amdgcn_exp2f(s[i][j][r] - M);
+        x[i] = mfma(one, pr[i], x[i]);
+      }
+      // values: channel 16 ct + n of tokens t0 + 16 j + 4 q4 + r
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) {
+        half8 a;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = t0 + 16 * j + 4 * q4 + r;
+            const uint16_t v = vb[(size_t)min(t, count - 1) * stride + 16 * ct + n];
+            const float y = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
+            a[4 * j + r] = (_Float16)(t < count ? __builtin_amdgcn_fmed3f(y, -kHalfMax, kHalfMax) : 0.0f);
+          }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) o[i][ct] = mfma(a, pr[i], o[i][ct]);
       }
     }
 
     // ---- pages ----
     constexpr float kCodeUnit = 1.0f / (float)(1 << (24 - C::BPMIN));     // of a code in the sums
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      o[i][0] *= kCodeUnit;
-      o[i][1] *= kCodeUnit;
-    }
-    // the wave's groups in the staged metadata, its probabilities' weights, constants of the middle
-    const int gk = wave * 32 / P.g.k_group * 16, gv = wave * 32 / P.g.v_group * 16;
-    const int gb = n % 4 == 1 ? 64 : gv;     // the extra tile's second row: the rows' sums
-    const float even = (float)(BITS == 2 ? 2 * (wave % 2) : 4 * (wave % 2));
-    const float odd = (float)(BITS == 2 ? (wave == 0 || wave == 3 ? 4 : 2 * (wave - 1)) : 4 * (wave % 2));
-    for (int buf = 0; page < pages; page += step) {
-      const Staged& meta = s_meta[buf];
-      const int entry = entry_of(page + 3 * step);
-      // logits
-      float4v s[NR][2], start[NR];
-      half8 qd[NR][4];
+    for (int i = 0; i < NR; ++i)
 #pragma unroll
-      for (int i = 0; i < NR; ++i) start[i] = (float4v){0, 0, 0, 0};
+      for (int ct = 0; ct < 8; ++ct) o[i][ct] *= kCodeUnit;
+    const int gb = (n == 4 ? 64 : min(n, P.g.ngv - 1) * 16) + q4;         // this lane's row of the extra tile
+    for (; page < pages; page += step) {
+      const int entry = entry_of(page + 2 * step);
+      const float gone = pg0.held ? 0.0f : INFINITY;   // what is no page: its numbers are finite, its probabilities zeros
+      half8 pr[NR][4], qd[NR][4];
+      float4v start[NR];
+      // logits and probabilities of 64 tokens at a time
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        const half8 st = meta.k_step[gk + 4 * q4 + kk], base = meta.k_base[gk + 4 * q4 + kk];
-        const half8 mid = C::counterweight(kk) * (_Float16)-C::MID;
+      for (int half = 0; half < 2; ++half) {
+        float4v s[NR][4];
+#pragma unroll
+        for (int w = 2 * half; w < 2 * half + 2; ++w) {
+          if (ONE ? w == 0 : w * 32 % P.g.k_group == 0) {
+            const int gk = ONE ? 0 : w * 32 / P.g.k_group * 16;
+#pragma unroll
+            for (int i = 0; i < NR; ++i) start[i] = (float4v){0, 0, 0, 0};
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              const half8 st = meta.k_step[gk + 4 * q4 + kk], base = meta.k_base[gk + 4 * q4 + kk];
+              const half8 mid = lds.loop.mid[kk % 2];
+#pragma unroll
+              for (int i = 0; i < NR; ++i) {
+                const half8 qc = lds.loop.qc[i][kk][lane];
+                qd[i][kk] = qc * st;
+                start[i] = mfma(base, qc, start[i]);
+                start[i] = mfma(mid, qd[i][kk], start[i]);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < NR; ++i) start[i] *= 1.0f / (float)(1 << (24 - C::BPMAX));
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              const half8 a = C::operand(kc[w] + j * BITS, kk);
+#pragma unroll
+              for (int i = 0; i < NR; ++i) {
+                float4v& acc = s[i][2 * (w % 2) + j];
+                acc = mfma(a, qd[i][kk], kk == 0 ? start[i] : acc);
+              }
+            }
+        }
+        float mx[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) mx[i] = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4v nm = *reinterpret_cast<const float4v*>(&meta.norm[(4 * r + q4) * 8 + 4 * half]);
+#pragma unroll
+          for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              s[i][t][r] *= nm[t];
+              mx[i] = fmaxf(mx[i], s[i][t][r]);
+            }
+        }
+        bool past = false;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) past |= mx[i] > ref[i] + (kSlack + gone);
+        if (__any(past) || page_off < off)
+          move_to(mx, min(off, page_off), [&](int i, float alpha) {
+            if (half == 1) {
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk) pr[i][kk] *= (_Float16)alpha;
+            }
+          });
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          const half8 qc = s_qc[i][kk][lane];
-          qd[i][kk] = qc * st;
-          start[i] = mfma(base, qc, start[i]);
-          start[i] = mfma(mid, qd[i][kk], start[i]);
+          const float M = ref[i] - (float)off + gone;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int t = 0; t < 4; t += 2) {
+              const float Mk = M + (float)C::above(r, 4 * half + t);
+              const half2v p = pack2(__builtin_amdgcn_exp2f(s[i][t][r] - Mk), __builtin_amdgcn_exp2f(s[i][t + 1][r] - Mk));
+              pr[i][r][4 * half + t] = p[0];
+              pr[i][r][4 * half + t + 1] = p[1];
+            }
         }
       }
-#pragma unroll
-      for (int i = 0; i < NR; ++i) s[i][0] = s[i][1] = start[i] * (1.0f / (float)(1 << (24 - C::BPMAX)));
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const half8 a = C::operand(kc + j * BITS, kk);
-#pragma unroll
-          for (int i = 0; i < NR; ++i) s[i][j] = mfma(a, qd[i][kk], s[i][j]);
-        }
-      load_codes(k_pool + pg1.phys * k_stride, k_at, kc);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float2v nm = *reinterpret_cast<const float2v*>(&meta.norm[(4 * r + q4) * 8 + 2 * wave]);
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          s[i][0][r] *= nm[0];
-          s[i][1][r] *= nm[1];
-        }
-      }
-      softmax(s, __builtin_amdgcn_readfirstlane(meta.off), even, odd, pg0.held ? 0.0f : INFINITY);
+      load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1.phys), k_at, kc);
+      stage_keys(pg1.held);
+
       // values
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        const half8 st = meta.v_step[gv + 4 * kk + q4], base = meta.v_base[gb + 4 * kk + q4];
-        const half8 mid = C::counterweight(kk) * (_Float16)(n % 4 == 0 ? -C::MID : 0.0f);
-        const half8 a0 = C::operand(vc, kk), a1 = C::operand(vc + BITS, kk);
+        const half8 base = meta.v_base[gb + 4 * kk];
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          const half8 p = *reinterpret_cast<const half8*>(s_p[turn][i][kk][lane]);
-          const half8 pd = p * st;
-          x[i] = mfma(base, p, x[i]);
-          x[i] = mfma(mid, pd, x[i]);
-          o[i][0] = mfma(a0, pd, o[i][0]);
-          o[i][1] = mfma(a1, pd, o[i][1]);
-        }
+        for (int i = 0; i < NR; ++i) x[i] = mfma(base, pr[i][kk], x[i]);
       }
-      load_codes(v_pool + pg1.phys * v_stride, v_at, vc);
-      // every wave has left the page before this one: its buffer takes the page after next
-      const int into = buf == 0 ? 2 : buf - 1;
-      stage_meta(s_meta[into], pg2.held);
+      half8 pd[NR][4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        if (w * 32 % P.g.v_group == 0) {
+          const int gv = w * 32 / P.g.v_group;
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            const half8 st = meta.v_step[gv * 16 + 4 * kk + q4];
+            const half8 mid = (n == gv ? lds.loop.mid : lds.loop.none)[kk % 2];
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+              pd[i][kk] = pr[i][kk] * st;
+              x[i] = mfma(mid, pd[i][kk], x[i]);
+            }
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            const half8 a = C::operand(vc[w] + j * BITS, kk);
+#pragma unroll
+            for (int i = 0; i < NR; ++i) o[i][2 * w + j] = mfma(a, pd[i][kk], o[i][2 * w + j]);
+          }
+      }
+      load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg1.phys), v_at, vc);
+      page_off = stage_values(pg1.held);
       pg0 = pg1;
-      pg1 = pg2;
-      pg2 = page_of(page + 3 * step, entry);
-      fetch_meta(pg2);
-      buf = buf == 2 ? 0 : buf + 1;
+      pg1 = page_of(page + 2 * step, entry);
+      fetch_meta(pg1);
     }
+    // back to numbers: codes' unit, mean terms of each channel's value group
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      x[i] *= (float)(1 << UNITS);
+      float zb[4];
+#pragma unroll
+      for (int gv = 0; gv < 4; ++gv) zb[gv] = __shfl(x[i][gv], n, 64);
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) {
+        const int gv = ct * 16 / P.g.v_group;
+        const float z = gv == 0 ? zb[0] : gv == 1 ? zb[1] : gv == 2 ? zb[2] : zb[3];
+        o[i][ct] = o[i][ct] * (float)(1 << (24 - C::BPMIN)) + z;
+      }
+    }
+    __syncthreads();
   }
 
-  // ---- back to numbers, and out ----
+  // ---- the four waves joined ----
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
-    const int row = row0 + 16 * i + n;
-    if (row >= P.T * g) continue;
-    const bool there = 16 * i + n < rows;
-    const float zero = x[i][0] * (float)(1 << UNITS), l = x[i][1] * (float)(1 << UNITS);
-    const size_t out_row = ((size_t)b * P.T + row / g) * Hq + kvh * g + row % g;
-    const float inv = there && l > 0.0f ? 1.0f / l : 0.0f;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int c = 32 * wave + 16 * j + 4 * q4;
-      float4v y = o[i][j] * (float)(1 << (24 - C::BPMIN)) + zero;
-      if (!there) y = (float4v){0, 0, 0, 0};
-      if (P.num_splits > 1) {
-        float* rec = P.ws + (out_row * P.num_splits + split) * WS_STRIDE + c;
-        *reinterpret_cast<float2v*>(rec) = (float2v){y[0], y[1]};
-        *reinterpret_cast<float2v*>(rec + 2) = (float2v){y[2], y[3]};
-      } else {
-        uint16_t v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[e] = bf16 ? __builtin_bit_cast(uint16_t, __float2bfloat16(y[e] * inv))
-                      : __builtin_bit_cast(uint16_t, __float2half_rn(y[e] * inv));
-        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(P.out) + out_row * D + c) =
-            make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
-      }
+    const float l = __shfl(x[i][0], 16 + n, 64);
+    if (q4 == 0) {
+      lds.join.m[wave][16 * i + n] = ref[i] > kNone ? ref[i] - (float)off : -INFINITY;
+      lds.join.l[wave][16 * i + n] = l;
     }
-    if (P.num_splits > 1 && wave == 0 && q4 == 0)
-      *reinterpret_cast<float2v*>(P.ws + (out_row * P.num_splits + split) * WS_STRIDE + D) =
-          there && ref[i] > kNone ? (float2v){ref[i] - (float)off, l} : (float2v){-INFINITY, 0};
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) *reinterpret_cast<float4v*>(&lds.join.o[wave][16 * i + n][16 * ct + 4 * q4]) = o[i][ct];
+  }
+  __syncthreads();
+  const int c4 = (tid & 31) * 4;
+  for (int row = tid >> 5; row < ROWS; row += 8) {
+    if (row0 + row >= P.T * g) break;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) M = fmaxf(M, lds.join.m[w][row]);
+    float4v y = {0, 0, 0, 0};
+    float l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (lds.join.m[w][row] == -INFINITY) continue;
+      const float f = __builtin_amdgcn_exp2f(lds.join.m[w][row] - M);
+      y += *reinterpret_cast<const float4v*>(&lds.join.o[w][row][c4]) * f;
+      l = fmaf(lds.join.l[w][row], f, l);
+    }
+    const bool there = row < rows;
+    const int t = (row0 + row) / g, h = kvh * g + (row0 + row) % g;
+    const size_t out_row = ((size_t)b * P.T + t) * Hq + h;
+    if (!there) y = (float4v){0, 0, 0, 0};
+    if (P.num_splits > 1) {
+      float* rec = P.ws + (out_row * P.num_splits + split) * WS_STRIDE;
+      *reinterpret_cast<float2v*>(rec + c4) = (float2v){y[0], y[1]};
+      *reinterpret_cast<float2v*>(rec + c4 + 2) = (float2v){y[2], y[3]};
+      if (c4 == 0) *reinterpret_cast<float2v*>(rec + D) = there ? (float2v){M, l} : (float2v){-INFINITY, 0};
+    } else {
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      uint16_t v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        v[e] = bf16 ? __builtin_bit_cast(uint16_t, __float2bfloat16(y[e] * inv)) : __builtin_bit_cast(uint16_t, __float2half_rn(y[e] * inv));
+      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(P.out) + out_row * D + c4) =
+          make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
+    }
   }
 }
 
+template <int BITS, bool M32, bool ONE> void launch(const DraftParams& P, int nr, dim3 grid, hipStream_t st) {
+  if (nr == 1)
+    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 1>), grid, dim3(256), 0, st, P);
+  else
+    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 2>), grid, dim3(256), 0, st, P);
+}
 template <int BITS, bool M32> void launch(const DraftParams& P, int nr, dim3 grid, hipStream_t st) {
-  switch (nr) {
-    case 1: hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 1>), grid, dim3(256), 0, st, P); break;
-    case 2: hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 2>), grid, dim3(256), 0, st, P); break;
-    case 3: hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 3>), grid, dim3(256), 0, st, P); break;
-    default: hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, 4>), grid, dim3(256), 0, st, P); break;
-  }
+  if (P.g.ngk == 1)
+    launch<BITS, M32, true>(P, nr, grid, st);
+  else
+    launch<BITS, M32, false>(P, nr, grid, st);
 }
 
-// tiles of 16 query rows a workgroup takes
-int row_tiles(const oscar_config& cfg, int T) {
-  const int64_t tiles = ((int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) + 15) / 16;
-  return tiles < 4 ? (int)tiles : 4;
-}
+// tiles of 16 query rows a wave holds
+int row_tiles(const oscar_config& cfg, int T) { return (int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) <= 16 ? 1 : 2; }
 int64_t row_blocks(const oscar_config& cfg, int T) {
   const int rows = 16 * row_tiles(cfg, T);
   return ((int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) + rows - 1) / rows;
@@ -640,7 +709,7 @@ extern "C" int32_t oscar_draft_auto_splits(const oscar_config* cfg, int32_t batc
   const int64_t units = (int64_t)batch * cfg->n_kv_heads * row_blocks(*cfg, T);
   const int64_t pages = max_seq_len > 0 ? ((int64_t)max_seq_len + R - 1) / R : 1;
   int64_t splits = wgs_per_cu(row_tiles(*cfg, T)) * (int64_t)oscar_compute_units() / units;
-  if (splits > pages) splits = pages;
+  if (splits > (pages + 3) / 4) splits = (pages + 3) / 4;
   if (splits > 512) splits = 512;
   return splits < 1 ? 1 : (int32_t)splits;
 }
