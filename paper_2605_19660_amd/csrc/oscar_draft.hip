@@ -146,11 +146,11 @@ __device__ __forceinline__ float max_of_row(float v) {   // over the four lanes 
 constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens)
 
 // Workgroups a CU that a variant's registers are held to.
-__host__ __device__ constexpr int wgs_per_cu(int nr) { return nr == 1 ? 3 : 2; }
+__host__ __device__ constexpr int wgs_per_cu(int bits, bool m32, int nr) { return nr == 1 && bits == 2 && !m32 ? 3 : 2; }
 
 // ONE: k_group is the whole page.
 template <int BITS, bool M32, bool ONE, int NR>
-__global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftParams P) {
+__global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
   using C = Codes<BITS>;
   constexpr int ROWS = NR * 16;
   constexpr int UNITS = C::BPMAX - C::BPMIN;         // log2 of what the counterweights leave in the extra tile
@@ -186,13 +186,15 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
 
   float4v o[NR][8];   // channels 16 ct + 4 q4 + r of row n, in units of the codes once pages have begun
   float4v x[NR];      // row 4 q4 + r of the extra tile: 0 .. 3 the value groups' mean terms, 4 the row's sum
-  float ref[NR];      // what the row's probabilities are taken against, log2 units
+  float M[NR];        // the row's reference, log2 units, less the exponent `off` its probability has there
+  float most[NR];     // how far a logit may be above M; kNone before the row's first token
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) o[i][ct] = (float4v){0, 0, 0, 0};
     x[i] = (float4v){0, 0, 0, 0};
-    ref[i] = kNone;
+    M[i] = 0.0f;
+    most[i] = kNone;
   }
   int off = kOff;
 
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
       half8 st, base;
       fk.step_and_base(zp_min, C::MID, st, base);
       base *= lds.loop.cw[lane % 2];
-      if (!held) st = base = (half8)(_Float16)0.0f;
+      if (!held) [[unlikely]] st = base = (half8)(_Float16)0.0f, fn = (u32x4){0, 0, 0, 0};
       meta.k_step[lane] = st;
       meta.k_base[lane] = base;
       float v[2];
@@ -264,8 +266,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
         v[0] = (float)h[0], v[1] = (float)h[1];
       }
       constexpr float unit_of_codes = (float)(1 << (24 - C::BPMIN - kQShift));
-      *reinterpret_cast<float2v*>(&meta.norm[2 * lane]) =
-          held ? (float2v){v[0] * unit_of_codes, v[1] * unit_of_codes} : (float2v){0.0f, 0.0f};
+      *reinterpret_cast<float2v*>(&meta.norm[2 * lane]) = (float2v){v[0] * unit_of_codes, v[1] * unit_of_codes};
     };
     // returns the exponent that the probabilities can carry
     auto stage_values = [&](bool held) {
@@ -374,21 +375,25 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
     __syncthreads();
     stage_keys(pg0.held);
     int page_off = stage_values(pg0.held);
-    fetch_meta(pg1);
     __syncthreads();
 
     // New references where a row has passed its own (or the exponent has to give way), and the state against them;
-    // in whole powers of two, so that probabilities already packed only change their exponents.
-    auto move_to = [&](const float (&mx)[NR], int now, auto&& packed) {
+    // in whole powers of two, so that probabilities already packed only change their exponents.  top: the lane's
+    // largest logit above M; what is added to logits above M is left in shift.
+    auto move_to = [&](const float (&top)[NR], int now, float (&shift)[NR], auto&& packed) {
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        const float to = fmaxf(ref[i], ceilf(max_of_row(mx[i])));
-        const float alpha = __builtin_amdgcn_exp2f(fmaxf(ref[i] - to, -200.0f) + (float)(now - off));
+        const bool none = most[i] == kNone;
+        const float to = fmaxf(none ? -INFINITY : M[i] + (float)off, ceilf(max_of_row(top[i]) + M[i]));
+        const float Mn = to == -INFINITY ? 0.0f : to - (float)now;
+        shift[i] = M[i] - Mn;
+        const float alpha = none ? 0.0f : __builtin_amdgcn_exp2f(shift[i]);
 #pragma unroll
         for (int ct = 0; ct < 8; ++ct) o[i][ct] *= alpha;
         x[i] *= alpha;
         packed(i, alpha);
-        ref[i] = to;
+        M[i] = Mn;
+        most[i] = to == -INFINITY ? kNone : (float)now + kSlack;
       }
       off = now;
     };
@@ -445,24 +450,24 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
           }
         }
       }
-      float mx[NR];
+      float top[NR], shift[NR];
       bool past = false;
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        mx[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
-                      fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3])));
-        past |= mx[i] > ref[i] + kSlack;
+        top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
+                       fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) - M[i];
+        shift[i] = 0.0f;
+        past |= top[i] > most[i];
       }
-      if (__any(past)) move_to(mx, off, [](int, float) {});
+      if (__any(past)) move_to(top, off, shift, [](int, float) {});
       half8 pr[NR];
       const half8 one = (_Float16)(n == 4 ? 1.0f / (1 << UNITS) : 0.0f);
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        const float M = ref[i] - (float)off;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) pr[i][4 * j + r] = (_Float16)__builtin_amdgcn_exp2f(s[i][j][r] - M);
+          for (int r = 0; r < 4; ++r) pr[i][4 * j + r] = (_Float16)__builtin_amdgcn_exp2f(s[i][j][r] - M[i]);
         x[i] = mfma(one, pr[i], x[i]);
       }
       // values: channel 16 ct + n of tokens t0 + 16 j + 4 q4 + r
@@ -532,9 +537,10 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
               }
             }
         }
-        float mx[NR];
+        // logits above M, less the bit position's exponent; what is no page has none
+        float top[NR];
 #pragma unroll
-        for (int i = 0; i < NR; ++i) mx[i] = -INFINITY;
+        for (int i = 0; i < NR; ++i) top[i] = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float4v nm = *reinterpret_cast<const float4v*>(&meta.norm[(4 * r + q4) * 8 + 4 * half]);
@@ -542,36 +548,47 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
           for (int i = 0; i < NR; ++i)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              s[i][t][r] *= nm[t];
-              mx[i] = fmaxf(mx[i], s[i][t][r]);
+              s[i][t][r] = fmaf(s[i][t][r], nm[t], -(M[i] + ((float)C::above(r, 4 * half + t) + gone)));
+              top[i] = fmaxf(top[i], s[i][t][r]);
             }
         }
-        bool past = false;
+        bool past = page_off < off;
 #pragma unroll
-        for (int i = 0; i < NR; ++i) past |= mx[i] > ref[i] + (kSlack + gone);
-        if (__any(past) || page_off < off)
-          move_to(mx, min(off, page_off), [&](int i, float alpha) {
+        for (int i = 0; i < NR; ++i) past |= top[i] > most[i];
+        if (__any(past)) {
+          float shift[NR];
+#pragma unroll
+          for (int i = 0; i < NR; ++i) {
+            top[i] = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int t = 0; t < 4; ++t) top[i] = fmaxf(top[i], s[i][t][r] + (float)C::above(r, 4 * half + t));
+          }
+          move_to(top, min(off, page_off), shift, [&](int i, float alpha) {
             if (half == 1) {
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk) pr[i][kk] *= (_Float16)alpha;
             }
           });
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          const float M = ref[i] - (float)off + gone;
+          for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[i][t] += shift[i];
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int t = 0; t < 4; t += 2) {
-              const float Mk = M + (float)C::above(r, 4 * half + t);
-              const half2v p = pack2(__builtin_amdgcn_exp2f(s[i][t][r] - Mk), __builtin_amdgcn_exp2f(s[i][t + 1][r] - Mk));
+              const half2v p = pack2(__builtin_amdgcn_exp2f(s[i][t][r]), __builtin_amdgcn_exp2f(s[i][t + 1][r]));
               pr[i][r][4 * half + t] = p[0];
               pr[i][r][4 * half + t + 1] = p[1];
             }
-        }
       }
       load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1.phys), k_at, kc);
-      stage_keys(pg1.held);
+      fetch_meta(pg1);
 
       // values
 #pragma unroll
@@ -606,10 +623,10 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
           }
       }
       load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg1.phys), v_at, vc);
+      stage_keys(pg1.held);
       page_off = stage_values(pg1.held);
       pg0 = pg1;
       pg1 = page_of(page + 2 * step, entry);
-      fetch_meta(pg1);
     }
     // back to numbers: codes' unit, mean terms of each channel's value group
 #pragma unroll
@@ -633,7 +650,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
   for (int i = 0; i < NR; ++i) {
     const float l = __shfl(x[i][0], 16 + n, 64);
     if (q4 == 0) {
-      lds.join.m[wave][16 * i + n] = ref[i] > kNone ? ref[i] - (float)off : -INFINITY;
+      lds.join.m[wave][16 * i + n] = most[i] == kNone ? -INFINITY : M[i];
       lds.join.l[wave][16 * i + n] = l;
     }
 #pragma unroll
@@ -643,15 +660,15 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
   const int c4 = (tid & 31) * 4;
   for (int row = tid >> 5; row < ROWS; row += 8) {
     if (row0 + row >= P.T * g) break;
-    float M = -INFINITY;
+    float mx = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, lds.join.m[w][row]);
+    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, lds.join.m[w][row]);
     float4v y = {0, 0, 0, 0};
     float l = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       if (lds.join.m[w][row] == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(lds.join.m[w][row] - M);
+      const float f = __builtin_amdgcn_exp2f(lds.join.m[w][row] - mx);
       y += *reinterpret_cast<const float4v*>(&lds.join.o[w][row][c4]) * f;
       l = fmaf(lds.join.l[w][row], f, l);
     }
@@ -663,7 +680,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(NR)) void oscar_draft_kernel(DraftP
       float* rec = P.ws + (out_row * P.num_splits + split) * WS_STRIDE;
       *reinterpret_cast<float2v*>(rec + c4) = (float2v){y[0], y[1]};
       *reinterpret_cast<float2v*>(rec + c4 + 2) = (float2v){y[2], y[3]};
-      if (c4 == 0) *reinterpret_cast<float2v*>(rec + D) = there ? (float2v){M, l} : (float2v){-INFINITY, 0};
+      if (c4 == 0) *reinterpret_cast<float2v*>(rec + D) = there ? (float2v){mx, l} : (float2v){-INFINITY, 0};
     } else {
       const float inv = l > 0.0f ? 1.0f / l : 0.0f;
       uint16_t v[4];
@@ -708,7 +725,7 @@ extern "C" int32_t oscar_draft_auto_splits(const oscar_config* cfg, int32_t batc
   if (check_draft_config(cfg) != OSCAR_OK || batch <= 0 || T <= 0) return 1;
   const int64_t units = (int64_t)batch * cfg->n_kv_heads * row_blocks(*cfg, T);
   const int64_t pages = max_seq_len > 0 ? ((int64_t)max_seq_len + R - 1) / R : 1;
-  int64_t splits = wgs_per_cu(row_tiles(*cfg, T)) * (int64_t)oscar_compute_units() / units;
+  int64_t splits = wgs_per_cu(cfg->bits, cfg->meta_dtype == OSCAR_F32, row_tiles(*cfg, T)) * (int64_t)oscar_compute_units() / units;
   if (splits > (pages + 3) / 4) splits = (pages + 3) / 4;
   if (splits > 512) splits = 512;
   return splits < 1 ? 1 : (int32_t)splits;
