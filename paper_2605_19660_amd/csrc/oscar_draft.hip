@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
     load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg0.phys), k_at, kc);
     load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0.phys), v_at, vc);
 
-    // ---- queries: lane's row, channels 32 q4 .. + 31; wave i rotates tile i ----
+    // ---- queries: lane's row ----
     const uint16_t* q_row[NR];
     int row_t[NR];
 #pragma unroll
@@ -308,50 +308,58 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
       const bool there = row < n_new * g;
       q_row[i] = reinterpret_cast<const uint16_t*>(P.q) +
                  (((size_t)b * P.T + (there ? row_t[i] : 0)) * Hq + (size_t)kvh * g + (there ? row % g : 0)) * D + 32 * q4;
-      if (wave != i) continue;
-      float y[32];
+    }
+    // Wave i rotates tile i, on the matrix cores: out = H q, H's signs exact in either type.  Row m of output tile
+    // ot is channel 32 (m / 4) + 4 ot + m % 4, so that a lane ends with channels 32 q4 .. + 31 of its query row, as
+    // the keys' operands have them; its input channels are 32 q4 + 8 kk + e.  The sign of H[i][j] is the parity of
+    // i & j, taken apart into what depends on (n, e), on (ot, kk, e) and on (n, q4).
+    if (wave < NR) {
+      const uint16_t* row = NR == 1 || wave == 0 ? q_row[0] : q_row[NR - 1];
+      u32x4 in[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(q_row[i] + 8 * u);
+      for (int kk = 0; kk < 4; ++kk) in[kk] = *reinterpret_cast<const u32x4*>(row + 8 * kk);
+      const bool there = row0 + 16 * wave + n < n_new * g;
+      const bool rotate = P.c.cfg.rotation == OSCAR_ROTATION_ON;
+      const float mul = there ? P.scale_log2 * (float)(1 << kQShift) * (rotate ? 0.08838834764831845f : 1.0f) : 0.0f;
+      const uint32_t one = bf16 ? 0x3f803f80u : 0x3c003c00u;
+      // low two bits: e % 4 against n % 4; top two: q4 against n / 4
+      u32x4 signs;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint16_t v = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
-          const float t = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
-          y[8 * u + e] = there ? t : 0.0f;
-        }
+      for (int d = 0; d < 4; ++d) {
+        const uint32_t even = __popc((2 * d) % 4 & n), odd = __popc((2 * d + 1) % 4 & n), top = __popc(q4 & (n >> 2));
+        signs[d] = one | (even + top) << 15 & 0x8000u | (odd + top) << 31;
       }
-      float mul = P.scale_log2 * (float)(1 << kQShift);
-      if (P.c.cfg.rotation == OSCAR_ROTATION_ON) {
+#pragma unroll 1
+      for (int ot = 0; ot < 8; ++ot) {
+        float4v acc = {0, 0, 0, 0};
+        if (rotate) {
 #pragma unroll
-        for (int h = 1; h < 32; h <<= 1) {
+          for (int kk = 0; kk < 4; ++kk) {
+            // bits 2 .. 4 of the input channel are 2 kk + e / 4 (8 kk + e below 32)
+            const uint32_t lo = __popc(ot & 2 * kk) << 15 & 0x8000u, hi = __popc(ot & (2 * kk + 1)) << 15 & 0x8000u;
+            const uint32_t flip[2] = {lo | lo << 16, hi | hi << 16};
+            const u32x4 h = {signs[0] ^ flip[0], signs[1] ^ flip[0], signs[2] ^ flip[1], signs[3] ^ flip[1]};
+            if (bf16)
+              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, h), __builtin_bit_cast(bf16x8, in[kk]),
+                                                            acc, 0, 0, 0);
+            else
+              acc = mfma(__builtin_bit_cast(half8, h), __builtin_bit_cast(half8, in[kk]), acc);
+          }
+        } else {
 #pragma unroll
-          for (int u = 0; u < 32; ++u) {
-            if ((u & h) == 0) {
-              const float a = y[u], c = y[u | h];
-              y[u] = a + c;
-              y[u | h] = a - c;
-            }
+          for (int r = 0; r < 4; ++r) {
+            const uint16_t v = row[4 * ot + r];
+            acc[r] = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
           }
         }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const float sg = (q4 >> s) & 1 ? -1.0f : 1.0f;
-#pragma unroll
-          for (int u = 0; u < 32; ++u) {
-            // (each call leaves the two lanes' numbers side by side in both)
-            const uint32_t v = __float_as_uint(y[u]);
-            const auto two = s == 0 ? __builtin_amdgcn_permlane16_swap(v, v, false, false)
-                                    : __builtin_amdgcn_permlane32_swap(v, v, false, false);
-            y[u] = fmaf(__uint_as_float(two[1]), sg, __uint_as_float(two[0]));
-          }
-        }
-        mul *= 0.08838834764831845f;
+        const half2v a = pack2(there ? acc[0] * mul : 0.0f, there ? acc[1] * mul : 0.0f);
+        const half2v c = pack2(there ? acc[2] * mul : 0.0f, there ? acc[3] * mul : 0.0f);
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(&lds.loop.qh[wave][0][lane]) + (ot / 2) * sizeof(half8) * 64 + (ot % 2) * 8) =
+            make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
       }
       half8 qh[4];
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qh[kk][e] = (_Float16)(y[8 * kk + e] * mul);
+      for (int kk = 0; kk < 4; ++kk) qh[kk] = lds.loop.qh[wave][kk][lane];
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         half8 qc;   // in the codes' order, with the counterweights of their bit positions
@@ -360,8 +368,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
           const int u = slot_index(BITS, kk, e);
           qc[e] = qh[u / 8][u % 8] * (_Float16)(1.0f / (float)(1 << C::above(kk, e)));
         }
-        lds.loop.qh[i][kk][lane] = qh[kk];
-        lds.loop.qc[i][kk][lane] = qc;
+        lds.loop.qc[wave][kk][lane] = qc;
       }
     }
     // (constants of the page loop wait in LDS: the registers are spoken for)
