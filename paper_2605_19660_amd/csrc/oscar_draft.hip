@@ -24,8 +24,8 @@
 // the zero-points is of the size of a group's mean, and both are products on the matrix cores too: for the keys
 // what a tile's sums start from, for the values one extra tile, whose other rows are the rows' sums.  Seen from
 // code 0 the same roundings moved the logits three times as far.  Roundings: Q, Q Delta, P, P Delta and the
-// mean terms to fp16, half a step (2^-11) each.  The probabilities are scaled by 2^9 .. 2^15 (less where a value
-// step of 2 or more would carry P Delta past the fp16 range): a token counts down to 2^-33 of the largest.  Sums,
+// mean terms to fp16, half a step (2^-11) each.  The probabilities are scaled by 2^7 .. 2^15 (less where a value
+// step of 2 or more would carry P Delta past the fp16 range): a token counts down to 2^-27 of the largest at least.  Sums,
 // maxima and outputs are fp32.
 #include "oscar_decode_common.h"
 
@@ -94,8 +94,8 @@ struct Staged {
 // A row's probabilities are taken against a reference that follows its maximum only when that has passed it by
 // 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs a rescaling of the
 // whole state.
-constexpr float kSlack = 6.0f, kNone = -3e38f;
-constexpr int kOff = 9;          // exponent of a probability at its reference: kOff + kSlack stay inside fp16
+constexpr float kSlack = 8.0f, kNone = -3e38f;
+constexpr int kOff = 7;          // exponent of a probability at its reference: kOff + kSlack stay inside fp16
 // What a lane holds of the metadata of a page to come: 8 steps and 8 zeros of the keys or of the values.
 template <bool M32> struct Fetched {
   u32x4 a[M32 ? 2 : 1], b[M32 ? 2 : 1];
@@ -384,25 +384,24 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
     int page_off = stage_values(pg0.held);
     __syncthreads();
 
-    // New references where a row has passed its own (or the exponent has to give way), and the state against them;
-    // in whole powers of two, so that probabilities already packed only change their exponents.  top: the lane's
-    // largest logit above M; what is added to logits above M is left in shift.
-    auto move_to = [&](const float (&top)[NR], int now, float (&shift)[NR], auto&& packed) {
+    auto scale = [&](int i, float by) {
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
-        const bool none = most[i] == kNone;
-        const float to = fmaxf(none ? -INFINITY : M[i] + (float)off, ceilf(max_of_row(top[i]) + M[i]));
-        const float Mn = to == -INFINITY ? 0.0f : to - (float)now;
-        shift[i] = M[i] - Mn;
-        const float alpha = none ? 0.0f : __builtin_amdgcn_exp2f(shift[i]);
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct) o[i][ct] *= alpha;
-        x[i] *= alpha;
-        packed(i, alpha);
-        M[i] = Mn;
-        most[i] = to == -INFINITY ? kNone : (float)now + kSlack;
-      }
-      off = now;
+      for (int ct = 0; ct < 8; ++ct) o[i][ct] *= by;
+      x[i] *= by;
+    };
+    // New references for a tile one of whose rows has passed its own, and the state against them; in whole powers of
+    // two, so that probabilities already packed only change their exponents.  top: the lane's largest logit above M;
+    // returns what comes on top of logits above M, and leaves its power of two in `by`.
+    auto move = [&](int i, float top, float& by) {
+      const bool none = most[i] == kNone;
+      const float to = fmaxf(none ? -INFINITY : M[i] + (float)off, ceilf(max_of_row(top) + M[i]));
+      const float Mn = to == -INFINITY ? 0.0f : to - (float)off;
+      const float shift = M[i] - Mn;
+      by = none ? 0.0f : __builtin_amdgcn_exp2f(shift);
+      scale(i, by);
+      M[i] = Mn;
+      most[i] = to == -INFINITY ? kNone : (float)off + kSlack;
+      return shift;
     };
 
     // ---- 16-bit tokens ----
@@ -457,16 +456,13 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
           }
         }
       }
-      float top[NR], shift[NR];
-      bool past = false;
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
-                       fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) - M[i];
-        shift[i] = 0.0f;
-        past |= top[i] > most[i];
+        const float top = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
+                                fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) - M[i];
+        float by;
+        if (__any(top > most[i])) move(i, top, by);
       }
-      if (__any(past)) move_to(top, off, shift, [](int, float) {});
       half8 pr[NR];
       const half8 one = (_Float16)(n == 4 ? 1.0f / (1 << UNITS) : 0.0f);
 #pragma unroll
@@ -505,6 +501,15 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
     for (; page < pages; page += step) {
       const int entry = entry_of(page + 2 * step);
       const float gone = pg0.held ? 0.0f : INFINITY;   // what is no page: its numbers are finite, its probabilities zeros
+      if (page_off < off) [[unlikely]] {
+        // the page's value steps are larger than any before: the exponent gives way
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          scale(i, __builtin_amdgcn_exp2f((float)(page_off - off)));
+          if (most[i] != kNone) M[i] += (float)(off - page_off), most[i] = (float)page_off + kSlack;
+        }
+        off = page_off;
+      }
       half8 pr[NR][4], qd[NR][4];
       float4v start[NR];
       // logits and probabilities of 64 tokens at a time
@@ -559,29 +564,21 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
               top[i] = fmaxf(top[i], s[i][t][r]);
             }
         }
-        bool past = page_off < off;
 #pragma unroll
-        for (int i = 0; i < NR; ++i) past |= top[i] > most[i];
-        if (__any(past)) {
-          float shift[NR];
+        for (int i = 0; i < NR; ++i) {
+          if (!__any(top[i] > most[i])) continue;
+          float most_of = -INFINITY, by;
 #pragma unroll
-          for (int i = 0; i < NR; ++i) {
-            top[i] = -INFINITY;
+          for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int t = 0; t < 4; ++t) most_of = fmaxf(most_of, s[i][t][r] + (float)C::above(r, 4 * half + t));
+          const float shift = move(i, most_of, by);
+          if (half == 1) {
 #pragma unroll
-              for (int t = 0; t < 4; ++t) top[i] = fmaxf(top[i], s[i][t][r] + (float)C::above(r, 4 * half + t));
+            for (int kk = 0; kk < 4; ++kk) pr[i][kk] *= (_Float16)by;
           }
-          move_to(top, min(off, page_off), shift, [&](int i, float alpha) {
-            if (half == 1) {
 #pragma unroll
-              for (int kk = 0; kk < 4; ++kk) pr[i][kk] *= (_Float16)alpha;
-            }
-          });
-#pragma unroll
-          for (int i = 0; i < NR; ++i)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) s[i][t] += shift[i];
+          for (int t = 0; t < 4; ++t) s[i][t] += shift;
         }
 #pragma unroll
         for (int i = 0; i < NR; ++i)
