@@ -38,8 +38,18 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// (said to be in device memory: through pointers of which the compiler does not know that, loads are counted with
+// those of LDS and every wait for one is a wait for all)
+typedef const __attribute__((address_space(1))) uint8_t* DevicePtr;
+template <typename T> __device__ __forceinline__ T load_as(DevicePtr p) {
+  return *reinterpret_cast<const __attribute__((address_space(1))) T*>(p);
+}
+
 constexpr float kHalfMax = 65504.0f;
 constexpr int kQShift = 2;           // the queries carry 2^2
+
+// What loads of a page that is none take: its codes and parameters are zeros, and nothing that follows is NaN.
+__device__ __align__(256) const uint8_t kNoPage[8192] = {};
 
 struct DraftParams {
   const void *q, *k_new, *v_new;
@@ -99,34 +109,36 @@ constexpr int kOff = 7;          // exponent of a probability at its reference: 
 // What a lane holds of the metadata of a page to come: 8 steps and 8 zeros of the keys or of the values.
 template <bool M32> struct Fetched {
   u32x4 a[M32 ? 2 : 1], b[M32 ? 2 : 1];
-  __device__ __forceinline__ void load(const uint8_t* src, const uint8_t* zsrc, uint32_t at) {
+  __device__ __forceinline__ void load(DevicePtr src, DevicePtr zsrc, uint32_t at) {
 #pragma unroll
     for (int i = 0; i < (M32 ? 2 : 1); ++i) {
-      a[i] = *reinterpret_cast<const u32x4*>(src + at + 16 * i);
-      b[i] = *reinterpret_cast<const u32x4*>(zsrc + at + 16 * i);
+      a[i] = load_as<u32x4>(src + at + 16 * i);
+      b[i] = load_as<u32x4>(zsrc + at + 16 * i);
     }
   }
   __device__ __forceinline__ static float number(const u32x4* x, int e) {
     if (M32) return __uint_as_float(x[e / 4][e % 4]);
     return (float)__builtin_bit_cast(half8, x[0])[e];
   }
-  // step and mean term: x = step (c - mid) + base
-  __device__ __forceinline__ void step_and_base(bool zp_min, float mid, half8& step, half8& base) const {
+  // Step and mean term, x = step (c - mid) + base: base = step (mid - z) for integer zero-points (ints = 1),
+  // step mid + zero for float ones (ints = 0), as one form: nothing here branches.
+  __device__ __forceinline__ void step_and_base(float ints, float mid, half8& step, half8& base) const {
     if (M32) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float s = number(a, e), z = number(b, e);
         step[e] = (_Float16)fminf(s, kHalfMax);
-        base[e] = (_Float16)__builtin_amdgcn_fmed3f(zp_min ? fmaf(s, mid, z) : (mid - z) * s, -kHalfMax, kHalfMax);
+        base[e] = (_Float16)__builtin_amdgcn_fmed3f(fmaf(s, fmaf(z, -ints, mid), z * (1.0f - ints)), -kHalfMax, kHalfMax);
       }
     } else {
       step = __builtin_bit_cast(half8, a[0]);
       const half8 z = __builtin_bit_cast(half8, b[0]), most = (_Float16)kHalfMax;
-      const uint32_t two = __builtin_bit_cast(uint32_t, (half2v)(_Float16)mid);
-      u32x4 w = {two, two, two, two};
-      asm("" : "+v"(w));   // (as a constant it is taken apart into single halves)
-      const half8 m = __builtin_bit_cast(half8, w);
-      base = zp_min ? __builtin_elementwise_fma(step, m, z) : (m - z) * step;
+      // (registers: as constants or halves of one they are taken apart into single operations)
+      uint32_t two[3] = {__builtin_bit_cast(uint32_t, (half2v)(_Float16)mid), __builtin_bit_cast(uint32_t, (half2v)(_Float16)-ints),
+                         __builtin_bit_cast(uint32_t, (half2v)(_Float16)(1.0f - ints))};
+      asm("" : "+v"(two[0]), "+v"(two[1]), "+v"(two[2]));
+      auto splat = [](uint32_t w) { return __builtin_bit_cast(half8, (u32x4){w, w, w, w}); };
+      base = __builtin_elementwise_fma(step, __builtin_elementwise_fma(z, splat(two[1]), splat(two[0])), z * splat(two[2]));
       base = __builtin_elementwise_min(__builtin_elementwise_max(base, -most), most);
     }
   }
@@ -176,12 +188,25 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
   const int kvh = unit % Hkv, b = unit / Hkv;
   const int row0 = blockIdx.y * ROWS;
 
+  // the queries' loads wait for nothing
+  const uint16_t* q_row[NR];
+  int row_t[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    const int row = min(row0 + 16 * i + n, P.T * g - 1);
+    row_t[i] = row / g;
+    q_row[i] = reinterpret_cast<const uint16_t*>(P.q) + (((size_t)b * P.T + row_t[i]) * Hq + (size_t)kvh * g + row % g) * D + 32 * q4;
+  }
+  u32x4 q_in[4];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) q_in[kk] = *reinterpret_cast<const u32x4*>((wave == 0 ? q_row[0] : q_row[NR - 1]) + 8 * kk);
+
   const int n_new = P.new_lens ? min(max(P.new_lens[b], 0), P.T) : P.T;
   const int seq_len = max(P.c.seq_lens[b], 0);
   const int res = min(max(P.c.res_lens[b], 0), min(R, seq_len));
   const int pages = min((seq_len - res) / R, P.c.max_pages_per_seq);
   const int rows = min(max(n_new * g - row0, 0), ROWS);         // of this block that are there
-  const bool zp_min = P.c.cfg.zp_mode == OSCAR_ZP_MIN;
+  const float ints = P.c.cfg.zp_mode == OSCAR_ZP_MIN ? 0.0f : 1.0f;
   const bool bf16 = P.c.cfg.io_dtype == OSCAR_BF16;
 
   float4v o[NR][8];   // channels 16 ct + 4 q4 + r of row n, in units of the codes once pages have begun
@@ -208,54 +233,49 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
     // (read as constant memory, by the scalar unit: a vector load's wait would be one for every load ahead)
     const auto table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
         reinterpret_cast<uintptr_t>(P.c.block_table + (size_t)b * P.c.max_pages_per_seq));
-    // Physical page of page p; what is none is marked (its metadata is staged as zeros and its tokens are left
-    // out), and loads past the end take a page again: every iteration then makes the same loads.
+    // What is no page (past the end, or not of the pools) takes the zeros: every iteration makes the same loads.
     struct Page {
       int phys;
       bool held;
     };
     auto entry_of = [&](int p) { return table[min(max(p, 0), max(pages - 1, 0))]; };
-    auto page_of = [&](int p, int phys) {
-      const bool ok = phys >= 0 && phys < P.c.num_pages;
-      return Page{ok ? phys : 0, ok && p < pages};
-    };
+    auto page_of = [&](int p, int phys) { return Page{phys, p < pages && phys >= 0 && phys < P.c.num_pages}; };
 
     // ---- loads ahead ----
     uint32_t kc[4][2 * BITS], vc[4][2 * BITS];
-    auto pool_of = [&](const void* pool, int bytes, int phys) {
-      return reinterpret_cast<const uint8_t*>(pool) + ((size_t)phys * Hkv + kvh) * bytes;
+    auto pool_of = [&](const void* pool, int bytes, const Page& pg) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(pool) + ((size_t)pg.phys * Hkv + kvh) * bytes;
+      return reinterpret_cast<DevicePtr>(pg.held ? at : reinterpret_cast<uintptr_t>(kNoPage));
     };
     const uint32_t k_at = chunk_offset(BITS, 0, 4 * (n % 4) + n / 4, q4), v_at = chunk_offset(BITS, 0, n, q4);
-    auto load_codes = [&](const uint8_t* page, uint32_t at, uint32_t (&w)[4][2 * BITS]) {
+    auto load_codes = [&](DevicePtr page, uint32_t at, uint32_t (&w)[4][2 * BITS]) {
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int j = 0; j < BITS / 2; ++j)
-          *reinterpret_cast<u32x4*>(&w[c][4 * j]) = *reinterpret_cast<const u32x4*>(page + at + chunk_offset(BITS, 2 * c, 0, 0) + 16 * j);
+          *reinterpret_cast<u32x4*>(&w[c][4 * j]) = load_as<u32x4>(page + at + chunk_offset(BITS, 2 * c, 0, 0) + 16 * j);
     };
     constexpr int MB = M32 ? 4 : 2;
     const uint32_t km_at = (uint32_t)min(lane, 16 * P.g.ngk - 1) * 8 * MB, vm_at = (uint32_t)min(lane, 16 * P.g.ngv - 1) * 8 * MB;
     Fetched<M32> fk, fv;
     u32x4 fn;
     auto fetch_meta = [&](const Page& pg) {
-      const uint8_t* km = pool_of(P.c.k_meta, P.g.k_meta_bytes, pg.phys);
-      const uint8_t* vm = pool_of(P.c.v_meta, P.g.v_meta_bytes, pg.phys);
+      const DevicePtr km = pool_of(P.c.k_meta, P.g.k_meta_bytes, pg);
+      const DevicePtr vm = pool_of(P.c.v_meta, P.g.v_meta_bytes, pg);
       fk.load(km, km + P.g.k_meta_bytes / 2, km_at);
       fv.load(vm, vm + P.g.v_meta_bytes / 2, vm_at);
-      const uint8_t* kn = pool_of(P.c.k_norms, P.g.k_norms_bytes, pg.phys);
+      const DevicePtr kn = pool_of(P.c.k_norms, P.g.k_norms_bytes, pg);
       if (M32) {
-        const uint2 v = *reinterpret_cast<const uint2*>(kn + lane * 8);
-        fn[0] = v.x, fn[1] = v.y;
+        fn[0] = load_as<uint32_t>(kn + lane * 8), fn[1] = load_as<uint32_t>(kn + lane * 8 + 4);
       } else {
-        fn[0] = *reinterpret_cast<const uint32_t*>(kn + lane * 4);
+        fn[0] = load_as<uint32_t>(kn + lane * 4);
       }
     };
     Staged& meta = lds.loop.meta[wave];
-    auto stage_keys = [&](bool held) {
+    auto stage_keys = [&] {
       half8 st, base;
-      fk.step_and_base(zp_min, C::MID, st, base);
+      fk.step_and_base(ints, C::MID, st, base);
       base *= lds.loop.cw[lane % 2];
-      if (!held) [[unlikely]] st = base = (half8)(_Float16)0.0f, fn = (u32x4){0, 0, 0, 0};
       meta.k_step[lane] = st;
       meta.k_base[lane] = base;
       float v[2];
@@ -269,11 +289,10 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
       *reinterpret_cast<float2v*>(&meta.norm[2 * lane]) = (float2v){v[0] * unit_of_codes, v[1] * unit_of_codes};
     };
     // returns the exponent that the probabilities can carry
-    auto stage_values = [&](bool held) {
+    auto stage_values = [&] {
       half8 st, base;
-      fv.step_and_base(zp_min, C::MID, st, base);
+      fv.step_and_base(ints, C::MID, st, base);
       base *= lds.loop.cw[lane / 4 % 2];
-      if (!held) st = base = (half8)(_Float16)0.0f;
       meta.v_step[lane] = st;
       meta.v_base[lane] = base;
       // the exponent of the largest step (fp16 bits; steps are not negative), bit by bit over the wave
@@ -288,36 +307,23 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
 #pragma unroll
       for (int bit = 14; bit >= 10; --bit) {
         const uint64_t have = __ballot(big >> bit & 1) & among;
-        if (have) among = have, exponent |= 1 << (bit - 10);
+        among = have ? have : among;
+        exponent |= have ? 1 << (bit - 10) : 0;
       }
       return kOff - max(exponent - 14, 0);
     };
 
     Page pg0 = page_of(page, entry_of(page)), pg1 = page_of(page + step, entry_of(page + step));
     fetch_meta(pg0);
-    load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg0.phys), k_at, kc);
-    load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0.phys), v_at, vc);
+    load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg0), k_at, kc);
+    load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0), v_at, vc);
 
-    // ---- queries: lane's row ----
-    const uint16_t* q_row[NR];
-    int row_t[NR];
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int row = row0 + 16 * i + n;
-      row_t[i] = row / g;
-      const bool there = row < n_new * g;
-      q_row[i] = reinterpret_cast<const uint16_t*>(P.q) +
-                 (((size_t)b * P.T + (there ? row_t[i] : 0)) * Hq + (size_t)kvh * g + (there ? row % g : 0)) * D + 32 * q4;
-    }
+    // ---- queries ----
     // Wave i rotates tile i, on the matrix cores: out = H q, H's signs exact in either type.  Row m of output tile
     // ot is channel 32 (m / 4) + 4 ot + m % 4, so that a lane ends with channels 32 q4 .. + 31 of its query row, as
     // the keys' operands have them; its input channels are 32 q4 + 8 kk + e.  The sign of H[i][j] is the parity of
     // i & j, taken apart into what depends on (n, e), on (ot, kk, e) and on (n, q4).
     if (wave < NR) {
-      const uint16_t* row = NR == 1 || wave == 0 ? q_row[0] : q_row[NR - 1];
-      u32x4 in[4];
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) in[kk] = *reinterpret_cast<const u32x4*>(row + 8 * kk);
       const bool there = row0 + 16 * wave + n < n_new * g;
       const bool rotate = P.c.cfg.rotation == OSCAR_ROTATION_ON;
       const float mul = there ? P.scale_log2 * (float)(1 << kQShift) * (rotate ? 0.08838834764831845f : 1.0f) : 0.0f;
@@ -340,15 +346,15 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
             const uint32_t flip[2] = {lo | lo << 16, hi | hi << 16};
             const u32x4 h = {signs[0] ^ flip[0], signs[1] ^ flip[0], signs[2] ^ flip[1], signs[3] ^ flip[1]};
             if (bf16)
-              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, h), __builtin_bit_cast(bf16x8, in[kk]),
+              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, h), __builtin_bit_cast(bf16x8, q_in[kk]),
                                                             acc, 0, 0, 0);
             else
-              acc = mfma(__builtin_bit_cast(half8, h), __builtin_bit_cast(half8, in[kk]), acc);
+              acc = mfma(__builtin_bit_cast(half8, h), __builtin_bit_cast(half8, q_in[kk]), acc);
           }
         } else {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const uint16_t v = row[4 * ot + r];
+            const uint16_t v = (wave == 0 ? q_row[0] : q_row[NR - 1])[4 * ot + r];
             acc[r] = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
           }
         }
@@ -380,8 +386,8 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
       lds.loop.none[lane] = (half8)(_Float16)0.0f;
     }
     __syncthreads();
-    stage_keys(pg0.held);
-    int page_off = stage_values(pg0.held);
+    stage_keys();
+    int page_off = stage_values();
     __syncthreads();
 
     auto scale = [&](int i, float by) {
@@ -518,7 +524,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
         float4v s[NR][4];
 #pragma unroll
         for (int w = 2 * half; w < 2 * half + 2; ++w) {
-          if (ONE ? w == 0 : w * 32 % P.g.k_group == 0) {
+          if (!ONE || w == 0) {
             const int gk = ONE ? 0 : w * 32 / P.g.k_group * 16;
 #pragma unroll
             for (int i = 0; i < NR; ++i) start[i] = (float4v){0, 0, 0, 0};
@@ -591,7 +597,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
               pr[i][r][4 * half + t + 1] = p[1];
             }
       }
-      load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1.phys), k_at, kc);
+      load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1), k_at, kc);
       fetch_meta(pg1);
 
       // values
@@ -604,17 +610,16 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
       half8 pd[NR][4];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        if (w * 32 % P.g.v_group == 0) {
-          const int gv = w * 32 / P.g.v_group;
+        // (a group of several of these shares its products; without a branch they cost less than with one)
+        const int gv = w * 32 / P.g.v_group;
+        const half8* mids = n == gv && w * 32 % P.g.v_group == 0 ? lds.loop.mid : lds.loop.none;
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            const half8 st = meta.v_step[gv * 16 + 4 * kk + q4];
-            const half8 mid = (n == gv ? lds.loop.mid : lds.loop.none)[kk % 2];
+        for (int kk = 0; kk < 4; ++kk) {
+          const half8 st = meta.v_step[gv * 16 + 4 * kk + q4];
 #pragma unroll
-            for (int i = 0; i < NR; ++i) {
-              pd[i][kk] = pr[i][kk] * st;
-              x[i] = mfma(mid, pd[i][kk], x[i]);
-            }
+          for (int i = 0; i < NR; ++i) {
+            pd[i][kk] = pr[i][kk] * st;
+            x[i] = mfma(mids[kk % 2], pd[i][kk], x[i]);
           }
         }
 #pragma unroll
@@ -626,9 +631,9 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
             for (int i = 0; i < NR; ++i) o[i][2 * w + j] = mfma(a, pd[i][kk], o[i][2 * w + j]);
           }
       }
-      load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg1.phys), v_at, vc);
-      stage_keys(pg1.held);
-      page_off = stage_values(pg1.held);
+      load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg1), v_at, vc);
+      stage_keys();
+      page_off = stage_values();
       pg0 = pg1;
       pg1 = page_of(page + 2 * step, entry);
     }
