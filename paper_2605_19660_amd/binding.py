@@ -540,21 +540,32 @@ def rope_axes(sections, interleaved: bool = False) -> bytes:
     return bytes(a for a, n in enumerate(sections) for _ in range(n))
 
 
-def _token_rows(x):
-    """Heads and elements between tokens of a [..., heads, 128] tensor whose tokens lie evenly apart."""
-    assert x.is_cuda and x.dim() >= 2 and x.shape[-1] == 128 and x.stride(-1) == 1
-    heads = x.shape[-2]
-    assert heads == 1 or x.stride(-2) == 128
+def _token_stride(x) -> int:
+    """Elements between the tokens of a [..., heads, 128] tensor, whose tokens must lie evenly apart."""
+    shape, stride = x.shape, x.stride()
+    heads = shape[-2]
+    assert x.is_cuda and shape[-1] == 128 and stride[-1] == 1 and (heads == 1 or stride[-2] == 128)
+    if len(shape) == 3 and shape[0] != 1:
+        return stride[0]
     step = None
-    for size, stride in zip(reversed(x.shape[:-2]), reversed(x.stride()[:-2])):
+    for size, st in zip(reversed(shape[:-2]), reversed(stride[:-2])):
         if size == 1:
             continue
-        assert step is None or stride == step * inner, "tokens do not lie evenly apart"
+        assert step is None or st == step * inner, "tokens do not lie evenly apart"
         if step is None:
-            step, inner = stride, size
+            step, inner = st, size
         else:
             inner *= size
-    return heads, heads * 128 if step is None else step
+    return heads * 128 if step is None else step
+
+
+def _int32_ptr(t, n: int):
+    """Address of an int32 device tensor of n numbers, or None."""
+    if t is None:
+        return None
+    import torch
+    assert t.is_cuda and t.dtype == torch.int32 and t.numel() == n and t.is_contiguous()
+    return t.data_ptr()
 
 
 def rope(q, k, positions, inv_freq, axes: bytes | None = None, adjacent: bool = False, inverse: bool = False,
@@ -564,43 +575,51 @@ def rope(q, k, positions, inv_freq, axes: bytes | None = None, adjacent: bool = 
     [rotary_dim / 2]; axes: see rope_axes.  Returns (q, k) turned, in new tensors unless out_q, out_k
     say where (q and k themselves for in place)."""
     import torch
-    lead = (q if q is not None else k).shape[:-2]
-    n = lead.numel()
+    x = k if q is None else q
+    lead, dtype = x.shape[:-2], x.dtype
+    n, pairs = lead.numel(), inv_freq.numel()
     n_axes = positions.shape[0] if positions.dim() == 2 else 1
-    assert positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32
-    assert positions.numel() == n_axes * n and inv_freq.is_cuda and inv_freq.is_contiguous() and inv_freq.dtype == torch.float32
-    pairs = inv_freq.numel()
+    assert inv_freq.is_cuda and inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
     assert axes is None or len(axes) == pairs
-    ptr, heads, strides, outs = [None] * 4, [0, 0], [0] * 4, [None, None]
-    dtype = (q if q is not None else k).dtype
-    for i, (x, o) in enumerate(((q, out_q), (k, out_k))):
-        if x is None:
-            continue
-        assert x.dtype == dtype and x.shape[:-2] == lead
-        if o is None:
-            o = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        assert o.shape == x.shape and o.dtype == dtype
-        heads[i], strides[i] = _token_rows(x)
-        strides[2 + i] = _token_rows(o)[1]
-        ptr[i], ptr[2 + i], outs[i] = x.data_ptr(), o.data_ptr(), o
-    rc = lib().oscar_rope(*ptr, n, *heads, *strides, positions.data_ptr(), inv_freq.data_ptr(), axes, n_axes, 2 * pairs,
-                          dtype_code(dtype), (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0),
+    hq = hk = sq = sk = soq = sok = 0
+    if q is not None:
+        hq, sq = q.shape[-2], _token_stride(q)
+        if out_q is None:
+            out_q, soq = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape), hq * 128
+        else:
+            assert out_q.shape == q.shape and out_q.dtype == dtype
+            soq = _token_stride(out_q)
+    else:
+        out_q = None
+    if k is not None:
+        hk, sk = k.shape[-2], _token_stride(k)
+        assert k.dtype == dtype and k.shape[:-2] == lead
+        if out_k is None:
+            out_k, sok = torch.empty_like(k) if k.is_contiguous() else k.new_empty(k.shape), hk * 128
+        else:
+            assert out_k.shape == k.shape and out_k.dtype == dtype
+            sok = _token_stride(out_k)
+    else:
+        out_k = None
+    rc = lib().oscar_rope(None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
+                          None if q is None else out_q.data_ptr(), None if k is None else out_k.data_ptr(),
+                          n, hq, hk, sq, sk, soq, sok, _int32_ptr(positions, n_axes * n), inv_freq.data_ptr(), axes, n_axes,
+                          2 * pairs, dtype_code(dtype), (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0),
                           _stream_ptr(stream))
-    _check(rc, "oscar_rope")
-    return tuple(outs)
+    if rc != OK:
+        _check(rc, "oscar_rope")
+    return out_q, out_k
 
 
 def cache_read(cache: Cache, starts=None, k=None, v=None, stream=None):
     """oscar_cache_read: fills k and v ([batch, T, n_kv_heads, 128], one type of the three, either may be
     None) with the tokens from starts[b] on (int32 [batch]; None = 0) and returns them; rows of tokens that
     a sequence does not hold stay as they are."""
-    import torch
     shape, dtype = (k if k is not None else v).shape, (k if k is not None else v).dtype
     assert shape[0] == cache.batch and tuple(shape[2:]) == (cache.cfg.n_kv_heads, cache.cfg.head_dim)
     for x in (k, v):
         assert x is None or (x.is_cuda and x.is_contiguous() and x.shape == shape and x.dtype == dtype)
-    assert starts is None or (starts.is_cuda and starts.is_contiguous() and starts.dtype == torch.int32 and starts.numel() == cache.batch)
-    rc = lib().oscar_cache_read(C.byref(cache.c), None if starts is None else starts.data_ptr(), shape[1],
+    rc = lib().oscar_cache_read(C.byref(cache.c), _int32_ptr(starts, cache.batch), shape[1],
                                 None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
                                 dtype_code(dtype), _stream_ptr(stream))
     _check(rc, "oscar_cache_read")
@@ -622,26 +641,29 @@ def draft_attn(cache: Cache, q, k_new, v_new, new_lens=None, out=None, scale: fl
     """oscar_draft_attn: q [batch, T, n_q_heads, 128], k_new and v_new [batch, T, n_kv_heads, 128], all of the io
     dtype; returns `out` (of q's shape and type)."""
     import torch
-    cfg, shape = cache.cfg, q.shape
-    assert q.is_cuda and q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous()
-    assert q.dtype == k_new.dtype == v_new.dtype == torch_dtype(cfg.io_dtype)
-    assert shape[0] == cache.batch and tuple(shape[2:]) == (cfg.n_q_heads, cfg.head_dim)
-    assert k_new.shape == v_new.shape == (shape[0], shape[1], cfg.n_kv_heads, cfg.head_dim)
-    assert new_lens is None or (new_lens.is_cuda and new_lens.is_contiguous() and new_lens.dtype == torch.int32 and new_lens.numel() == cache.batch)
+    cfg, shape, dtype = cache.cfg, q.shape, q.dtype
+    batch, T, hkv = shape[0], shape[1], cfg.n_kv_heads
+    assert q.is_cuda and dtype == k_new.dtype == v_new.dtype == torch_dtype(cfg.io_dtype)
+    assert batch == cache.batch and shape[2] == cfg.n_q_heads and shape[3] == cfg.head_dim
+    assert k_new.shape == v_new.shape == (batch, T, hkv, cfg.head_dim)
+    assert q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous()
     if out is None:
         out = torch.empty_like(q)
-    assert out.is_contiguous() and out.shape == shape and out.dtype == q.dtype
-    L, cc = lib(), C.byref(cache.c.cfg)
+    assert out.shape == shape and out.dtype == dtype and out.is_contiguous()
+    L, c = lib(), cache.c
     if num_splits == 0:
-        num_splits = L.oscar_draft_auto_splits(cc, shape[0], shape[1], max_seq_len_hint)
-    if workspace is None and num_splits > 1:
-        workspace = torch.empty(L.oscar_draft_workspace_bytes(cc, shape[0], shape[1], num_splits),
-                                dtype=torch.uint8, device=q.device)
-    rc = L.oscar_draft_attn(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), shape[1],
-                            None if new_lens is None else new_lens.data_ptr(), C.byref(cache.c), out.data_ptr(), scale,
-                            max_seq_len_hint, num_splits, None if workspace is None else workspace.data_ptr(),
-                            0 if workspace is None else workspace.numel(), _stream_ptr(stream))
-    _check(rc, "oscar_draft_attn")
+        num_splits = L.oscar_draft_auto_splits(C.byref(c.cfg), batch, T, max_seq_len_hint)
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif num_splits > 1:
+        ws_bytes = L.oscar_draft_workspace_bytes(C.byref(c.cfg), batch, T, num_splits)
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+        ws = workspace.data_ptr()
+    rc = L.oscar_draft_attn(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), T, _int32_ptr(new_lens, batch), C.byref(c),
+                            out.data_ptr(), scale, max_seq_len_hint, num_splits, ws, ws_bytes, _stream_ptr(stream))
+    if rc != OK:
+        _check(rc, "oscar_draft_attn")
     return out
 
 
@@ -653,24 +675,25 @@ def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=
     """oscar_verify_drafts: target [batch, T + 1, vocab] and draft [batch, T, vocab] of one type, drafts int32
     [batch, T], u fp32 [batch, T + 1]; returns (n_new int32 [batch], tokens int32 [batch, T + 1])."""
     import torch
-    batch, T, vocab = target.shape[0], target.shape[1] - 1, target.shape[2]
-    assert target.is_cuda and target.is_contiguous() and draft.is_contiguous() and target.dtype == draft.dtype
-    assert tuple(draft.shape) == (batch, T, vocab) and tuple(drafts.shape) == (batch, T) and tuple(u.shape) == (batch, T + 1)
-    assert drafts.is_contiguous() and drafts.dtype == torch.int32 and u.is_contiguous() and u.dtype == torch.float32
-    assert draft_lens is None or (draft_lens.is_cuda and draft_lens.is_contiguous() and draft_lens.dtype == torch.int32 and draft_lens.numel() == batch)
+    batch, T1, vocab = target.shape
+    T = T1 - 1
+    assert target.is_cuda and target.dtype == draft.dtype and target.is_contiguous() and draft.is_contiguous()
+    assert draft.shape == (batch, T, vocab) and drafts.shape == (batch, T) and u.shape == (batch, T1)
+    assert u.dtype == torch.float32 and u.is_contiguous()
     if n_new is None:
         n_new = torch.empty(batch, dtype=torch.int32, device=target.device)
     if tokens is None:
-        tokens = torch.empty(batch, T + 1, dtype=torch.int32, device=target.device)
-    assert n_new.is_contiguous() and n_new.dtype == torch.int32 and n_new.numel() == batch
-    assert tokens.is_contiguous() and tokens.dtype == torch.int32 and tuple(tokens.shape) == (batch, T + 1)
+        tokens = torch.empty((batch, T1), dtype=torch.int32, device=target.device)
+    assert tokens.shape == (batch, T1)
+    L = lib()
     if workspace is None:
-        workspace = torch.empty(verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=target.device)
-    rc = lib().oscar_verify_drafts(target.data_ptr(), draft.data_ptr(), drafts.data_ptr(),
-                                   None if draft_lens is None else draft_lens.data_ptr(), u.data_ptr(), batch, T, vocab,
-                                   dtype_code(target.dtype), n_new.data_ptr(), tokens.data_ptr(), workspace.data_ptr(),
-                                   workspace.numel(), _stream_ptr(stream))
-    _check(rc, "oscar_verify_drafts")
+        workspace = torch.empty(L.oscar_verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=target.device)
+    rc = L.oscar_verify_drafts(target.data_ptr(), draft.data_ptr(), _int32_ptr(drafts, batch * T), _int32_ptr(draft_lens, batch),
+                               u.data_ptr(), batch, T, vocab, dtype_code(target.dtype), _int32_ptr(n_new, batch),
+                               _int32_ptr(tokens, batch * T1), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                               _stream_ptr(stream))
+    if rc != OK:
+        _check(rc, "oscar_verify_drafts")
     return n_new, tokens
 
 
