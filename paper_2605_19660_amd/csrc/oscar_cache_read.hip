@@ -5,11 +5,11 @@
 // and from the window K_u and V as they stand (float zero-points: Delta c + zero).
 //
 // What bounds it: 86 bytes a token and kv head are read (2-bit codes) and 512 written (16-bit), so it is a
-// stream of writes.  A workgroup takes the keys or the values of one page of one kv head, and each of its waves a
-// quarter without waiting for the others: 32 tokens' keys (two tiles, whose chunks a lane loads with one access,
-// 1 KB a wave) or 32 channels' values.  A lane holds 32 channels of a token: five Hadamard stages are in its
-// registers, two are exchanges inside a quad of lanes.  Either goes through LDS so that a wave writes rows of
-// 256 (keys) or 64 bytes (values) whole.
+// stream of writes, and the vector ALU is the next wall (400 operations a wave and tile of 16 tokens).  A workgroup
+// takes the keys or the values of one page of one kv head: a wave 32 tokens' keys (two tiles, whose chunks a lane
+// loads with one access, 1 KB a wave) or 32 channels' values.  A lane holds 32 channels of a token: five Hadamard
+// stages are in its registers, two are exchanges inside a quad of lanes.  Either goes through LDS so that rows of
+// 128 channels are written whole.
 #include "oscar_decode_common.h"
 #include "oscar_rowops.h"
 
@@ -23,28 +23,39 @@ struct ReadParams {
   int64_t T;
 };
 
-// the 32 codes of a lane's chunk as floats, in their natural order
+// The 32 codes of a lane's chunk as floats, in their natural order: spread over the bytes of a register, which
+// convert without being cut out.
 template <int BITS> __device__ __forceinline__ void unpack_chunk(const uint32_t* w, float (&x)[32]) {
+  constexpr int PER = 8 / BITS;   // codes of a byte
 #pragma unroll
-  for (int u = 0; u < 32; ++u) x[u] = (float)((w[u * BITS / 32] >> (u * BITS % 32)) & ((1u << BITS) - 1u));
+  for (int i = 0; i < BITS; ++i)
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const uint32_t v = w[i] >> (k * BITS) & (BITS == 2 ? 0x03030303u : 0x0f0f0f0fu);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[(4 * i + j) * PER + k] = (float)(v >> (8 * j) & 0xffu);
+    }
 }
 
-// 8 metadata numbers from 16-byte aligned storage
-template <bool M32> __device__ __forceinline__ void load_meta8(const uint8_t* base, int idx, float (&x)[8]) {
-  if (M32) {
-    const float4* p = reinterpret_cast<const float4*>(base + (size_t)idx * 4);
-    const float4 a = p[0], b = p[1];
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-  } else {
-    const uint4 w = *reinterpret_cast<const uint4*>(base + (size_t)idx * 2);
-    const __half* h = reinterpret_cast<const __half*>(&w);
+// A lane's 32 steps or zeros as they are stored, in operand order (8 kk + e); widened where they are used.
+template <bool M32> struct Meta32 {
+  uint4 q[M32 ? 8 : 4];
+  // 8 of them every `stride` numbers from `idx` on
+  __device__ __forceinline__ void load(const uint8_t* base, int idx, int stride) {
+    constexpr int PER = M32 ? 2 : 1;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __half2float(h[i]);
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        q[kk * PER + i] = reinterpret_cast<const uint4*>(base + (size_t)(idx + kk * stride) * (M32 ? 4 : 2))[i];
   }
-}
-
-__device__ __forceinline__ float dequant(float c, float step, float zero, bool zp_min) {
-  return zp_min ? fmaf(c, step, zero) : (c - zero) * step;
+  __device__ __forceinline__ float at(int i) const {
+    if (M32) return __uint_as_float(reinterpret_cast<const uint32_t*>(q)[i]);
+    return __half2float(__ushort_as_half((uint16_t)(reinterpret_cast<const uint32_t*>(q)[i / 2] >> (16 * (i % 2)))));
+  }
+};
+template <int BITS> __device__ constexpr int meta_of_code(int u) {   // where code number u's parameters are
+  return kmeta_pos_of_chan(BITS, u);
 }
 
 // Between a wave's writes to its own LDS and its reads of what other lanes wrote: LDS operations of one wave
@@ -68,12 +79,33 @@ __device__ __forceinline__ void rotate_quad(float (&x)[32], float mul) {
       }
     }
   }
+  // Across the quad: own += partner * s with s = +1 in the lower lane and -1 in the upper one, which leaves the
+  // upper lane b - a for a - b; the sign a lane has collected goes into the factor.  (A DPP operand must not be read
+  // in the two issue slots after it was written: the block starts with that wait, and inside it every element is
+  // rewritten eight instructions before it is read again.)
   const int q4 = threadIdx.x & 3;
   const float s0 = q4 & 1 ? -1.0f : 1.0f, s1 = q4 & 2 ? -1.0f : 1.0f;
+#define OSCAR_QUAD_STAGE(S, CTRL)                                            \
+  "v_fmac_f32_dpp %0, %0, " S " " CTRL " row_mask:0xf bank_mask:0xf\n\t"      \
+  "v_fmac_f32_dpp %1, %1, " S " " CTRL " row_mask:0xf bank_mask:0xf\n\t"      \
+  "v_fmac_f32_dpp %2, %2, " S " " CTRL " row_mask:0xf bank_mask:0xf\n\t"      \
+  "v_fmac_f32_dpp %3, %3, " S " " CTRL " row_mask:0xf bank_mask:0xf\n\t"      \
+  "v_fmac_f32_dpp %4, %4, " S " " CTRL " row_mask:0xf bank_mask:0xf\n\t"      \
+  "v_fmac_f32_dpp %5, %5, " S " " CTRL " row_mask:0xf bank_mask:0xf\n\t"      \
+  "v_fmac_f32_dpp %6, %6, " S " " CTRL " row_mask:0xf bank_mask:0xf\n\t"      \
+  "v_fmac_f32_dpp %7, %7, " S " " CTRL " row_mask:0xf bank_mask:0xf\n\t"
 #pragma unroll
-  for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], s0, partner<0>(x[i]));
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("s_nop 1\n\t"
+                 OSCAR_QUAD_STAGE("%8", "quad_perm:[1,0,3,2]")
+                 OSCAR_QUAD_STAGE("%9", "quad_perm:[2,3,0,1]")
+                 : "+v"(x[i]), "+v"(x[i + 1]), "+v"(x[i + 2]), "+v"(x[i + 3]), "+v"(x[i + 4]), "+v"(x[i + 5]),
+                   "+v"(x[i + 6]), "+v"(x[i + 7])
+                 : "v"(s0), "v"(s1));
+#undef OSCAR_QUAD_STAGE
+  mul *= s0 * s1;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], s1, partner<1>(x[i])) * mul;
+  for (int i = 0; i < 32; ++i) x[i] *= mul;
 }
 
 // Two numbers to the output's type, in one conversion.
@@ -92,14 +124,30 @@ template <typename OUT> __device__ __forceinline__ typename Pair<OUT>::Type pair
   return __builtin_convertvector((float2v){a, b}, typename Pair<OUT>::Type);
 }
 
+// 8 numbers of the window's type
+__device__ __forceinline__ void load8_io(const void* base, int64_t at, int dt, float (&x)[8]) {
+  if (dt == OSCAR_F32) {
+    const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(base) + at);
+    const float4 a = p[0], b = p[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  } else {
+    const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(base) + at);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint16_t e = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+      x[i] = dt == OSCAR_BF16 ? bf16_bits_to_f32(e) : __half2float(__ushort_as_half(e));
+    }
+  }
+}
+
 template <int BITS, typename OUT, bool M32>
-__global__ __launch_bounds__(256) void oscar_cache_read_kernel(ReadParams P) {
+__global__ __launch_bounds__(256, sizeof(OUT) == 2 ? 4 : 2) void oscar_cache_read_kernel(ReadParams P) {
   typedef typename Pair<OUT>::Type Two;
-  // a wave's rows: 16 tokens' keys, or 128 tokens' values of 32 channels; padded so that rows written at once by
+  // a wave's 16 tokens of keys, or the workgroup's 128 tokens of values; padded so that rows written at once by
   // different lanes fall on other banks
-  constexpr int KROW = D * sizeof(OUT) + 32, VROW = 32 * sizeof(OUT) + 16;
-  constexpr int BYTES = 16 * KROW > R * VROW ? 16 * KROW : R * VROW;
-  __shared__ __align__(16) uint8_t s_rows[4][BYTES];
+  constexpr int KROW = D * sizeof(OUT) + 32, VROW = D * sizeof(OUT) + 32;
+  __shared__ __align__(16) uint8_t s_rows[4][R / 4 * VROW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   uint8_t* rows = s_rows[wave];
   const int h = blockIdx.y, b = blockIdx.z, Hkv = P.c.cfg.n_kv_heads;
@@ -131,7 +179,8 @@ __global__ __launch_bounds__(256) void oscar_cache_read_kernel(ReadParams P) {
     uint8_t* out = reinterpret_cast<uint8_t*>(reinterpret_cast<OUT*>(P.k) + out_row);
     const bool rotated = P.c.cfg.rotation == OSCAR_ROTATION_ON;
     uint32_t w[2 * BITS];
-    float norm[2], step[32], zero[32];
+    float norm[2];
+    Meta32<M32> step, zero;
     if (!window) {
       const uint8_t* codes = reinterpret_cast<const uint8_t*>(P.c.k_codes) + unit * P.g.k_codes_bytes;
       const uint4* src = reinterpret_cast<const uint4*>(codes + chunk_offset(BITS, 2 * wave, n, q4));
@@ -140,14 +189,8 @@ __global__ __launch_bounds__(256) void oscar_cache_read_kernel(ReadParams P) {
       // the two tiles lie in one group of 32, 64 or 128 tokens
       const uint8_t* meta = reinterpret_cast<const uint8_t*>(P.c.k_meta) + unit * P.g.k_meta_bytes;
       const int group = wave * 32 / P.g.k_group;
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        float a[8], z[8];
-        load_meta8<M32>(meta, group * D + 32 * q4 + 8 * kk, a);
-        load_meta8<M32>(meta, (P.g.ngk + group) * D + 32 * q4 + 8 * kk, z);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) step[slot_index(BITS, kk, e)] = a[e], zero[slot_index(BITS, kk, e)] = z[e];
-      }
+      step.load(meta, group * D + 32 * q4, 8);
+      zero.load(meta, (P.g.ngk + group) * D + 32 * q4, 8);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         norm[i] = load_meta(reinterpret_cast<const uint8_t*>(P.c.k_norms) + unit * P.g.k_norms_bytes,
@@ -160,13 +203,18 @@ __global__ __launch_bounds__(256) void oscar_cache_read_kernel(ReadParams P) {
       float x[32], nm;
       if (!window) {
         unpack_chunk<BITS>(w + i * BITS, x);
+        if (zp_min) {
 #pragma unroll
-        for (int u = 0; u < 32; ++u) x[u] = dequant(x[u], step[u], zero[u], zp_min);
+          for (int u = 0; u < 32; ++u) x[u] = fmaf(x[u], step.at(meta_of_code<BITS>(u)), zero.at(meta_of_code<BITS>(u)));
+        } else {
+#pragma unroll
+          for (int u = 0; u < 32; ++u) x[u] = (x[u] - zero.at(meta_of_code<BITS>(u))) * step.at(meta_of_code<BITS>(u));
+        }
         nm = norm[i];
       } else {
-        const __half* src = reinterpret_cast<const __half*>(P.c.res_k) + (unit * R + t0 + n) * D + 32 * q4;
 #pragma unroll
-        for (int u = 0; u < 32; ++u) x[u] = __half2float(src[u]);
+        for (int u = 0; u < 4; ++u)
+          load8_io(P.c.res_k, (unit * R + t0 + n) * D + 32 * q4 + 8 * u, OSCAR_F16, reinterpret_cast<float(&)[8]>(x[8 * u]));
         nm = load_meta(P.c.res_norm, unit * R + t0 + n, M32 ? 4 : 2);
       }
       if (rotated) {
@@ -191,15 +239,15 @@ __global__ __launch_bounds__(256) void oscar_cache_read_kernel(ReadParams P) {
     return;
   }
 
-  uint8_t* out = reinterpret_cast<uint8_t*>(reinterpret_cast<OUT*>(P.v) + out_row) + 32 * wave * sizeof(OUT);
+  uint8_t* out = reinterpret_cast<uint8_t*>(reinterpret_cast<OUT*>(P.v) + out_row);
   if (window) {
-    // 32 channels of a token a lane
-    for (int t = t_lo + lane; t < t_hi; t += 64) {
-      Two* row = reinterpret_cast<Two*>(out + t * row_bytes);
-      const int64_t at = (unit * R + t) * D + 32 * wave;
-#pragma unroll 4
-      for (int u = 0; u < 32; u += 2)
-        row[u / 2] = pair<OUT>(load_io(P.c.res_v, at + u, P.c.cfg.io_dtype), load_io(P.c.res_v, at + u + 1, P.c.cfg.io_dtype));
+    // 8 channels of a token a thread
+    for (int t = t_lo + tid / 16; t < t_hi; t += 16) {
+      float x[8];
+      load8_io(P.c.res_v, (unit * R + t) * D + 8 * (tid % 16), P.c.cfg.io_dtype, x);
+      Two* row = reinterpret_cast<Two*>(out + t * row_bytes) + 4 * (tid % 16);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) row[u] = pair<OUT>(x[2 * u], x[2 * u + 1]);
     }
     return;
   }
@@ -210,44 +258,50 @@ __global__ __launch_bounds__(256) void oscar_cache_read_kernel(ReadParams P) {
   for (int i = 0; i < BITS / 2; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = src[i];
   const uint8_t* meta = reinterpret_cast<const uint8_t*>(P.c.v_meta) + unit * P.g.v_meta_bytes;
   const int group = wave * 32 / P.g.v_group;
-  float a[4][8], z[4][8];
+  Meta32<M32> step, zero;
+  step.load(meta, group * R + q4 * 8, 32);
+  zero.load(meta, (P.g.ngv + group) * R + q4 * 8, 32);
+  // channels 32 w + n and 32 w + 16 + n of a token lie side by side in LDS: one write for both
+  uint8_t* image = &s_rows[0][0];
+  uint8_t* column = image + q4 * VROW + (16 * wave + n) * sizeof(Two);
+  constexpr int PER = 8 / BITS;   // codes of a byte
+  auto write = [&](auto&& number) {
 #pragma unroll
-  for (int kk = 0; kk < 4; ++kk) {
-    load_meta8<M32>(meta, group * R + (4 * kk + q4) * 8, a[kk]);
-    load_meta8<M32>(meta, (P.g.ngv + group) * R + (4 * kk + q4) * 8, z[kk]);
-  }
-  float x[2][32];
-  unpack_chunk<BITS>(w, x[0]);
-  unpack_chunk<BITS>(w + BITS, x[1]);
+    for (int i = 0; i < BITS; ++i)
 #pragma unroll
-  for (int kk = 0; kk < 4; ++kk)
+      for (int k = 0; k < PER; ++k) {
+        constexpr uint32_t mask = BITS == 2 ? 0x03030303u : 0x0f0f0f0fu;
+        const uint32_t v0 = w[i] >> (k * BITS) & mask, v1 = w[BITS + i] >> (k * BITS) & mask;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      // channels n and 16 + n of a token lie side by side in LDS: one write for both
-      const int t = 16 * e + 4 * kk + q4, u = slot_index(BITS, kk, e);
-      *reinterpret_cast<Two*>(rows + t * VROW + n * sizeof(Two)) =
-          pair<OUT>(dequant(x[0][u], a[kk][e], z[kk][e], zp_min), dequant(x[1][u], a[kk][e], z[kk][e], zp_min));
-    }
-  wave_lds_fence();
-  // a lane takes 16 bytes of channels n .. and the 16 bytes of channels 16 + n .. beside them
-  constexpr int N = 16 / sizeof(OUT), LANES = 16 / N;
+        for (int j = 0; j < 4; ++j) {
+          const int m = meta_of_code<BITS>((4 * i + j) * PER + k);   // 8 kk + e: token 16 e + 4 kk + q4
+          const float a = step.at(m), z = zero.at(m);
+          *reinterpret_cast<Two*>(column + (16 * (m % 8) + 4 * (m / 8)) * VROW) =
+              pair<OUT>(number((float)(v0 >> (8 * j) & 0xffu), a, z), number((float)(v1 >> (8 * j) & 0xffu), a, z));
+        }
+      }
+  };
+  if (zp_min)
+    write([](float c, float a, float z) { return fmaf(c, a, z); });
+  else
+    write([](float c, float a, float z) { return (c - z) * a; });
+  __syncthreads();
+  // a lane's 16 bytes are N channels of one of the two: the same half of N pairs
+  constexpr int N = 16 / sizeof(OUT), LANES = D / N;
+  const int c = tid % LANES * N, second = c / 16 % 2;
 #pragma unroll 4
-  for (int t = t_lo + lane / LANES; t < t_hi; t += 64 / LANES) {
-    const int c = lane % LANES;
-    const uint4* p = reinterpret_cast<const uint4*>(rows + t * VROW + c * 32);
+  for (int t = t_lo + tid / LANES; t < t_hi; t += 256 / LANES) {
+    const uint4* p = reinterpret_cast<const uint4*>(image + t * VROW + (c / 32 * 16 + c % 16) * sizeof(Two));
     const uint4 lo4 = p[0], hi4 = p[1];
-    uint4 first, second;
+    uint4 v;
     if (sizeof(OUT) == 2) {
-      first = make_uint4(__builtin_amdgcn_perm(lo4.y, lo4.x, 0x05040100u), __builtin_amdgcn_perm(lo4.w, lo4.z, 0x05040100u),
-                         __builtin_amdgcn_perm(hi4.y, hi4.x, 0x05040100u), __builtin_amdgcn_perm(hi4.w, hi4.z, 0x05040100u));
-      second = make_uint4(__builtin_amdgcn_perm(lo4.y, lo4.x, 0x07060302u), __builtin_amdgcn_perm(lo4.w, lo4.z, 0x07060302u),
-                          __builtin_amdgcn_perm(hi4.y, hi4.x, 0x07060302u), __builtin_amdgcn_perm(hi4.w, hi4.z, 0x07060302u));
+      const uint32_t half = second ? 0x07060302u : 0x05040100u;
+      v = make_uint4(__builtin_amdgcn_perm(lo4.y, lo4.x, half), __builtin_amdgcn_perm(lo4.w, lo4.z, half),
+                     __builtin_amdgcn_perm(hi4.y, hi4.x, half), __builtin_amdgcn_perm(hi4.w, hi4.z, half));
     } else {
-      first = make_uint4(lo4.x, lo4.z, hi4.x, hi4.z);
-      second = make_uint4(lo4.y, lo4.w, hi4.y, hi4.w);
+      v = second ? make_uint4(lo4.y, lo4.w, hi4.y, hi4.w) : make_uint4(lo4.x, lo4.z, hi4.x, hi4.z);
     }
-    *reinterpret_cast<uint4*>(out + t * row_bytes + c * 16) = first;
-    *reinterpret_cast<uint4*>(out + t * row_bytes + 16 * sizeof(OUT) + c * 16) = second;
+    *reinterpret_cast<uint4*>(out + t * row_bytes + c * sizeof(OUT)) = v;
   }
 }
 
