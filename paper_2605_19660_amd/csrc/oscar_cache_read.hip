@@ -49,15 +49,16 @@ template <bool M32> struct Meta32 {
       for (int i = 0; i < PER; ++i)
         q[kk * PER + i] = reinterpret_cast<const uint4*>(base + (size_t)(idx + kk * stride) * (M32 ? 4 : 2))[i];
   }
+  // what is worked out of them is not carried beyond this point
+  __device__ __forceinline__ void keep() {
+#pragma unroll
+    for (int i = 0; i < (M32 ? 8 : 4); ++i) asm volatile("" : "+v"(q[i].x), "+v"(q[i].y), "+v"(q[i].z), "+v"(q[i].w));
+  }
   __device__ __forceinline__ float at(int i) const {
     if (M32) return __uint_as_float(reinterpret_cast<const uint32_t*>(q)[i]);
     return __half2float(__ushort_as_half((uint16_t)(reinterpret_cast<const uint32_t*>(q)[i / 2] >> (16 * (i % 2)))));
   }
 };
-template <int BITS> __device__ constexpr int meta_of_code(int u) {   // where code number u's parameters are
-  return kmeta_pos_of_chan(BITS, u);
-}
-
 // Between a wave's writes to its own LDS and its reads of what other lanes wrote: LDS operations of one wave
 // execute in order, the compiler must not move them.
 __device__ __forceinline__ void wave_lds_fence() {
@@ -141,8 +142,8 @@ __device__ __forceinline__ void load8_io(const void* base, int64_t at, int dt, f
   }
 }
 
-template <int BITS, typename OUT, bool M32>
-__global__ __launch_bounds__(256, sizeof(OUT) == 2 ? 4 : 2) void oscar_cache_read_kernel(ReadParams P) {
+template <int BITS, typename OUT, bool M32, bool ZP_MIN>
+__global__ __launch_bounds__(256, sizeof(OUT) == 2 && !M32 ? 4 : 2) void oscar_cache_read_kernel(ReadParams P) {
   typedef typename Pair<OUT>::Type Two;
   // a wave's 16 tokens of keys, or the workgroup's 128 tokens of values; padded so that rows written at once by
   // different lanes fall on other banks
@@ -170,7 +171,6 @@ __global__ __launch_bounds__(256, sizeof(OUT) == 2 ? 4 : 2) void oscar_cache_rea
   }
   const int64_t unit = window ? (int64_t)b * Hkv + h : phys * Hkv + h;
   const int n = lane >> 2, q4 = lane & 3;
-  const bool zp_min = P.c.cfg.zp_mode == OSCAR_ZP_MIN;
   // row `page * R + t` of the outputs
   const int64_t out_row = (((int64_t)b * P.T + page * R - start) * Hkv + h) * D;
   const int64_t row_bytes = (int64_t)Hkv * D * sizeof(OUT);
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256, sizeof(OUT) == 2 ? 4 : 2) void oscar_cache_rea
     const bool rotated = P.c.cfg.rotation == OSCAR_ROTATION_ON;
     uint32_t w[2 * BITS];
     float norm[2];
-    Meta32<M32> step, zero;
+    Meta32<M32> step, zero;   // (widened for each tile: as 64 floats they cost registers, and waves, 83 -> 162 us)
     if (!window) {
       const uint8_t* codes = reinterpret_cast<const uint8_t*>(P.c.k_codes) + unit * P.g.k_codes_bytes;
       const uint4* src = reinterpret_cast<const uint4*>(codes + chunk_offset(BITS, 2 * wave, n, q4));
@@ -202,13 +202,13 @@ __global__ __launch_bounds__(256, sizeof(OUT) == 2 ? 4 : 2) void oscar_cache_rea
       if (t0 >= t_hi || t0 + 16 <= t_lo) continue;
       float x[32], nm;
       if (!window) {
+        step.keep();
+        zero.keep();
         unpack_chunk<BITS>(w + i * BITS, x);
-        if (zp_min) {
 #pragma unroll
-          for (int u = 0; u < 32; ++u) x[u] = fmaf(x[u], step.at(meta_of_code<BITS>(u)), zero.at(meta_of_code<BITS>(u)));
-        } else {
-#pragma unroll
-          for (int u = 0; u < 32; ++u) x[u] = (x[u] - zero.at(meta_of_code<BITS>(u))) * step.at(meta_of_code<BITS>(u));
+        for (int u = 0; u < 32; ++u) {
+          const float a = step.at(kmeta_pos_of_chan(BITS, u)), z = zero.at(kmeta_pos_of_chan(BITS, u));
+          x[u] = ZP_MIN ? fmaf(x[u], a, z) : (x[u] - z) * a;
         }
         nm = norm[i];
       } else {
@@ -265,26 +265,21 @@ __global__ __launch_bounds__(256, sizeof(OUT) == 2 ? 4 : 2) void oscar_cache_rea
   uint8_t* image = &s_rows[0][0];
   uint8_t* column = image + q4 * VROW + (16 * wave + n) * sizeof(Two);
   constexpr int PER = 8 / BITS;   // codes of a byte
-  auto write = [&](auto&& number) {
 #pragma unroll
-    for (int i = 0; i < BITS; ++i)
+  for (int i = 0; i < BITS; ++i)
 #pragma unroll
-      for (int k = 0; k < PER; ++k) {
-        constexpr uint32_t mask = BITS == 2 ? 0x03030303u : 0x0f0f0f0fu;
-        const uint32_t v0 = w[i] >> (k * BITS) & mask, v1 = w[BITS + i] >> (k * BITS) & mask;
+    for (int k = 0; k < PER; ++k) {
+      constexpr uint32_t mask = BITS == 2 ? 0x03030303u : 0x0f0f0f0fu;
+      const uint32_t v0 = w[i] >> (k * BITS) & mask, v1 = w[BITS + i] >> (k * BITS) & mask;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int m = meta_of_code<BITS>((4 * i + j) * PER + k);   // 8 kk + e: token 16 e + 4 kk + q4
-          const float a = step.at(m), z = zero.at(m);
-          *reinterpret_cast<Two*>(column + (16 * (m % 8) + 4 * (m / 8)) * VROW) =
-              pair<OUT>(number((float)(v0 >> (8 * j) & 0xffu), a, z), number((float)(v1 >> (8 * j) & 0xffu), a, z));
-        }
+      for (int j = 0; j < 4; ++j) {
+        const int m = kmeta_pos_of_chan(BITS, (4 * i + j) * PER + k);   // 8 kk + e: token 16 e + 4 kk + q4
+        const float a = step.at(m), z = zero.at(m);
+        const float c0 = (float)(v0 >> (8 * j) & 0xffu), c1 = (float)(v1 >> (8 * j) & 0xffu);
+        *reinterpret_cast<Two*>(column + (16 * (m % 8) + 4 * (m / 8)) * VROW) =
+            ZP_MIN ? pair<OUT>(fmaf(c0, a, z), fmaf(c1, a, z)) : pair<OUT>((c0 - z) * a, (c1 - z) * a);
       }
-  };
-  if (zp_min)
-    write([](float c, float a, float z) { return fmaf(c, a, z); });
-  else
-    write([](float c, float a, float z) { return (c - z) * a; });
+    }
   __syncthreads();
   // a lane's 16 bytes are N channels of one of the two: the same half of N pairs
   constexpr int N = 16 / sizeof(OUT), LANES = D / N;
@@ -305,11 +300,17 @@ __global__ __launch_bounds__(256, sizeof(OUT) == 2 ? 4 : 2) void oscar_cache_rea
   }
 }
 
+template <int BITS, typename OUT, bool M32> void launch(const ReadParams& P, dim3 grid, hipStream_t st) {
+  if (P.c.cfg.zp_mode == OSCAR_ZP_MIN)
+    hipLaunchKernelGGL((oscar_cache_read_kernel<BITS, OUT, M32, true>), grid, dim3(256), 0, st, P);
+  else
+    hipLaunchKernelGGL((oscar_cache_read_kernel<BITS, OUT, M32, false>), grid, dim3(256), 0, st, P);
+}
 template <int BITS, typename OUT> void launch(const ReadParams& P, dim3 grid, hipStream_t st) {
   if (P.g.meta_bytes == 4)
-    hipLaunchKernelGGL((oscar_cache_read_kernel<BITS, OUT, true>), grid, dim3(256), 0, st, P);
+    launch<BITS, OUT, true>(P, grid, st);
   else
-    hipLaunchKernelGGL((oscar_cache_read_kernel<BITS, OUT, false>), grid, dim3(256), 0, st, P);
+    launch<BITS, OUT, false>(P, grid, st);
 }
 template <typename OUT> void launch(const ReadParams& P, dim3 grid, hipStream_t st) {
   if (P.g.bits == 2)
