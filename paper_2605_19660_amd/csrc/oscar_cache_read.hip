@@ -125,6 +125,11 @@ template <typename OUT> __device__ __forceinline__ typename Pair<OUT>::Type pair
   return __builtin_convertvector((float2v){a, b}, typename Pair<OUT>::Type);
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void store_row(uint8_t* p, const uint4& v) {
+  __builtin_nontemporal_store((u32x4){v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
+}
+
 // 8 numbers of the window's type
 __device__ __forceinline__ void load8_io(const void* base, int64_t at, int dt, float (&x)[8]) {
   if (dt == OSCAR_F32) {
@@ -232,7 +237,7 @@ __global__ __launch_bounds__(256, sizeof(OUT) == 2 && !M32 ? 4 : 2) void oscar_c
       for (int r = 0; r < 16; r += 64 / LANES) {
         const int t = t0 + r + lane / LANES, c = lane % LANES * 16;
         const uint4 v = *reinterpret_cast<const uint4*>(rows + (r + lane / LANES) * KROW + c);
-        if (t >= t_lo && t < t_hi) *reinterpret_cast<uint4*>(out + t * row_bytes + c) = v;
+        if (t >= t_lo && t < t_hi) store_row(out + t * row_bytes + c, v);
       }
       wave_lds_fence();
     }
@@ -296,7 +301,7 @@ __global__ __launch_bounds__(256, sizeof(OUT) == 2 && !M32 ? 4 : 2) void oscar_c
     } else {
       v = second ? make_uint4(lo4.y, lo4.w, hi4.y, hi4.w) : make_uint4(lo4.x, lo4.z, hi4.x, hi4.z);
     }
-    *reinterpret_cast<uint4*>(out + t * row_bytes + c * sizeof(OUT)) = v;
+    store_row(out + t * row_bytes + c * sizeof(OUT), v);
   }
 }
 
