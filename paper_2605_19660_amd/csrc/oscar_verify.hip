@@ -84,33 +84,32 @@ template <typename E, int N> __device__ __forceinline__ void load_part(const E* 
 
 __device__ __forceinline__ double weight(float p, float q) { return fmax((double)p - (double)q, 0.0); }
 
-// exclusive sum over the workgroup's threads, in their order; *total = the whole
-__device__ __forceinline__ double scan256(double v, double* s_wave, double* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double x = v;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const double y = __shfl_up(x, m, 64);
-    if (lane >= m) x += y;
-  }
-  if (lane == 63) s_wave[wave] = x;
-  double before = __shfl_up(x, 1, 64);
-  if (lane == 0) before = 0.0;
-  __syncthreads();
-  double all = 0.0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w == wave) before += all;
-    all += s_wave[w];
-  }
-  __syncthreads();
-  *total = all;
-  return before;
+// The sum over the lanes up to this one, of a wave: four steps inside rows of 16 lanes, two that carry a row's last
+// lane on (as lane permutations through LDS the six steps wait for it six times).
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double v) {
+  const uint64_t bits = __double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(bits >> 32), CTRL, ROWS, 0xf, false);
+  return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));   // 0 where no lane gives
+}
+__device__ __forceinline__ double wave_scan(double v) {
+  v += moved<0x111, 0xf>(v);   // row_shr:1, 2, 4, 8
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);   // row_bcast:15 into rows 1 and 3
+  v += moved<0x143, 0xc>(v);   // row_bcast:31 into rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ double of_lane(double v, int lane) {   // lane: the same in all
+  const uint64_t bits = __double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)bits, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(bits >> 32), lane);
+  return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
 }
 
 template <typename E> __global__ __launch_bounds__(256) void oscar_verify_sums_kernel(VerifyParams P) {
   __shared__ int s_first;
-  __shared__ double s_wave[4];
+  __shared__ double2 s_wave[4];
   const int b = blockIdx.y, piece = blockIdx.x, tid = threadIdx.x;
   const int n = P.draft_lens ? min(max(P.draft_lens[b], 0), P.T) : P.T;
   const int a = standing<E>(P, b, &s_first);
@@ -131,90 +130,87 @@ template <typename E> __global__ __launch_bounds__(256) void oscar_verify_sums_k
     r += weight(p[i], q[i]);
     s += p[i];
   }
-  double sum_r, sum_p;
-  scan256(r, s_wave, &sum_r);
-  scan256(s, s_wave, &sum_p);
+  r = wave_scan(r);
+  s = wave_scan(s);
+  if (tid % 64 == 63) s_wave[tid / 64] = make_double2(r, s);
+  __syncthreads();
   if (tid == 0) {
-    P.sums[(int64_t)b * P.pieces + piece] = make_double2(sum_r, sum_p);
+    P.sums[(int64_t)b * P.pieces + piece] = make_double2((s_wave[0].x + s_wave[1].x) + (s_wave[2].x + s_wave[3].x),
+                                                        (s_wave[0].y + s_wave[1].y) + (s_wave[2].y + s_wave[3].y));
     if (piece == 0) P.rows[b] = a;
   }
 }
 
 template <typename E> __global__ __launch_bounds__(256) void oscar_verify_pick_kernel(VerifyParams P) {
   __shared__ double s_wave[4];
-  __shared__ double s_base;
-  __shared__ int s_piece, s_last, s_token;
-  const int b = blockIdx.x, tid = threadIdx.x;
+  __shared__ int s_hit, s_last;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = P.draft_lens ? min(max(P.draft_lens[b], 0), P.T) : P.T;
   const int a = P.rows[b];
-  const double2* sums = P.sums + (int64_t)b * P.pieces;
-  // which weights, and their sum
-  double r = 0.0, s = 0.0;
-  for (int c = tid; c < P.pieces; c += 256) {
-    r += sums[c].x;
-    s += sums[c].y;
-  }
-  double sum_r, sum_p;
-  scan256(r, s_wave, &sum_r);
-  scan256(s, s_wave, &sum_p);
-  const bool rest = sum_r > 0.0;
   const float u = P.u[(int64_t)b * (P.T + 1) + P.T];
+  const double2* sums = P.sums + (int64_t)b * P.pieces;
+  if (tid == 0) s_hit = PIECE, s_last = -1;
+  // Which weights, and their sum: every wave for itself, 64 pieces at a time.
+  double sum_r = 0.0, sum_p = 0.0;
+  for (int c0 = 0; c0 < P.pieces; c0 += 64) {
+    const double2 w = c0 + lane < P.pieces ? sums[c0 + lane] : make_double2(0.0, 0.0);
+    sum_r += of_lane(wave_scan(w.x), 63);
+    sum_p += of_lane(wave_scan(w.y), 63);
+  }
+  const bool rest = sum_r > 0.0;
   const double target = (u > 0.0f ? (double)u : 0.0) * (rest ? sum_r : sum_p);
   // the first piece whose sums pass the target; if rounding lets none pass, the last with any weight
-  if (tid == 0) s_piece = P.pieces, s_last = -1, s_token = 0;
-  __syncthreads();
-  double done = 0.0;
-  for (int c0 = 0; c0 < P.pieces; c0 += 256) {
-    const int c = c0 + tid;
-    const double w = c < P.pieces ? (rest ? sums[c].x : sums[c].y) : 0.0;
-    double total;
-    const double before = done + scan256(w, s_wave, &total);
-    if (w > 0.0) {
-      if (before + w > target) atomicMin(&s_piece, c);
-      atomicMax(&s_last, c);
+  int piece = -1, last_piece = -1;
+  double base = 0.0, done = 0.0;
+  for (int c0 = 0; c0 < P.pieces && piece < 0; c0 += 64) {
+    const double2 both = c0 + lane < P.pieces ? sums[c0 + lane] : make_double2(0.0, 0.0);
+    const double w = rest ? both.x : both.y, upto = wave_scan(w);
+    const uint64_t some = __ballot(w > 0.0), past = __ballot(w > 0.0 && done + upto > target);
+    if (some) last_piece = c0 + 63 - __builtin_clzll(some);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      piece = c0 + at;
+      base = at == 0 ? done : done + of_lane(upto, max(at - 1, 0));
     }
-    __syncthreads();
-    if (c == s_piece) s_base = before;
-    if (s_piece < P.pieces) break;
-    done += total;
+    done += of_lane(upto, 63);
   }
+  const bool passed = piece >= 0;
+  if (!passed) piece = last_piece;
   __syncthreads();
-  const bool passed = s_piece < P.pieces;
-  const int piece = passed ? s_piece : s_last;
-  const double base = passed ? s_base : 0.0;
-  if (piece >= 0) {
+  if (piece >= 0) {   // (the same for all)
     const Rows<E> rows(P, b, a, n);
     const int64_t i0 = (int64_t)piece * PIECE + tid * PER;
     const int count = (int)min(max(P.V - i0, (int64_t)0), (int64_t)PER);
     float p[PER], q[PER] = {};
     load_part<E, PER>(rows.p + i0, count, p);
     if (rest && rows.q) load_part<E, PER>(rows.q + i0, count, q);
-    double part = 0.0;
+    double w[PER], part = 0.0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) part += weight(p[i], q[i]);
-    double total;
-    double cum = base + scan256(part, s_wave, &total);
+    for (int i = 0; i < PER; ++i) part += w[i] = weight(p[i], q[i]);
+    const double upto = wave_scan(part);
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    double cum = base;
+#pragma unroll
+    for (int v = 0; v < 3; ++v) cum += v < wave ? s_wave[v] : 0.0;
+    cum += upto - part;
     int hit = PIECE, last = -1;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const double w = weight(p[i], q[i]);
-      cum += w;
-      if (w > 0.0) {
-        last = tid * PER + i;
-        if (passed && hit == PIECE && cum > target) hit = last;
-      }
+      cum += w[i];
+      last = w[i] > 0.0 ? tid * PER + i : last;
+      hit = hit == PIECE && w[i] > 0.0 && cum > target ? tid * PER + i : hit;
     }
-    if (tid == 0) s_piece = PIECE, s_last = -1;
+    // the wave's first that passes and its last with any weight
+    const uint64_t past = __ballot(hit < PIECE), some = __ballot(last >= 0);
+    if (past && lane == __builtin_ctzll(past)) atomicMin(&s_hit, hit);
+    if (some && lane == 63 - __builtin_clzll(some)) atomicMax(&s_last, last);
     __syncthreads();
-    if (hit < PIECE) atomicMin(&s_piece, hit);
-    if (last >= 0) atomicMax(&s_last, last);
-    __syncthreads();
-    if (tid == 0) s_token = piece * PIECE + (s_piece < PIECE ? s_piece : s_last);
   }
-  __syncthreads();
+  const int token = piece < 0 ? 0 : piece * PIECE + (passed && s_hit < PIECE ? s_hit : s_last);
   int32_t* out = P.tokens + (int64_t)b * (P.T + 1);
   for (int t = tid; t <= P.T; t += 256)
-    out[t] = t < a ? P.drafts[(int64_t)b * P.T + t] : t == a ? s_token : -1;
+    out[t] = t < a ? P.drafts[(int64_t)b * P.T + t] : t == a ? token : -1;
   if (tid == 0) P.n_new[b] = a + 1;
 }
 
