@@ -545,8 +545,8 @@ def _token_stride(x) -> int:
     shape, stride = x.shape, x.stride()
     heads = shape[-2]
     assert x.is_cuda and shape[-1] == 128 and stride[-1] == 1 and (heads == 1 or stride[-2] == 128)
-    if len(shape) == 3 and shape[0] != 1:
-        return stride[0]
+    if len(shape) == 3:
+        return stride[0] if shape[0] != 1 else heads * 128
     step = None
     for size, st in zip(reversed(shape[:-2]), reversed(stride[:-2])):
         if size == 1:

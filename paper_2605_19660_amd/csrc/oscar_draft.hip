@@ -735,7 +735,9 @@ extern "C" int32_t oscar_draft_auto_splits(const oscar_config* cfg, int32_t batc
   const int64_t units = (int64_t)batch * cfg->n_kv_heads * row_blocks(*cfg, T);
   const int64_t pages = max_seq_len > 0 ? ((int64_t)max_seq_len + R - 1) / R : 1;
   int64_t splits = wgs_per_cu(cfg->bits, cfg->meta_dtype == OSCAR_F32, row_tiles(*cfg, T)) * (int64_t)oscar_compute_units() / units;
-  if (splits > (pages + 3) / 4) splits = (pages + 3) / 4;
+  // no more waves than pieces of work: the pages, up to four pieces of a window, the new tokens' pieces
+  const int64_t pieces = pages + R / TAIL + ((int64_t)T + TAIL - 1) / TAIL;
+  if (splits > (pieces + 3) / 4) splits = (pieces + 3) / 4;
   if (splits > 512) splits = 512;
   return splits < 1 ? 1 : (int32_t)splits;
 }
