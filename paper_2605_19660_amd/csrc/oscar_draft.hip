@@ -160,13 +160,9 @@ constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens
 // Workgroups a CU that a variant's registers are held to.
 __host__ __device__ constexpr int wgs_per_cu(int bits, bool m32, int nr) { return nr == 1 && bits == 2 && !m32 ? 3 : 2; }
 
-// ONE: k_group is the whole page.
-template <int BITS, bool M32, bool ONE, int NR>
-__global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
-  using C = Codes<BITS>;
-  constexpr int ROWS = NR * 16;
-  constexpr int UNITS = C::BPMAX - C::BPMIN;         // log2 of what the counterweights leave in the extra tile
-  constexpr int OROW = D + 4;
+constexpr int OROW = D + 4;
+template <int NR> struct Lds {
+  static constexpr int ROWS = NR * 16;
   struct Loop {
     half8 qh[NR][4][64], qc[NR][4][64];              // queries as operands: natural order, codes' order
     Staged meta[4];                                  // of each wave's page
@@ -175,18 +171,24 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
   struct Join {
     float o[4][ROWS][OROW], m[4][ROWS], l[4][ROWS];
   };
-  __shared__ __align__(16) union Lds {
+  union {
     Loop loop;
     Join join;
-    __device__ Lds() {}
-  } lds;
+  };
+  __device__ Lds() {}
+};
+
+// ONE: k_group is the whole page.
+template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int row0) {
+  using C = Codes<BITS>;
+  constexpr int ROWS = NR * 16;
+  constexpr int UNITS = C::BPMAX - C::BPMIN;         // log2 of what the counterweights leave in the extra tile
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, q4 = lane >> 4;
   const int Hkv = P.c.cfg.n_kv_heads, Hq = P.c.cfg.n_q_heads, g = Hq / Hkv;
   const int split = blockIdx.x % P.num_splits, unit = blockIdx.x / P.num_splits;
   const int kvh = unit % Hkv, b = unit / Hkv;
-  const int row0 = blockIdx.y * ROWS;
 
   // the queries' loads wait for nothing
   const uint16_t* q_row[NR];
@@ -700,6 +702,19 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
           make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
     }
   }
+}
+
+// A workgroup of NR tiles; the last rows take one tile where that holds them (35 rows, seven query heads and five
+// tokens, over 128K tokens: 39.9 us, 45.2 as twice two tiles).  Not with 4-bit codes: beside the second body the
+// first one's registers no longer suffice (500 new tokens over 2 x 8K: 145 us, 181 with it).
+template <int BITS, bool M32, bool ONE, int NR>
+__global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
+  __shared__ __align__(16) Lds<NR> lds;
+  const int row0 = blockIdx.y * NR * 16, rows = P.T * (P.c.cfg.n_q_heads / P.c.cfg.n_kv_heads) - row0;
+  if (BITS == 2 && NR > 1 && rows <= 16)
+    attend<BITS, M32, ONE, 1>(P, reinterpret_cast<Lds<1>&>(lds), row0);
+  else
+    attend<BITS, M32, ONE, NR>(P, lds, row0);
 }
 
 template <int BITS, bool M32, bool ONE> void launch(const DraftParams& P, int nr, dim3 grid, hipStream_t st) {
