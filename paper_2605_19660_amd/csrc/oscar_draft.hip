@@ -244,15 +244,18 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
     auto page_of = [&](int p, int phys) { return Page{phys, p < pages && phys >= 0 && phys < P.c.num_pages}; };
 
     // ---- loads ahead ----
+    // (all of a page's codes a page ahead; 4-bit ones of two tiles a half each, into what the other half has left: the
+    // registers do not hold more.  500 new tokens over 2 x 8K: 128 us, 159 with all of them ahead and spilled)
+    constexpr int AHEAD = BITS == 4 && NR == 2 ? 2 : 4;
     uint32_t kc[4][2 * BITS], vc[4][2 * BITS];
     auto pool_of = [&](const void* pool, int bytes, const Page& pg) {
       const uintptr_t at = reinterpret_cast<uintptr_t>(pool) + ((size_t)pg.phys * Hkv + kvh) * bytes;
       return reinterpret_cast<DevicePtr>(pg.held ? at : reinterpret_cast<uintptr_t>(kNoPage));
     };
     const uint32_t k_at = chunk_offset(BITS, 0, 4 * (n % 4) + n / 4, q4), v_at = chunk_offset(BITS, 0, n, q4);
-    auto load_codes = [&](DevicePtr page, uint32_t at, uint32_t (&w)[4][2 * BITS]) {
+    auto load_codes = [&](DevicePtr page, uint32_t at, uint32_t (&w)[4][2 * BITS], int first, int end) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = first; c < end; ++c)
 #pragma unroll
         for (int j = 0; j < BITS / 2; ++j)
           *reinterpret_cast<u32x4*>(&w[c][4 * j]) = load_as<u32x4>(page + at + chunk_offset(BITS, 2 * c, 0, 0) + 16 * j);
@@ -317,8 +320,8 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 
     Page pg0 = page_of(page, entry_of(page)), pg1 = page_of(page + step, entry_of(page + step));
     fetch_meta(pg0);
-    load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg0), k_at, kc);
-    load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0), v_at, vc);
+    load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg0), k_at, kc, 0, 4);
+    load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0), v_at, vc, 0, AHEAD);
 
     // ---- queries ----
     // Wave i rotates tile i, on the matrix cores: out = H q, H's signs exact in either type.  Row m of output tile
@@ -598,8 +601,9 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
               pr[i][r][4 * half + t] = p[0];
               pr[i][r][4 * half + t + 1] = p[1];
             }
+        if (half == 0) load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0), v_at, vc, AHEAD, 4);
       }
-      load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1), k_at, kc);
+      load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1), k_at, kc, 0, AHEAD);
       fetch_meta(pg1);
 
       // values
@@ -632,8 +636,9 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 #pragma unroll
             for (int i = 0; i < NR; ++i) o[i][2 * w + j] = mfma(a, pd[i][kk], o[i][2 * w + j]);
           }
+        if (w == 1) load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1), k_at, kc, AHEAD, 4);
       }
-      load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg1), v_at, vc);
+      load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg1), v_at, vc, 0, AHEAD);
       stage_keys();
       page_off = stage_values();
       pg0 = pg1;
@@ -704,24 +709,32 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
   }
 }
 
-// A workgroup of NR tiles; the last rows take one tile where that holds them (35 rows, seven query heads and five
-// tokens, over 128K tokens: 39.9 us, 45.2 as twice two tiles).  Not with 4-bit codes: beside the second body the
-// first one's registers no longer suffice (500 new tokens over 2 x 8K: 145 us, 181 with it).
-template <int BITS, bool M32, bool ONE, int NR>
+// A workgroup of NR tiles.  LAST: the last rows are 16 at most and take one tile (35 rows, seven query heads and
+// five tokens, over 128K tokens: 41 us, 45 as twice two tiles).  A variant of its own, for the second body costs
+// the first one registers (32 rows, 8 x 32K tokens: 67 us, 71 with it), and with 4-bit codes more than it gains (500
+// new tokens over 2 x 8K: 145 us, 181 with it).
+template <int BITS, bool M32, bool ONE, int NR, bool LAST>
 __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
   __shared__ __align__(16) Lds<NR> lds;
-  const int row0 = blockIdx.y * NR * 16, rows = P.T * (P.c.cfg.n_q_heads / P.c.cfg.n_kv_heads) - row0;
-  if (BITS == 2 && NR > 1 && rows <= 16)
-    attend<BITS, M32, ONE, 1>(P, reinterpret_cast<Lds<1>&>(lds), row0);
-  else
+  const int row0 = blockIdx.y * NR * 16;
+  if constexpr (LAST) {
+    if (blockIdx.y == gridDim.y - 1)
+      attend<BITS, M32, ONE, 1>(P, reinterpret_cast<Lds<1>&>(lds), row0);
+    else
+      attend<BITS, M32, ONE, NR>(P, lds, row0);
+  } else {
     attend<BITS, M32, ONE, NR>(P, lds, row0);
+  }
 }
 
 template <int BITS, bool M32, bool ONE> void launch(const DraftParams& P, int nr, dim3 grid, hipStream_t st) {
+  const int64_t rows = (int64_t)P.T * (P.c.cfg.n_q_heads / P.c.cfg.n_kv_heads);
   if (nr == 1)
-    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 1>), grid, dim3(256), 0, st, P);
+    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 1, false>), grid, dim3(256), 0, st, P);
+  else if (BITS == 2 && (rows - 1) % 32 < 16)
+    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 2, BITS == 2>), grid, dim3(256), 0, st, P);
   else
-    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 2>), grid, dim3(256), 0, st, P);
+    hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 2, false>), grid, dim3(256), 0, st, P);
 }
 template <int BITS, bool M32> void launch(const DraftParams& P, int nr, dim3 grid, hipStream_t st) {
   if (P.g.ngk == 1)
