@@ -426,12 +426,12 @@ int oscar_cache_read(const oscar_cache *cache, const int32_t *starts, int32_t T,
  *                           scale * <q[b][t][h], k_new[b][j]>, j <= t ) . values
  * with the cached tokens' logits and values as in oscar_decode_attn.  The new tokens are not in the
  * cache and the call does not put them there.  T is the last token and its drafts, or a piece of a
- * prompt.
+ * prompt.  Cached tokens in a page whose block_table entry is no page are left out.
  *   q            : device, [batch][T][n_q_heads][head_dim], io_dtype, un-rotated
  *   k_new, v_new : device, [batch][T][n_kv_heads][head_dim], io_dtype (keys after RoPE)
  *   new_lens     : device int32[batch] or NULL; sequence b has new_lens[b] (0..T) new tokens, the
  *                  rows behind them are zeros; NULL = T for all
- *   out          : device, [batch][T][n_q_heads][head_dim], io_dtype
+ *   out          : device, [batch][T][n_q_heads][head_dim], io_dtype; no part of the inputs
  *   softmax_scale, max_seq_len_hint, num_splits (<= 512, 0 = oscar_draft_auto_splits): as in
  *                  oscar_decode_attn
  *   workspace    : at least oscar_draft_workspace_bytes(...), 8-byte aligned; NULL where that is 0
@@ -439,7 +439,9 @@ int oscar_cache_read(const oscar_cache *cache, const int32_t *starts, int32_t T,
  * io_dtype BF16 or F16 (OSCAR_ERR_UNSUPPORTED for F32); every other field of the configuration as
  * for oscar_decode_attn.  Operands of the matrix products are fp16 (steps, zero terms,
  * probabilities; values and zero terms beyond its range, infinities and NaNs among the values of
- * new tokens, count as +-65504), sums are fp32.  The same call gives the same bits every time.
+ * new tokens, count as +-65504; a query is finite, and 6 softmax_scale |H q| / sqrt(128), times the
+ * largest key step of a channel, stays inside it), sums are fp32.  The same call gives the same bits
+ * every time.
  * q, k_new, v_new, out: 16-byte aligned.  One launch, two with several splits. */
 int32_t oscar_draft_auto_splits(const oscar_config *cfg, int32_t batch, int32_t T, int32_t max_seq_len);
 size_t oscar_draft_workspace_bytes(const oscar_config *cfg, int32_t batch, int32_t T, int32_t num_splits);
@@ -462,7 +464,8 @@ int oscar_draft_attn(const void *q, const void *k_new, const void *v_new, int32_
  *   drafts : device int32 [batch][T];   u : device fp32 [batch][T+1], in [0, 1)
  *   n_new  : device int32 [batch]: a + 1, the tokens the step yields, which is also the new_lens of
  *            oscar_quantize_append for the keys and values of the last token and the drafts
- *   tokens : device int32 [batch][T+1]: the drafts that stand, the next token, then -1
+ *   tokens : device int32 [batch][T+1]: the drafts that stand, the next token, then -1; no part
+ *            of the inputs, as n_new
  *   workspace : at least oscar_verify_workspace_bytes(...), 16-byte aligned; its contents do not
  *            matter.  Calls that share one must be ordered.
  * Numbers that are not above zero, NaNs among them, count as 0, infinities as the largest fp32.

@@ -6,6 +6,7 @@ the import of any entry point raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -526,6 +527,27 @@ def bf16_decode_attn(q, k, v, seq_lens, out=None, scale: float = 0.0, max_seq_le
 ROPE_ADJACENT, ROPE_INVERSE = 1, 2
 
 
+def _current_device() -> int:
+    global _current_device
+    import torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _current_device()
+
+
+def _here(*tensors):
+    """The calls launch on the current device: so that is where what they read and write must be."""
+    device = _current_device()
+    for t in tensors:
+        assert t is None or t.get_device() == device, f"a tensor is not on the current device, {device}"
+
+
+def _made_for(stream):
+    """Where a call makes tensors itself: on the stream that will use them, so that what the allocator still has
+    in use, or gives away again, on another stream is not theirs."""
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def rope_axes(sections, interleaved: bool = False) -> bytes:
     """The axis of every pair, for `rope`: sections[a] pairs turn with axis a, in that order or
     (interleaved) dealt out one after the other, an axis leaving the round when its share is used up."""
@@ -544,7 +566,7 @@ def _token_stride(x) -> int:
     """Elements between the tokens of a [..., heads, 128] tensor, whose tokens must lie evenly apart."""
     shape, stride = x.shape, x.stride()
     heads = shape[-2]
-    assert x.is_cuda and shape[-1] == 128 and stride[-1] == 1 and (heads == 1 or stride[-2] == 128)
+    assert shape[-1] == 128 and stride[-1] == 1 and (heads == 1 or stride[-2] == 128)
     if len(shape) == 3:
         return stride[0] if shape[0] != 1 else heads * 128
     step = None
@@ -564,7 +586,7 @@ def _int32_ptr(t, n: int):
     if t is None:
         return None
     import torch
-    assert t.is_cuda and t.dtype == torch.int32 and t.numel() == n and t.is_contiguous()
+    assert t.dtype == torch.int32 and t.numel() == n and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -575,32 +597,34 @@ def rope(q, k, positions, inv_freq, axes: bytes | None = None, adjacent: bool = 
     [rotary_dim / 2]; axes: see rope_axes.  Returns (q, k) turned, in new tensors unless out_q, out_k
     say where (q and k themselves for in place)."""
     import torch
+    _here(q, k, positions, inv_freq, out_q, out_k)
     x = k if q is None else q
     lead, dtype = x.shape[:-2], x.dtype
     n, pairs = lead.numel(), inv_freq.numel()
     n_axes = positions.shape[0] if positions.dim() == 2 else 1
-    assert inv_freq.is_cuda and inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
+    assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
     assert axes is None or len(axes) == pairs
     hq = hk = sq = sk = soq = sok = 0
-    if q is not None:
-        hq, sq = q.shape[-2], _token_stride(q)
-        if out_q is None:
-            out_q, soq = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape), hq * 128
+    with _made_for(stream):
+        if q is not None:
+            hq, sq = q.shape[-2], _token_stride(q)
+            if out_q is None:
+                out_q, soq = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape), hq * 128
+            else:
+                assert out_q.shape == q.shape and out_q.dtype == dtype
+                soq = _token_stride(out_q)
         else:
-            assert out_q.shape == q.shape and out_q.dtype == dtype
-            soq = _token_stride(out_q)
-    else:
-        out_q = None
-    if k is not None:
-        hk, sk = k.shape[-2], _token_stride(k)
-        assert k.dtype == dtype and k.shape[:-2] == lead
-        if out_k is None:
-            out_k, sok = torch.empty_like(k) if k.is_contiguous() else k.new_empty(k.shape), hk * 128
+            out_q = None
+        if k is not None:
+            hk, sk = k.shape[-2], _token_stride(k)
+            assert k.dtype == dtype and k.shape[:-2] == lead
+            if out_k is None:
+                out_k, sok = torch.empty_like(k) if k.is_contiguous() else k.new_empty(k.shape), hk * 128
+            else:
+                assert out_k.shape == k.shape and out_k.dtype == dtype
+                sok = _token_stride(out_k)
         else:
-            assert out_k.shape == k.shape and out_k.dtype == dtype
-            sok = _token_stride(out_k)
-    else:
-        out_k = None
+            out_k = None
     rc = lib().oscar_rope(None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
                           None if q is None else out_q.data_ptr(), None if k is None else out_k.data_ptr(),
                           n, hq, hk, sq, sk, soq, sok, _int32_ptr(positions, n_axes * n), inv_freq.data_ptr(), axes, n_axes,
@@ -617,8 +641,9 @@ def cache_read(cache: Cache, starts=None, k=None, v=None, stream=None):
     a sequence does not hold stay as they are."""
     shape, dtype = (k if k is not None else v).shape, (k if k is not None else v).dtype
     assert shape[0] == cache.batch and tuple(shape[2:]) == (cache.cfg.n_kv_heads, cache.cfg.head_dim)
+    _here(k, v, starts, cache.seq_lens)
     for x in (k, v):
-        assert x is None or (x.is_cuda and x.is_contiguous() and x.shape == shape and x.dtype == dtype)
+        assert x is None or (x.is_contiguous() and x.shape == shape and x.dtype == dtype)
     rc = lib().oscar_cache_read(C.byref(cache.c), _int32_ptr(starts, cache.batch), shape[1],
                                 None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
                                 dtype_code(dtype), _stream_ptr(stream))
@@ -643,23 +668,26 @@ def draft_attn(cache: Cache, q, k_new, v_new, new_lens=None, out=None, scale: fl
     import torch
     cfg, shape, dtype = cache.cfg, q.shape, q.dtype
     batch, T, hkv = shape[0], shape[1], cfg.n_kv_heads
-    assert q.is_cuda and dtype == k_new.dtype == v_new.dtype == torch_dtype(cfg.io_dtype)
+    _here(q, k_new, v_new, new_lens, out, workspace, cache.seq_lens)
+    assert dtype == k_new.dtype == v_new.dtype == torch_dtype(cfg.io_dtype)
     assert batch == cache.batch and shape[2] == cfg.n_q_heads and shape[3] == cfg.head_dim
     assert k_new.shape == v_new.shape == (batch, T, hkv, cfg.head_dim)
     assert q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous()
-    if out is None:
-        out = torch.empty_like(q)
-    assert out.shape == shape and out.dtype == dtype and out.is_contiguous()
     L, c = lib(), cache.c
     if num_splits == 0:
         num_splits = L.oscar_draft_auto_splits(C.byref(c.cfg), batch, T, max_seq_len_hint)
     ws, ws_bytes = None, 0
-    if workspace is not None:
-        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    elif num_splits > 1:
-        ws_bytes = L.oscar_draft_workspace_bytes(C.byref(c.cfg), batch, T, num_splits)
-        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
-        ws = workspace.data_ptr()
+    with _made_for(stream):
+        if out is None:
+            out = torch.empty_like(q)
+        if workspace is None and num_splits > 1:
+            ws_bytes = L.oscar_draft_workspace_bytes(C.byref(c.cfg), batch, T, num_splits)
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            ws = workspace.data_ptr()
+        elif workspace is not None:
+            assert workspace.is_contiguous()
+            ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    assert out.shape == shape and out.dtype == dtype and out.is_contiguous()
     rc = L.oscar_draft_attn(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), T, _int32_ptr(new_lens, batch), C.byref(c),
                             out.data_ptr(), scale, max_seq_len_hint, num_splits, ws, ws_bytes, _stream_ptr(stream))
     if rc != OK:
@@ -677,17 +705,19 @@ def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=
     import torch
     batch, T1, vocab = target.shape
     T = T1 - 1
-    assert target.is_cuda and target.dtype == draft.dtype and target.is_contiguous() and draft.is_contiguous()
+    _here(target, draft, drafts, u, draft_lens, n_new, tokens, workspace)
+    assert target.dtype == draft.dtype and target.is_contiguous() and draft.is_contiguous()
     assert draft.shape == (batch, T, vocab) and drafts.shape == (batch, T) and u.shape == (batch, T1)
     assert u.dtype == torch.float32 and u.is_contiguous()
-    if n_new is None:
-        n_new = torch.empty(batch, dtype=torch.int32, device=target.device)
-    if tokens is None:
-        tokens = torch.empty((batch, T1), dtype=torch.int32, device=target.device)
-    assert tokens.shape == (batch, T1)
     L = lib()
-    if workspace is None:
-        workspace = torch.empty(L.oscar_verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=target.device)
+    with _made_for(stream):
+        if n_new is None:
+            n_new = torch.empty(batch, dtype=torch.int32, device=target.device)
+        if tokens is None:
+            tokens = torch.empty((batch, T1), dtype=torch.int32, device=target.device)
+        if workspace is None:
+            workspace = torch.empty(L.oscar_verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=target.device)
+    assert tokens.shape == (batch, T1) and workspace.is_contiguous()
     rc = L.oscar_verify_drafts(target.data_ptr(), draft.data_ptr(), _int32_ptr(drafts, batch * T), _int32_ptr(draft_lens, batch),
                                u.data_ptr(), batch, T, vocab, dtype_code(target.dtype), _int32_ptr(n_new, batch),
                                _int32_ptr(tokens, batch * T1), workspace.data_ptr(), workspace.numel() * workspace.element_size(),

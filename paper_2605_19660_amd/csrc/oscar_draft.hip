@@ -793,7 +793,8 @@ extern "C" int oscar_draft_attn(const void* q, const void* k_new, const void* v_
     return OSCAR_ERR_INVALID_ARG;
   if (num_splits == 0) num_splits = oscar_draft_auto_splits(&cfg, cache->batch, T, max_seq_len_hint);
   const int64_t blocks = row_blocks(cfg, T), units = (int64_t)cache->batch * cfg.n_kv_heads * num_splits;
-  if (blocks > 65535 || units > 0x7fffffff || cache->batch > 65535 || (int64_t)T * cfg.n_q_heads > 0x7fffffff)
+  // (a launch takes 65535 blocks behind the first dimension and fewer than 2^32 threads along it)
+  if (blocks > 65535 || units >= 1 << 24 || cache->batch > 65535 || (int64_t)T * cfg.n_q_heads >= 1 << 24)
     return OSCAR_ERR_INVALID_ARG;
   const size_t need = oscar_draft_workspace_bytes(&cfg, cache->batch, T, num_splits);
   if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 7) != 0))

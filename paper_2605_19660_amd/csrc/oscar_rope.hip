@@ -185,7 +185,7 @@ extern "C" int oscar_rope(const void* q, const void* k, void* q_out, void* k_out
   // one token a workgroup until they fill the chip twice over, then four
   P.tokens = n_tokens > 8 * (int64_t)oscar_compute_units() ? kMaxTokens : 1;
   const int64_t blocks = (n_tokens + P.tokens - 1) / P.tokens;
-  if (blocks > 0x7fffffff) return OSCAR_ERR_INVALID_ARG;
+  if (blocks >= 1 << 24) return OSCAR_ERR_INVALID_ARG;   // (fewer than 2^32 threads)
   const dim3 grid((unsigned)blocks);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const bool adjacent = flags & OSCAR_ROPE_ADJACENT;

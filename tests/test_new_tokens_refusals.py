@@ -123,3 +123,19 @@ def test_verify_drafts_refuses():
     for kw in (dict(ws=None), dict(wb=need - 1), dict(ws=P + 8)):
         assert verify(**kw) == ob.ERR_WORKSPACE, kw
     assert verify(batch=0) == ob.OK
+
+
+def test_host_tensors_are_refused(monkeypatch):
+    import torch
+    monkeypatch.setattr(ob, "_current_device", lambda: 0)
+    x, i = torch.zeros(2, 3, 4, 128), torch.zeros(6, dtype=torch.int32)
+    with pytest.raises(AssertionError, match="current device"):
+        ob.rope(x, None, i, torch.ones(64))
+    with pytest.raises(AssertionError, match="current device"):
+        ob.verify_drafts(torch.rand(2, 4, 10), torch.rand(2, 3, 10), i.view(2, 3), torch.rand(2, 4))
+
+
+def test_grids_past_what_a_launch_takes_are_refused():
+    assert rope(n=4 * ((1 << 24) - 1) + 1, hk=0) == ob.ERR_INVALID_ARG
+    assert draft(cache_struct(batch=65535, n_q_heads=128, n_kv_heads=128), splits=512, ws=P, wb=1 << 60) == ob.ERR_INVALID_ARG
+    assert draft(cache_struct(batch=1, n_q_heads=8, n_kv_heads=1), T=1 << 22, splits=2, ws=P, wb=1 << 60) == ob.ERR_INVALID_ARG
