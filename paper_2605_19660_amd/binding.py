@@ -6,7 +6,6 @@ the import of any entry point raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -541,13 +540,6 @@ def _here(*tensors):
         assert t is None or t.get_device() == device, f"a tensor is not on the current device, {device}"
 
 
-def _made_for(stream):
-    """Where a call makes tensors itself: on the stream that will use them, so that what the allocator still has
-    in use, or gives away again, on another stream is not theirs."""
-    import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
-
-
 def rope_axes(sections, interleaved: bool = False) -> bytes:
     """The axis of every pair, for `rope`: sections[a] pairs turn with axis a, in that order or
     (interleaved) dealt out one after the other, an axis leaving the round when its share is used up."""
@@ -597,6 +589,9 @@ def rope(q, k, positions, inv_freq, axes: bytes | None = None, adjacent: bool = 
     [rotary_dim / 2]; axes: see rope_axes.  Returns (q, k) turned, in new tensors unless out_q, out_k
     say where (q and k themselves for in place)."""
     import torch
+    if stream is not None:   # (what the call makes belongs to the stream that uses it)
+        with torch.cuda.stream(stream):
+            return rope(q, k, positions, inv_freq, axes, adjacent, inverse, out_q, out_k)
     _here(q, k, positions, inv_freq, out_q, out_k)
     x = k if q is None else q
     lead, dtype = x.shape[:-2], x.dtype
@@ -605,31 +600,30 @@ def rope(q, k, positions, inv_freq, axes: bytes | None = None, adjacent: bool = 
     assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
     assert axes is None or len(axes) == pairs
     hq = hk = sq = sk = soq = sok = 0
-    with _made_for(stream):
-        if q is not None:
-            hq, sq = q.shape[-2], _token_stride(q)
-            if out_q is None:
-                out_q, soq = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape), hq * 128
-            else:
-                assert out_q.shape == q.shape and out_q.dtype == dtype
-                soq = _token_stride(out_q)
+    if q is not None:
+        hq, sq = q.shape[-2], _token_stride(q)
+        if out_q is None:
+            out_q, soq = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape), hq * 128
         else:
-            out_q = None
-        if k is not None:
-            hk, sk = k.shape[-2], _token_stride(k)
-            assert k.dtype == dtype and k.shape[:-2] == lead
-            if out_k is None:
-                out_k, sok = torch.empty_like(k) if k.is_contiguous() else k.new_empty(k.shape), hk * 128
-            else:
-                assert out_k.shape == k.shape and out_k.dtype == dtype
-                sok = _token_stride(out_k)
+            assert out_q.shape == q.shape and out_q.dtype == dtype
+            soq = _token_stride(out_q)
+    else:
+        out_q = None
+    if k is not None:
+        hk, sk = k.shape[-2], _token_stride(k)
+        assert k.dtype == dtype and k.shape[:-2] == lead
+        if out_k is None:
+            out_k, sok = torch.empty_like(k) if k.is_contiguous() else k.new_empty(k.shape), hk * 128
         else:
-            out_k = None
+            assert out_k.shape == k.shape and out_k.dtype == dtype
+            sok = _token_stride(out_k)
+    else:
+        out_k = None
     rc = lib().oscar_rope(None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
                           None if q is None else out_q.data_ptr(), None if k is None else out_k.data_ptr(),
                           n, hq, hk, sq, sk, soq, sok, _int32_ptr(positions, n_axes * n), inv_freq.data_ptr(), axes, n_axes,
                           2 * pairs, dtype_code(dtype), (ROPE_ADJACENT if adjacent else 0) | (ROPE_INVERSE if inverse else 0),
-                          _stream_ptr(stream))
+                          _stream_ptr(None))
     if rc != OK:
         _check(rc, "oscar_rope")
     return out_q, out_k
@@ -666,6 +660,9 @@ def draft_attn(cache: Cache, q, k_new, v_new, new_lens=None, out=None, scale: fl
     """oscar_draft_attn: q [batch, T, n_q_heads, 128], k_new and v_new [batch, T, n_kv_heads, 128], all of the io
     dtype; returns `out` (of q's shape and type)."""
     import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return draft_attn(cache, q, k_new, v_new, new_lens, out, scale, max_seq_len_hint, num_splits, workspace)
     cfg, shape, dtype = cache.cfg, q.shape, q.dtype
     batch, T, hkv = shape[0], shape[1], cfg.n_kv_heads
     _here(q, k_new, v_new, new_lens, out, workspace, cache.seq_lens)
@@ -677,19 +674,18 @@ def draft_attn(cache: Cache, q, k_new, v_new, new_lens=None, out=None, scale: fl
     if num_splits == 0:
         num_splits = L.oscar_draft_auto_splits(C.byref(c.cfg), batch, T, max_seq_len_hint)
     ws, ws_bytes = None, 0
-    with _made_for(stream):
-        if out is None:
-            out = torch.empty_like(q)
-        if workspace is None and num_splits > 1:
-            ws_bytes = L.oscar_draft_workspace_bytes(C.byref(c.cfg), batch, T, num_splits)
-            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
-            ws = workspace.data_ptr()
-        elif workspace is not None:
-            assert workspace.is_contiguous()
-            ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is not None:
+        assert workspace.is_contiguous()
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif num_splits > 1:
+        ws_bytes = L.oscar_draft_workspace_bytes(C.byref(c.cfg), batch, T, num_splits)
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+        ws = workspace.data_ptr()
     assert out.shape == shape and out.dtype == dtype and out.is_contiguous()
     rc = L.oscar_draft_attn(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), T, _int32_ptr(new_lens, batch), C.byref(c),
-                            out.data_ptr(), scale, max_seq_len_hint, num_splits, ws, ws_bytes, _stream_ptr(stream))
+                            out.data_ptr(), scale, max_seq_len_hint, num_splits, ws, ws_bytes, _stream_ptr(None))
     if rc != OK:
         _check(rc, "oscar_draft_attn")
     return out
@@ -703,6 +699,9 @@ def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=
     """oscar_verify_drafts: target [batch, T + 1, vocab] and draft [batch, T, vocab] of one type, drafts int32
     [batch, T], u fp32 [batch, T + 1]; returns (n_new int32 [batch], tokens int32 [batch, T + 1])."""
     import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return verify_drafts(target, draft, drafts, u, draft_lens, n_new, tokens, workspace)
     batch, T1, vocab = target.shape
     T = T1 - 1
     _here(target, draft, drafts, u, draft_lens, n_new, tokens, workspace)
@@ -710,18 +709,17 @@ def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=
     assert draft.shape == (batch, T, vocab) and drafts.shape == (batch, T) and u.shape == (batch, T1)
     assert u.dtype == torch.float32 and u.is_contiguous()
     L = lib()
-    with _made_for(stream):
-        if n_new is None:
-            n_new = torch.empty(batch, dtype=torch.int32, device=target.device)
-        if tokens is None:
-            tokens = torch.empty((batch, T1), dtype=torch.int32, device=target.device)
-        if workspace is None:
-            workspace = torch.empty(L.oscar_verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=target.device)
+    if n_new is None:
+        n_new = torch.empty(batch, dtype=torch.int32, device=target.device)
+    if tokens is None:
+        tokens = torch.empty((batch, T1), dtype=torch.int32, device=target.device)
+    if workspace is None:
+        workspace = torch.empty(L.oscar_verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=target.device)
     assert tokens.shape == (batch, T1) and workspace.is_contiguous()
     rc = L.oscar_verify_drafts(target.data_ptr(), draft.data_ptr(), _int32_ptr(drafts, batch * T), _int32_ptr(draft_lens, batch),
                                u.data_ptr(), batch, T, vocab, dtype_code(target.dtype), _int32_ptr(n_new, batch),
                                _int32_ptr(tokens, batch * T1), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                               _stream_ptr(stream))
+                               _stream_ptr(None))
     if rc != OK:
         _check(rc, "oscar_verify_drafts")
     return n_new, tokens
