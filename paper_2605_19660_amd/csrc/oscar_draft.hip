@@ -103,7 +103,7 @@ struct Staged {
 };
 // A row's probabilities are taken against a reference that follows its maximum only when that has passed it by
 // 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs a rescaling of the
-// whole state.
+// whole state (8 new tokens over 8 x 32K: 76 us, 81 with a reference that follows at once).
 constexpr float kSlack = 8.0f, kNone = -3e38f;
 constexpr int kOff = 7;          // exponent of a probability at its reference: kOff + kSlack stay inside fp16
 // What a lane holds of the metadata of a page to come: 8 steps and 8 zeros of the keys or of the values.
@@ -157,7 +157,8 @@ __device__ __forceinline__ float max_of_row(float v) {   // over the four lanes 
 
 constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens)
 
-// Workgroups a CU that a variant's registers are held to.
+// Workgroups a CU that a variant's registers are held to.  Three where they fit: four new tokens of 8 x 32K 49 us, 52
+// with two; with fp32 metadata 67, 55 with two, with 4-bit codes 119, 68 with two (registers in scratch).
 __host__ __device__ constexpr int wgs_per_cu(int bits, bool m32, int nr) { return nr == 1 && bits == 2 && !m32 ? 3 : 2; }
 
 constexpr int OROW = D + 4;
@@ -743,7 +744,8 @@ template <int BITS, bool M32> void launch(const DraftParams& P, int nr, dim3 gri
     launch<BITS, M32, false>(P, nr, grid, st);
 }
 
-// tiles of 16 query rows a wave holds
+// Tiles of 16 query rows a wave holds: two read every page half as often (32 rows over 8 x 32K 76 us, 82 with one; 500
+// new tokens of 32 heads over 2 x 8K 229, 256 with one), one has no idle half (16 rows 49 us, 53 with two; 4-bit 68, 79).
 int row_tiles(const oscar_config& cfg, int T) { return (int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) <= 16 ? 1 : 2; }
 int64_t row_blocks(const oscar_config& cfg, int T) {
   const int rows = 16 * row_tiles(cfg, T);
@@ -766,7 +768,11 @@ extern "C" int32_t oscar_draft_auto_splits(const oscar_config* cfg, int32_t batc
   // no more waves than pieces of work: the pages, up to four pieces of a window, the new tokens' pieces
   const int64_t pieces = pages + R / TAIL + ((int64_t)T + TAIL - 1) / TAIL;
   if (splits > (pieces + 3) / 4) splits = (pieces + 3) / 4;
-  if (splits > 512) splits = 512;
+  // Past 64 splits the reduce pass pays for each (0.07 us), the waves save less and less: four new tokens of 8 heads
+  // over 131001 take 24 us with 64, 25 with 96, 38 with 256, over 500000 53 with 64, 42 with 128, 47 with 256.
+  int64_t most = 64;
+  while (most < 512 && most * most < 4 * pages) most += 8;
+  if (splits > most) splits = most;
   return splits < 1 ? 1 : (int32_t)splits;
 }
 

@@ -6,10 +6,12 @@
 // 2 pi and cut to the nearest whole turn, keeps the angle to 2e-7 at the largest int32 position, where a
 // 32-bit product would be off by whole turns.  Only the remaining fraction of a turn goes to 32 bits.
 //
-// What bounds it: every channel is read and written once, a few operations each.  The sines are the dear
-// part, and all heads of a token share them: a workgroup takes 1 or 4 tokens, one thread works out the
+// What bounds it: every channel is read and written once, a few operations each: memory.  The sines are the dear
+// part, and all heads of a token share them: a workgroup takes one to four tokens, one thread works out the
 // sine and cosine of one (token, pair), and LDS hands them to the threads that turn the heads' channels,
-// 16 bytes of each half a thread.
+// 16 bytes of each half a thread.  32768 tokens of 28 + 4 heads in bf16, three axes: 98 us, 5.5 TB/s read + written
+// (a copy reaches 5.0); 2999 of 32 + 8 in fp32, half of the channels in adjacent pairs: 19.9 us, 6.2 TB/s, part of
+// it out of the caches; one token 2.8 us, a launch.
 #include "oscar_common.h"
 
 namespace {
@@ -106,13 +108,14 @@ template <typename T, int PAIRS> __global__ __launch_bounds__(256) void oscar_ro
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
         Vec<T> x;
-        x.load(src + (2 * j + v) * N);
+        const int at = j + v * ITEMS;   // (lanes side by side: a wave's access takes whole lines)
+        x.load(src + at * N);
 #pragma unroll
         for (int e = 0; e < N; e += 2) {
-          const int i = ((2 * j + v) * N + e) / 2;
+          const int i = (at * N + e) / 2;
           if (i < P.half) turn(x.x[e], x.x[e + 1], s_cs[t][i]);
         }
-        x.store(dst + (2 * j + v) * N);
+        x.store(dst + at * N);
       }
     } else {
       // halves that do not start on 16 bytes: one pair a thread, and one of the channels behind
@@ -182,13 +185,18 @@ extern "C" int oscar_rope(const void* q, const void* k, void* q_out, void* k_out
   P.positions = positions;
   P.inv_freq = inv_freq;
   P.sign = flags & OSCAR_ROPE_INVERSE ? -1.0f : 1.0f;
-  // one token a workgroup until they fill the chip twice over, then four
-  P.tokens = n_tokens > 8 * (int64_t)oscar_compute_units() ? kMaxTokens : 1;
+  // One token a workgroup, or up to four where there are many and one's pieces leave threads idle.  32768 tokens in
+  // bf16: of 5 heads 33 us with one, 22 with four, of 18 68 and 58, of 32 103, 98 with two, 101 with four, of 40 117
+  // and 123; in fp32, with twice the bytes a sine: of 5 heads 38 and 32, of 9 52 and 57.  1000 tokens of 18 heads in
+  // bf16, which do not fill the chip twice over: 4.4 and 5.5.
+  const bool adjacent = flags & OSCAR_ROPE_ADJACENT;
+  const int64_t pieces = (n_q_heads + n_kv_heads) * (int64_t)(adjacent || P.half % vec == 0 ? D / 2 / vec : D / 2);
+  const int64_t fit = (io_dtype == OSCAR_F32 ? 256 : 512) / pieces;
+  P.tokens = n_tokens <= 8 * (int64_t)oscar_compute_units() || fit < 1 ? 1 : fit < kMaxTokens ? (int)fit : kMaxTokens;
   const int64_t blocks = (n_tokens + P.tokens - 1) / P.tokens;
   if (blocks >= 1 << 24) return OSCAR_ERR_INVALID_ARG;   // (fewer than 2^32 threads)
   const dim3 grid((unsigned)blocks);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const bool adjacent = flags & OSCAR_ROPE_ADJACENT;
   if (io_dtype == OSCAR_F32)
     launch<float>(P, adjacent, grid, st);
   else if (io_dtype == OSCAR_BF16)
