@@ -760,20 +760,30 @@ int check_draft_config(const oscar_config* cfg) {
 
 }  // namespace
 
+// The split count whose estimate is the shortest.  A wave takes a piece (a page, or 32 tokens of the window or of the
+// new ones) in 3 us with one tile of rows and in 4 with two, 1.4 times that with 4-bit codes; workgroups that share a
+// CU take 0.75 times as long each as one after the other; a workgroup's start costs 2 more.  Splitting costs the
+// reduce pass: 3 us, 0.4 ns a record, and past 64 splits 1.5 us and 0.07 each (another kernel).  Over 186 calls of 1 ..
+// 64 sequences, 30 .. 131001 tokens and 1 .. 128 new ones the choice takes 1 % longer than the best count (17 at the
+// most); as many splits as the chip has room for, 7 % (82 at the most): 4 new tokens of 48 x 260 14 us with one split,
+// 25 with two; 8 of 24 x 32K 170 with four, which put three workgroups on every CU, 195 with two.
 extern "C" int32_t oscar_draft_auto_splits(const oscar_config* cfg, int32_t batch, int32_t T, int32_t max_seq_len) {
   if (check_draft_config(cfg) != OSCAR_OK || batch <= 0 || T <= 0) return 1;
-  const int64_t units = (int64_t)batch * cfg->n_kv_heads * row_blocks(*cfg, T);
-  const int64_t pages = max_seq_len > 0 ? ((int64_t)max_seq_len + R - 1) / R : 1;
-  int64_t splits = wgs_per_cu(cfg->bits, cfg->meta_dtype == OSCAR_F32, row_tiles(*cfg, T)) * (int64_t)oscar_compute_units() / units;
-  // no more waves than pieces of work: the pages, up to four pieces of a window, the new tokens' pieces
-  const int64_t pieces = pages + R / TAIL + ((int64_t)T + TAIL - 1) / TAIL;
-  if (splits > (pieces + 3) / 4) splits = (pieces + 3) / 4;
-  // Past 64 splits the reduce pass pays for each (0.07 us), the waves save less and less: four new tokens of 8 heads
-  // over 131001 take 24 us with 64, 25 with 96, 38 with 256, over 500000 53 with 64, 42 with 128, 47 with 256.
-  int64_t most = 64;
-  while (most < 512 && most * most < 4 * pages) most += 8;
-  if (splits > most) splits = most;
-  return splits < 1 ? 1 : (int32_t)splits;
+  const int64_t units = (int64_t)batch * cfg->n_kv_heads * row_blocks(*cfg, T), cus = oscar_compute_units();
+  const int64_t len = max_seq_len > 0 ? max_seq_len : 0;
+  const int64_t pieces = len / R + (len % R + TAIL - 1) / TAIL + ((int64_t)T + TAIL - 1) / TAIL;
+  const float piece_us = (row_tiles(*cfg, T) == 1 ? 3.0f : 4.0f) * (cfg->bits == 4 ? 1.4f : 1.0f);
+  const float record_us = 4e-4f * (float)batch * (float)T * (float)cfg->n_q_heads;
+  float best = INFINITY;
+  int32_t splits = 1;
+  for (int32_t s = 1; s <= 512 && s <= (pieces + 3) / 4; s += s < 64 ? 1 : 8) {
+    const int64_t share = (units * s + cus - 1) / cus;   // workgroups a CU
+    const float us = (float)share * ((float)((pieces + 4 * s - 1) / (4 * s)) * piece_us * (share > 1 ? 0.75f : 1.0f) + 2.0f) +
+                     (s > 1 ? 3.0f + record_us * (float)s : 0.0f) + (s > 64 ? 1.5f + 0.07f * (float)(s - 64) : 0.0f);
+    if (us < best) best = us, splits = s;
+    if (share > 8) break;   // no better from here on: more starts, and the same pages
+  }
+  return splits;
 }
 
 extern "C" size_t oscar_draft_workspace_bytes(const oscar_config* cfg, int32_t batch, int32_t T, int32_t num_splits) {
