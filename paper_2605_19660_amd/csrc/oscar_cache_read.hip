@@ -9,7 +9,9 @@
 // takes the keys or the values of one page of one kv head: a wave 32 tokens' keys (two tiles, whose chunks a lane
 // loads with one access, 1 KB a wave) or 32 channels' values.  A lane holds 32 channels of a token: five Hadamard
 // stages are in its registers, two are exchanges inside a quad of lanes.  Either goes through LDS so that rows of
-// 128 channels are written whole.
+// 128 channels are written whole, and past the caches, where nothing reads them soon (145 us with ordinary stores).
+// 4 x 32768 tokens of 8 kv heads, 2-bit to bf16: 124 us, 5.1 TB/s read + written (a copy reaches 5.0, a fill 6.9);
+// 8 x 900 4-bit to fp32: 17 us, 4.0 TB/s; 1000 tokens: 5.9 us, the chain of lengths, table and page.
 #include "oscar_decode_common.h"
 #include "oscar_rowops.h"
 

@@ -25,8 +25,15 @@
 // what a tile's sums start from, for the values one extra tile, whose other rows are the rows' sums.  Seen from
 // code 0 the same roundings moved the logits three times as far.  Roundings: Q, Q Delta, P, P Delta and the
 // mean terms to fp16, half a step (2^-11) each.  The probabilities are scaled by 2^7 .. 2^15 (less where a value
-// step of 2 or more would carry P Delta past the fp16 range): a token counts down to 2^-27 of the largest at least.  Sums,
-// maxima and outputs are fp32.
+// step of 2 or more would carry P Delta past the fp16 range), so that a token counts with all its bits down to 2^-17
+// of the largest at least, and with fewer down to 2^-27.  Sums, maxima and outputs are fp32.
+//
+// What bounds it: the issue of instructions.  A page costs a wave with two tiles 184 matrix and about 700 vector
+// instructions, and the two do not overlap across the waves of a SIMD (measured: the time is the sum of both): 3.4 us
+// a page and wave, whether one or two waves share the SIMD.  8 new tokens of 32 heads over 8 x 32768: 66 us, and 5 in
+// the reduce pass, 2.8 TB/s; 5 of 28 heads over 131001: 42 + 5; 500 of 32 heads over 2 x 8100,
+// 4-bit: 126 us, 410 TFLOP/s of the products that the formula has; 4 over 1000: 12 + 4, a chain of lengths, block
+// table, page and window.
 #include "oscar_decode_common.h"
 
 namespace {
@@ -246,7 +253,7 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 
     // ---- loads ahead ----
     // (all of a page's codes a page ahead; 4-bit ones of two tiles a half each, into what the other half has left: the
-    // registers do not hold more.  500 new tokens over 2 x 8K: 128 us, 159 with all of them ahead and spilled)
+    // registers do not hold more.  500 new tokens over 2 x 8K: 126 us, 159 with all of them ahead and spilled)
     constexpr int AHEAD = BITS == 4 && NR == 2 ? 2 : 4;
     uint32_t kc[4][2 * BITS], vc[4][2 * BITS];
     auto pool_of = [&](const void* pool, int bytes, const Page& pg) {
