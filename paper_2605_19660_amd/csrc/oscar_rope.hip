@@ -156,7 +156,7 @@ extern "C" int oscar_rope(const void* q, const void* k, void* q_out, void* k_out
   const int heads[2] = {n_q_heads, n_kv_heads};
   const int64_t in_stride[2] = {q_stride, k_stride}, out_stride[2] = {q_out_stride, k_out_stride};
   for (int i = 0; i < 2; ++i) {
-    if (heads[i] == 0) continue;
+    if (heads[i] == 0 || n_tokens == 0) continue;   // (tensors of no tokens have no addresses)
     if (!in[i] || !out[i] || heads[i] > 65536) return OSCAR_ERR_INVALID_ARG;
     // 16-byte accesses; tokens do not overlap
     if (((reinterpret_cast<uintptr_t>(in[i]) | reinterpret_cast<uintptr_t>(out[i])) & 15) != 0 ||
@@ -170,7 +170,7 @@ extern "C" int oscar_rope(const void* q, const void* k, void* q_out, void* k_out
     P.in_stride[i] = in_stride[i];
     P.out_stride[i] = out_stride[i];
   }
-  if (!positions || !inv_freq) return OSCAR_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (!positions || !inv_freq)) return OSCAR_ERR_INVALID_ARG;
   P.half = rotary_dim / 2;
   if (pair_axis) {
     for (int i = 0; i < P.half; ++i) {

@@ -124,3 +124,51 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
             m.setattr(ob, "_current_device", lambda: 1)
             with pytest.raises(AssertionError, match="current device"):
                 call()
+
+
+def test_one_layer_of_many():
+    """A layer behind a shared block table answers as a cache of its own does."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    cfg = ob.Config(8, 2)
+    m, plain = ob.MultiLayerCache(cfg, 2, 4, 3), ob.Cache(cfg, 2, 4)
+    g = torch.Generator().manual_seed(4)
+    k = torch.randn(3, 2, 300, 2, 128, generator=g).bfloat16().cuda()
+    for l in range(3):
+        ob.quantize_append(m.layer(l), k[l], k[l].flip(0), eager=True)
+    ob.quantize_append(plain, k[1], k[1].flip(0), eager=True)
+    q, kn, vn = (torch.randn(2, 5, h, 128, generator=g).bfloat16().cuda() for h in (8, 2, 2))
+    for splits in (1, 2):
+        assert torch.equal(ob.draft_attn(m.layer(1), q, kn, vn, num_splits=splits), ob.draft_attn(plain, q, kn, vn, num_splits=splits))
+
+
+def test_nothing_to_do():
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    c = filled_cache([140], hk=2, hq=8)
+    empty = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")
+    assert ob.draft_attn(c, empty(1, 0, 8, 128), empty(1, 0, 2, 128), empty(1, 0, 2, 128)).shape == (1, 0, 8, 128)
+    assert ob.cache_read(c, None, k=empty(1, 0, 2, 128))[0].shape == (1, 0, 2, 128)
+    pos, inv = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda")
+    assert ob.rope(empty(0, 8, 128), None, pos, inv)[0].shape == (0, 8, 128)
+    n, tokens = ob.verify_drafts(torch.empty(0, 4, 10, device="cuda"), torch.empty(0, 3, 10, device="cuda"),
+                                 torch.empty(0, 3, dtype=torch.int32, device="cuda"), torch.empty(0, 4, device="cuda"))
+    assert n.shape == (0,) and tokens.shape == (0, 4)
+
+
+@pytest.mark.parametrize("bits,heads", [(2, 3), (4, 1)])
+def test_a_long_piece_attends_to_itself(bits, heads):
+    """Many blocks of rows, the last of 16 rows and fewer, over a short cache: against the short call's rows, whose
+    causal past is the same."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    c = filled_cache([150], hk=1, hq=heads, bits=bits)
+    g = torch.Generator().manual_seed(5)
+    q, k, v = (torch.randn(1, 1500, h, 128, generator=g).bfloat16().cuda() for h in (heads, 1, 1))
+    got = ob.draft_attn(c, q, k, v, num_splits=1)
+    for n in (7, 40, 333, 1024):
+        part = ob.draft_attn(c, q[:, :n].contiguous(), k[:, :n].contiguous(), v[:, :n].contiguous(), num_splits=1)
+        # the same sums; which rows share a tile decides when its reference moves (whole powers of two, fp16 operands:
+        # 2^-11 of each probability), and the outputs are rounded to bf16
+        err = (got[:, :n].double() - part.double()).abs()
+        assert bool((err <= 2.0 ** -8 * part.double().abs() + 2.0 ** -10 * float(v.abs().max())).all())
