@@ -58,6 +58,16 @@ constexpr int kQShift = 2;           // the queries carry 2^2
 // What loads of a page that is none take: its codes and parameters are zeros, and nothing that follows is NaN.
 __device__ __align__(256) const uint8_t kNoPage[8192] = {};
 
+// Division of n < 2^31 by a number known on the host (as a division it is 20 instructions, one after the other).
+struct Divisor {
+  uint32_t d, m;   // m = (2^32 - 1) / d: the product falls short by less than one
+  __device__ __forceinline__ int of(int n) const {
+    const uint32_t q = __umulhi((uint32_t)n, m);
+    return (int)(q + ((q + 1) * d <= (uint32_t)n ? 1 : 0));
+  }
+};
+Divisor divisor(int d) { return {(uint32_t)d, 0xffffffffu / (uint32_t)d}; }
+
 struct DraftParams {
   const void *q, *k_new, *v_new;
   void* out;
@@ -65,7 +75,8 @@ struct DraftParams {
   const int32_t* new_lens;
   oscar_cache c;
   PageGeom g;
-  int T, num_splits;
+  int T, num_splits, group;   // group: query heads of a kv head
+  Divisor by_splits, by_kv_heads, by_group;
   float scale_log2;
 };
 
@@ -194,9 +205,9 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, q4 = lane >> 4;
-  const int Hkv = P.c.cfg.n_kv_heads, Hq = P.c.cfg.n_q_heads, g = Hq / Hkv;
-  const int split = blockIdx.x % P.num_splits, unit = blockIdx.x / P.num_splits;
-  const int kvh = unit % Hkv, b = unit / Hkv;
+  const int Hkv = P.c.cfg.n_kv_heads, Hq = P.c.cfg.n_q_heads, g = P.group;
+  const int unit = P.by_splits.of(blockIdx.x), split = blockIdx.x - unit * P.num_splits;
+  const int b = P.by_kv_heads.of(unit), kvh = unit - b * Hkv;
 
   // the queries' loads wait for nothing
   const uint16_t* q_row[NR];
@@ -204,8 +215,9 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
     const int row = min(row0 + 16 * i + n, P.T * g - 1);
-    row_t[i] = row / g;
-    q_row[i] = reinterpret_cast<const uint16_t*>(P.q) + (((size_t)b * P.T + row_t[i]) * Hq + (size_t)kvh * g + row % g) * D + 32 * q4;
+    row_t[i] = P.by_group.of(row);
+    q_row[i] = reinterpret_cast<const uint16_t*>(P.q) +
+               (((size_t)b * P.T + row_t[i]) * Hq + (size_t)kvh * g + (row - row_t[i] * g)) * D + 32 * q4;
   }
   u32x4 q_in[4];
 #pragma unroll
@@ -235,11 +247,12 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 
   if (rows > 0) {
     // ---- what this wave takes: 16-bit pieces (window, then new tokens) and pages, dealt to the waves of all splits ----
-    const int last_t = (row0 + rows - 1) / g;                            // last new token any row here sees
+    const int last_t = P.by_group.of(row0 + rows - 1);                            // last new token any row here sees
     const int n_win = (res + TAIL - 1) / TAIL;
     const int n_tail = n_win + (min(n_new, last_t + 1) + TAIL - 1) / TAIL;
     const int step = P.num_splits * 4, own = split * 4 + wave;
-    int page = own < n_tail ? own + (n_tail - own + step - 1) / step * step - n_tail : own - n_tail;
+    int page = own - n_tail;
+    while (page < 0) page += step;
     // (read as constant memory, by the scalar unit: a vector load's wait would be one for every load ahead)
     const auto table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
         reinterpret_cast<uintptr_t>(P.c.block_table + (size_t)b * P.c.max_pages_per_seq));
@@ -256,8 +269,11 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
     // registers do not hold more.  500 new tokens over 2 x 8K: 126 us, 159 with all of them ahead and spilled)
     constexpr int AHEAD = BITS == 4 && NR == 2 ? 2 : 4;
     uint32_t kc[4][2 * BITS], vc[4][2 * BITS];
-    auto pool_of = [&](const void* pool, int bytes, const Page& pg) {
-      const uintptr_t at = reinterpret_cast<uintptr_t>(pool) + ((size_t)pg.phys * Hkv + kvh) * bytes;
+    // (every part of a page has a power of two of bytes)
+    constexpr int code_shift = BITS == 2 ? 12 : 13, norm_shift = M32 ? 9 : 8;
+    const int k_shift = norm_shift + 1 + (ONE ? 0 : P.g.ngk >> 1), v_shift = norm_shift + 1 + (P.g.ngv >> 1);
+    auto pool_of = [&](const void* pool, int shift, const Page& pg) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(pool) + (((size_t)pg.phys * Hkv + kvh) << shift);
       return reinterpret_cast<DevicePtr>(pg.held ? at : reinterpret_cast<uintptr_t>(kNoPage));
     };
     const uint32_t k_at = chunk_offset(BITS, 0, 4 * (n % 4) + n / 4, q4), v_at = chunk_offset(BITS, 0, n, q4);
@@ -273,11 +289,11 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
     Fetched<M32> fk, fv;
     u32x4 fn;
     auto fetch_meta = [&](const Page& pg) {
-      const DevicePtr km = pool_of(P.c.k_meta, P.g.k_meta_bytes, pg);
-      const DevicePtr vm = pool_of(P.c.v_meta, P.g.v_meta_bytes, pg);
-      fk.load(km, km + P.g.k_meta_bytes / 2, km_at);
-      fv.load(vm, vm + P.g.v_meta_bytes / 2, vm_at);
-      const DevicePtr kn = pool_of(P.c.k_norms, P.g.k_norms_bytes, pg);
+      const DevicePtr km = pool_of(P.c.k_meta, k_shift, pg);
+      const DevicePtr vm = pool_of(P.c.v_meta, v_shift, pg);
+      fk.load(km, km + (1 << k_shift >> 1), km_at);
+      fv.load(vm, vm + (1 << v_shift >> 1), vm_at);
+      const DevicePtr kn = pool_of(P.c.k_norms, norm_shift, pg);
       if (M32) {
         fn[0] = load_as<uint32_t>(kn + lane * 8), fn[1] = load_as<uint32_t>(kn + lane * 8 + 4);
       } else {
@@ -328,8 +344,8 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 
     Page pg0 = page_of(page, entry_of(page)), pg1 = page_of(page + step, entry_of(page + step));
     fetch_meta(pg0);
-    load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg0), k_at, kc, 0, 4);
-    load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0), v_at, vc, 0, AHEAD);
+    load_codes(pool_of(P.c.k_codes, code_shift, pg0), k_at, kc, 0, 4);
+    load_codes(pool_of(P.c.v_codes, code_shift, pg0), v_at, vc, 0, AHEAD);
 
     // ---- queries ----
     // Wave i rotates tile i, on the matrix cores: out = H q, H's signs exact in either type.  Row m of output tile
@@ -492,21 +508,29 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
           for (int r = 0; r < 4; ++r) pr[i][4 * j + r] = (_Float16)__builtin_amdgcn_exp2f(s[i][j][r] - M[i]);
         x[i] = mfma(one, pr[i], x[i]);
       }
-      // values: channel 16 ct + n of tokens t0 + 16 j + 4 q4 + r
+      // values: channel 16 ct + n of tokens t0 + 16 j + 4 q4 + r; 32 loads at a time, all of them before the first use
 #pragma unroll
-      for (int ct = 0; ct < 8; ++ct) {
-        half8 a;
+      for (int c0 = 0; c0 < 8; c0 += 4) {
+        uint16_t v[4][8];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int e = 0; e < 8; ++e) {
+          const uint16_t* row = vb + (size_t)min(t0 + 16 * (e / 4) + 4 * q4 + e % 4, count - 1) * stride + 16 * c0 + n;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = t0 + 16 * j + 4 * q4 + r;
-            const uint16_t v = vb[(size_t)min(t, count - 1) * stride + 16 * ct + n];
-            const float y = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
-            a[4 * j + r] = (_Float16)(t < count ? __builtin_amdgcn_fmed3f(y, -kHalfMax, kHalfMax) : 0.0f);
+          for (int ct = 0; ct < 4; ++ct) v[ct][e] = row[16 * ct];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) {
+          half8 a;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int t = t0 + 16 * (e / 4) + 4 * q4 + e % 4;
+            const float y = bf16 ? __uint_as_float((uint32_t)v[ct][e] << 16) : __half2float(__ushort_as_half(v[ct][e]));
+            a[e] = (_Float16)(t < count ? __builtin_amdgcn_fmed3f(y, -kHalfMax, kHalfMax) : 0.0f);
           }
 #pragma unroll
-        for (int i = 0; i < NR; ++i) o[i][ct] = mfma(a, pr[i], o[i][ct]);
+          for (int i = 0; i < NR; ++i) o[i][c0 + ct] = mfma(a, pr[i], o[i][c0 + ct]);
+        }
       }
     }
 
@@ -538,7 +562,7 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 #pragma unroll
         for (int w = 2 * half; w < 2 * half + 2; ++w) {
           if (!ONE || w == 0) {
-            const int gk = ONE ? 0 : w * 32 / P.g.k_group * 16;
+            const int gk = ONE ? 0 : (w * P.g.ngk >> 2) * 16;
 #pragma unroll
             for (int i = 0; i < NR; ++i) start[i] = (float4v){0, 0, 0, 0};
 #pragma unroll
@@ -609,9 +633,9 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
               pr[i][r][4 * half + t] = p[0];
               pr[i][r][4 * half + t + 1] = p[1];
             }
-        if (half == 0) load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg0), v_at, vc, AHEAD, 4);
+        if (half == 0) load_codes(pool_of(P.c.v_codes, code_shift, pg0), v_at, vc, AHEAD, 4);
       }
-      load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1), k_at, kc, 0, AHEAD);
+      load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, 0, AHEAD);
       fetch_meta(pg1);
 
       // values
@@ -625,8 +649,8 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         // (a group of several of these shares its products; without a branch they cost less than with one)
-        const int gv = w * 32 / P.g.v_group;
-        const half8* mids = n == gv && w * 32 % P.g.v_group == 0 ? lds.loop.mid : lds.loop.none;
+        const int gv = w * P.g.ngv >> 2;
+        const half8* mids = n == gv && (w * P.g.ngv & 3) == 0 ? lds.loop.mid : lds.loop.none;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
           const half8 st = meta.v_step[gv * 16 + 4 * kk + q4];
@@ -644,9 +668,9 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 #pragma unroll
             for (int i = 0; i < NR; ++i) o[i][2 * w + j] = mfma(a, pd[i][kk], o[i][2 * w + j]);
           }
-        if (w == 1) load_codes(pool_of(P.c.k_codes, P.g.k_codes_bytes, pg1), k_at, kc, AHEAD, 4);
+        if (w == 1) load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, AHEAD, 4);
       }
-      load_codes(pool_of(P.c.v_codes, P.g.v_codes_bytes, pg1), v_at, vc, 0, AHEAD);
+      load_codes(pool_of(P.c.v_codes, code_shift, pg1), v_at, vc, 0, AHEAD);
       stage_keys();
       page_off = stage_values();
       pg0 = pg1;
@@ -656,15 +680,14 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       x[i] *= (float)(1 << UNITS);
-      float zb[4];
+      float zb[4];   // of channels 32 w .. 32 w + 31
 #pragma unroll
       for (int gv = 0; gv < 4; ++gv) zb[gv] = __shfl(x[i][gv], n, 64);
+      if (P.g.ngv == 2) zb[3] = zb[2] = zb[1];
+      if (P.g.ngv < 4) zb[1] = zb[0];
+      if (P.g.ngv == 1) zb[3] = zb[2] = zb[0];
 #pragma unroll
-      for (int ct = 0; ct < 8; ++ct) {
-        const int gv = ct * 16 / P.g.v_group;
-        const float z = gv == 0 ? zb[0] : gv == 1 ? zb[1] : gv == 2 ? zb[2] : zb[3];
-        o[i][ct] = o[i][ct] * (float)(1 << (24 - C::BPMIN)) + z;
-      }
+      for (int ct = 0; ct < 8; ++ct) o[i][ct] = o[i][ct] * (float)(1 << (24 - C::BPMIN)) + zb[ct / 2];
     }
     __syncthreads();
   }
@@ -697,7 +720,7 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
       l = fmaf(lds.join.l[w][row], f, l);
     }
     const bool there = row < rows;
-    const int t = (row0 + row) / g, h = kvh * g + (row0 + row) % g;
+    const int t = P.by_group.of(row0 + row), h = kvh * g + (row0 + row - t * g);
     const size_t out_row = ((size_t)b * P.T + t) * Hq + h;
     if (!there) y = (float4v){0, 0, 0, 0};
     if (P.num_splits > 1) {
@@ -736,7 +759,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_ke
 }
 
 template <int BITS, bool M32, bool ONE> void launch(const DraftParams& P, int nr, dim3 grid, hipStream_t st) {
-  const int64_t rows = (int64_t)P.T * (P.c.cfg.n_q_heads / P.c.cfg.n_kv_heads);
+  const int64_t rows = (int64_t)P.T * P.group;
   if (nr == 1)
     hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 1, false>), grid, dim3(256), 0, st, P);
   else if (BITS == 2 && (rows - 1) % 32 < 16)
@@ -833,6 +856,10 @@ extern "C" int oscar_draft_attn(const void* q, const void* k_new, const void* v_
   P.g = make_geom(cfg.bits, cfg.k_group, cfg.v_group, cfg.meta_dtype);
   P.T = T;
   P.num_splits = num_splits;
+  P.group = cfg.n_q_heads / cfg.n_kv_heads;
+  P.by_splits = divisor(num_splits);
+  P.by_kv_heads = divisor(cfg.n_kv_heads);
+  P.by_group = divisor(P.group);
   P.scale_log2 = (softmax_scale > 0.0f ? softmax_scale : 0.08838834764831845f) * 1.4426950408889634f;
   // row blocks of one page range are a multiple of the XCDs' number apart wherever the ranges are
   const dim3 grid((unsigned)units, (unsigned)blocks);
