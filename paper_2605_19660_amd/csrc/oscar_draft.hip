@@ -456,18 +456,24 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
         stride = (size_t)Hkv * D;
       }
       // logits: tile j holds tokens t0 + 16 j .., row n of the tile = token n of it
+      u32x4 ka[2][4];
+      float norm[2][4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint16_t* row = kb + (size_t)min(t0 + 16 * j + n, count - 1) * stride + 32 * q4;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) ka[j][kk] = *reinterpret_cast<const u32x4*>(row + 8 * kk);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) norm[j][r] = load_meta(P.c.res_norm, head * R + min(t0 + 16 * j + 4 * q4 + r, R - 1), MB);
+      }
+      __builtin_amdgcn_sched_barrier(0);   // (all loads before the first use; left alone they go out one by one)
       float4v s[NR][2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int t = min(t0 + 16 * j + n, count - 1);
-        u32x4 a[4];
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) a[kk] = *reinterpret_cast<const u32x4*>(kb + (size_t)t * stride + 32 * q4 + 8 * kk);
+        u32x4 (&a)[4] = ka[j];
         float f[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          f[r] = win ? load_meta(P.c.res_norm, head * R + min(t0 + 16 * j + 4 * q4 + r, R - 1), MB) * (1.0f / (1 << kQShift))
-                     : P.scale_log2;
+        for (int r = 0; r < 4; ++r) f[r] = win ? norm[j][r] * (1.0f / (1 << kQShift)) : P.scale_log2;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
           float4v acc = {0, 0, 0, 0};
