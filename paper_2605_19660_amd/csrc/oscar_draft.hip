@@ -39,7 +39,9 @@
 namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float2v __attribute__((ext_vector_type(2)));
@@ -173,6 +175,14 @@ __device__ __forceinline__ float max_of_row(float v) {   // over the four lanes 
   return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
+// Between a wave's writes to its own LDS and its reads of what other lanes wrote: LDS operations of one wave
+// execute in order, the compiler must not move them.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens)
 
 // Workgroups a CU that a variant's registers are held to.  Three where they fit: four new tokens of 8 x 32K 49 us, 52
@@ -183,9 +193,11 @@ constexpr int OROW = D + 4;
 template <int NR> struct Lds {
   static constexpr int ROWS = NR * 16;
   struct Loop {
-    half8 qh[NR][4][64], qc[NR][4][64];              // queries as operands: natural order, codes' order
+    u32x4 q[NR][4][64];                              // queries as they came,
+    half8 qh[NR][4][64], qc[NR][4][64];              // rotated and scaled, and in the codes' order
     Staged meta[4];                                  // of each wave's page
     half8 cw[2], mid[2], none[2];                    // counterweights of even and odd k-steps, times -MID, zeros
+    half8 tail[4][TAIL][9];                          // of each wave's 16-bit piece: half of its values' channels
   };
   struct Join {
     float o[4][ROWS][OROW], m[4][ROWS], l[4][ROWS];
@@ -394,7 +406,10 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
       }
       half8 qh[4];
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) qh[kk] = lds.loop.qh[wave][kk][lane];
+      for (int kk = 0; kk < 4; ++kk) {
+        lds.loop.q[wave][kk][lane] = q_in[kk];
+        qh[kk] = lds.loop.qh[wave][kk][lane];
+      }
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         half8 qc;   // in the codes' order, with the counterweights of their bit positions
@@ -466,6 +481,17 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 #pragma unroll
         for (int r = 0; r < 4; ++r) norm[j][r] = load_meta(P.c.res_norm, head * R + min(t0 + 16 * j + 4 * q4 + r, R - 1), MB);
       }
+      // Values: rows of 64 channels in, a lane 8 channels of four tokens; through LDS, and columns of four tokens out.
+      // (Loaded as columns, 64 times two bytes a lane: 500 new tokens over 2 x 8100 4-bit 225 us, 205 so; 2000 over 130
+      // 271 and 160.)
+      u32x4 va[4];
+      auto load_values = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          va[i] = *reinterpret_cast<const u32x4*>(vb + (size_t)min(t0 + 8 * i + lane / 8, count - 1) * stride + 64 * half +
+                                                  8 * (lane % 8));
+        __builtin_amdgcn_sched_barrier(0);
+      };
       __builtin_amdgcn_sched_barrier(0);   // (all loads before the first use; left alone they go out one by one)
       float4v s[NR][2];
 #pragma unroll
@@ -482,7 +508,7 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
             if (win) {
               acc = mfma(__builtin_bit_cast(half8, a[kk]), lds.loop.qh[i][kk][lane], acc);
             } else {
-              const u32x4 r = *reinterpret_cast<const u32x4*>(q_row[i] + 8 * kk);
+              const u32x4 r = lds.loop.q[i][kk][lane];
               if (bf16)
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[kk]),
                                                               __builtin_bit_cast(bf16x8, r), acc, 0, 0, 0);
@@ -514,28 +540,43 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
           for (int r = 0; r < 4; ++r) pr[i][4 * j + r] = (_Float16)__builtin_amdgcn_exp2f(s[i][j][r] - M[i]);
         x[i] = mfma(one, pr[i], x[i]);
       }
-      // values: channel 16 ct + n of tokens t0 + 16 j + 4 q4 + r; 32 loads at a time, all of them before the first use
+      load_values(0);
 #pragma unroll
-      for (int c0 = 0; c0 < 8; c0 += 4) {
-        uint16_t v[4][8];
+      for (int half = 0; half < 2; ++half) {
+        wave_lds_fence();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint16_t* row = vb + (size_t)min(t0 + 16 * (e / 4) + 4 * q4 + e % 4, count - 1) * stride + 16 * c0 + n;
+        for (int i = 0; i < 4; ++i) {
+          half8 a;
+          if (bf16) {
 #pragma unroll
-          for (int ct = 0; ct < 4; ++ct) v[ct][e] = row[16 * ct];
+            for (int e = 0; e < 4; ++e) {
+              const half2v two =
+                  pack2(__builtin_amdgcn_fmed3f(__uint_as_float(va[i][e] << 16), -kHalfMax, kHalfMax),
+                        __builtin_amdgcn_fmed3f(__uint_as_float(va[i][e] & 0xffff0000u), -kHalfMax, kHalfMax));
+              a[2 * e] = two[0], a[2 * e + 1] = two[1];
+            }
+          } else {
+            const half8 most = (_Float16)kHalfMax;
+            a = __builtin_elementwise_min(__builtin_elementwise_max(__builtin_bit_cast(half8, va[i]), -most), most);
+          }
+          lds.loop.tail[wave][8 * i + lane / 8][lane % 8] = a;
         }
-        __builtin_amdgcn_sched_barrier(0);
+        if (half == 0) load_values(1);
+        wave_lds_fence();
+        // channel 64 half + 16 ct + n of tokens t0 + 16 j + 4 q4 + r: columns of what was written as rows
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct) {
           half8 a;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int t = t0 + 16 * (e / 4) + 4 * q4 + e % 4;
-            const float y = bf16 ? __uint_as_float((uint32_t)v[ct][e] << 16) : __half2float(__ushort_as_half(v[ct][e]));
-            a[e] = (_Float16)(t < count ? __builtin_amdgcn_fmed3f(y, -kHalfMax, kHalfMax) : 0.0f);
+          for (int j = 0; j < 2; ++j) {
+            const auto at = (__attribute__((address_space(3))) short4v*)(reinterpret_cast<_Float16*>(
+                                &lds.loop.tail[wave][16 * j + 4 * q4 + n / 4][0]) + 16 * ct + 4 * (n % 4));
+            const half4v four = __builtin_bit_cast(half4v, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) a[4 * j + r] = four[r];
           }
 #pragma unroll
-          for (int i = 0; i < NR; ++i) o[i][c0 + ct] = mfma(a, pr[i], o[i][c0 + ct]);
+          for (int i = 0; i < NR; ++i) o[i][4 * half + ct] = mfma(a, pr[i], o[i][4 * half + ct]);
         }
       }
     }
