@@ -78,7 +78,7 @@ struct DraftParams {
   oscar_cache c;
   PageGeom g;
   int T, num_splits, group;   // group: query heads of a kv head
-  Divisor by_splits, by_kv_heads, by_group;
+  Divisor by_splits, by_kv_heads, by_group, by_step;   // by_step: the waves of all splits
   float scale_log2;
 };
 
@@ -235,6 +235,14 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 #pragma unroll
   for (int kk = 0; kk < 4; ++kk) q_in[kk] = *reinterpret_cast<const u32x4*>((wave == 0 ? q_row[0] : q_row[NR - 1]) + 8 * kk);
 
+  // ---- what this wave takes: pages, then 16-bit pieces (window, then new tokens), dealt to the waves of all splits ----
+  // (the first pages are known ahead of the lengths, so that their table entries are read together with those; the
+  // table as constant memory, by the scalar unit: a vector load's wait would be one for every load ahead)
+  const int step = P.num_splits * 4, own = split * 4 + wave;
+  const auto table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+      reinterpret_cast<uintptr_t>(P.c.block_table + (size_t)b * P.c.max_pages_per_seq));
+  auto entry_of = [&](int p) { return table[min(p, P.c.max_pages_per_seq - 1)]; };
+  const int entry0 = entry_of(own), entry1 = entry_of(own + step);
   const int n_new = P.new_lens ? min(max(P.new_lens[b], 0), P.T) : P.T;
   const int seq_len = max(P.c.seq_lens[b], 0);
   const int res = min(max(P.c.res_lens[b], 0), min(R, seq_len));
@@ -258,22 +266,17 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
   int off = kOff;
 
   if (rows > 0) {
-    // ---- what this wave takes: 16-bit pieces (window, then new tokens) and pages, dealt to the waves of all splits ----
-    const int last_t = P.by_group.of(row0 + rows - 1);                            // last new token any row here sees
+    const int last_t = P.by_group.of(row0 + rows - 1);                   // last new token any row here sees
     const int n_win = (res + TAIL - 1) / TAIL;
     const int n_tail = n_win + (min(n_new, last_t + 1) + TAIL - 1) / TAIL;
-    const int step = P.num_splits * 4, own = split * 4 + wave;
-    int page = own - n_tail;
-    while (page < 0) page += step;
-    // (read as constant memory, by the scalar unit: a vector load's wait would be one for every load ahead)
-    const auto table = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
-        reinterpret_cast<uintptr_t>(P.c.block_table + (size_t)b * P.c.max_pages_per_seq));
+    int piece = own - (pages - P.by_step.of(pages) * step);
+    piece += piece < 0 ? step : 0;
+    int page = own;
     // What is no page (past the end, or not of the pools) takes the zeros: every iteration makes the same loads.
     struct Page {
       int phys;
       bool held;
     };
-    auto entry_of = [&](int p) { return table[min(max(p, 0), max(pages - 1, 0))]; };
     auto page_of = [&](int p, int phys) { return Page{phys, p < pages && phys >= 0 && phys < P.c.num_pages}; };
 
     // ---- loads ahead ----
@@ -354,7 +357,7 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
       return kOff - max(exponent - 14, 0);
     };
 
-    Page pg0 = page_of(page, entry_of(page)), pg1 = page_of(page + step, entry_of(page + step));
+    Page pg0 = page_of(page, entry0), pg1 = page_of(page + step, entry1);
     fetch_meta(pg0);
     load_codes(pool_of(P.c.k_codes, code_shift, pg0), k_at, kc, 0, 4);
     load_codes(pool_of(P.c.v_codes, code_shift, pg0), v_at, vc, 0, AHEAD);
@@ -455,7 +458,7 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
     };
 
     // ---- 16-bit tokens ----
-    for (int u = own; u < n_tail; u += step) {
+    for (int u = piece; u < n_tail; u += step) {
       const bool win = u < n_win;
       const int t0 = (win ? u : u - n_win) * TAIL, count = win ? res : n_new;
       const size_t head = (size_t)b * Hkv + kvh;
@@ -905,6 +908,7 @@ extern "C" int oscar_draft_attn(const void* q, const void* k_new, const void* v_
   P.num_splits = num_splits;
   P.group = cfg.n_q_heads / cfg.n_kv_heads;
   P.by_splits = divisor(num_splits);
+  P.by_step = divisor(4 * num_splits);
   P.by_kv_heads = divisor(cfg.n_kv_heads);
   P.by_group = divisor(P.group);
   P.scale_log2 = (softmax_scale > 0.0f ? softmax_scale : 0.08838834764831845f) * 1.4426950408889634f;
