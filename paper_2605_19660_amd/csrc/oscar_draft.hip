@@ -28,12 +28,11 @@
 // step of 2 or more would carry P Delta past the fp16 range), so that a token counts with all its bits down to 2^-17
 // of the largest at least, and with fewer down to 2^-27.  Sums, maxima and outputs are fp32.
 //
-// What bounds it: the issue of instructions.  A page costs a wave with two tiles 184 matrix and about 700 vector
-// instructions, and the two do not overlap across the waves of a SIMD (measured: the time is the sum of both): 3.4 us
-// a page and wave, whether one or two waves share the SIMD.  8 new tokens of 32 heads over 8 x 32768: 66 us, and 5 in
-// the reduce pass, 2.8 TB/s; 5 of 28 heads over 131001: 42 + 5; 500 of 32 heads over 2 x 8100,
-// 4-bit: 126 us, 410 TFLOP/s of the products that the formula has; 4 over 1000: 12 + 4, a chain of lengths, block
-// table, page and window.
+// What bounds it: the issue of instructions.  A page costs a wave with two tiles 184 matrix and about 750 vector
+// instructions, and the two do not overlap across the waves of a SIMD (measured: the time is the sum of both).  8 new
+// tokens of 32 heads over 8 x 32768: 63 us, 2.9 TB/s, and 5 in the reduce pass; 5 of 28 heads over 131001, G_k = 32:
+// 40 + 5; 500 of 32 heads over two ragged caches of up to 8100, 4-bit: 114 us, 455 TFLOP/s of the products that the
+// formula has; 4 over 1000: 11 + 4, a chain of lengths, page, window and reduce pass.
 #include "oscar_decode_common.h"
 
 namespace {
@@ -123,7 +122,7 @@ struct Staged {
 };
 // A row's probabilities are taken against a reference that follows its maximum only when that has passed it by
 // 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs a rescaling of the
-// whole state (8 new tokens over 8 x 32K: 76 us, 81 with a reference that follows at once).
+// whole state (8 new tokens over 8 x 32K: 71 us, 75 with a reference that follows at once).
 constexpr float kSlack = 8.0f, kNone = -3e38f;
 constexpr int kOff = 7;          // exponent of a probability at its reference: kOff + kSlack stay inside fp16
 // What a lane holds of the metadata of a page to come: 8 steps and 8 zeros of the keys or of the values.
@@ -185,8 +184,8 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens)
 
-// Workgroups a CU that a variant's registers are held to.  Three where they fit: four new tokens of 8 x 32K 49 us, 52
-// with two; with fp32 metadata 67, 55 with two, with 4-bit codes 119, 68 with two (registers in scratch).
+// Workgroups a CU that a variant's registers are held to.  Three where they fit: four new tokens of 48 x 8000 66 us, 76
+// with two; with 4-bit codes 8 x 32K 89, 64 with two (registers in scratch).
 __host__ __device__ constexpr int wgs_per_cu(int bits, bool m32, int nr) { return nr == 1 && bits == 2 && !m32 ? 3 : 2; }
 
 constexpr int OROW = D + 4;
@@ -281,7 +280,7 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
 
     // ---- loads ahead ----
     // (all of a page's codes a page ahead; 4-bit ones of two tiles a half each, into what the other half has left: the
-    // registers do not hold more.  500 new tokens over 2 x 8K: 126 us, 159 with all of them ahead and spilled)
+    // registers do not hold more.  500 new tokens over 2 x 8100: 207 us, 250 with all of them ahead and spilled)
     constexpr int AHEAD = BITS == 4 && NR == 2 ? 2 : 4;
     uint32_t kc[4][2 * BITS], vc[4][2 * BITS];
     // (every part of a page has a power of two of bytes)
@@ -485,8 +484,8 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
         for (int r = 0; r < 4; ++r) norm[j][r] = load_meta(P.c.res_norm, head * R + min(t0 + 16 * j + 4 * q4 + r, R - 1), MB);
       }
       // Values: rows of 64 channels in, a lane 8 channels of four tokens; through LDS, and columns of four tokens out.
-      // (Loaded as columns, 64 times two bytes a lane: 500 new tokens over 2 x 8100 4-bit 225 us, 205 so; 2000 over 130
-      // 271 and 160.)
+      // (Loaded as columns, 64 times two bytes a lane, 500 new tokens over 2 x 8100 4-bit take 225 us, 207 so; 2000
+      // over 130 271 and 159.)
       u32x4 va[4];
       auto load_values = [&](int half) {
 #pragma unroll
@@ -790,10 +789,10 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
   }
 }
 
-// A workgroup of NR tiles.  LAST: the last rows are 16 at most and take one tile (35 rows, seven query heads and
-// five tokens, over 128K tokens: 41 us, 45 as twice two tiles).  A variant of its own, for the second body costs
-// the first one registers (32 rows, 8 x 32K tokens: 67 us, 71 with it), and with 4-bit codes more than it gains (500
-// new tokens over 2 x 8K: 145 us, 181 with it).
+// A workgroup of NR tiles.  LAST: the second and last block of rows is 16 of them at most and takes one tile (35 rows,
+// seven query heads and five tokens, over 131001 tokens: 37.6 us, 43.4 as twice two tiles).  For the second body costs
+// the first one registers, it is a variant of its own, not taken with more blocks (77 rows 57.4 us, 56.5 without it,
+// 2000 rows over 2 x 8100 203 and 197), nor with 4-bit codes.
 template <int BITS, bool M32, bool ONE, int NR, bool LAST>
 __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
   __shared__ __align__(16) Lds<NR> lds;
@@ -812,7 +811,7 @@ template <int BITS, bool M32, bool ONE> void launch(const DraftParams& P, int nr
   const int64_t rows = (int64_t)P.T * P.group;
   if (nr == 1)
     hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 1, false>), grid, dim3(256), 0, st, P);
-  else if (BITS == 2 && (rows - 1) % 32 < 16)
+  else if (BITS == 2 && rows > 32 && rows <= 48)
     hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 2, BITS == 2>), grid, dim3(256), 0, st, P);
   else
     hipLaunchKernelGGL((oscar_draft_kernel<BITS, M32, ONE, 2, false>), grid, dim3(256), 0, st, P);
@@ -824,8 +823,9 @@ template <int BITS, bool M32> void launch(const DraftParams& P, int nr, dim3 gri
     launch<BITS, M32, false>(P, nr, grid, st);
 }
 
-// Tiles of 16 query rows a wave holds: two read every page half as often (32 rows over 8 x 32K 76 us, 82 with one; 500
-// new tokens of 32 heads over 2 x 8K 229, 256 with one), one has no idle half (16 rows 49 us, 53 with two; 4-bit 68, 79).
+// Tiles of 16 query rows a wave holds: two read every page half as often (32 rows over 8 x 32K 71 us, 85 with one; 500
+// new tokens of 32 heads over 2 x 8100 206 and 241, 4-bit 207 and 302), one has no idle half (16 rows 48 us, 50 with
+// two; 4-bit 64 and 75).
 int row_tiles(const oscar_config& cfg, int T) { return (int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) <= 16 ? 1 : 2; }
 int64_t row_blocks(const oscar_config& cfg, int T) {
   const int rows = 16 * row_tiles(cfg, T);
@@ -844,7 +844,7 @@ int check_draft_config(const oscar_config* cfg) {
 // new ones) in 3 us with one tile of rows and in 4 with two, 1.4 times that with 4-bit codes; workgroups that share a
 // CU take 0.75 times as long each as one after the other; a workgroup's start costs 2 more.  Splitting costs the
 // reduce pass: 3 us, 0.4 ns a record, and past 64 splits 1.5 us and 0.07 each (another kernel).  Over 186 calls of 1 ..
-// 64 sequences, 30 .. 131001 tokens and 1 .. 128 new ones the choice takes 1 % longer than the best count (17 at the
+// 64 sequences, 30 .. 131001 tokens and 1 .. 128 new ones the choice takes 1 % longer than the best count (9 at the
 // most); as many splits as the chip has room for, 7 % (82 at the most): 4 new tokens of 48 x 260 14 us with one split,
 // 25 with two; 8 of 24 x 32K 170 with four, which put three workgroups on every CU, 195 with two.
 extern "C" int32_t oscar_draft_auto_splits(const oscar_config* cfg, int32_t batch, int32_t T, int32_t max_seq_len) {
