@@ -153,7 +153,8 @@ template <bool M32> struct Fetched {
       step = __builtin_bit_cast(half8, a[0]);
       const half8 z = __builtin_bit_cast(half8, b[0]), most = (_Float16)kHalfMax;
       // (registers: as constants or halves of one they are taken apart into single operations)
-      uint32_t two[3] = {__builtin_bit_cast(uint32_t, (half2v)(_Float16)mid), __builtin_bit_cast(uint32_t, (half2v)(_Float16)-ints),
+      uint32_t two[3] = {__builtin_bit_cast(uint32_t, (half2v)(_Float16)mid),
+                         __builtin_bit_cast(uint32_t, (half2v)(_Float16)-ints),
                          __builtin_bit_cast(uint32_t, (half2v)(_Float16)(1.0f - ints))};
       asm("" : "+v"(two[0]), "+v"(two[1]), "+v"(two[2]));
       auto splat = [](uint32_t w) { return __builtin_bit_cast(half8, (u32x4){w, w, w, w}); };
@@ -209,7 +210,8 @@ template <int NR> struct Lds {
 };
 
 // ONE: k_group is the whole page.
-template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int row0) {
+template <int BITS, bool M32, bool ONE, int NR>
+__device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int row0) {
   using C = Codes<BITS>;
   constexpr int ROWS = NR * 16;
   constexpr int UNITS = C::BPMAX - C::BPMIN;         // log2 of what the counterweights leave in the extra tile
@@ -403,7 +405,8 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
         }
         const half2v a = pack2(there ? acc[0] * mul : 0.0f, there ? acc[1] * mul : 0.0f);
         const half2v c = pack2(there ? acc[2] * mul : 0.0f, there ? acc[3] * mul : 0.0f);
-        *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(&lds.loop.qh[wave][0][lane]) + (ot / 2) * sizeof(half8) * 64 + (ot % 2) * 8) =
+        uint8_t* at = reinterpret_cast<uint8_t*>(&lds.loop.qh[wave][0][lane]) + (ot / 2) * sizeof(half8) * 64 + (ot % 2) * 8;
+        *reinterpret_cast<uint2*>(at) =
             make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
       }
       half8 qh[4];
@@ -782,7 +785,8 @@ template <int BITS, bool M32, bool ONE, int NR> __device__ __forceinline__ void 
       uint16_t v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        v[e] = bf16 ? __builtin_bit_cast(uint16_t, __float2bfloat16(y[e] * inv)) : __builtin_bit_cast(uint16_t, __float2half_rn(y[e] * inv));
+        v[e] = bf16 ? __builtin_bit_cast(uint16_t, __float2bfloat16(y[e] * inv))
+                    : __builtin_bit_cast(uint16_t, __float2half_rn(y[e] * inv));
       *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(P.out) + out_row * D + c4) =
           make_uint2(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16);
     }

@@ -94,7 +94,8 @@ template <typename T, int PAIRS> __global__ __launch_bounds__(256) void oscar_ro
       // vectors j and j + half / N turn together; those behind the rotated channels are copied
       const int per = P.half / N;
       const bool on = j < per;
-      const int a = on ? j : per + j, b = on ? j + per : D / (2 * N) + j;   // a copied pair: 2 per + (j - per), and D / (2 N) further
+      // (a copied pair: 2 per + (j - per), and D / (2 N) further)
+      const int a = on ? j : per + j, b = on ? j + per : D / (2 * N) + j;
       Vec<T> x, y;
       x.load(src + a * N);
       y.load(src + b * N);

@@ -106,7 +106,8 @@ __device__ __forceinline__ double wave_scan(double v) {
 }
 __device__ __forceinline__ double of_lane(double v, int lane) {   // lane: the same in all
   const uint64_t bits = __double_as_longlong(v);
-  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)bits, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(bits >> 32), lane);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)bits, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(bits >> 32), lane);
   return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
 }
 
