@@ -488,7 +488,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
       }
       // Values: rows of 64 channels in, a lane 8 channels of four tokens; through LDS, and columns of four tokens out.
       // (Loaded as columns, 64 times two bytes a lane, 500 new tokens over 2 x 8100 4-bit take 225 us, 207 so; 2000
-      // over 130 271 and 159.)
+      // over 130 271 and 159, in the rows' order.)
       u32x4 va[4];
       auto load_values = [&](int half) {
 #pragma unroll
@@ -800,7 +800,9 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
 template <int BITS, bool M32, bool ONE, int NR, bool LAST>
 __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
   __shared__ __align__(16) Lds<NR> lds;
-  const int row0 = blockIdx.y * NR * 16;
+  // The longest work first: the last rows see the most new tokens (2000 over 130: 139 us, 158 in the rows' order), two
+  // tiles take longer than one (those 35 rows 44 us, 50 with the one tile first).
+  const int row0 = (LAST ? blockIdx.y : gridDim.y - 1 - blockIdx.y) * NR * 16;
   if constexpr (LAST) {
     if (blockIdx.y == gridDim.y - 1)
       attend<BITS, M32, ONE, 1>(P, reinterpret_cast<Lds<1>&>(lds), row0);
