@@ -31,7 +31,7 @@
 // What bounds it: the issue of instructions.  A page costs a wave with two tiles 184 matrix and about 750 vector
 // instructions, and the two do not overlap across the waves of a SIMD (measured: the time is the sum of both).  8 new
 // tokens of 32 heads over 8 x 32768: 63 us, 2.9 TB/s, and 5 in the reduce pass; 5 of 28 heads over 131001, G_k = 32:
-// 40 + 5; 500 of 32 heads over two ragged caches of up to 8100, 4-bit: 114 us, 455 TFLOP/s of the products that the
+// 40 + 5; 500 of 32 heads over two ragged caches of up to 8100, 4-bit: 115 us, 450 TFLOP/s of the products that the
 // formula has; 4 over 1000: 11 + 4, a chain of lengths, page, window and reduce pass.
 #include "oscar_decode_common.h"
 
@@ -77,6 +77,7 @@ struct DraftParams {
   oscar_cache c;
   PageGeom g;
   int T, num_splits, group;   // group: query heads of a kv head
+  bool last_first;            // order of the blocks of rows
   Divisor by_splits, by_kv_heads, by_group, by_step;   // by_step: the waves of all splits
   float scale_log2;
 };
@@ -800,11 +801,9 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
 template <int BITS, bool M32, bool ONE, int NR, bool LAST>
 __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
   __shared__ __align__(16) Lds<NR> lds;
-  // The longest work first: the last rows see the most new tokens (2000 over 130: 139 us, 158 in the rows' order), two
-  // tiles take longer than one (those 35 rows 44 us, 50 with the one tile first).
-  const int row0 = (LAST ? blockIdx.y : gridDim.y - 1 - blockIdx.y) * NR * 16;
+  const int row0 = (P.last_first ? gridDim.y - 1 - blockIdx.y : blockIdx.y) * NR * 16;
   if constexpr (LAST) {
-    if (blockIdx.y == gridDim.y - 1)
+    if (row0 > 0)
       attend<BITS, M32, ONE, 1>(P, reinterpret_cast<Lds<1>&>(lds), row0);
     else
       attend<BITS, M32, ONE, NR>(P, lds, row0);
@@ -913,6 +912,10 @@ extern "C" int oscar_draft_attn(const void* q, const void* k_new, const void* v_
   P.T = T;
   P.num_splits = num_splits;
   P.group = cfg.n_q_heads / cfg.n_kv_heads;
+  // Where the new tokens outnumber the cached ones the last rows, which see the most of them, go first (2000 over 130:
+  // 139 us, 158 the other way round); elsewhere that gains nothing, and ragged new_lens, whose empty blocks then come
+  // first, lose (24 and 269 new tokens over 8100 and 5394: 126 us, 116 in the rows' order).
+  P.last_first = T > max_seq_len_hint;
   P.by_splits = divisor(num_splits);
   P.by_step = divisor(4 * num_splits);
   P.by_kv_heads = divisor(cfg.n_kv_heads);
