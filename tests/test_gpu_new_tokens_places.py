@@ -1,9 +1,8 @@
 """rope, cache_read, draft_attn and verify_drafts where their memory is unusual: far into large pools and tensors
 (byte offsets past 32 bits), made on a stream that is not the current one, or not on the current device."""
-import numpy as np
 import pytest
 
-from tests.cache_numbers import filled_cache
+from cache_numbers import filled_cache
 
 pytestmark = pytest.mark.gpu
 
