@@ -19,20 +19,20 @@
 // the LDS traffic, 1.4 times the matrix products and a barrier a page; 8 new tokens over 8 x 32K took 99 us.)
 //
 // Codes become fp16 operands with a mask (a code parked in the mantissa of a subnormal: c 2^(s - 24)); the
-// steps go to the other operand, Q Delta_k and P Delta_v, and 2^-s with them.  Codes count from their middle:
-// the term that takes it off again is a product of the same rounded operands with a constant, what is left of
-// the zero-points is of the size of a group's mean, and both are products on the matrix cores too: for the keys
-// what a tile's sums start from, for the values one extra tile, whose other rows are the rows' sums.  Seen from
-// code 0 the same roundings moved the logits three times as far.  Roundings: Q, Q Delta, P, P Delta and the
-// mean terms to fp16, half a step (2^-11) each.  The probabilities are scaled by 2^7 .. 2^15 (less where a value
-// step of 2 or more would carry P Delta past the fp16 range), so that a token counts with all its bits down to 2^-17
-// of the largest at least, and with fewer down to 2^-27.  Sums, maxima and outputs are fp32.
+// steps go to the other operand, Q Delta_k and P Delta_v, and 2^-s with them.  As in the decode kernels that operand is
+// carried in two fp16 limbs, hi + lo, each a matrix product of its own: 22 bits.  The limbs come out of packed fp16
+// arithmetic on a multiplicand split once (times()).  The zero terms are products on the matrix cores too, in limbs
+// themselves: for the keys what a tile's sums start from, for the values one extra tile, whose other rows are the rows'
+// sums.  With one limb, half a step (2^-11) each for Q, Q Delta, P, P Delta and the zero terms, fp16 outputs were off by
+// 4e-4 .. 3e-3 of their length, where their own rounding is 2e-4; the second limb costs 1.6 times the time.
+// The probabilities are scaled by 2^7 .. 2^15 (less where a value step of 1 or more would carry P Delta past the fp16
+// range).  Sums, maxima and outputs are fp32.
 //
-// What bounds it: the issue of instructions.  A page costs a wave with two tiles 184 matrix and about 750 vector
+// What bounds it: the issue of instructions.  A page costs a wave with two tiles 304 matrix and about 1200 vector
 // instructions, and the two do not overlap across the waves of a SIMD (measured: the time is the sum of both).  8 new
-// tokens of 32 heads over 8 x 32768: 63 us, 2.9 TB/s, and 5 in the reduce pass; 5 of 28 heads over 131001, G_k = 32:
-// 40 + 5; 500 of 32 heads over two ragged caches of up to 8100, 4-bit: 115 us, 450 TFLOP/s of the products that the
-// formula has; 4 over 1000: 11 + 4, a chain of lengths, page, window and reduce pass.
+// tokens of 32 heads over 8 x 32768: 104 us, and 5 in the reduce pass; 5 of 28 heads over 131001, G_k = 32:
+// 59 + 5; 500 of 32 heads over two ragged caches of up to 8100, 4-bit: 217 us; 4 over 1000: 14 + 4, a chain of
+// lengths, page, window and reduce pass.
 #include "oscar_decode_common.h"
 
 namespace {
@@ -54,7 +54,7 @@ template <typename T> __device__ __forceinline__ T load_as(DevicePtr p) {
 }
 
 constexpr float kHalfMax = 65504.0f;
-constexpr int kQShift = 2;           // the queries carry 2^2
+constexpr int kQTop = 14;            // the largest channel of a block of queries is scaled to below 2^14
 
 // What loads of a page that is none take: its codes and parameters are zeros, and nothing that follows is NaN.
 __device__ __align__(256) const uint8_t kNoPage[8192] = {};
@@ -84,7 +84,6 @@ struct DraftParams {
 
 template <int BITS> struct Codes {
   static constexpr int BPMIN = BITS == 2 ? 4 : 2, BPMAX = BITS == 2 ? 8 : 6;
-  static constexpr float MID = 0.5f * (float)((1 << BITS) - 1);
   // the operand of k-step kk from a chunk
   __device__ static __forceinline__ half8 operand(const uint32_t* w, int kk) {
     u32x4 r;
@@ -114,12 +113,24 @@ template <int BITS> struct Codes {
   }
 };
 
-// A page's metadata as the waves read it: steps and mean terms (with their counterweights) as fp16 in operand
-// order, norms as fp32 with the codes' unit taken out.
+// A number in two fp16 limbs: 22 bits of it, while its low limb stays above the smallest fp16 number.
+struct Limbs {
+  half8 hi, lo;
+};
+__device__ __forceinline__ half8 fma8(half8 a, half8 b, half8 c) { return __builtin_elementwise_fma(a, b, c); }
+// The product of two limbs and a factor: its high limb, the rest of that product, which fp16 holds exactly, and the low
+// limb's product.
+__device__ __forceinline__ Limbs times(half8 hi, half8 lo, half8 by) {
+  const half8 h = hi * by;
+  return {h, fma8(lo, by, fma8(hi, by, -h))};
+}
+
+// A page's metadata as the waves read it: steps and zero terms (with their counterweights, in two limbs) as fp16 in
+// operand order, norms as fp32 with the codes' unit taken out.
 struct Staged {
-  half8 k_step[64], k_base[64];   // [group][quarter][k-step]
-  half8 v_step[64], v_base[80];   // [group][k-step][quarter]; behind the four groups the counterweights alone
-  float norm[R];                  // position (token % 16) * 8 + token / 16
+  half8 k_step[64], k_zero[2][64];   // [limb][group][quarter][k-step]
+  half8 v_step[64], v_zero[2][80];   // [limb][group][k-step][quarter]; behind the four groups the counterweights alone
+  float norm[R];                     // position (token % 16) * 8 + token / 16
 };
 // A row's probabilities are taken against a reference that follows its maximum only when that has passed it by
 // 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs a rescaling of the
@@ -140,27 +151,31 @@ template <bool M32> struct Fetched {
     if (M32) return __uint_as_float(x[e / 4][e % 4]);
     return (float)__builtin_bit_cast(half8, x[0])[e];
   }
-  // Step and mean term, x = step (c - mid) + base: base = step (mid - z) for integer zero-points (ints = 1),
-  // step mid + zero for float ones (ints = 0), as one form: nothing here branches.
-  __device__ __forceinline__ void step_and_base(float ints, float mid, half8& step, half8& base) const {
+  // Step and zero term, x = step c + zero: zero = -step z for integer zero-points (ints = 1), z itself for float ones
+  // (ints = 0), as one form: nothing here branches.
+  __device__ __forceinline__ void step_and_zero(float ints, half8& step, Limbs& zero) const {
     if (M32) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float s = number(a, e), z = number(b, e);
         step[e] = (_Float16)fminf(s, kHalfMax);
-        base[e] = (_Float16)__builtin_amdgcn_fmed3f(fmaf(s, fmaf(z, -ints, mid), z * (1.0f - ints)), -kHalfMax, kHalfMax);
+        const float base = __builtin_amdgcn_fmed3f(z * fmaf(-(s + 1.0f), ints, 1.0f), -kHalfMax, kHalfMax);
+        zero.hi[e] = (_Float16)base;
+        zero.lo[e] = (_Float16)(base - (float)zero.hi[e]);
       }
     } else {
       step = __builtin_bit_cast(half8, a[0]);
       const half8 z = __builtin_bit_cast(half8, b[0]), most = (_Float16)kHalfMax;
       // (registers: as constants or halves of one they are taken apart into single operations)
-      uint32_t two[3] = {__builtin_bit_cast(uint32_t, (half2v)(_Float16)mid),
-                         __builtin_bit_cast(uint32_t, (half2v)(_Float16)-ints),
-                         __builtin_bit_cast(uint32_t, (half2v)(_Float16)(1.0f - ints))};
-      asm("" : "+v"(two[0]), "+v"(two[1]), "+v"(two[2]));
+      uint32_t two[2] = {__builtin_bit_cast(uint32_t, (half2v)(_Float16)ints),
+                         __builtin_bit_cast(uint32_t, (half2v)(_Float16)(1.0f - 2.0f * ints))};
+      asm("" : "+v"(two[0]), "+v"(two[1]));
       auto splat = [](uint32_t w) { return __builtin_bit_cast(half8, (u32x4){w, w, w, w}); };
-      base = __builtin_elementwise_fma(step, __builtin_elementwise_fma(z, splat(two[1]), splat(two[0])), z * splat(two[2]));
-      base = __builtin_elementwise_min(__builtin_elementwise_max(base, -most), most);
+      const half8 one = (_Float16)1.0f;
+      const half8 f = fma8(step, splat(two[0]), one - splat(two[0])), m = z * splat(two[1]);   // step or 1, -z or z
+      zero.hi = __builtin_elementwise_min(__builtin_elementwise_max(f * m, -most), most);
+      zero.lo = fma8(f, m, -zero.hi);
+      zero.lo = __builtin_elementwise_min(__builtin_elementwise_max(zero.lo, -most), most);
     }
   }
 };
@@ -169,6 +184,12 @@ __device__ __forceinline__ float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ half2v pack2(float a, float b) { return __builtin_convertvector((float2v){a, b}, half2v); }
+// Two numbers into limbs, as elements e and e + 1 (constants where this is used).
+__device__ __forceinline__ void split2(float a, float b, Limbs& x, int e) {
+  const half2v hi = pack2(a, b), lo = pack2(a - (float)hi[0], b - (float)hi[1]);
+  x.hi[e] = hi[0], x.hi[e + 1] = hi[1];
+  x.lo[e] = lo[0], x.lo[e + 1] = lo[1];
+}
 __device__ __forceinline__ float max_of_row(float v) {   // over the four lanes that hold a query row
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
@@ -195,10 +216,13 @@ template <int NR> struct Lds {
   static constexpr int ROWS = NR * 16;
   struct Loop {
     u32x4 q[NR][4][64];                              // queries as they came,
-    half8 qh[NR][4][64], qc[NR][4][64];              // rotated and scaled, and in the codes' order
-    Staged meta[4];                                  // of each wave's page
-    half8 cw[2], mid[2], none[2];                    // counterweights of even and odd k-steps, times -MID, zeros
-    half8 tail[4][TAIL][9];                          // of each wave's 16-bit piece: half of its values' channels
+    half8 qh[NR][2][4][64], qc[NR][2][4][64];        // rotated and scaled, in limbs, and in the codes' order
+    half8 cw[2];                                     // counterweights of even and odd k-steps
+    float top[NR];                                   // the largest channel of a tile's queries
+    union {
+      Staged meta;                                   // of a wave's page,
+      half8 tail[TAIL][9];                           // of its 16-bit piece: half of its values' channels
+    } of_wave[4];
   };
   struct Join {
     float o[4][ROWS][OROW], m[4][ROWS], l[4][ROWS];
@@ -317,13 +341,16 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         fn[0] = load_as<uint32_t>(kn + lane * 4);
       }
     };
-    Staged& meta = lds.loop.meta[wave];
+    Staged& meta = lds.loop.of_wave[wave].meta;
+    float norm_unit;   // what a stored norm is multiplied by
     auto stage_keys = [&] {
-      half8 st, base;
-      fk.step_and_base(ints, C::MID, st, base);
-      base *= lds.loop.cw[lane % 2];
+      half8 st;
+      Limbs zero;
+      fk.step_and_zero(ints, st, zero);
+      const half8 cw = lds.loop.cw[lane % 2];
       meta.k_step[lane] = st;
-      meta.k_base[lane] = base;
+      meta.k_zero[0][lane] = zero.hi * cw;
+      meta.k_zero[1][lane] = zero.lo * cw;
       float v[2];
       if (M32) {
         v[0] = __uint_as_float(fn[0]), v[1] = __uint_as_float(fn[1]);
@@ -331,16 +358,17 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         const half2v h = __builtin_bit_cast(half2v, fn[0]);
         v[0] = (float)h[0], v[1] = (float)h[1];
       }
-      constexpr float unit_of_codes = (float)(1 << (24 - C::BPMIN - kQShift));
-      *reinterpret_cast<float2v*>(&meta.norm[2 * lane]) = (float2v){v[0] * unit_of_codes, v[1] * unit_of_codes};
+      *reinterpret_cast<float2v*>(&meta.norm[2 * lane]) = (float2v){v[0] * norm_unit, v[1] * norm_unit};
     };
     // returns the exponent that the probabilities can carry
     auto stage_values = [&] {
-      half8 st, base;
-      fv.step_and_base(ints, C::MID, st, base);
-      base *= lds.loop.cw[lane / 4 % 2];
+      half8 st;
+      Limbs zero;
+      fv.step_and_zero(ints, st, zero);
+      const half8 cw = lds.loop.cw[lane / 4 % 2];
       meta.v_step[lane] = st;
-      meta.v_base[lane] = base;
+      meta.v_zero[0][lane] = zero.hi * cw;
+      meta.v_zero[1][lane] = zero.lo * cw;
       // the exponent of the largest step (fp16 bits; steps are not negative), bit by bit over the wave
       uint32_t big = 0;
 #pragma unroll
@@ -369,10 +397,12 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
     // ot is channel 32 (m / 4) + 4 ot + m % 4, so that a lane ends with channels 32 q4 .. + 31 of its query row, as
     // the keys' operands have them; its input channels are 32 q4 + 8 kk + e.  The sign of H[i][j] is the parity of
     // i & j, taken apart into what depends on (n, e), on (ot, kk, e) and on (n, q4).
+    float y[8][4];   // channels 32 q4 + 4 ot + r
+    float top_q = 0.0f;
     if (wave < NR) {
       const bool there = row0 + 16 * wave + n < n_new * g;
       const bool rotate = P.c.cfg.rotation == OSCAR_ROTATION_ON;
-      const float mul = there ? P.scale_log2 * (float)(1 << kQShift) * (rotate ? 0.08838834764831845f : 1.0f) : 0.0f;
+      const float mul = P.scale_log2 * (rotate ? 0.08838834764831845f : 1.0f);
       const uint32_t one = bf16 ? 0x3f803f80u : 0x3c003c00u;
       // low two bits: e % 4 against n % 4; top two: q4 against n / 4
       u32x4 signs;
@@ -381,7 +411,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         const uint32_t even = __popc((2 * d) % 4 & n), odd = __popc((2 * d + 1) % 4 & n), top = __popc(q4 & (n >> 2));
         signs[d] = one | (even + top) << 15 & 0x8000u | (odd + top) << 31;
       }
-#pragma unroll 1
+#pragma unroll
       for (int ot = 0; ot < 8; ++ot) {
         float4v acc = {0, 0, 0, 0};
         if (rotate) {
@@ -398,46 +428,63 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
               acc = mfma(__builtin_bit_cast(half8, h), __builtin_bit_cast(half8, q_in[kk]), acc);
           }
         } else {
+          const u32x4 two = q_in[ot / 2];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const uint16_t v = (wave == 0 ? q_row[0] : q_row[NR - 1])[4 * ot + r];
-            acc[r] = bf16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
+            const uint32_t v = two[(ot % 2) * 2 + r / 2] >> (16 * (r % 2)) & 0xffffu;
+            acc[r] = bf16 ? __uint_as_float(v << 16) : __half2float(__ushort_as_half((uint16_t)v));
           }
         }
-        const half2v a = pack2(there ? acc[0] * mul : 0.0f, there ? acc[1] * mul : 0.0f);
-        const half2v c = pack2(there ? acc[2] * mul : 0.0f, there ? acc[3] * mul : 0.0f);
-        uint8_t* at = reinterpret_cast<uint8_t*>(&lds.loop.qh[wave][0][lane]) + (ot / 2) * sizeof(half8) * 64 + (ot % 2) * 8;
-        *reinterpret_cast<uint2*>(at) =
-            make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, c));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          y[ot][r] = there ? acc[r] * mul : 0.0f;
+          top_q = fmaxf(top_q, fabsf(y[ot][r]));
+        }
       }
-      half8 qh[4];
+      top_q = max_of_row(top_q);
+#pragma unroll
+      for (int m = 1; m < 16; m <<= 1) top_q = fmaxf(top_q, __shfl_xor(top_q, m, 64));
+      if (lane == 0) lds.loop.top[wave] = top_q;
+    }
+    __syncthreads();
+    // The queries' scale, one power of two for the block of rows: limbs then hold the largest products to 2^-22 and all
+    // others to 2^-38 of the largest.
+    top_q = lds.loop.top[0];
+    if (NR == 2) top_q = fmaxf(top_q, lds.loop.top[NR - 1]);
+    const int q_exp = min(max(kQTop - 1 + 127 - (int)(__float_as_uint(top_q) >> 23), -100), 100);
+    const float q_unit = __uint_as_float((uint32_t)(127 - q_exp) << 23);
+    norm_unit = (float)(1 << (24 - C::BPMIN)) * q_unit;
+    if (wave < NR) {
+      const float by = __uint_as_float((uint32_t)(127 + q_exp) << 23);
+      Limbs qh[4];
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float v = y[2 * kk + e / 4][e % 4] * by;
+          qh[kk].hi[e] = (_Float16)v;
+          qh[kk].lo[e] = (_Float16)(v - (float)qh[kk].hi[e]);
+        }
         lds.loop.q[wave][kk][lane] = q_in[kk];
-        qh[kk] = lds.loop.qh[wave][kk][lane];
+        lds.loop.qh[wave][0][kk][lane] = qh[kk].hi;
+        lds.loop.qh[wave][1][kk][lane] = qh[kk].lo;
       }
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        half8 qc;   // in the codes' order, with the counterweights of their bit positions
+        Limbs qc;   // in the codes' order, with the counterweights of their bit positions
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int u = slot_index(BITS, kk, e);
-          qc[e] = qh[u / 8][u % 8] * (_Float16)(1.0f / (float)(1 << C::above(kk, e)));
+          const _Float16 w = (_Float16)(1.0f / (float)(1 << C::above(kk, e)));
+          qc.hi[e] = qh[u / 8].hi[u % 8] * w;
+          qc.lo[e] = qh[u / 8].lo[u % 8] * w;
         }
-        lds.loop.qc[wave][kk][lane] = qc;
+        lds.loop.qc[wave][0][kk][lane] = qc.hi;
+        lds.loop.qc[wave][1][kk][lane] = qc.lo;
       }
     }
     // (constants of the page loop wait in LDS: the registers are spoken for)
-    if (lane < 16) meta.v_base[64 + lane] = lane / 4 % 2 == 0 ? C::counterweight(0) : C::counterweight(1);
-    if (lane < 2) {
-      const half8 cw = lane == 0 ? C::counterweight(0) : C::counterweight(1);
-      lds.loop.cw[lane] = cw;   // (the same from every wave)
-      lds.loop.mid[lane] = cw * (_Float16)-C::MID;
-      lds.loop.none[lane] = (half8)(_Float16)0.0f;
-    }
-    __syncthreads();
-    stage_keys();
-    int page_off = stage_values();
+    if (lane < 2) lds.loop.cw[lane] = lane == 0 ? C::counterweight(0) : C::counterweight(1);   // (the same from every wave)
     __syncthreads();
 
     auto scale = [&](int i, float by) {
@@ -505,14 +552,15 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         u32x4 (&a)[4] = ka[j];
         float f[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) f[r] = win ? norm[j][r] * (1.0f / (1 << kQShift)) : P.scale_log2;
+        for (int r = 0; r < 4; ++r) f[r] = win ? norm[j][r] * q_unit : P.scale_log2;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
           float4v acc = {0, 0, 0, 0};
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
             if (win) {
-              acc = mfma(__builtin_bit_cast(half8, a[kk]), lds.loop.qh[i][kk][lane], acc);
+              acc = mfma(__builtin_bit_cast(half8, a[kk]), lds.loop.qh[i][0][kk][lane], acc);
+              acc = mfma(__builtin_bit_cast(half8, a[kk]), lds.loop.qh[i][1][kk][lane], acc);
             } else {
               const u32x4 r = lds.loop.q[i][kk][lane];
               if (bf16)
@@ -536,15 +584,17 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         float by;
         if (__any(top > most[i])) move(i, top, by);
       }
-      half8 pr[NR];
+      Limbs pr[NR];
       const half8 one = (_Float16)(n == 4 ? 1.0f / (1 << UNITS) : 0.0f);
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) pr[i][4 * j + r] = (_Float16)__builtin_amdgcn_exp2f(s[i][j][r] - M[i]);
-        x[i] = mfma(one, pr[i], x[i]);
+          for (int r = 0; r < 4; r += 2)
+            split2(__builtin_amdgcn_exp2f(s[i][j][r] - M[i]), __builtin_amdgcn_exp2f(s[i][j][r + 1] - M[i]), pr[i], 4 * j + r);
+        x[i] = mfma(one, pr[i].hi, x[i]);
+        x[i] = mfma(one, pr[i].lo, x[i]);
       }
       load_values(0);
 #pragma unroll
@@ -565,7 +615,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
             const half8 most = (_Float16)kHalfMax;
             a = __builtin_elementwise_min(__builtin_elementwise_max(__builtin_bit_cast(half8, va[i]), -most), most);
           }
-          lds.loop.tail[wave][8 * i + lane / 8][lane % 8] = a;
+          lds.loop.of_wave[wave].tail[8 * i + lane / 8][lane % 8] = a;
         }
         if (half == 0) load_values(1);
         wave_lds_fence();
@@ -576,19 +626,30 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const auto at = (__attribute__((address_space(3))) short4v*)(reinterpret_cast<_Float16*>(
-                                &lds.loop.tail[wave][16 * j + 4 * q4 + n / 4][0]) + 16 * ct + 4 * (n % 4));
+                                &lds.loop.of_wave[wave].tail[16 * j + 4 * q4 + n / 4][0]) + 16 * ct + 4 * (n % 4));
             const half4v four = __builtin_bit_cast(half4v, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at));
 #pragma unroll
             for (int r = 0; r < 4; ++r) a[4 * j + r] = four[r];
           }
 #pragma unroll
-          for (int i = 0; i < NR; ++i) o[i][4 * half + ct] = mfma(a, pr[i], o[i][4 * half + ct]);
+          for (int i = 0; i < NR; ++i) {
+            o[i][4 * half + ct] = mfma(a, pr[i].hi, o[i][4 * half + ct]);
+            o[i][4 * half + ct] = mfma(a, pr[i].lo, o[i][4 * half + ct]);
+          }
         }
       }
     }
 
     // ---- pages ----
     constexpr float kCodeUnit = 1.0f / (float)(1 << (24 - C::BPMIN));     // of a code in the sums
+    wave_lds_fence();                                                     // (the last piece's values have been read)
+    if (lane < 16) {
+      meta.v_zero[0][64 + lane] = lane / 4 % 2 == 0 ? C::counterweight(0) : C::counterweight(1);
+      meta.v_zero[1][64 + lane] = (half8)(_Float16)0.0f;
+    }
+    stage_keys();
+    int page_off = stage_values();
+    wave_lds_fence();
 #pragma unroll
     for (int i = 0; i < NR; ++i)
 #pragma unroll
@@ -606,49 +667,60 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         }
         off = page_off;
       }
-      half8 pr[NR][4], qd[NR][4];
+      // Logits.  The queries' products with the steps are made for one k-step at a time, for SPAN quarters of the
+      // page's tokens: for all k-steps at once they take registers that are not there.
+      constexpr int SPAN = ONE ? AHEAD : 1;
+      float4v s[NR][8];
       float4v start[NR];
-      // logits and probabilities of 64 tokens at a time
+      int q_lane = lane;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        float4v s[NR][4];
+      for (int w0 = 0; w0 < 4; w0 += SPAN) {
+        const int gk = ONE ? 0 : (w0 * P.g.ngk >> 2) * 16;
+        if (!ONE || w0 == 0) {
+          // what the zero terms add to every token of the group
 #pragma unroll
-        for (int w = 2 * half; w < 2 * half + 2; ++w) {
-          if (!ONE || w == 0) {
-            const int gk = ONE ? 0 : (w * P.g.ngk >> 2) * 16;
+          for (int i = 0; i < NR; ++i) start[i] = (float4v){0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < NR; ++i) start[i] = (float4v){0, 0, 0, 0};
+          for (int kk = 0; kk < 4; ++kk) {
+            const half8 zh = meta.k_zero[0][gk + 4 * q4 + kk], zl = meta.k_zero[1][gk + 4 * q4 + kk];
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              const half8 st = meta.k_step[gk + 4 * q4 + kk], base = meta.k_base[gk + 4 * q4 + kk];
-              const half8 mid = lds.loop.mid[kk % 2];
-#pragma unroll
-              for (int i = 0; i < NR; ++i) {
-                const half8 qc = lds.loop.qc[i][kk][lane];
-                qd[i][kk] = qc * st;
-                start[i] = mfma(base, qc, start[i]);
-                start[i] = mfma(mid, qd[i][kk], start[i]);
-              }
+            for (int i = 0; i < NR; ++i) {
+              const half8 qh = lds.loop.qc[i][0][kk][q_lane], ql = lds.loop.qc[i][1][kk][q_lane];
+              start[i] = mfma(zh, qh, start[i]);
+              start[i] = mfma(zh, ql, start[i]);
+              start[i] = mfma(zl, qh, start[i]);
             }
-#pragma unroll
-            for (int i = 0; i < NR; ++i) start[i] *= 1.0f / (float)(1 << (24 - C::BPMAX));
           }
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              const half8 a = C::operand(kc[w] + j * BITS, kk);
-#pragma unroll
-              for (int i = 0; i < NR; ++i) {
-                float4v& acc = s[i][2 * (w % 2) + j];
-                acc = mfma(a, qd[i][kk], kk == 0 ? start[i] : acc);
-              }
-            }
+          for (int i = 0; i < NR; ++i) start[i] *= 1.0f / (float)(1 << (24 - C::BPMAX));
         }
-        // logits above M, less the bit position's exponent; what is no page has none
-        float top[NR];
+        asm("" : "+v"(q_lane));   // (read again: kept, the queries fill the registers)
 #pragma unroll
-        for (int i = 0; i < NR; ++i) top[i] = -INFINITY;
+        for (int kk = 0; kk < 4; ++kk) {
+          const half8 st = meta.k_step[gk + 4 * q4 + kk];
+          Limbs qd[NR];
+#pragma unroll
+          for (int i = 0; i < NR; ++i) qd[i] = times(lds.loop.qc[i][0][kk][q_lane], lds.loop.qc[i][1][kk][q_lane], st);
+#pragma unroll
+          for (int t = 2 * w0; t < 2 * (w0 + SPAN); ++t) {
+            const half8 a = C::operand(kc[t / 2] + t % 2 * BITS, kk);
+#pragma unroll
+            for (int i = 0; i < NR; ++i) s[i][t] = mfma(a, qd[i].hi, kk == 0 ? start[i] : s[i][t]);
+#pragma unroll
+            for (int i = 0; i < NR; ++i) s[i][t] = mfma(a, qd[i].lo, s[i][t]);
+          }
+        }
+        if (AHEAD < 4 && w0 == 0 && SPAN == AHEAD) load_codes(pool_of(P.c.v_codes, code_shift, pg0), v_at, vc, AHEAD, 4);
+        if (AHEAD < 4 && w0 == 1 && SPAN == 1) load_codes(pool_of(P.c.v_codes, code_shift, pg0), v_at, vc, AHEAD, 4);
+      }
+      load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, 0, AHEAD);
+      fetch_meta(pg1);
+      // logits above M, less the bit position's exponent; what is no page has none
+      float top[NR];
+#pragma unroll
+      for (int i = 0; i < NR; ++i) top[i] = -INFINITY;
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float4v nm = *reinterpret_cast<const float4v*>(&meta.norm[(4 * r + q4) * 8 + 4 * half]);
@@ -656,80 +728,71 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
           for (int i = 0; i < NR; ++i)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              s[i][t][r] = fmaf(s[i][t][r], nm[t], -(M[i] + ((float)C::above(r, 4 * half + t) + gone)));
-              top[i] = fmaxf(top[i], s[i][t][r]);
+              s[i][4 * half + t][r] = fmaf(s[i][4 * half + t][r], nm[t], -(M[i] + ((float)C::above(r, 4 * half + t) + gone)));
+              top[i] = fmaxf(top[i], s[i][4 * half + t][r]);
             }
         }
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          if (!__any(top[i] > most[i])) continue;
-          float most_of = -INFINITY, by;
+      for (int i = 0; i < NR; ++i) {
+        if (!__any(top[i] > most[i])) continue;
+        float most_of = -INFINITY, by;
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) most_of = fmaxf(most_of, s[i][t][r] + (float)C::above(r, 4 * half + t));
-          const float shift = move(i, most_of, by);
-          if (half == 1) {
+          for (int t = 0; t < 8; ++t) most_of = fmaxf(most_of, s[i][t][r] + (float)C::above(r, t));
+        const float shift = move(i, most_of, by);
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) pr[i][kk] *= (_Float16)by;
-          }
-#pragma unroll
-          for (int t = 0; t < 4; ++t) s[i][t] += shift;
-        }
-#pragma unroll
-        for (int i = 0; i < NR; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int t = 0; t < 4; t += 2) {
-              const half2v p = pack2(__builtin_amdgcn_exp2f(s[i][t][r]), __builtin_amdgcn_exp2f(s[i][t + 1][r]));
-              pr[i][r][4 * half + t] = p[0];
-              pr[i][r][4 * half + t + 1] = p[1];
-            }
-        if (half == 0) load_codes(pool_of(P.c.v_codes, code_shift, pg0), v_at, vc, AHEAD, 4);
+        for (int t = 0; t < 8; ++t) s[i][t] += shift;
       }
-      load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, 0, AHEAD);
-      fetch_meta(pg1);
+      Limbs pr[NR][4];
+#pragma unroll
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int t = 0; t < 8; t += 2)
+            split2(__builtin_amdgcn_exp2f(s[i][t][r]), __builtin_amdgcn_exp2f(s[i][t + 1][r]), pr[i][r], t);
 
       // values
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        const half8 base = meta.v_base[gb + 4 * kk];
+        const half8 zh = meta.v_zero[0][gb + 4 * kk], zl = meta.v_zero[1][gb + 4 * kk];
 #pragma unroll
-        for (int i = 0; i < NR; ++i) x[i] = mfma(base, pr[i][kk], x[i]);
+        for (int i = 0; i < NR; ++i) {
+          x[i] = mfma(zh, pr[i][kk].hi, x[i]);
+          x[i] = mfma(zh, pr[i][kk].lo, x[i]);
+          x[i] = mfma(zl, pr[i][kk].hi, x[i]);
+        }
       }
-      half8 pd[NR][4];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        // (a group of several of these shares its products; without a branch they cost less than with one)
         const int gv = w * P.g.ngv >> 2;
-        const half8* mids = n == gv && (w * P.g.ngv & 3) == 0 ? lds.loop.mid : lds.loop.none;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
           const half8 st = meta.v_step[gv * 16 + 4 * kk + q4];
+          Limbs pd[NR];
 #pragma unroll
-          for (int i = 0; i < NR; ++i) {
-            pd[i][kk] = pr[i][kk] * st;
-            x[i] = mfma(mids[kk % 2], pd[i][kk], x[i]);
-          }
-        }
+          for (int i = 0; i < NR; ++i) pd[i] = times(pr[i][kk].hi, pr[i][kk].lo, st);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
+          for (int j = 0; j < 2; ++j) {
             const half8 a = C::operand(vc[w] + j * BITS, kk);
 #pragma unroll
-            for (int i = 0; i < NR; ++i) o[i][2 * w + j] = mfma(a, pd[i][kk], o[i][2 * w + j]);
+            for (int i = 0; i < NR; ++i) o[i][2 * w + j] = mfma(a, pd[i].hi, o[i][2 * w + j]);
+#pragma unroll
+            for (int i = 0; i < NR; ++i) o[i][2 * w + j] = mfma(a, pd[i].lo, o[i][2 * w + j]);
           }
+        }
         if (w == 1) load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, AHEAD, 4);
       }
       load_codes(pool_of(P.c.v_codes, code_shift, pg1), v_at, vc, 0, AHEAD);
+      wave_lds_fence();
       stage_keys();
       page_off = stage_values();
+      wave_lds_fence();
       pg0 = pg1;
       pg1 = page_of(page + 2 * step, entry);
     }
-    // back to numbers: codes' unit, mean terms of each channel's value group
+    // back to numbers: codes' unit, zero terms of each channel's value group
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       x[i] *= (float)(1 << UNITS);
