@@ -25,8 +25,13 @@
 // themselves: for the keys what a tile's sums start from, for the values one extra tile, whose other rows are the rows'
 // sums.  With one limb, half a step (2^-11) each for Q, Q Delta, P, P Delta and the zero terms, fp16 outputs were off by
 // 4e-4 .. 3e-3 of their length, where their own rounding is 2e-4; the second limb costs 1.6 times the time.
-// The probabilities are scaled by 2^7 .. 2^15 (less where a value step of 1 or more would carry P Delta past the fp16
-// range).  Sums, maxima and outputs are fp32.
+// Everything that meets a limb is first brought to fp16's middle by powers of two, in both directions, and the fp32 sums
+// carry the exponents: queries by the block of rows' largest channel, a page's key steps and zero terms by its largest,
+// its value steps and zero terms by the largest of their value group so far.  The probabilities are stored below 2^15.
+// So a product keeps its 22 bits down to 2^-28 of the largest the group can have, and a step its own 11 down to 2^-14 of
+// the largest step; an unscaled P Delta lost 0.3 .. 15 % of what values of 1e-2 .. 3e-4 add beside a token that takes the
+// softmax without values.  16-bit values of the window and of new tokens: fp16 ones as they are, bf16 ones as bf16
+// against probabilities of three bf16 limbs, so that they keep their range.  Sums, maxima and outputs are fp32.
 //
 // What bounds it: the issue of instructions.  A page costs a wave with two tiles 304 matrix and about 1200 vector
 // instructions, and the two do not overlap across the waves of a SIMD (measured: the time is the sum of both).  8 new
@@ -44,6 +49,7 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float2v __attribute__((ext_vector_type(2)));
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // (said to be in device memory: through pointers of which the compiler does not know that, loads are counted with
@@ -54,6 +60,7 @@ template <typename T> __device__ __forceinline__ T load_as(DevicePtr p) {
 }
 
 constexpr float kHalfMax = 65504.0f;
+constexpr float kBf16Most = 1152921504606846976.0f;   // 2^60: bf16 values beyond it count as that
 constexpr int kQTop = 14;            // the largest channel of a block of queries is scaled to below 2^14
 
 // What loads of a page that is none take: its codes and parameters are zeros, and nothing that follows is NaN.
@@ -83,7 +90,7 @@ struct DraftParams {
 };
 
 template <int BITS> struct Codes {
-  static constexpr int BPMIN = BITS == 2 ? 4 : 2, BPMAX = BITS == 2 ? 8 : 6;
+  static constexpr int BPMIN = BITS == 2 ? 4 : 2;
   // the operand of k-step kk from a chunk
   __device__ static __forceinline__ half8 operand(const uint32_t* w, int kk) {
     u32x4 r;
@@ -104,11 +111,11 @@ template <int BITS> struct Codes {
   }
   // what an element's bit position is above the lowest
   __host__ __device__ static constexpr int above(int kk, int e) { return slot_bitpos(BITS, kk, e) - BPMIN; }
-  // 2^(above - (BPMAX - BPMIN)), the other operand's counterweight for what is no code (kk counts modulo 2)
+  // 2^above, the other operand's counterweight for what is no code (kk counts modulo 2)
   __device__ static __forceinline__ half8 counterweight(int kk) {
     half8 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (_Float16)(1.0f / (float)(1 << (BPMAX - BPMIN - above(kk, e))));
+    for (int e = 0; e < 8; ++e) r[e] = (_Float16)(float)(1 << above(kk, e));
     return r;
   }
 };
@@ -137,6 +144,7 @@ struct Staged {
 // whole state (8 new tokens over 8 x 32K: 71 us, 75 with a reference that follows at once).
 constexpr float kSlack = 8.0f, kNone = -3e38f;
 constexpr int kOff = 7;          // exponent of a probability at its reference: kOff + kSlack stay inside fp16
+__device__ __forceinline__ float exp2i(int x) { return __uint_as_float((uint32_t)(127 + x) << 23); }   // |x| < 127
 // What a lane holds of the metadata of a page to come: 8 steps and 8 zeros of the keys or of the values.
 template <bool M32> struct Fetched {
   u32x4 a[M32 ? 2 : 1], b[M32 ? 2 : 1];
@@ -151,37 +159,83 @@ template <bool M32> struct Fetched {
     if (M32) return __uint_as_float(x[e / 4][e % 4]);
     return (float)__builtin_bit_cast(half8, x[0])[e];
   }
-  // Step and zero term, x = step c + zero: zero = -step z for integer zero-points (ints = 1), z itself for float ones
-  // (ints = 0), as one form: nothing here branches.
-  __device__ __forceinline__ void step_and_zero(float ints, half8& step, Limbs& zero) const {
+  // x with all eight steps below 2^x (within its limits) and all zero terms below 2^(x + 11): times 2^-x, and with their
+  // counterweights (2^4 at most), fp16 holds them.
+  __device__ __forceinline__ int exponent(float ints) const {
+    if (M32) {
+      float s = 0.0f, t = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s = fmaxf(s, number(a, e));
+        t = fmaxf(t, fabsf(zero_term(ints, number(a, e), number(b, e))));
+      }
+      return min(max(max((int)(__float_as_uint(s) >> 23), (int)(__float_as_uint(t) >> 23) - 11) - 126, -40), 100);
+    }
+    // fp16 bits as logarithms: those of a product are the factors' added, and one more at most
+    const bool whole = ints != 0.0f;
+    const uint32_t with = whole ? 0xffffffffu : 0u, less = whole ? 0x64006400u : 0x2c002c00u;   // 25 and 11 in the exponent
+    ushort2v most = {0, 0};
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const uint32_t st = a[0][d], z = b[0][d] & 0x7fff7fffu, s = st & with;   // (a bit cast of a vector's element takes its first)
+      most = __builtin_elementwise_max(most, __builtin_bit_cast(ushort2v, st));
+      most = __builtin_elementwise_max(most, __builtin_elementwise_sub_sat(__builtin_bit_cast(ushort2v, z) + __builtin_bit_cast(ushort2v, s),
+                                                                           __builtin_bit_cast(ushort2v, less)));
+    }
+    return (max((int)most[0], (int)most[1]) >> 10) - 14;
+  }
+  __device__ __forceinline__ static float zero_term(float ints, float s, float z) { return z * fmaf(-(s + 1.0f), ints, 1.0f); }
+  // Step and zero term times 2^-x; a number is step c + zero: zero = -step z for integer zero-points (ints = 1), z itself
+  // for float ones (ints = 0), as one form: nothing here branches.
+  __device__ __forceinline__ void step_and_zero(float ints, int x, half8& step, Limbs& zero) const {
+    const float by = exp2i(-x);
     if (M32) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float s = number(a, e), z = number(b, e);
-        step[e] = (_Float16)fminf(s, kHalfMax);
-        const float base = __builtin_amdgcn_fmed3f(z * fmaf(-(s + 1.0f), ints, 1.0f), -kHalfMax, kHalfMax);
-        zero.hi[e] = (_Float16)base;
-        zero.lo[e] = (_Float16)(base - (float)zero.hi[e]);
+        const float t = __builtin_amdgcn_fmed3f(zero_term(ints, s, z) * by, -kHalfMax, kHalfMax);   // (infinite ones)
+        step[e] = (_Float16)fminf(s * by, kHalfMax);
+        zero.hi[e] = (_Float16)t;
+        zero.lo[e] = (_Float16)(t - (float)zero.hi[e]);
       }
     } else {
-      step = __builtin_bit_cast(half8, a[0]);
-      const half8 z = __builtin_bit_cast(half8, b[0]), most = (_Float16)kHalfMax;
+      const half8 z = __builtin_bit_cast(half8, b[0]);
       // (registers: as constants or halves of one they are taken apart into single operations)
-      uint32_t two[2] = {__builtin_bit_cast(uint32_t, (half2v)(_Float16)ints),
-                         __builtin_bit_cast(uint32_t, (half2v)(_Float16)(1.0f - 2.0f * ints))};
-      asm("" : "+v"(two[0]), "+v"(two[1]));
+      uint32_t two[3] = {__builtin_bit_cast(uint32_t, (half2v)(_Float16)by),
+                         __builtin_bit_cast(uint32_t, (half2v)(_Float16)ints),
+                         __builtin_bit_cast(uint32_t, (half2v)(_Float16)(ints != 0.0f ? -1.0f : by))};
+      asm("" : "+v"(two[0]), "+v"(two[1]), "+v"(two[2]));
       auto splat = [](uint32_t w) { return __builtin_bit_cast(half8, (u32x4){w, w, w, w}); };
       const half8 one = (_Float16)1.0f;
-      const half8 f = fma8(step, splat(two[0]), one - splat(two[0])), m = z * splat(two[1]);   // step or 1, -z or z
-      zero.hi = __builtin_elementwise_min(__builtin_elementwise_max(f * m, -most), most);
+      step = __builtin_bit_cast(half8, a[0]) * splat(two[0]);
+      const half8 f = fma8(step, splat(two[1]), one - splat(two[1])), m = z * splat(two[2]);   // step or 1, -z or z 2^-x
+      zero.hi = f * m;
       zero.lo = fma8(f, m, -zero.hi);
-      zero.lo = __builtin_elementwise_min(__builtin_elementwise_max(zero.lo, -most), most);
     }
   }
 };
 
 __device__ __forceinline__ float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float4v mfma(bf16x8 a, bf16x8 b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// The largest of the 16 lanes of a row, in all of them.
+template <int CTRL> __device__ __forceinline__ int row_max_step(int v) {
+  return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ int row16_max(int v) {
+  v = row_max_step<0x128>(v);   // row_ror:8, 4, 2, 1
+  v = row_max_step<0x124>(v);
+  v = row_max_step<0x122>(v);
+  return row_max_step<0x121>(v);
+}
+__device__ __forceinline__ int max_of_rows(int v) {   // over the four rows
+  auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max((int)a[0], (int)a[1]);
+  a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max((int)a[0], (int)a[1]);
 }
 __device__ __forceinline__ half2v pack2(float a, float b) { return __builtin_convertvector((float2v){a, b}, half2v); }
 // Two numbers into limbs, as elements e and e + 1 (constants where this is used).
@@ -239,7 +293,6 @@ template <int BITS, bool M32, bool ONE, int NR>
 __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int row0) {
   using C = Codes<BITS>;
   constexpr int ROWS = NR * 16;
-  constexpr int UNITS = C::BPMAX - C::BPMIN;         // log2 of what the counterweights leave in the extra tile
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, q4 = lane >> 4;
@@ -279,7 +332,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
 
   float4v o[NR][8];   // channels 16 ct + 4 q4 + r of row n, in units of the codes once pages have begun
   float4v x[NR];      // row 4 q4 + r of the extra tile: 0 .. 3 the value groups' mean terms, 4 the row's sum
-  float M[NR];        // the row's reference, log2 units, less the exponent `off` its probability has there
+  float M[NR];        // the row's reference, log2 units, less the exponent kOff its probability has there
   float most[NR];     // how far a logit may be above M; kNone before the row's first token
 #pragma unroll
   for (int i = 0; i < NR; ++i) {
@@ -289,7 +342,6 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
     M[i] = 0.0f;
     most[i] = kNone;
   }
-  int off = kOff;
 
   if (rows > 0) {
     const int last_t = P.by_group.of(row0 + rows - 1);                   // last new token any row here sees
@@ -346,7 +398,9 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
     auto stage_keys = [&] {
       half8 st;
       Limbs zero;
-      fk.step_and_zero(ints, st, zero);
+      const int x_keys = max_of_rows(row16_max(fk.exponent(ints)));   // of the page
+      fk.step_and_zero(ints, x_keys, st, zero);
+      const float unit = norm_unit * exp2i(x_keys);
       const half8 cw = lds.loop.cw[lane % 2];
       meta.k_step[lane] = st;
       meta.k_zero[0][lane] = zero.hi * cw;
@@ -358,33 +412,19 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         const half2v h = __builtin_bit_cast(half2v, fn[0]);
         v[0] = (float)h[0], v[1] = (float)h[1];
       }
-      *reinterpret_cast<float2v*>(&meta.norm[2 * lane]) = (float2v){v[0] * norm_unit, v[1] * norm_unit};
+      *reinterpret_cast<float2v*>(&meta.norm[2 * lane]) = (float2v){v[0] * unit, v[1] * unit};
     };
-    // returns the exponent that the probabilities can carry
-    auto stage_values = [&] {
+    // Values are summed in units of 2^x, x the lane's value group's largest exponent so far (of lane / 16).
+    auto stage_values = [&](int x_before) {
       half8 st;
       Limbs zero;
-      fv.step_and_zero(ints, st, zero);
+      const int x_now = max(x_before, row16_max(fv.exponent(ints)));
+      fv.step_and_zero(ints, x_now, st, zero);
       const half8 cw = lds.loop.cw[lane / 4 % 2];
       meta.v_step[lane] = st;
       meta.v_zero[0][lane] = zero.hi * cw;
       meta.v_zero[1][lane] = zero.lo * cw;
-      // the exponent of the largest step (fp16 bits; steps are not negative), bit by bit over the wave
-      uint32_t big = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t two = __builtin_bit_cast(u32x4, st)[e];
-        big = max(big, max(two & 0xffffu, two >> 16));
-      }
-      uint64_t among = ~0ull;
-      int exponent = 0;
-#pragma unroll
-      for (int bit = 14; bit >= 10; --bit) {
-        const uint64_t have = __ballot(big >> bit & 1) & among;
-        among = have ? have : among;
-        exponent |= have ? 1 << (bit - 10) : 0;
-      }
-      return kOff - max(exponent - 14, 0);
+      return x_now;
     };
 
     Page pg0 = page_of(page, entry0), pg1 = page_of(page + step, entry1);
@@ -497,13 +537,13 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
     // returns what comes on top of logits above M, and leaves its power of two in `by`.
     auto move = [&](int i, float top, float& by) {
       const bool none = most[i] == kNone;
-      const float to = fmaxf(none ? -INFINITY : M[i] + (float)off, ceilf(max_of_row(top) + M[i]));
-      const float Mn = to == -INFINITY ? 0.0f : to - (float)off;
+      const float to = fmaxf(none ? -INFINITY : M[i] + (float)kOff, ceilf(max_of_row(top) + M[i]));
+      const float Mn = to == -INFINITY ? 0.0f : to - (float)kOff;
       const float shift = M[i] - Mn;
       by = none ? 0.0f : __builtin_amdgcn_exp2f(shift);
       scale(i, by);
       M[i] = Mn;
-      most[i] = to == -INFINITY ? kNone : (float)off + kSlack;
+      most[i] = to == -INFINITY ? kNone : (float)kOff + kSlack;
       return shift;
     };
 
@@ -584,17 +624,37 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         float by;
         if (__any(top > most[i])) move(i, top, by);
       }
-      Limbs pr[NR];
-      const half8 one = (_Float16)(n == 4 ? 1.0f / (1 << UNITS) : 0.0f);
+      // Probabilities: two fp16 limbs beside fp16 values, three bf16 ones beside bf16 values, whose range is an fp32's.
+      half8 pr[NR][3];   // (16 bits of either type)
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
+        float p[8];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; r += 2)
-            split2(__builtin_amdgcn_exp2f(s[i][j][r] - M[i]), __builtin_amdgcn_exp2f(s[i][j][r + 1] - M[i]), pr[i], 4 * j + r);
-        x[i] = mfma(one, pr[i].hi, x[i]);
-        x[i] = mfma(one, pr[i].lo, x[i]);
+          for (int r = 0; r < 4; ++r) p[4 * j + r] = __builtin_amdgcn_exp2f(s[i][j][r] - M[i]);
+        if (bf16) {
+          const bf16x8 one = (__bf16)(n == 4 ? 1.0f : 0.0f);
+#pragma unroll
+          for (int limb = 0; limb < 3; ++limb) {
+            bf16x8 b;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              b[e] = (__bf16)p[e];
+              p[e] -= (float)b[e];
+            }
+            x[i] = mfma(one, b, x[i]);
+            pr[i][limb] = __builtin_bit_cast(half8, b);
+          }
+        } else {
+          const half8 one = (_Float16)(n == 4 ? 1.0f : 0.0f);
+          Limbs two;
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) split2(p[e], p[e + 1], two, e);
+          x[i] = mfma(one, two.hi, x[i]);
+          x[i] = mfma(one, two.lo, x[i]);
+          pr[i][0] = two.hi, pr[i][1] = pr[i][2] = two.lo;
+        }
       }
       load_values(0);
 #pragma unroll
@@ -604,13 +664,14 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         for (int i = 0; i < 4; ++i) {
           half8 a;
           if (bf16) {
+            u32x4 w;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const half2v two =
-                  pack2(__builtin_amdgcn_fmed3f(__uint_as_float(va[i][e] << 16), -kHalfMax, kHalfMax),
-                        __builtin_amdgcn_fmed3f(__uint_as_float(va[i][e] & 0xffff0000u), -kHalfMax, kHalfMax));
-              a[2 * e] = two[0], a[2 * e + 1] = two[1];
+              const float lo = __builtin_amdgcn_fmed3f(__uint_as_float(va[i][e] << 16), -kBf16Most, kBf16Most);
+              const float hi = __builtin_amdgcn_fmed3f(__uint_as_float(va[i][e] & 0xffff0000u), -kBf16Most, kBf16Most);
+              w[e] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
             }
+            a = __builtin_bit_cast(half8, w);
           } else {
             const half8 most = (_Float16)kHalfMax;
             a = __builtin_elementwise_min(__builtin_elementwise_max(__builtin_bit_cast(half8, va[i]), -most), most);
@@ -633,8 +694,14 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
           }
 #pragma unroll
           for (int i = 0; i < NR; ++i) {
-            o[i][4 * half + ct] = mfma(a, pr[i].hi, o[i][4 * half + ct]);
-            o[i][4 * half + ct] = mfma(a, pr[i].lo, o[i][4 * half + ct]);
+            float4v& acc = o[i][4 * half + ct];
+            if (bf16) {
+#pragma unroll
+              for (int limb = 0; limb < 3; ++limb) acc = mfma(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, pr[i][limb]), acc);
+            } else {
+              acc = mfma(a, pr[i][0], acc);
+              acc = mfma(a, pr[i][1], acc);
+            }
           }
         }
       }
@@ -648,24 +715,34 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
       meta.v_zero[1][64 + lane] = (half8)(_Float16)0.0f;
     }
     stage_keys();
-    int page_off = stage_values();
+    int x_page = stage_values(-100), x_sum = x_page;   // of the page to come, of the sums
     wave_lds_fence();
+    // of the group that channels 32 w .. are in
+    auto of_group = [&](int v, int w) { return __builtin_amdgcn_readlane(v, 16 * (w * P.g.ngv >> 2)); };
 #pragma unroll
     for (int i = 0; i < NR; ++i)
 #pragma unroll
-      for (int ct = 0; ct < 8; ++ct) o[i][ct] *= kCodeUnit;
+      for (int ct = 0; ct < 8; ++ct) o[i][ct] *= kCodeUnit * exp2i(-of_group(x_sum, ct / 2));
     const int gb = (n == 4 ? 64 : min(n, P.g.ngv - 1) * 16) + q4;         // this lane's row of the extra tile
     for (; page < pages; page += step) {
       const int entry = entry_of(page + 2 * step);
       const float gone = pg0.held ? 0.0f : INFINITY;   // what is no page: its numbers are finite, its probabilities zeros
-      if (page_off < off) [[unlikely]] {
-        // the page's value steps are larger than any before: the exponent gives way
+      if (__any(x_page != x_sum)) [[unlikely]] {   // the page's value steps are larger than any before
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          scale(i, __builtin_amdgcn_exp2f((float)(page_off - off)));
-          if (most[i] != kNone) M[i] += (float)(off - page_off), most[i] = (float)page_off + kSlack;
+        for (int w = 0; w < 4; ++w) {
+          const float by = exp2i(max(of_group(x_sum, w) - of_group(x_page, w), -126));
+#pragma unroll
+          for (int i = 0; i < NR; ++i) o[i][2 * w] *= by, o[i][2 * w + 1] *= by;
         }
-        off = page_off;
+        // (rows 0 .. 3 of the extra tile: groups 0 .. 3)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * min(r, P.g.ngv - 1);
+          const int by = __builtin_amdgcn_readlane(x_sum, row) - __builtin_amdgcn_readlane(x_page, row);
+#pragma unroll
+          for (int i = 0; i < NR; ++i) x[i][r] *= q4 == 0 ? exp2i(max(by, -126)) : 1.0f;
+        }
+        x_sum = x_page;
       }
       // Logits.  The queries' products with the steps are made for one k-step at a time, for SPAN quarters of the
       // page's tokens: for all k-steps at once they take registers that are not there.
@@ -692,7 +769,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
             }
           }
 #pragma unroll
-          for (int i = 0; i < NR; ++i) start[i] *= 1.0f / (float)(1 << (24 - C::BPMAX));
+          for (int i = 0; i < NR; ++i) start[i] *= kCodeUnit;
         }
         asm("" : "+v"(q_lane));   // (read again: kept, the queries fill the registers)
 #pragma unroll
@@ -787,15 +864,14 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
       load_codes(pool_of(P.c.v_codes, code_shift, pg1), v_at, vc, 0, AHEAD);
       wave_lds_fence();
       stage_keys();
-      page_off = stage_values();
+      x_page = stage_values(x_sum);
       wave_lds_fence();
       pg0 = pg1;
       pg1 = page_of(page + 2 * step, entry);
     }
-    // back to numbers: codes' unit, zero terms of each channel's value group
+    // back to numbers: codes' unit, exponents, zero terms of each channel's value group
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-      x[i] *= (float)(1 << UNITS);
       float zb[4];   // of channels 32 w .. 32 w + 31
 #pragma unroll
       for (int gv = 0; gv < 4; ++gv) zb[gv] = __shfl(x[i][gv], n, 64);
@@ -803,7 +879,8 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
       if (P.g.ngv < 4) zb[1] = zb[0];
       if (P.g.ngv == 1) zb[3] = zb[2] = zb[0];
 #pragma unroll
-      for (int ct = 0; ct < 8; ++ct) o[i][ct] = o[i][ct] * (float)(1 << (24 - C::BPMIN)) + zb[ct / 2];
+      for (int ct = 0; ct < 8; ++ct)
+        o[i][ct] = (o[i][ct] * (float)(1 << (24 - C::BPMIN)) + zb[ct / 2]) * exp2i(of_group(x_sum, ct / 2));
     }
     __syncthreads();
   }

@@ -128,3 +128,73 @@ def test_a_lost_token_shows(n, at):
     check(c, *x, "bf16")
     lost, tol = attention(c, *(y.double().cpu().numpy() for y in x), None, "bf16", leave_out=at)
     assert (np.abs(run(c, *x) - lost) > tol).any()
+
+
+def appended(k, v, cfg, eager=True):
+    """A cache holding k and v [batch, tokens, kv heads, 128] after one prompt."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    c = ob.Cache(cfg, k.shape[0], k.shape[1] // 128 + 1)
+    dt = torch_type({v: n for n, v in DT.items()}[cfg.io_dtype])
+    ob.quantize_append(c, *(torch.from_numpy(x.astype(np.float32)).to(dt).cuda() for x in (k, v)), eager=eager, max_seq_len_hint=0)
+    return c
+
+
+@pytest.mark.parametrize("gain", [1e-2, 1e-3, 3e-4])
+@pytest.mark.parametrize("sharp", [12.0, 15.0])
+@pytest.mark.parametrize("bits,vg", [(2, 32), (4, 128)])
+def test_small_values_beside_a_token_that_takes_the_softmax(bits, vg, sharp, gain):
+    """What the other tokens have left of the softmax keeps its bits, though their products with small value steps lie
+    2^15 and more below the dominant token's probability; values of pages, window and new tokens."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(int(sharp))
+    n, T = 1700, 2
+    k, v = (rng.standard_normal((1, n, 2, 128)) for _ in range(2))
+    d = rng.standard_normal((2, 128))
+    d /= np.linalg.norm(d, axis=-1, keepdims=True)
+    k[0, 5] = sharp * d
+    v *= gain
+    v[0, 5] *= 1e-3
+    c = appended(k, v, ob.Config(2, 2, bits=bits, v_group=vg))
+    q = np.sqrt(128) * d + 0.1 * rng.standard_normal((1, T, 2, 128))
+    dev = lambda x: torch.from_numpy(x.astype(np.float32)).bfloat16().cuda()
+    kn, vn = rng.standard_normal((1, T, 2, 128)), gain * rng.standard_normal((1, T, 2, 128))
+    check(c, dev(q), dev(kn), dev(vn), "bf16", splits=(1, 2))
+
+
+@pytest.mark.parametrize("growth", [3.0, 1 / 3.0])
+@pytest.mark.parametrize("io,vg", [("bf16", 32), ("f16", 64)])
+def test_values_that_grow_and_shrink_along_the_sequence(io, vg, growth):
+    """Each page's values are three times (a third of) the page's before, and the groups' sizes differ by 2^9: what is
+    summed is rescaled on the way, group by group."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(7)
+    n, T = 1500, 3
+    k, v = (rng.standard_normal((1, n, 1, 128)) for _ in range(2))
+    v *= (growth ** (np.arange(n) // 128 - 6.0))[None, :, None, None] * (2.0 ** (-3 * (np.arange(128) // vg)))
+    c = appended(k, v, ob.Config(4, 1, v_group=vg, io_dtype=DT[io]))
+    x = new_tokens(c, T, io, vmul=0.1)
+    check(c, *x, io, splits=(1, 3))
+
+
+@pytest.mark.parametrize("kmul", [1e-3, 200.0])
+@pytest.mark.parametrize("bits", [2, 4])
+def test_keys_and_queries_of_opposite_sizes(bits, kmul):
+    """Keys without a norm (their steps are their own size), and queries that bring the logits back to 1."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(9)
+    k, v = rng.standard_normal((2, 400, 2, 128)) * kmul, rng.standard_normal((2, 400, 2, 128))
+    c = appended(k, v, ob.Config(4, 2, bits=bits, io_dtype=ob.F16, scale_mode=ob.SCALE_NONE))
+    q, kn, vn = new_tokens(c, 3, "f16", qmul=1 / kmul)
+    check(c, q, kn, vn, "f16")
+
+
+def test_large_new_and_window_values_in_bf16():
+    """bf16 values beyond fp16's range are what they are."""
+    from paper_2605_19660_amd import binding as ob
+    c = filled_cache([40, 300], hq=4, hk=2, gain=3e5, meta="f32")
+    q, k, v = new_tokens(c, 5, "bf16", vmul=1e7)
+    check(c, q, k, v, "bf16", splits=(1, 2))
