@@ -437,11 +437,14 @@ int oscar_cache_read(const oscar_cache *cache, const int32_t *starts, int32_t T,
  *   workspace    : at least oscar_draft_workspace_bytes(...), 8-byte aligned; NULL where that is 0
  *                  (one split).  Calls that share one must be ordered.
  * io_dtype BF16 or F16 (OSCAR_ERR_UNSUPPORTED for F32); every other field of the configuration as
- * for oscar_decode_attn.  Operands of the matrix products are fp16 (steps, zero terms,
- * probabilities; values and zero terms beyond its range, infinities and NaNs among the values of
- * new tokens, count as +-65504; a query is finite, and 6 softmax_scale |H q| / sqrt(128), times the
- * largest key step of a channel, stays inside it), sums are fp32.  The same call gives the same bits
- * every time.
+ * for oscar_decode_attn, and so is the precision: what is rounded before a matrix product (queries,
+ * their products with the key steps, probabilities, their products with the value steps, zero terms,
+ * fp32 steps) is carried in two fp16 limbs, 22 bits, and sums are fp32.  Powers of two taken out
+ * first keep that whatever the size of values, keys and queries: a step keeps all its bits from
+ * 2^-14 of the largest of its page (keys) or value group (values) on; a group of equal numbers has
+ * step 1.  fp16 values of the window and of new tokens beyond +-65504, infinities and NaNs among
+ * them, count as +-65504, bf16 ones beyond 2^60 as +-2^60.  Queries and logits are finite.  The same
+ * call gives the same bits every time.
  * q, k_new, v_new, out: 16-byte aligned.  One launch, two with several splits. */
 int32_t oscar_draft_auto_splits(const oscar_config *cfg, int32_t batch, int32_t T, int32_t max_seq_len);
 size_t oscar_draft_workspace_bytes(const oscar_config *cfg, int32_t batch, int32_t T, int32_t num_splits);

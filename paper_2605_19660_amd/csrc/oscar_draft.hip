@@ -125,19 +125,22 @@ struct Limbs {
   half8 hi, lo;
 };
 __device__ __forceinline__ half8 fma8(half8 a, half8 b, half8 c) { return __builtin_elementwise_fma(a, b, c); }
-// The product of two limbs and a factor: its high limb, the rest of that product, which fp16 holds exactly, and the low
-// limb's product.
-__device__ __forceinline__ Limbs times(half8 hi, half8 lo, half8 by) {
-  const half8 h = hi * by;
-  return {h, fma8(lo, by, fma8(hi, by, -h))};
+// The product of two numbers in limbs: of the high limbs its high limb and the rest, which fp16 holds exactly, and the
+// products of a high and a low limb.  FINE: the factor has a low limb (fp16 steps have none).
+template <bool FINE> __device__ __forceinline__ Limbs times(half8 hi, half8 lo, const half8* by) {
+  const half8 h = hi * by[0];
+  half8 rest = fma8(lo, by[0], fma8(hi, by[0], -h));
+  if (FINE) rest = fma8(hi, by[1], rest);
+  return {h, rest};
 }
 
 // A page's metadata as the waves read it: steps and zero terms (with their counterweights, in two limbs) as fp16 in
 // operand order, norms as fp32 with the codes' unit taken out.
-struct Staged {
-  half8 k_step[64], k_zero[2][64];   // [limb][group][quarter][k-step]
-  half8 v_step[64], v_zero[2][80];   // [limb][group][k-step][quarter]; behind the four groups the counterweights alone
-  float norm[R];                     // position (token % 16) * 8 + token / 16
+template <bool M32> struct Staged {
+  static constexpr int LIMBS = M32 ? 2 : 1;   // of a step
+  half8 k_step[LIMBS][64], k_zero[2][64];   // [limb][group][quarter][k-step]
+  half8 v_step[LIMBS][64], v_zero[2][80];   // [limb][group][k-step][quarter]; behind the four groups the counterweights alone
+  float norm[R];                            // position (token % 16) * 8 + token / 16
 };
 // A row's probabilities are taken against a reference that follows its maximum only when that has passed it by
 // 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs a rescaling of the
@@ -184,17 +187,19 @@ template <bool M32> struct Fetched {
     }
     return (max((int)most[0], (int)most[1]) >> 10) - 14;
   }
-  __device__ __forceinline__ static float zero_term(float ints, float s, float z) { return z * fmaf(-(s + 1.0f), ints, 1.0f); }
+  __device__ __forceinline__ static float zero_term(float ints, float s, float z) { return z * (ints != 0.0f ? -s : 1.0f); }
   // Step and zero term times 2^-x; a number is step c + zero: zero = -step z for integer zero-points (ints = 1), z itself
   // for float ones (ints = 0), as one form: nothing here branches.
-  __device__ __forceinline__ void step_and_zero(float ints, int x, half8& step, Limbs& zero) const {
+  __device__ __forceinline__ void step_and_zero(float ints, int x, Limbs& step, Limbs& zero) const {
     const float by = exp2i(-x);
     if (M32) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float s = number(a, e), z = number(b, e);
         const float t = __builtin_amdgcn_fmed3f(zero_term(ints, s, z) * by, -kHalfMax, kHalfMax);   // (infinite ones)
-        step[e] = (_Float16)fminf(s * by, kHalfMax);
+        const float u = fminf(s * by, kHalfMax);
+        step.hi[e] = (_Float16)u;
+        step.lo[e] = (_Float16)(u - (float)step.hi[e]);
         zero.hi[e] = (_Float16)t;
         zero.lo[e] = (_Float16)(t - (float)zero.hi[e]);
       }
@@ -207,8 +212,8 @@ template <bool M32> struct Fetched {
       asm("" : "+v"(two[0]), "+v"(two[1]), "+v"(two[2]));
       auto splat = [](uint32_t w) { return __builtin_bit_cast(half8, (u32x4){w, w, w, w}); };
       const half8 one = (_Float16)1.0f;
-      step = __builtin_bit_cast(half8, a[0]) * splat(two[0]);
-      const half8 f = fma8(step, splat(two[1]), one - splat(two[1])), m = z * splat(two[2]);   // step or 1, -z or z 2^-x
+      step.hi = __builtin_bit_cast(half8, a[0]) * splat(two[0]);
+      const half8 f = fma8(step.hi, splat(two[1]), one - splat(two[1])), m = z * splat(two[2]);   // step or 1, -z or z 2^-x
       zero.hi = f * m;
       zero.lo = fma8(f, m, -zero.hi);
     }
@@ -266,7 +271,7 @@ constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens
 __host__ __device__ constexpr int wgs_per_cu(int bits, bool m32, int nr) { return nr == 1 && bits == 2 && !m32 ? 3 : 2; }
 
 constexpr int OROW = D + 4;
-template <int NR> struct Lds {
+template <int NR, bool M32> struct Lds {
   static constexpr int ROWS = NR * 16;
   struct Loop {
     u32x4 q[NR][4][64];                              // queries as they came,
@@ -274,7 +279,7 @@ template <int NR> struct Lds {
     half8 cw[2];                                     // counterweights of even and odd k-steps
     float top[NR];                                   // the largest channel of a tile's queries
     union {
-      Staged meta;                                   // of a wave's page,
+      Staged<M32> meta;                              // of a wave's page,
       half8 tail[TAIL][9];                           // of its 16-bit piece: half of its values' channels
     } of_wave[4];
   };
@@ -290,7 +295,7 @@ template <int NR> struct Lds {
 
 // ONE: k_group is the whole page.
 template <int BITS, bool M32, bool ONE, int NR>
-__device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int row0) {
+__device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, int row0) {
   using C = Codes<BITS>;
   constexpr int ROWS = NR * 16;
 
@@ -393,16 +398,16 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         fn[0] = load_as<uint32_t>(kn + lane * 4);
       }
     };
-    Staged& meta = lds.loop.of_wave[wave].meta;
+    Staged<M32>& meta = lds.loop.of_wave[wave].meta;
     float norm_unit;   // what a stored norm is multiplied by
     auto stage_keys = [&] {
-      half8 st;
-      Limbs zero;
+      Limbs st, zero;
       const int x_keys = max_of_rows(row16_max(fk.exponent(ints)));   // of the page
       fk.step_and_zero(ints, x_keys, st, zero);
       const float unit = norm_unit * exp2i(x_keys);
       const half8 cw = lds.loop.cw[lane % 2];
-      meta.k_step[lane] = st;
+      meta.k_step[0][lane] = st.hi;
+      if (M32) meta.k_step[M32 ? 1 : 0][lane] = st.lo;
       meta.k_zero[0][lane] = zero.hi * cw;
       meta.k_zero[1][lane] = zero.lo * cw;
       float v[2];
@@ -416,12 +421,12 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
     };
     // Values are summed in units of 2^x, x the lane's value group's largest exponent so far (of lane / 16).
     auto stage_values = [&](int x_before) {
-      half8 st;
-      Limbs zero;
+      Limbs st, zero;
       const int x_now = max(x_before, row16_max(fv.exponent(ints)));
       fv.step_and_zero(ints, x_now, st, zero);
       const half8 cw = lds.loop.cw[lane / 4 % 2];
-      meta.v_step[lane] = st;
+      meta.v_step[0][lane] = st.hi;
+      if (M32) meta.v_step[M32 ? 1 : 0][lane] = st.lo;
       meta.v_zero[0][lane] = zero.hi * cw;
       meta.v_zero[1][lane] = zero.lo * cw;
       return x_now;
@@ -774,10 +779,12 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         asm("" : "+v"(q_lane));   // (read again: kept, the queries fill the registers)
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-          const half8 st = meta.k_step[gk + 4 * q4 + kk];
+          half8 st[2];
+          st[0] = meta.k_step[0][gk + 4 * q4 + kk];
+          if (M32) st[1] = meta.k_step[M32 ? 1 : 0][gk + 4 * q4 + kk];
           Limbs qd[NR];
 #pragma unroll
-          for (int i = 0; i < NR; ++i) qd[i] = times(lds.loop.qc[i][0][kk][q_lane], lds.loop.qc[i][1][kk][q_lane], st);
+          for (int i = 0; i < NR; ++i) qd[i] = times<M32>(lds.loop.qc[i][0][kk][q_lane], lds.loop.qc[i][1][kk][q_lane], st);
 #pragma unroll
           for (int t = 2 * w0; t < 2 * (w0 + SPAN); ++t) {
             const half8 a = C::operand(kc[t / 2] + t % 2 * BITS, kk);
@@ -846,10 +853,12 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
         const int gv = w * P.g.ngv >> 2;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-          const half8 st = meta.v_step[gv * 16 + 4 * kk + q4];
+          half8 st[2];
+          st[0] = meta.v_step[0][gv * 16 + 4 * kk + q4];
+          if (M32) st[1] = meta.v_step[M32 ? 1 : 0][gv * 16 + 4 * kk + q4];
           Limbs pd[NR];
 #pragma unroll
-          for (int i = 0; i < NR; ++i) pd[i] = times(pr[i][kk].hi, pr[i][kk].lo, st);
+          for (int i = 0; i < NR; ++i) pd[i] = times<M32>(pr[i][kk].hi, pr[i][kk].lo, st);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const half8 a = C::operand(vc[w] + j * BITS, kk);
@@ -940,11 +949,11 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR>& lds, int r
 // 2000 rows over 2 x 8100 203 and 197), nor with 4-bit codes.
 template <int BITS, bool M32, bool ONE, int NR, bool LAST>
 __global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
-  __shared__ __align__(16) Lds<NR> lds;
+  __shared__ __align__(16) Lds<NR, M32> lds;
   const int row0 = (P.last_first ? gridDim.y - 1 - blockIdx.y : blockIdx.y) * NR * 16;
   if constexpr (LAST) {
     if (row0 > 0)
-      attend<BITS, M32, ONE, 1>(P, reinterpret_cast<Lds<1>&>(lds), row0);
+      attend<BITS, M32, ONE, 1>(P, reinterpret_cast<Lds<1, M32>&>(lds), row0);
     else
       attend<BITS, M32, ONE, NR>(P, lds, row0);
   } else {

@@ -198,3 +198,18 @@ def test_large_new_and_window_values_in_bf16():
     c = filled_cache([40, 300], hq=4, hk=2, gain=3e5, meta="f32")
     q, k, v = new_tokens(c, 5, "bf16", vmul=1e7)
     check(c, q, k, v, "bf16", splits=(1, 2))
+
+
+@pytest.mark.parametrize("bits,kg,vg,zp_min", [(2, 128, 32, False), (4, 64, 128, True), (2, 32, 64, True), (4, 128, 32, False)])
+@pytest.mark.parametrize("T", [2, 9])
+def test_fp32_metadata_is_not_narrowed(bits, kg, vg, zp_min, T):
+    c = filled_cache([700, 128, 0, 383], hk=2, hq=8, bits=bits, kg=kg, vg=vg, io="f16", meta="f32", zp_min=zp_min, seed=bits + kg)
+    check(c, *new_tokens(c, T, "f16"), "f16", splits=(1, 3))
+
+
+@pytest.mark.parametrize("gain", [1e-6, 1e-10, 1e6, 1e15])
+@pytest.mark.parametrize("bits,vg", [(2, 32), (4, 128)])
+def test_fp32_metadata_of_any_size(bits, vg, gain):
+    """Steps below fp16's smallest number and above its largest."""
+    c = filled_cache([520, 300], hk=2, hq=4, bits=bits, vg=vg, meta="f32", gain=gain)
+    check(c, *new_tokens(c, 3, "bf16", vmul=gain), "bf16", splits=(1, 2))
