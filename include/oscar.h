@@ -390,8 +390,9 @@ int oscar_bf16_decode_attn(const void *q, const void *k, const void *v, const in
  *     a = positions[pair_axis[i]][token] * inv_freq[i]
  *     y1 = x1 cos a - x2 sin a,  y2 = x2 cos a + x1 sin a
  * where x1, x2 are channels i and i + rotary_dim / 2, or 2i and 2i + 1 with OSCAR_ROPE_ADJACENT.
- * Channels from rotary_dim on are copied.  The angle is the exact product, reduced in 64 bits, so
- * far positions lose nothing; the turn is fp32 and rounded once.
+ * Channels from rotary_dim on are copied.  The angle counts as the exact product at any position:
+ * its sine and cosine are worked out in 64 bits and rounded once, to fp32; the turn is fp32 and
+ * rounded once.
  *   q, k    : device, io_dtype, n_tokens rows of n_q_heads (n_kv_heads) vectors of 128 channels; a
  *             row's heads are contiguous, rows are q_stride (k_stride) elements apart, so q and k
  *             may lie side by side in one projection's output.  0 heads: that side is left out.

@@ -2,9 +2,10 @@
 //
 // Pair i of a vector (channels i and i + r/2, or 2i and 2i + 1) turns by the angle
 //   a = position[axis(i)][token] * inv_freq[i],   y1 = x1 cos a - x2 sin a,   y2 = x2 cos a + x1 sin a.
-// The angle is worked out in 64 bits: the product of a 32-bit position and a 24-bit frequency, divided by
-// 2 pi and cut to the nearest whole turn, keeps the angle to 2e-7 at the largest int32 position, where a
-// 32-bit product would be off by whole turns.  Only the remaining fraction of a turn goes to 32 bits.
+// The angle is worked out in 64 bits and their rest: the product of a 32-bit position and a 24-bit frequency has up to
+// 56 bits, 1 / 2 pi is held to 106, and of turns the fraction counts, to 2^-52 at any position (in 64 bits alone the
+// largest ones were off by 3e-7).  Sine and cosine are 64-bit series about the nearest quarter turn, rounded once to
+// 32 bits: the turn's own roundings are all there is.
 //
 // What bounds it: every channel is read and written once, a few operations each: memory.  The sines are the dear
 // part, and all heads of a token share them: a workgroup takes one to four tokens, one thread works out the
@@ -53,6 +54,26 @@ template <typename T> struct Vec {
   }
 };
 
+// (cos, sin) of 2 pi times position times frequency / 2 pi.
+__device__ __forceinline__ float2 cos_sin(int32_t position, float inv_freq) {
+#pragma clang fp contract(off)   // (products are rounded where their rests are taken)
+  constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;   // 1 / 2 pi
+  const double p = position, f = inv_freq;
+  const double a = p * f, a_rest = fma(p, f, -a);   // exact together
+  const double t = a * kHi, t_rest = fma(a, kHi, -t) + fma(a, kLo, a_rest * kHi);
+  const double r = (t - rint(t)) + t_rest;          // turns, within half a turn
+  const double quarter = rint(4.0 * r);
+  const double y = fma(quarter, -0.25, r) * 6.283185307179586, z = y * y;   // |y| <= pi / 4
+  // the series' next terms are 7e-12 and 5e-13 there
+  double s = fma(z, fma(z, fma(z, fma(z, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6);
+  double c = fma(z, fma(z, fma(z, fma(z, fma(z, 1.0 / 479001600, -1.0 / 3628800), 1.0 / 40320), -1.0 / 720), 1.0 / 24), -0.5);
+  s = fma(y * z, s, y);
+  c = fma(z, c, 1.0);
+  const int q = (int)quarter & 3;
+  const float cf = (float)(q & 1 ? s : c), sf = (float)(q & 1 ? c : s);
+  return make_float2(q == 1 || q == 2 ? -cf : cf, q >= 2 ? -sf : sf);
+}
+
 __device__ __forceinline__ void turn(float& a, float& b, float2 cs) {
   const float y = a * cs.x - b * cs.y;
   b = b * cs.x + a * cs.y;
@@ -70,10 +91,8 @@ template <typename T, int PAIRS> __global__ __launch_bounds__(256) void oscar_ro
     const int t = tid >> 6, i = tid & 63;
     if (t < nt && i < P.half) {
       const int axis = (int)((i < 32 ? P.axis_lo >> (2 * i) : P.axis_hi >> (2 * i - 64)) & 3);
-      const double turns = (double)P.positions[axis * P.n_tokens + t0 + t] * (double)P.inv_freq[i] * 0.15915494309189533577;
-      float s, c;
-      sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-      s_cs[t][i] = make_float2(c, s * P.sign);
+      const float2 cs = cos_sin(P.positions[axis * P.n_tokens + t0 + t], P.inv_freq[i]);
+      s_cs[t][i] = make_float2(cs.x, cs.y * P.sign);
     }
   }
   __syncthreads();
