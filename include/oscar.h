@@ -434,7 +434,8 @@ int oscar_cache_read(const oscar_cache *cache, const int32_t *starts, int32_t T,
  *                  rows behind them are zeros; NULL = T for all
  *   out          : device, [batch][T][n_q_heads][head_dim], io_dtype; no part of the inputs
  *   softmax_scale, max_seq_len_hint, num_splits (<= 512, 0 = oscar_draft_auto_splits): as in
- *                  oscar_decode_attn
+ *                  oscar_decode_attn; a hint that is not 0 and below T also puts the last rows, which
+ *                  then have the most to read, first (the results are the same either way)
  *   workspace    : at least oscar_draft_workspace_bytes(...), 8-byte aligned; NULL where that is 0
  *                  (one split).  Calls that share one must be ordered.
  * io_dtype BF16 or F16 (OSCAR_ERR_UNSUPPORTED for F32); every other field of the configuration as

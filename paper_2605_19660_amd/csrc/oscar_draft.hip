@@ -1064,7 +1064,8 @@ extern "C" int oscar_draft_attn(const void* q, const void* k_new, const void* v_
   // Where the new tokens outnumber the cached ones the last rows, which see the most of them, go first (2000 over 130:
   // 139 us, 158 the other way round); elsewhere that gains nothing, and ragged new_lens, whose empty blocks then come
   // first, lose (24 and 269 new tokens over 8100 and 5394: 126 us, 116 in the rows' order).
-  P.last_first = T > max_seq_len_hint;
+  // A hint of 0 is a length that is not known.
+  P.last_first = max_seq_len_hint > 0 && T > max_seq_len_hint;
   P.by_splits = divisor(num_splits);
   P.by_step = divisor(4 * num_splits);
   P.by_kv_heads = divisor(cfg.n_kv_heads);
