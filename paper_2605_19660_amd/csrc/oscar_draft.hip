@@ -31,7 +31,7 @@
 // So a product keeps its 22 bits down to 2^-28 of the largest the group can have, and a step its own 11 down to 2^-14 of
 // the largest step; an unscaled P Delta lost 0.3 .. 15 % of what values of 1e-2 .. 3e-4 add beside a token that takes the
 // softmax without values.  16-bit values of the window and of new tokens: fp16 ones as they are, bf16 ones as bf16
-// against probabilities of three bf16 limbs, so that they keep their range.  Sums, maxima and outputs are fp32.
+// against probabilities of two bf16 limbs, so that they keep their range.  Sums, maxima and outputs are fp32.
 //
 // What bounds it: the issue of instructions.  A page costs a wave with two tiles 304 matrix and about 1200 vector
 // instructions, and the two do not overlap across the waves of a SIMD (measured: the time is the sum of both).  8 new
@@ -266,10 +266,6 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens)
 
-// Workgroups a CU that a variant's registers are held to.  Three where they fit: four new tokens of 48 x 8000 66 us, 76
-// with two; with 4-bit codes 8 x 32K 89, 64 with two (registers in scratch).
-__host__ __device__ constexpr int wgs_per_cu(int bits, bool m32, int nr) { return nr == 1 && bits == 2 && !m32 ? 3 : 2; }
-
 constexpr int OROW = D + 4;
 template <int NR, bool M32> struct Lds {
   static constexpr int ROWS = NR * 16;
@@ -363,9 +359,11 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
     auto page_of = [&](int p, int phys) { return Page{phys, p < pages && phys >= 0 && phys < P.c.num_pages}; };
 
     // ---- loads ahead ----
-    // (all of a page's codes a page ahead; 4-bit ones of two tiles a half each, into what the other half has left: the
-    // registers do not hold more.  500 new tokens over 2 x 8100: 207 us, 250 with all of them ahead and spilled)
+    // (a page ahead; of two tiles the keys' codes and the metadata go out halfway through the values, and 4-bit values'
+    // codes by halves: the registers do not hold more.  8 new tokens over 8 x 32K 97 us, 103 with the keys' codes ahead of
+    // all values and spilled; 4-bit 117 and 138)
     constexpr int AHEAD = BITS == 4 && NR == 2 ? 2 : 4;
+    constexpr bool LATE = NR == 2;
     uint32_t kc[4][2 * BITS], vc[4][2 * BITS];
     // (every part of a page has a power of two of bytes)
     constexpr int code_shift = BITS == 2 ? 12 : 13, norm_shift = M32 ? 9 : 8;
@@ -629,8 +627,10 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
         float by;
         if (__any(top > most[i])) move(i, top, by);
       }
-      // Probabilities: two fp16 limbs beside fp16 values, three bf16 ones beside bf16 values, whose range is an fp32's.
-      half8 pr[NR][3];   // (16 bits of either type)
+      // Probabilities: two fp16 limbs beside fp16 values, two bf16 ones beside bf16 values, whose range is an fp32's: 2^-18
+      // of each, where the outputs are rounded to 2^-9 of themselves (a third limb: 2000 new tokens over 130 183 -> 174 us
+      // without it).
+      half8 pr[NR][2];   // (16 bits of either type)
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
         float p[8];
@@ -641,7 +641,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
         if (bf16) {
           const bf16x8 one = (__bf16)(n == 4 ? 1.0f : 0.0f);
 #pragma unroll
-          for (int limb = 0; limb < 3; ++limb) {
+          for (int limb = 0; limb < 2; ++limb) {
             bf16x8 b;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -658,7 +658,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
           for (int e = 0; e < 8; e += 2) split2(p[e], p[e + 1], two, e);
           x[i] = mfma(one, two.hi, x[i]);
           x[i] = mfma(one, two.lo, x[i]);
-          pr[i][0] = two.hi, pr[i][1] = pr[i][2] = two.lo;
+          pr[i][0] = two.hi, pr[i][1] = two.lo;
         }
       }
       load_values(0);
@@ -702,7 +702,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
             float4v& acc = o[i][4 * half + ct];
             if (bf16) {
 #pragma unroll
-              for (int limb = 0; limb < 3; ++limb) acc = mfma(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, pr[i][limb]), acc);
+              for (int limb = 0; limb < 2; ++limb) acc = mfma(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, pr[i][limb]), acc);
             } else {
               acc = mfma(a, pr[i][0], acc);
               acc = mfma(a, pr[i][1], acc);
@@ -797,8 +797,10 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
         if (AHEAD < 4 && w0 == 0 && SPAN == AHEAD) load_codes(pool_of(P.c.v_codes, code_shift, pg0), v_at, vc, AHEAD, 4);
         if (AHEAD < 4 && w0 == 1 && SPAN == 1) load_codes(pool_of(P.c.v_codes, code_shift, pg0), v_at, vc, AHEAD, 4);
       }
-      load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, 0, AHEAD);
-      fetch_meta(pg1);
+      if (!LATE) {
+        load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, 0, AHEAD);
+        fetch_meta(pg1);
+      }
       // logits above M, less the bit position's exponent; what is no page has none
       float top[NR];
 #pragma unroll
@@ -868,8 +870,12 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
             for (int i = 0; i < NR; ++i) o[i][2 * w + j] = mfma(a, pd[i].lo, o[i][2 * w + j]);
           }
         }
-        if (w == 1) load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, AHEAD, 4);
+        if (w == 1 && LATE) {
+          load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, 0, AHEAD);
+          fetch_meta(pg1);
+        }
       }
+      if (AHEAD < 4) load_codes(pool_of(P.c.k_codes, code_shift, pg1), k_at, kc, AHEAD, 4);
       load_codes(pool_of(P.c.v_codes, code_shift, pg1), v_at, vc, 0, AHEAD);
       wave_lds_fence();
       stage_keys();
@@ -948,7 +954,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
 // the first one registers, it is a variant of its own, not taken with more blocks (77 rows 57.4 us, 56.5 without it,
 // 2000 rows over 2 x 8100 203 and 197), nor with 4-bit codes.
 template <int BITS, bool M32, bool ONE, int NR, bool LAST>
-__global__ __launch_bounds__(256, wgs_per_cu(BITS, M32, NR)) void oscar_draft_kernel(DraftParams P) {
+__global__ __launch_bounds__(256, 2) void oscar_draft_kernel(DraftParams P) {
   __shared__ __align__(16) Lds<NR, M32> lds;
   const int row0 = (P.last_first ? gridDim.y - 1 - blockIdx.y : blockIdx.y) * NR * 16;
   if constexpr (LAST) {
