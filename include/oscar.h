@@ -468,7 +468,9 @@ int oscar_draft_attn(const void *q, const void *k_new, const void *v_new, int32_
  *   draft  : device, [batch][T][vocab] of dtype, what the drafts were drawn from
  *   drafts : device int32 [batch][T];   u : device fp32 [batch][T+1], in [0, 1)
  *   n_new  : device int32 [batch]: a + 1, the tokens the step yields, which is also the new_lens of
- *            oscar_quantize_append for the keys and values of the last token and the drafts
+ *            oscar_quantize_append for the keys and values of the last token and the drafts.  It is 1
+ *            at least: for a sequence that takes no part in the step (new_lens[b] == 0 in
+ *            oscar_draft_attn) the caller puts 0 there before the append
  *   tokens : device int32 [batch][T+1]: the drafts that stand, the next token, then -1; no part
  *            of the inputs, as n_new
  *   workspace : at least oscar_verify_workspace_bytes(...), 16-byte aligned; its contents do not
