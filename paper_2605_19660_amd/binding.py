@@ -633,6 +633,8 @@ def cache_read(cache: Cache, starts=None, k=None, v=None, stream=None):
     """oscar_cache_read: fills k and v ([batch, T, n_kv_heads, 128], one type of the three, either may be
     None) with the tokens from starts[b] on (int32 [batch]; None = 0) and returns them; rows of tokens that
     a sequence does not hold stay as they are."""
+    if k is None and v is None:
+        raise OscarError(ERR_INVALID_ARG, "oscar_cache_read")
     shape, dtype = (k if k is not None else v).shape, (k if k is not None else v).dtype
     assert shape[0] == cache.batch and tuple(shape[2:]) == (cache.cfg.n_kv_heads, cache.cfg.head_dim)
     _here(k, v, starts, cache.seq_lens)
