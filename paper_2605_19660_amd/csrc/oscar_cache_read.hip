@@ -348,7 +348,9 @@ extern "C" int oscar_cache_read(const oscar_cache* cache, const int32_t* starts,
   // pages that T tokens from anywhere can touch, and no more than a sequence has with its window
   int64_t blocks = starts ? ((int64_t)T - 1) / R + 2 : ((int64_t)T - 1) / R + 1;
   if (blocks > (int64_t)cache->max_pages_per_seq + 1) blocks = (int64_t)cache->max_pages_per_seq + 1;
-  const dim3 grid((unsigned)(k && v ? 2 * blocks : blocks), cache->cfg.n_kv_heads, cache->batch);
+  if (k && v) blocks *= 2;
+  if (blocks >= 1 << 24) return OSCAR_ERR_INVALID_ARG;   // (fewer than 2^32 threads)
+  const dim3 grid((unsigned)blocks, cache->cfg.n_kv_heads, cache->batch);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (out_dtype == OSCAR_F32)
     launch<float>(P, grid, st);

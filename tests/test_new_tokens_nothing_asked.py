@@ -10,3 +10,8 @@ def test_reading_neither_keys_nor_values_is_the_abi_s_error():
         ob.cache_read(None)
     assert e.value.status == ob.ERR_INVALID_ARG
     assert read(cache_struct(), k=None, v=None) == ob.ERR_INVALID_ARG
+
+
+def test_a_read_past_what_a_launch_takes_is_refused():
+    c = cache_struct(max_pages=1 << 24, num_pages=1 << 24, batch=1)
+    assert read(c, T=(1 << 31) - 1) == ob.ERR_INVALID_ARG
