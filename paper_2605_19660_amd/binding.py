@@ -699,7 +699,8 @@ def verify_workspace_bytes(batch: int, vocab: int) -> int:
 
 def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=None, workspace=None, stream=None):
     """oscar_verify_drafts: target [batch, T + 1, vocab] and draft [batch, T, vocab] of one type, drafts int32
-    [batch, T], u fp32 [batch, T + 1]; returns (n_new int32 [batch], tokens int32 [batch, T + 1])."""
+    [batch, T] (both may be None with T = 0), u fp32 [batch, T + 1]; returns (n_new int32 [batch], tokens int32
+    [batch, T + 1])."""
     import torch
     if stream is not None:
         with torch.cuda.stream(stream):
@@ -707,8 +708,10 @@ def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=
     batch, T1, vocab = target.shape
     T = T1 - 1
     _here(target, draft, drafts, u, draft_lens, n_new, tokens, workspace)
-    assert target.dtype == draft.dtype and target.is_contiguous() and draft.is_contiguous()
-    assert draft.shape == (batch, T, vocab) and drafts.shape == (batch, T) and u.shape == (batch, T1)
+    assert target.is_contiguous() and u.shape == (batch, T1)
+    if draft is not None:
+        assert draft.dtype == target.dtype and draft.is_contiguous() and draft.shape == (batch, T, vocab)
+    assert T == 0 if draft is None or drafts is None else drafts.shape == (batch, T)
     assert u.dtype == torch.float32 and u.is_contiguous()
     L = lib()
     if n_new is None:
@@ -718,8 +721,8 @@ def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=
     if workspace is None:
         workspace = torch.empty(L.oscar_verify_workspace_bytes(batch, vocab), dtype=torch.uint8, device=target.device)
     assert tokens.shape == (batch, T1) and workspace.is_contiguous()
-    rc = L.oscar_verify_drafts(target.data_ptr(), draft.data_ptr(), _int32_ptr(drafts, batch * T), _int32_ptr(draft_lens, batch),
-                               u.data_ptr(), batch, T, vocab, dtype_code(target.dtype), _int32_ptr(n_new, batch),
+    rc = L.oscar_verify_drafts(target.data_ptr(), None if draft is None else draft.data_ptr(), _int32_ptr(drafts, batch * T),
+                               _int32_ptr(draft_lens, batch), u.data_ptr(), batch, T, vocab, dtype_code(target.dtype), _int32_ptr(n_new, batch),
                                _int32_ptr(tokens, batch * T1), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                _stream_ptr(None))
     if rc != OK:
