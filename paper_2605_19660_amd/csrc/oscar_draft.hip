@@ -950,9 +950,8 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
 }
 
 // A workgroup of NR tiles.  LAST: the second and last block of rows is 16 of them at most and takes one tile (35 rows,
-// seven query heads and five tokens, over 131001 tokens: 37.6 us, 43.4 as twice two tiles).  For the second body costs
-// the first one registers, it is a variant of its own, not taken with more blocks (77 rows 57.4 us, 56.5 without it,
-// 2000 rows over 2 x 8100 203 and 197), nor with 4-bit codes.
+// seven query heads and five tokens, over 131001 tokens: 50 us, 60 as twice two tiles; with G_k = 32 57 and 71).  Not
+// with 4-bit codes, whose second body costs the first one more registers.
 template <int BITS, bool M32, bool ONE, int NR, bool LAST>
 __global__ __launch_bounds__(256, 2) void oscar_draft_kernel(DraftParams P) {
   __shared__ __align__(16) Lds<NR, M32> lds;
@@ -983,9 +982,9 @@ template <int BITS, bool M32> void launch(const DraftParams& P, int nr, dim3 gri
     launch<BITS, M32, false>(P, nr, grid, st);
 }
 
-// Tiles of 16 query rows a wave holds: two read every page half as often (32 rows over 8 x 32K 71 us, 85 with one; 500
-// new tokens of 32 heads over 2 x 8100 206 and 241, 4-bit 207 and 302), one has no idle half (16 rows 48 us, 50 with
-// two; 4-bit 64 and 75).
+// Tiles of 16 query rows a wave holds: two read every page half as often (32 rows over 8 x 32K 100 us, 111 with one; 500
+// new tokens of 32 heads over 2 x 8100 305 and 359, 4-bit 323 and 383), one has no idle half (16 rows 60 us, 89 with
+// two; 4-bit 70 and 111).
 int row_tiles(const oscar_config& cfg, int T) { return (int64_t)T * (cfg.n_q_heads / cfg.n_kv_heads) <= 16 ? 1 : 2; }
 int64_t row_blocks(const oscar_config& cfg, int T) {
   const int rows = 16 * row_tiles(cfg, T);
@@ -1001,12 +1000,12 @@ int check_draft_config(const oscar_config* cfg) {
 }  // namespace
 
 // The split count whose estimate is the shortest.  A wave takes a piece (a page, or 32 tokens of the window or of the
-// new ones) in 3 us with one tile of rows and in 4 with two, 1.4 times that with 4-bit codes; workgroups that share a
+// new ones) in 3 with one tile of rows and in 4 with two, 1.4 times that with 4-bit codes; workgroups that share a
 // CU take 0.75 times as long each as one after the other; a workgroup's start costs 2 more.  Splitting costs the
-// reduce pass: 3 us, 0.4 ns a record, and past 64 splits 1.5 us and 0.07 each (another kernel).  Over 186 calls of 1 ..
-// 64 sequences, 30 .. 131001 tokens and 1 .. 128 new ones the choice takes 1 % longer than the best count (9 at the
-// most); as many splits as the chip has room for, 7 % (82 at the most): 4 new tokens of 48 x 260 14 us with one split,
-// 25 with two; 8 of 24 x 32K 170 with four, which put three workgroups on every CU, 195 with two.
+// reduce pass: 3, 0.0004 a record, and past 64 splits 1.5 and 0.07 each (another kernel).  These are weights for the
+// choice, in us to begin with; a call takes 1.7 times the estimate in the median (1.0 .. 3.5).  Over 186 calls of 1 .. 64
+// sequences, 30 .. 131001 tokens and 1 .. 128 new ones the choice takes 0.9 % longer than the best count (14 at the
+// most); weights nearer to the times (4.5 and 7 a piece) 1.3 % (24).
 extern "C" int32_t oscar_draft_auto_splits(const oscar_config* cfg, int32_t batch, int32_t T, int32_t max_seq_len) {
   if (check_draft_config(cfg) != OSCAR_OK || batch <= 0 || T <= 0) return 1;
   const int64_t units = (int64_t)batch * cfg->n_kv_heads * row_blocks(*cfg, T), cus = oscar_compute_units();

@@ -25,7 +25,9 @@ def k_step_of_channel(bits):
 
 def largest_by_group(x, group):
     """x [.., n] added up over groups (numbers 0 .. of the n places), of each group its largest."""
-    return sum(x[..., group == i].max(-1) for i in np.unique(group))
+    order = np.argsort(group, kind="stable")
+    first = np.flatnonzero(np.diff(group[order], prepend=-1))
+    return np.maximum.reduceat(x[..., order], first, axis=-1).sum(-1)
 
 
 def attention(c, q, k_new, v_new, new_lens, io, leave_out=None):
@@ -213,3 +215,19 @@ def test_fp32_metadata_of_any_size(bits, vg, gain):
     """Steps below fp16's smallest number and above its largest."""
     c = filled_cache([520, 300], hk=2, hq=4, bits=bits, vg=vg, meta="f32", gain=gain)
     check(c, *new_tokens(c, 3, "bf16", vmul=gain), "bf16", splits=(1, 2))
+
+
+@pytest.mark.parametrize("splits", [17, 52, 65, 512])
+@pytest.mark.parametrize("hq,new_lens", [(4, [4, 2]), (14, [4, 3])])
+def test_many_splits(splits, hq, new_lens):
+    """Records of 17 .. 64 and of more splits, most of them of waves without a page; blocks of rows of one and two tiles."""
+    c = filled_cache([1290, 300], hk=2, hq=hq, scattered=True)
+    check(c, *new_tokens(c, 4, "bf16"), "bf16", new_lens=new_lens, splits=(splits,))
+
+
+@pytest.mark.parametrize("hq,T", [(4, 3), (7, 5)])
+def test_a_long_context_with_the_split_count_of_the_library(hq, T):
+    from paper_2605_19660_amd import binding as ob
+    c = filled_cache([33000], hk=1, hq=hq, io="f16")
+    assert ob.draft_auto_splits(c.cfg, 1, T, 33000) > 16
+    check(c, *new_tokens(c, T, "f16"), "f16")
