@@ -26,7 +26,7 @@
 // sums.  With one limb, half a step (2^-11) each for Q, Q Delta, P, P Delta and the zero terms, fp16 outputs were off by
 // 4e-4 .. 3e-3 of their length, where their own rounding is 2e-4; the second limb costs 1.6 times the time.
 // Everything that meets a limb is first brought to fp16's middle by powers of two, in both directions, and the fp32 sums
-// carry the exponents: queries by the block of rows' largest channel, a page's key steps and zero terms by its largest,
+// carry the exponents: a query by its largest channel, a page's key steps and zero terms by its largest,
 // its value steps and zero terms by the largest of their value group so far.  The probabilities are stored below 2^15.
 // So a product keeps its 22 bits down to 2^-28 of the largest the group can have, and a step its own 11 down to 2^-14 of
 // the largest step; an unscaled P Delta lost 0.3 .. 15 % of what values of 1e-2 .. 3e-4 add beside a token that takes the
@@ -61,7 +61,7 @@ template <typename T> __device__ __forceinline__ T load_as(DevicePtr p) {
 
 constexpr float kHalfMax = 65504.0f;
 constexpr float kBf16Most = 1152921504606846976.0f;   // 2^60: bf16 values beyond it count as that
-constexpr int kQTop = 14;            // the largest channel of a block of queries is scaled to below 2^14
+constexpr int kQTop = 14;            // a query's largest channel is scaled to below 2^14
 
 // What loads of a page that is none take: its codes and parameters are zeros, and nothing that follows is NaN.
 __device__ __align__(256) const uint8_t kNoPage[8192] = {};
@@ -135,7 +135,7 @@ template <bool FINE> __device__ __forceinline__ Limbs times(half8 hi, half8 lo, 
 }
 
 // A page's metadata as the waves read it: steps and zero terms (with their counterweights, in two limbs) as fp16 in
-// operand order, norms as fp32 with the codes' unit taken out.
+// operand order, norms as fp32 with the keys' exponent.
 template <bool M32> struct Staged {
   static constexpr int LIMBS = M32 ? 2 : 1;   // of a step
   half8 k_step[LIMBS][64], k_zero[2][64];   // [limb][group][quarter][k-step]
@@ -273,7 +273,7 @@ template <int NR, bool M32> struct Lds {
     u32x4 q[NR][4][64];                              // queries as they came,
     half8 qh[NR][2][4][64], qc[NR][2][4][64];        // rotated and scaled, in limbs, and in the codes' order
     half8 cw[2];                                     // counterweights of even and odd k-steps
-    float top[NR];                                   // the largest channel of a tile's queries
+    float unit[NR][16];                              // of a row's scaled query
     union {
       Staged<M32> meta;                              // of a wave's page,
       half8 tail[TAIL][9];                           // of its 16-bit piece: half of its values' channels
@@ -397,12 +397,11 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
       }
     };
     Staged<M32>& meta = lds.loop.of_wave[wave].meta;
-    float norm_unit;   // what a stored norm is multiplied by
     auto stage_keys = [&] {
       Limbs st, zero;
       const int x_keys = max_of_rows(row16_max(fk.exponent(ints)));   // of the page
       fk.step_and_zero(ints, x_keys, st, zero);
-      const float unit = norm_unit * exp2i(x_keys);
+      const float unit = exp2i(x_keys);
       const half8 cw = lds.loop.cw[lane % 2];
       meta.k_step[0][lane] = st.hi;
       if (M32) meta.k_step[M32 ? 1 : 0][lane] = st.lo;
@@ -440,9 +439,9 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
     // ot is channel 32 (m / 4) + 4 ot + m % 4, so that a lane ends with channels 32 q4 .. + 31 of its query row, as
     // the keys' operands have them; its input channels are 32 q4 + 8 kk + e.  The sign of H[i][j] is the parity of
     // i & j, taken apart into what depends on (n, e), on (ot, kk, e) and on (n, q4).
-    float y[8][4];   // channels 32 q4 + 4 ot + r
-    float top_q = 0.0f;
     if (wave < NR) {
+      float y[8][4];   // channels 32 q4 + 4 ot + r
+      float top_q = 0.0f;
       const bool there = row0 + 16 * wave + n < n_new * g;
       const bool rotate = P.c.cfg.rotation == OSCAR_ROTATION_ON;
       const float mul = P.scale_log2 * (rotate ? 0.08838834764831845f : 1.0f);
@@ -484,21 +483,12 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
           top_q = fmaxf(top_q, fabsf(y[ot][r]));
         }
       }
-      top_q = max_of_row(top_q);
-#pragma unroll
-      for (int m = 1; m < 16; m <<= 1) top_q = fmaxf(top_q, __shfl_xor(top_q, m, 64));
-      if (lane == 0) lds.loop.top[wave] = top_q;
-    }
-    __syncthreads();
-    // The queries' scale, one power of two for the block of rows: limbs then hold the largest products to 2^-22 and all
-    // others to 2^-38 of the largest.
-    top_q = lds.loop.top[0];
-    if (NR == 2) top_q = fmaxf(top_q, lds.loop.top[NR - 1]);
-    const int q_exp = min(max(kQTop - 1 + 127 - (int)(__float_as_uint(top_q) >> 23), -100), 100);
-    const float q_unit = __uint_as_float((uint32_t)(127 - q_exp) << 23);
-    norm_unit = (float)(1 << (24 - C::BPMIN)) * q_unit;
-    if (wave < NR) {
-      const float by = __uint_as_float((uint32_t)(127 + q_exp) << 23);
+      // A query's scale, a power of two of its own: limbs then hold its largest products to 2^-22 and all others to 2^-38
+      // of the largest.  (One for a block of rows would save a multiplication a logit, 2 %, and a query that is no number
+      // would spoil the other rows of its block.)
+      const int q_exp = min(max(kQTop - 1 + 127 - (int)(__float_as_uint(max_of_row(top_q)) >> 23), -100), 100);
+      if (q4 == 0) lds.loop.unit[wave][n] = exp2i(-q_exp);
+      const float by = exp2i(q_exp);
       Limbs qh[4];
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
@@ -529,22 +519,23 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
     // (constants of the page loop wait in LDS: the registers are spoken for)
     if (lane < 2) lds.loop.cw[lane] = lane == 0 ? C::counterweight(0) : C::counterweight(1);   // (the same from every wave)
     __syncthreads();
+    float q_unit[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) q_unit[i] = lds.loop.unit[i][n];
 
     auto scale = [&](int i, float by) {
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) o[i][ct] *= by;
       x[i] *= by;
     };
-    // New references for a tile one of whose rows has passed its own, and the state against them; in whole powers of
-    // two, so that probabilities already packed only change their exponents.  top: the lane's largest logit above M;
-    // returns what comes on top of logits above M, and leaves its power of two in `by`.
-    auto move = [&](int i, float top, float& by) {
+    // New references for a tile one of whose rows has passed its own, and the state against them, in whole powers of two.
+    // top: the lane's largest logit above M; returns what comes on top of logits above M.
+    auto move = [&](int i, float top) {
       const bool none = most[i] == kNone;
       const float to = fmaxf(none ? -INFINITY : M[i] + (float)kOff, ceilf(max_of_row(top) + M[i]));
       const float Mn = to == -INFINITY ? 0.0f : to - (float)kOff;
       const float shift = M[i] - Mn;
-      by = none ? 0.0f : __builtin_amdgcn_exp2f(shift);
-      scale(i, by);
+      scale(i, none ? 0.0f : __builtin_amdgcn_exp2f(shift));
       M[i] = Mn;
       most[i] = to == -INFINITY ? kNone : (float)kOff + kSlack;
       return shift;
@@ -593,9 +584,6 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         u32x4 (&a)[4] = ka[j];
-        float f[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) f[r] = win ? norm[j][r] * q_unit : P.scale_log2;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
           float4v acc = {0, 0, 0, 0};
@@ -616,7 +604,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int tok = t0 + 16 * j + 4 * q4 + r;
-            s[i][j][r] = tok < count && (win || tok <= row_t[i]) ? acc[r] * f[r] : -INFINITY;
+            s[i][j][r] = tok < count && (win || tok <= row_t[i]) ? acc[r] * (win ? norm[j][r] * q_unit[i] : P.scale_log2) : -INFINITY;
           }
         }
       }
@@ -624,8 +612,7 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
       for (int i = 0; i < NR; ++i) {
         const float top = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])),
                                 fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) - M[i];
-        float by;
-        if (__any(top > most[i])) move(i, top, by);
+        if (__any(top > most[i])) move(i, top);
       }
       // Probabilities: two fp16 limbs beside fp16 values, two bf16 ones beside bf16 values, whose range is an fp32's: 2^-18
       // of each, where the outputs are rounded to 2^-9 of themselves (a third limb: 2000 new tokens over 130 183 -> 174 us
@@ -802,9 +789,9 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
         fetch_meta(pg1);
       }
       // logits above M, less the bit position's exponent; what is no page has none
-      float top[NR];
+      float top[NR], unit[NR];
 #pragma unroll
-      for (int i = 0; i < NR; ++i) top[i] = -INFINITY;
+      for (int i = 0; i < NR; ++i) top[i] = -INFINITY, unit[i] = q_unit[i] * (float)(1 << (24 - C::BPMIN));
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -814,19 +801,19 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
           for (int i = 0; i < NR; ++i)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              s[i][4 * half + t][r] = fmaf(s[i][4 * half + t][r], nm[t], -(M[i] + ((float)C::above(r, 4 * half + t) + gone)));
+              s[i][4 * half + t][r] = fmaf(s[i][4 * half + t][r], nm[t] * unit[i], -(M[i] + ((float)C::above(r, 4 * half + t) + gone)));
               top[i] = fmaxf(top[i], s[i][4 * half + t][r]);
             }
         }
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
         if (!__any(top[i] > most[i])) continue;
-        float most_of = -INFINITY, by;
+        float most_of = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int t = 0; t < 8; ++t) most_of = fmaxf(most_of, s[i][t][r] + (float)C::above(r, t));
-        const float shift = move(i, most_of, by);
+        const float shift = move(i, most_of);
 #pragma unroll
         for (int t = 0; t < 8; ++t) s[i][t] += shift;
       }

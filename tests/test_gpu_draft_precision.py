@@ -231,3 +231,15 @@ def test_a_long_context_with_the_split_count_of_the_library(hq, T):
     c = filled_cache([33000], hk=1, hq=hq, io="f16")
     assert ob.draft_auto_splits(c.cfg, 1, T, 33000) > 16
     check(c, *new_tokens(c, T, "f16"), "f16")
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan"), 1e38])
+@pytest.mark.parametrize("T,splits", [(3, 1), (9, 2)])
+def test_a_query_that_is_no_number_spoils_its_own_row_only(bad, T, splits):
+    c = filled_cache([300, 140], hk=2, hq=8)
+    q, k, v = new_tokens(c, T, "bf16")
+    want, tol = attention(c, *(x.double().cpu().numpy() for x in (q, k, v)), None, "bf16")
+    q[0, 1, 2, 5] = bad
+    err = np.abs(run(c, q, k, v, None, splits) - want)
+    err[0, 1, 2] = 0
+    assert np.isfinite(err).all() and (err <= tol).all()
