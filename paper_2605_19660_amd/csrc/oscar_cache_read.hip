@@ -61,14 +61,6 @@ template <bool M32> struct Meta32 {
     return __half2float(__ushort_as_half((uint16_t)(reinterpret_cast<const uint32_t*>(q)[i / 2] >> (16 * (i % 2)))));
   }
 };
-// Between a wave's writes to its own LDS and its reads of what other lanes wrote: LDS operations of one wave
-// execute in order, the compiler must not move them.
-__device__ __forceinline__ void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // H over 128 channels, 32 consecutive ones in each lane of a quad (lane % 4 = which), times mul
 __device__ __forceinline__ void rotate_quad(float (&x)[32], float mul) {
 #pragma unroll

@@ -57,6 +57,14 @@ __device__ __forceinline__ int chunk_order(int bits, int t) {
   return vtok_q4(t) * 32 + vtok_slot(bits, t);
 }
 
+// Between a wave's writes to its own LDS and its reads of what other lanes wrote: LDS operations of one wave
+// execute in order, the compiler must not move them.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m, 64));

@@ -100,14 +100,6 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// wave-local LDS hand-off: LDS operations of one wave execute in order; this only stops
-// the compiler from moving accesses across the hand-off point.
-__device__ __forceinline__ void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // Reductions over the 16 lanes of a DPP row (= one head group): xor-1 and xor-2 inside
 // quads, then the two mirrors; every lane ends with the same bits.
 template <int CTRL> __device__ __forceinline__ float dpp_mov(float v) {

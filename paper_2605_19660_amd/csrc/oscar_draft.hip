@@ -256,14 +256,6 @@ __device__ __forceinline__ float max_of_row(float v) {   // over the four lanes 
   return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
-// Between a wave's writes to its own LDS and its reads of what other lanes wrote: LDS operations of one wave
-// execute in order, the compiler must not move them.
-__device__ __forceinline__ void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 constexpr int TAIL = 32;         // tokens of a 16-bit piece (window, new tokens)
 
 constexpr int OROW = D + 4;
