@@ -243,9 +243,12 @@ __device__ __forceinline__ int max_of_rows(int v) {   // over the four rows
   return max((int)a[0], (int)a[1]);
 }
 __device__ __forceinline__ half2v pack2(float a, float b) { return __builtin_convertvector((float2v){a, b}, half2v); }
-// Two numbers into limbs, as elements e and e + 1 (constants where this is used).
+// Two numbers into limbs, as elements e and e + 1 (constants where this is used).  (The rests as products with a
+// register of -1: mixed operations take the fp16 numbers as they are, subtractions widen them first.)
 __device__ __forceinline__ void split2(float a, float b, Limbs& x, int e) {
-  const half2v hi = pack2(a, b), lo = pack2(a - (float)hi[0], b - (float)hi[1]);
+  float less = -1.0f;
+  asm("" : "+s"(less));
+  const half2v hi = pack2(a, b), lo = pack2(fmaf((float)hi[0], less, a), fmaf((float)hi[1], less, b));
   x.hi[e] = hi[0], x.hi[e + 1] = hi[1];
   x.lo[e] = lo[0], x.lo[e + 1] = lo[1];
 }
