@@ -16,7 +16,8 @@
 // 16 T + 4 r + lane / 16, exactly those whose value codes the lane's chunk of the page holds for k-step r: the
 // probabilities are packed where they are and become operands without an exchange.
 // (Four waves on one page, a quarter of its tokens and of its channels each, probabilities through LDS: 2.3 times
-// the LDS traffic, 1.4 times the matrix products and a barrier a page; 8 new tokens over 8 x 32K took 99 us.)
+// the LDS traffic, 1.4 times the matrix products and a barrier a page; with one limb an operand, see below, 8 new tokens
+// over 8 x 32K took 99 us so and 73 as it is.)
 //
 // Codes become fp16 operands with a mask (a code parked in the mantissa of a subnormal: c 2^(s - 24)); the
 // steps go to the other operand, Q Delta_k and P Delta_v, and 2^-s with them.  As in the decode kernels that operand is
@@ -24,7 +25,7 @@
 // arithmetic on a multiplicand split once (times()).  The zero terms are products on the matrix cores too, in limbs
 // themselves: for the keys what a tile's sums start from, for the values one extra tile, whose other rows are the rows'
 // sums.  With one limb, half a step (2^-11) each for Q, Q Delta, P, P Delta and the zero terms, fp16 outputs were off by
-// 4e-4 .. 3e-3 of their length, where their own rounding is 2e-4; the second limb costs 1.6 times the time.
+// 4e-4 .. 3e-3 of their length, where their own rounding is 2e-4; the second limb costs 1.2 .. 1.55 times the time.
 // Everything that meets a limb is first brought to fp16's middle by powers of two, in both directions, and the fp32 sums
 // carry the exponents: a query by its largest channel, a page's key steps and zero terms by its largest,
 // its value steps and zero terms by the largest of their value group so far.  The probabilities are stored below 2^15.
@@ -33,11 +34,13 @@
 // softmax without values.  16-bit values of the window and of new tokens: fp16 ones as they are, bf16 ones as bf16
 // against probabilities of two bf16 limbs, so that they keep their range.  Sums, maxima and outputs are fp32.
 //
-// What bounds it: the issue of instructions.  A page costs a wave with two tiles 304 matrix and about 1200 vector
-// instructions, and the two do not overlap across the waves of a SIMD (measured: the time is the sum of both).  8 new
-// tokens of 32 heads over 8 x 32768: 104 us, and 5 in the reduce pass; 5 of 28 heads over 131001, G_k = 32:
-// 59 + 5; 500 of 32 heads over two ragged caches of up to 8100, 4-bit: 217 us; 4 over 1000: 14 + 4, a chain of
-// lengths, page, window and reduce pass.
+// What bounds it: the issue of instructions.  A page costs a wave with two tiles 304 matrix and about 1250 vector
+// instructions, and the two hardly overlap across the waves of a SIMD (matrix cores busy 40 % of the time, other vector
+// instructions being issued 52 %).  8 new tokens of 32 heads over 8 x 32768: 95 us, 1.9 TB/s, and 5 in the reduce pass; 5
+// of 28 heads over 131001, G_k = 32: 53 + 5; 500 of 32 heads over two caches of 8100, 4-bit: 324 us, 420 TFLOP/s of the
+// products that the formula has; 4 over 1000: 11 + 4, a chain of lengths, page, window and reduce pass.
+// Registers: two workgroups a CU leave a wave 256.  Two tiles with 4-bit codes, fp32 metadata or k_group below 128 keep
+// 5 .. 62 of theirs in scratch memory (up to 21 accesses a page), all other variants none.
 #include "oscar_decode_common.h"
 
 namespace {
@@ -144,7 +147,7 @@ template <bool M32> struct Staged {
 };
 // A row's probabilities are taken against a reference that follows its maximum only when that has passed it by
 // 2^kSlack: over long sequences the maximum creeps up in many small steps, and each costs a rescaling of the
-// whole state (8 new tokens over 8 x 32K: 71 us, 75 with a reference that follows at once).
+// whole state (8 new tokens over 8 x 32K: 102 us, 108 with a reference that follows at once).
 constexpr float kSlack = 8.0f, kNone = -3e38f;
 constexpr int kOff = 7;          // exponent of a probability at its reference: kOff + kSlack stay inside fp16
 __device__ __forceinline__ float exp2i(int x) { return __uint_as_float((uint32_t)(127 + x) << 23); }   // |x| < 127
@@ -564,8 +567,8 @@ __device__ __forceinline__ void attend(const DraftParams& P, Lds<NR, M32>& lds, 
         for (int r = 0; r < 4; ++r) norm[j][r] = load_meta(P.c.res_norm, head * R + min(t0 + 16 * j + 4 * q4 + r, R - 1), MB);
       }
       // Values: rows of 64 channels in, a lane 8 channels of four tokens; through LDS, and columns of four tokens out.
-      // (Loaded as columns, 64 times two bytes a lane, 500 new tokens over 2 x 8100 4-bit take 225 us, 207 so; 2000
-      // over 130 271 and 159, in the rows' order.)
+      // (Loaded as columns, 64 times two bytes a lane, and with one limb 500 new tokens over 2 x 8100 4-bit took 225 us, 207
+      // so; 2000 over 130 271 and 159.)
       u32x4 va[4];
       auto load_values = [&](int half) {
 #pragma unroll
@@ -1049,8 +1052,8 @@ extern "C" int oscar_draft_attn(const void* q, const void* k_new, const void* v_
   P.num_splits = num_splits;
   P.group = cfg.n_q_heads / cfg.n_kv_heads;
   // Where the new tokens outnumber the cached ones the last rows, which see the most of them, go first (2000 over 130:
-  // 139 us, 158 the other way round); elsewhere that gains nothing, and ragged new_lens, whose empty blocks then come
-  // first, lose (24 and 269 new tokens over 8100 and 5394: 126 us, 116 in the rows' order).
+  // 170 us, 197 the other way round); elsewhere that gains nothing, and ragged new_lens, whose empty blocks then come
+  // first, lose (24 and 269 new tokens over 8100 and 5394, 4-bit: 186 us, 173 in the rows' order).
   // A hint of 0 is a length that is not known.
   P.last_first = max_seq_len_hint > 0 && T > max_seq_len_hint;
   P.by_splits = divisor(num_splits);
