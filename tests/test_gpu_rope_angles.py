@@ -51,3 +51,24 @@ def test_turns_are_as_near_as_64_bit_angles_give():
     for got, (u, v) in ((y[..., :64], (a * c, -b * s)), (y[..., 64:], (b * c, a * s))):
         bound = 2.0 ** -24 * (2 * np.abs(u) + 2 * np.abs(v) + np.abs(u + v)) * (1 + 1e-6) + 2.0 ** -31
         assert (np.abs(got - (u + v)) <= bound).all()
+
+
+def test_frequencies_of_any_size():
+    """Against 60-digit arithmetic where the product has 51 bits before the point and more than the fraction's left;
+    beyond that a turn stays a turn."""
+    import torch
+    from decimal import Decimal, getcontext
+    from paper_2605_19660_amd import binding as ob
+    getcontext().prec = 60
+    two_pi = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899")
+    inv = np.array([3e5, 1e6, 1.7e7, 1e-30, 0.0, 3e38] + [1e12] * 58, np.float32)
+    pos = np.array([2 ** 31 - 1, -2 ** 31, 1999999999, -3, 0, 77], np.int32)
+    x = torch.zeros(len(pos), 1, 128, device="cuda")
+    x[:, :, :64] = 1.0
+    y = ob.rope(x, None, torch.from_numpy(pos).cuda(), torch.from_numpy(inv).cuda())[0][:, 0].double().cpu().numpy()
+    for i, p in enumerate(pos):
+        for j in range(5):
+            a = float(Decimal(int(p)) * Decimal(float(inv[j])) % two_pi)
+            for got, want in ((y[i, j], np.cos(a)), (y[i, 64 + j], np.sin(a))):
+                assert abs(got - want) <= abs(want) * 2.0 ** -24 * (1 + 1e-6) + 2.0 ** -40, (p, inv[j])
+    assert (np.abs(y[:, :64] ** 2 + y[:, 64:] ** 2 - 1) <= 4 * 2.0 ** -24).all()
