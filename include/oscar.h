@@ -486,6 +486,147 @@ int oscar_verify_drafts(const void *target, const void *draft, const int32_t *dr
                         int32_t vocab, int32_t dtype, int32_t *n_new, int32_t *tokens,
                         void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- a serving step over a paged 8-bit cache ------------------------------------------------
+ * For layers and models that 2 or 4 bits cost too much: keys and values as e4m3 numbers (8 bits: sign,
+ * four bits of exponent, three of mantissa; +-448 the largest) with one power-of-two scale for each block
+ * of tokens and kv head, and the last tokens in 16 bits.  A step of a server: oscar_plan_step decides on
+ * the GPU which requests take part and where their tokens go, oscar_q8_append puts keys and values there,
+ * oscar_q8_attn attends from the new tokens, oscar_sample draws the next ones; oscar_q8_read is the way
+ * back out of the cache. */
+
+/* Plans a step from what every sequence holds and wants: pages given back, pages handed out, and where
+ * every row of the step goes.  With ps = page_size, k = keep (within 0 .. lens) or lens where keep is NULL:
+ *   - pages ceil(k / ps) .. ceil(lens / ps) - 1 of every sequence go back on the stack of free pages, in
+ *     order of sequence and page (k = 0: the sequence is over, or another one takes its place)
+ *   - sequence b asks for want[b] tokens and need = ceil((k + want) / ps) - ceil(k / ps) pages.  It takes
+ *     part iff want > 0, k + want <= ps * max_pages_per_seq, need is 0 or the needs up to b (of sequences that
+ *     fit) are within the pages there are, and the wants up to b (of those that have their pages) are within
+ *     n_rows.  Otherwise it waits with what it keeps: nobody behind takes the pages it waits for
+ *   - pages are handed out from the top of the stack, in order of sequence and page, into block_table
+ *   lens, want  : device int32 [batch] (below 0 counts as 0); keep: the same, or NULL
+ *   block_table : device int32 [batch][max_pages_per_seq], changed in place
+ *   free_pages  : device int32 [num_pages], the stack, changed in place; n_free: device int32 [1], its height.
+ *                 Every page is in the stack or in one sequence's part of the table, once
+ *   n_rows      : rows of the step there is room for
+ *   lens_out    : device int32 [batch], k + tokens granted; may be lens, or keep
+ *   new_lens    : device int32 [batch], tokens granted (want or 0); may be want
+ *   n_free_out  : device int32 [1]; may be n_free
+ *   row_starts  : device int32 [batch + 1]: the rows of sequence b are row_starts[b] .. row_starts[b + 1] - 1
+ *   positions, row_seq, slots : device int32 [n_rows] or NULL: every row's position in its sequence (for
+ *                 oscar_rope), its sequence, and its place page * page_size + position % page_size in a
+ *                 paged pool; -1 in rows behind the last sequence
+ * The other outputs overlap nothing.  Works for any cache here (page_size 128).  batch <=
+ * OSCAR_PLAN_MAX_BATCH; num_pages * page_size and max_pages_per_seq * page_size below 2^31.  One launch, two for many rows. */
+#define OSCAR_PLAN_MAX_BATCH (1 << 20)
+int oscar_plan_step(const int32_t *lens, const int32_t *keep, const int32_t *want, int32_t batch,
+                    int32_t *block_table, int32_t max_pages_per_seq, int32_t num_pages, int32_t page_size,
+                    int32_t *free_pages, const int32_t *n_free, int32_t n_rows, int32_t *lens_out,
+                    int32_t *new_lens, int32_t *n_free_out, int32_t *row_starts, int32_t *positions,
+                    int32_t *row_seq, int32_t *slots, void *stream);
+
+/* The paged 8-bit cache.  Plain data; pointers are DEVICE memory of the caller, with the sizes
+ * oscar_q8_sizes reports, 16-byte aligned.  Lengths are not part of it: the calls take them, so that the layers of
+ * a model share them, and a block table.
+ *   codes  : [physical page][kv head][128 tokens x 128 channels] bytes, in the order the matrix cores take them:
+ *            keys, token t, channel c at
+ *              ((t/16 * 2 + c/64) * 4 + c%64/16) * 256 + t%16 * 16 + c%16
+ *            values at
+ *              (((t/32 * 4 + c/32) * 4 + t%16/4) * 16 + c%16) * 16 + c%32/16 * 8 + t%32/16 * 4 + t%4
+ *   scales : [physical page][kv head][128 / block] fp32, powers of two: a code stands for code * scale
+ *   window : [sequence][kv head][2 * block][128] of io_dtype, position p at p mod 2 * block
+ * Of a sequence of n tokens the first n / block * block (whole blocks) are codes in pages, the rest are in the window.
+ * The window also holds the 16-bit form of the last whole block (of those of its tokens that came through
+ * oscar_q8_append): a length may be taken back by up to `block` tokens, to as little as n / block * block -
+ * block, simply by saying so in the next call (drafted tokens that do not stand). */
+typedef struct oscar_q8_cache {
+  int32_t batch, max_pages_per_seq, num_pages;
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 128 */
+  int32_t page_size;   /* 128 */
+  int32_t block;       /* tokens of a scale: 32 | 64 | 128 */
+  int32_t io_dtype;    /* OSCAR_BF16 | OSCAR_F16 */
+  void *k_codes, *v_codes;
+  float *k_scales, *v_scales;
+  void *win_k, *win_v;
+  int32_t *block_table; /* [batch][max_pages_per_seq]; an entry outside [0, num_pages) is no page */
+} oscar_q8_cache;
+typedef struct oscar_q8_pool_sizes {
+  size_t codes, scales, window; /* bytes of each of the two */
+  size_t block_table;
+  size_t page_bytes_per_kv_head; /* codes and scales of both */
+} oscar_q8_pool_sizes;
+
+/* Checks the sizes in *cache (not its pointers) and fills *out.  Host only. */
+int oscar_q8_sizes(const oscar_q8_cache *cache, oscar_q8_pool_sizes *out);
+
+/* How rows of a step belong to sequences, in the two calls that follow: sequence b has n = new_lens[b]
+ * (within 0 .. T; NULL: T) new tokens, the last n of its lens[b], in rows row_starts[b] .. + n - 1
+ * (row_starts NULL: from b * T on).  T bounds new_lens; n_rows is how many rows there are, and rows past it
+ * are not touched.  lens counts the new tokens. */
+
+/* Puts the new tokens into the cache.  A block that is complete becomes codes: with a the block's largest
+ * absolute value, scale = 2^ceil(log2(a / 448)) (2^-100 at least, 1 for a block of zeros), code = x / scale
+ * rounded to the nearest e4m3 number, ties to even.  What a token becomes depends on its block's tokens only, not on how they
+ * were cut into calls.  A NaN counts as 0; numbers beyond +-65504 (F16) or +-2^60 (BF16), infinities among them, as those.
+ *   k, v : device, rows of n_kv_heads vectors of 128 channels of io_dtype, k_stride (v_stride) elements apart;
+ *          16-byte aligned, strides multiples of 8
+ * Tokens whose page is no page, or behind the table's end, are not kept.  One launch. */
+int oscar_q8_append(const void *k, const void *v, int64_t k_stride, int64_t v_stride, int64_t n_rows, int32_t T,
+                    const int32_t *row_starts, const int32_t *new_lens, const int32_t *lens,
+                    const oscar_q8_cache *cache, void *stream);
+
+/* Attention from the new tokens, which oscar_q8_append has put into the cache, over the cache:
+ *   out[row][h] = softmax_j( scale * <q[row][h], k_j> ) . v_j,   j <= the row's position
+ *   q   : device, rows of n_q_heads vectors of 128 channels of io_dtype, q_stride elements apart; 16-byte
+ *         aligned, the stride a multiple of 8; query head h reads kv head h / (n_q_heads / n_kv_heads)
+ *   out : device, [n_rows][n_q_heads][128] of out_dtype (io_dtype or F32), 16-byte aligned
+ *   softmax_scale <= 0 means 1 / sqrt(128); max_seq_len_hint: a bound on lens[], for the split count only
+ *   num_splits  : (<= 512), 0 = oscar_q8_auto_splits; workspace: oscar_q8_workspace_bytes(...), 16-byte
+ *         aligned, NULL where that is 0.  Calls that share one must be ordered
+ * Rows that belong to no sequence are left as they were; a row that sees no token gets zeros; tokens in a page
+ * that is no page are left out.  Queries and logits are finite.  Keys and values enter as they are, queries too;
+ * probabilities are carried in two bf16 limbs (16 bits), sums and statistics are fp32.  The same call gives the same
+ * bits every time.  One launch, two with several splits. */
+#define OSCAR_Q8_MAX_GROUP 64 /* n_q_heads / n_kv_heads */
+int32_t oscar_q8_auto_splits(const oscar_q8_cache *cache, int32_t n_q_heads, int32_t T, int32_t max_seq_len);
+size_t oscar_q8_workspace_bytes(const oscar_q8_cache *cache, int32_t n_q_heads, int32_t T, int32_t num_splits);
+int oscar_q8_attn(const void *q, int64_t q_stride, int64_t n_rows, int32_t n_q_heads, int32_t T,
+                  const int32_t *row_starts, const int32_t *new_lens, const int32_t *lens,
+                  const oscar_q8_cache *cache, void *out, int32_t out_dtype, float softmax_scale,
+                  int32_t max_seq_len_hint, int32_t num_splits, void *workspace, size_t workspace_bytes,
+                  void *stream);
+
+/* Keys and values of T tokens of every sequence from its token starts[b] on: whole blocks from their codes, the
+ * rest from the window.
+ *   lens   : device int32 [batch];  starts: device int32 [batch] or NULL = 0; may be negative
+ *   k, v   : device, [batch][T][n_kv_heads][128] of out_dtype (any of the three), 16-byte aligned; either may
+ *            be NULL
+ * Rows of tokens that a sequence does not hold (before 0, from lens[b] on, in a page that is no page) are left
+ * as they were.  One launch. */
+int oscar_q8_read(const oscar_q8_cache *cache, const int32_t *lens, const int32_t *starts, int32_t T, void *k,
+                  void *v, int32_t out_dtype, void *stream);
+
+/* Draws a token from every row of logits, from given random numbers.  With m the row's largest logit and
+ * w_i = exp((logit_i - m) / temperature), tokens in order of falling logits (equal ones: the lower index
+ * first) and the filters one after the other:
+ *   top_k : the first top_k of them stay (<= 0: all)
+ *   top_p : of those the smallest number whose weights sum up to top_p of their sum or more (1 and more, or
+ *           a NaN: all), the first in any case
+ *   min_p : of those the ones with w >= min_p (a NaN: all), the first in any case
+ *   token : the smallest i whose running sum of the weights that stay, in order of i, exceeds u * their sum
+ * A temperature of 0 or below, or a NaN, draws the largest logit (the lowest such index).  NaN logits count as -inf, which is
+ * never drawn; +inf as the largest fp32.  A row without a number above -inf gives token 0 and no probability.
+ *   logits : device, rows of vocab numbers of dtype (F32|BF16|F16), row_stride elements apart
+ *   temperature, top_p, min_p : device fp32 [batch] or NULL (1, 1, 0);  top_k: device int32 [batch] or NULL
+ *   u      : device fp32 [batch], in [0, 1)
+ *   tokens : device int32 [batch]
+ *   probs  : device fp32 [batch][vocab], or NULL: what each token was drawn with (0 for those that do not
+ *            stay), as oscar_verify_drafts takes it
+ * Weights and sums are in 64 bits.  vocab <= OSCAR_VERIFY_MAX_VOCAB.  One launch. */
+int oscar_sample(const void *logits, int64_t row_stride, int32_t batch, int32_t vocab, int32_t dtype,
+                 const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                 const float *u, int32_t *tokens, float *probs, void *stream);
+
 /* Test/debug: copy sequence b, kv head h back to the HOST in a layout-free
  * form (one code per byte). Synchronizes `stream`. Host outputs, each may be
  * NULL; `cap_tokens` is the token capacity of the caller's arrays.

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import numpy as np
 
@@ -33,7 +34,9 @@ EXPORTS = ("oscar_version", "oscar_status_string", "oscar_cache_sizes",
            "oscar_debug_force_generic_decode", "oscar_decode_attn_noalloc",
            "oscar_decode_step", "oscar_cache_layer", "oscar_rope", "oscar_cache_read",
            "oscar_draft_auto_splits", "oscar_draft_workspace_bytes", "oscar_draft_attn",
-           "oscar_verify_workspace_bytes", "oscar_verify_drafts")
+           "oscar_verify_workspace_bytes", "oscar_verify_drafts", "oscar_plan_step", "oscar_q8_sizes",
+           "oscar_q8_append", "oscar_q8_auto_splits", "oscar_q8_workspace_bytes", "oscar_q8_attn",
+           "oscar_q8_read", "oscar_sample")
 
 
 class OscarError(RuntimeError):
@@ -61,6 +64,16 @@ class CPoolSizes(C.Structure):
         "k_codes", "k_meta", "k_norms", "v_codes", "v_meta", "res_k", "res_v", "res_norm",
         "block_table", "seq_lens", "res_lens", "tickets", "page_bytes_per_kv_head",
         "bytes_per_token_kv_head")]
+
+
+class CQ8Cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "max_pages_per_seq", "num_pages", "n_kv_heads", "head_dim", "page_size",
+                                         "block", "io_dtype")] + [
+        (n, C.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales", "win_k", "win_v", "block_table")]
+
+
+class CQ8PoolSizes(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in ("codes", "scales", "window", "block_table", "page_bytes_per_kv_head")]
 
 
 _lib = None
@@ -135,6 +148,23 @@ def lib():
     L.oscar_verify_workspace_bytes.argtypes = [i32, i32]
     L.oscar_verify_drafts.restype = C.c_int
     L.oscar_verify_drafts.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+    i64, q8 = C.c_int64, C.POINTER(CQ8Cache)
+    L.oscar_plan_step.restype = C.c_int
+    L.oscar_plan_step.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, vp, vp, i32] + [vp] * 8
+    L.oscar_q8_sizes.restype = C.c_int
+    L.oscar_q8_sizes.argtypes = [q8, C.POINTER(CQ8PoolSizes)]
+    L.oscar_q8_append.restype = C.c_int
+    L.oscar_q8_append.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, vp, q8, vp]
+    L.oscar_q8_auto_splits.restype = i32
+    L.oscar_q8_auto_splits.argtypes = [q8, i32, i32, i32]
+    L.oscar_q8_workspace_bytes.restype = sz
+    L.oscar_q8_workspace_bytes.argtypes = [q8, i32, i32, i32]
+    L.oscar_q8_attn.restype = C.c_int
+    L.oscar_q8_attn.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp, q8, vp, i32, f32, i32, i32, vp, sz, vp]
+    L.oscar_q8_read.restype = C.c_int
+    L.oscar_q8_read.argtypes = [q8, vp, vp, i32, vp, vp, i32, vp]
+    L.oscar_sample.restype = C.c_int
+    L.oscar_sample.argtypes = [vp, i64, i32, i32, i32] + [vp] * 8
     _lib = L
     return L
 
@@ -728,6 +758,206 @@ def verify_drafts(target, draft, drafts, u, draft_lens=None, n_new=None, tokens=
     if rc != OK:
         _check(rc, "oscar_verify_drafts")
     return n_new, tokens
+
+
+class StepPlan(NamedTuple):
+    """What plan_step decided, device int32 tensors: see oscar_plan_step."""
+    lens: object
+    new_lens: object
+    n_free: object
+    row_starts: object
+    positions: object
+    row_seq: object
+    slots: object
+
+
+def plan_step(lens, want, block_table, free_pages, n_free, n_rows: int, keep=None, page_size: int = 128, lens_out=None,
+              new_lens=None, n_free_out=None, row_starts=None, positions=None, row_seq=None, slots=None, stream=None) -> StepPlan:
+    """oscar_plan_step: lens, want, keep int32 [batch]; block_table int32 [batch, max_pages] and free_pages int32
+    [num_pages] are changed in place, n_free int32 [1] is the stack's height.  The outputs are made where they are not
+    given (lens_out=lens, new_lens=want, n_free_out=n_free: in place)."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return plan_step(lens, want, block_table, free_pages, n_free, n_rows, keep, page_size, lens_out, new_lens,
+                             n_free_out, row_starts, positions, row_seq, slots)
+    _here(lens, want, keep, block_table, free_pages, n_free, lens_out, new_lens, n_free_out, row_starts, positions, row_seq, slots)
+    batch, max_pages = block_table.shape
+    new = lambda t, n: torch.empty(n, dtype=torch.int32, device=lens.device) if t is None else t
+    p = StepPlan(new(lens_out, batch), new(new_lens, batch), new(n_free_out, 1), new(row_starts, batch + 1),
+                 new(positions, n_rows), new(row_seq, n_rows), new(slots, n_rows))
+    rc = lib().oscar_plan_step(_int32_ptr(lens, batch), _int32_ptr(keep, batch), _int32_ptr(want, batch), batch,
+                               _int32_ptr(block_table, batch * max_pages), max_pages, free_pages.numel(), page_size,
+                               _int32_ptr(free_pages, free_pages.numel()), _int32_ptr(n_free, 1), n_rows,
+                               _int32_ptr(p.lens, batch), _int32_ptr(p.new_lens, batch), _int32_ptr(p.n_free, 1),
+                               _int32_ptr(p.row_starts, batch + 1), _int32_ptr(p.positions, n_rows),
+                               _int32_ptr(p.row_seq, n_rows), _int32_ptr(p.slots, n_rows), _stream_ptr(None))
+    if rc != OK:
+        _check(rc, "oscar_plan_step")
+    return p
+
+
+class Q8Cache:
+    """Device pools of one paged 8-bit cache (oscar_q8_cache), allocated through torch.
+
+    block_table defaults to sequence-major identity; pass a device int32 tensor [batch, max_pages_per_seq] to share one
+    between layers or with plan_step.  Lengths are the caller's: the calls take them."""
+
+    def __init__(self, n_kv_heads: int, batch: int, max_pages_per_seq: int, block: int = 32, io_dtype: int = BF16,
+                 device="cuda", num_pages: int | None = None, block_table=None):
+        import torch
+        self.n_kv_heads, self.batch, self.max_pages_per_seq = n_kv_heads, batch, max_pages_per_seq
+        self.num_pages = num_pages if num_pages is not None else batch * max_pages_per_seq
+        self.block, self.io_dtype, self.device = block, io_dtype, torch.device(device)
+        self._c = CQ8Cache(batch, max_pages_per_seq, self.num_pages, n_kv_heads, 128, 128, block, io_dtype)
+        self.sizes = CQ8PoolSizes()
+        _check(lib().oscar_q8_sizes(C.byref(self._c), C.byref(self.sizes)), "oscar_q8_sizes")
+
+        def pool(nbytes, dtype):
+            return torch.zeros(int(nbytes), dtype=torch.uint8, device=self.device).view(dtype)
+
+        sz, io = self.sizes, torch_dtype(io_dtype)
+        self.k_codes, self.v_codes = (pool(sz.codes, torch.uint8).view(self.num_pages, n_kv_heads, -1) for _ in "kv")
+        self.k_scales, self.v_scales = (pool(sz.scales, torch.float32).view(self.num_pages, n_kv_heads, -1) for _ in "kv")
+        self.win_k, self.win_v = (pool(sz.window, io).view(batch, n_kv_heads, 2 * block, 128) for _ in "kv")
+        if block_table is None:
+            assert batch * max_pages_per_seq <= self.num_pages
+            block_table = torch.arange(batch * max_pages_per_seq, dtype=torch.int32, device=self.device).view(batch, max_pages_per_seq)
+        assert block_table.dtype == torch.int32 and block_table.shape == (batch, max_pages_per_seq) and block_table.is_contiguous()
+        assert block_table.device == self.k_codes.device
+        self.block_table = block_table
+        for n in ("k_codes", "v_codes", "k_scales", "v_scales", "win_k", "win_v", "block_table"):
+            setattr(self._c, n, getattr(self, n).data_ptr())
+
+    @property
+    def c(self) -> CQ8Cache:
+        return self._c
+
+
+def _step_rows(cache: Q8Cache, x, heads: int, row_starts, max_new):
+    """Rows, most new tokens of a sequence and distance between rows of x: [batch, T, heads, 128], or (with
+    row_starts) [rows, heads, 128]."""
+    shape = x.shape
+    assert shape[-2] == heads and x.dtype == torch_dtype(cache.io_dtype)
+    if row_starts is None:
+        assert len(shape) == 4 and shape[0] == cache.batch and max_new in (None, shape[1])
+        return shape[0] * shape[1], shape[1], _token_stride(x)
+    assert len(shape) == 3 and max_new is not None, "rows by row_starts are [rows, heads, 128] and need max_new"
+    return shape[0], max_new, _token_stride(x)
+
+
+def _row_starts_ptr(t, batch: int):
+    """batch numbers, or batch + 1 as plan_step gives them."""
+    return None if t is None else _int32_ptr(t, batch + 1 if t.numel() == batch + 1 else batch)
+
+
+def q8_append(cache: Q8Cache, k, v, lens, new_lens=None, row_starts=None, max_new: int | None = None, stream=None):
+    """oscar_q8_append: k, v [batch, T, n_kv_heads, 128], or with row_starts (int32 [batch] or [batch + 1]) rows
+    [n_rows, n_kv_heads, 128] of any even distance, at most max_new a sequence; lens int32 [batch] counts the new
+    tokens, new_lens int32 [batch] says how many they are (None: T)."""
+    rows, T, k_stride = _step_rows(cache, k, cache.n_kv_heads, row_starts, max_new)
+    assert v.shape == k.shape and v.dtype == k.dtype
+    _here(k, v, lens, new_lens, row_starts, cache.k_codes)
+    rc = lib().oscar_q8_append(k.data_ptr(), v.data_ptr(), k_stride, _token_stride(v), rows, T, _row_starts_ptr(row_starts, cache.batch),
+                               _int32_ptr(new_lens, cache.batch), _int32_ptr(lens, cache.batch), C.byref(cache.c), _stream_ptr(stream))
+    if rc != OK:
+        _check(rc, "oscar_q8_append")
+
+
+def q8_auto_splits(cache: Q8Cache, n_q_heads: int, tokens: int, max_seq_len: int) -> int:
+    return int(lib().oscar_q8_auto_splits(C.byref(cache.c), n_q_heads, tokens, max_seq_len))
+
+
+def q8_workspace_bytes(cache: Q8Cache, n_q_heads: int, tokens: int, num_splits: int) -> int:
+    return int(lib().oscar_q8_workspace_bytes(C.byref(cache.c), n_q_heads, tokens, num_splits))
+
+
+def q8_attn(cache: Q8Cache, q, lens, new_lens=None, row_starts=None, max_new: int | None = None, out=None, scale: float = 0.0,
+            max_seq_len_hint: int = 0, num_splits: int = 0, workspace=None, stream=None):
+    """oscar_q8_attn: q [batch, T, n_q_heads, 128] or, with row_starts, [n_rows, n_q_heads, 128] of any even distance
+    between rows; the tokens they belong to are in the cache (q8_append) and in lens.  Returns `out`, of q's shape and
+    of its type or fp32; made here, rows that belong to no sequence are zeros, else they stay as they were."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return q8_attn(cache, q, lens, new_lens, row_starts, max_new, out, scale, max_seq_len_hint, num_splits, workspace)
+    heads = q.shape[-2]
+    rows, T, stride = _step_rows(cache, q, heads, row_starts, max_new)
+    _here(q, lens, new_lens, row_starts, out, workspace, cache.k_codes)
+    L, c = lib(), C.byref(cache.c)
+    if out is None:
+        # (every row of a full batch is written)
+        out = (torch.empty if new_lens is None and row_starts is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.is_contiguous()
+    if num_splits == 0:
+        num_splits = L.oscar_q8_auto_splits(c, heads, T, max_seq_len_hint)
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        assert workspace.is_contiguous()
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif num_splits > 1:
+        ws_bytes = L.oscar_q8_workspace_bytes(c, heads, T, num_splits)
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+        ws = workspace.data_ptr()
+    rc = L.oscar_q8_attn(q.data_ptr(), stride, rows, heads, T, _row_starts_ptr(row_starts, cache.batch),
+                         _int32_ptr(new_lens, cache.batch), _int32_ptr(lens, cache.batch), c, out.data_ptr(), dtype_code(out.dtype),
+                         scale, max_seq_len_hint, num_splits, ws, ws_bytes, _stream_ptr(None))
+    if rc != OK:
+        _check(rc, "oscar_q8_attn")
+    return out
+
+
+def q8_read(cache: Q8Cache, lens, starts=None, k=None, v=None, stream=None):
+    """oscar_q8_read: fills k and v ([batch, T, n_kv_heads, 128], one type of the three, either may be None) with the
+    tokens from starts[b] on (int32 [batch]; None = 0) and returns them; rows of tokens that a sequence does not hold
+    stay as they are."""
+    if k is None and v is None:
+        raise OscarError(ERR_INVALID_ARG, "oscar_q8_read")
+    shape, dtype = (k if k is not None else v).shape, (k if k is not None else v).dtype
+    assert shape[0] == cache.batch and tuple(shape[2:]) == (cache.n_kv_heads, 128)
+    _here(k, v, lens, starts, cache.k_codes)
+    for x in (k, v):
+        assert x is None or (x.is_contiguous() and x.shape == shape and x.dtype == dtype)
+    rc = lib().oscar_q8_read(C.byref(cache.c), _int32_ptr(lens, cache.batch), _int32_ptr(starts, cache.batch), shape[1],
+                             None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), dtype_code(dtype),
+                             _stream_ptr(stream))
+    if rc != OK:
+        _check(rc, "oscar_q8_read")
+    return k, v
+
+
+def _f32_ptr(t, n: int):
+    """Address of an fp32 device tensor of n numbers, or None."""
+    if t is None:
+        return None
+    import torch
+    assert t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()
+    return t.data_ptr()
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=False, stream=None):
+    """oscar_sample: logits [batch, vocab] of any distance between rows; u, temperature, top_p, min_p fp32 [batch], top_k
+    int32 [batch].  Returns (tokens int32 [batch], probabilities fp32 [batch, vocab] or None): probs is True, False or
+    the tensor that takes them."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return sample(logits, u, temperature, top_k, top_p, min_p, tokens, probs)
+    batch, vocab = logits.shape
+    if probs is True:
+        probs = torch.empty((batch, vocab), dtype=torch.float32, device=logits.device)
+    elif probs is False:
+        probs = None
+    _here(logits, u, temperature, top_k, top_p, min_p, tokens, probs)
+    assert vocab == 0 or logits.stride(1) == 1 or vocab == 1
+    if tokens is None:
+        tokens = torch.empty(batch, dtype=torch.int32, device=logits.device)
+    rc = lib().oscar_sample(logits.data_ptr(), logits.stride(0), batch, vocab, dtype_code(logits.dtype),
+                            _f32_ptr(temperature, batch), _int32_ptr(top_k, batch), _f32_ptr(top_p, batch), _f32_ptr(min_p, batch),
+                            _f32_ptr(u, batch), _int32_ptr(tokens, batch), _f32_ptr(probs, batch * vocab), _stream_ptr(None))
+    if rc != OK:
+        _check(rc, "oscar_sample")
+    return tokens, probs
 
 
 def debug_dump(cache: Cache, b: int, h: int, cap_tokens: int | None = None, stream=None) -> dict:

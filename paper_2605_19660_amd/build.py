@@ -36,6 +36,10 @@ SOURCES = {
     "oscar_cache_read.hip": [],
     "oscar_draft.hip": ["-fno-honor-nans"],   # (maxima as bare instructions; infinities count)
     "oscar_verify.hip": [],
+    "oscar_plan.hip": [],
+    "oscar_q8.hip": [],
+    "oscar_q8_attn.hip": [],
+    "oscar_sample.hip": [],
 }
 
 

@@ -1,0 +1,459 @@
+// oscar_q8_attn: attention from the new tokens over the paged 8-bit cache.
+//
+//   out[r] = sum_j exp(c <q_r, k_j> - m) v_j / sum_j exp(c <q_r, k_j> - m)     over positions j <= pos(r)
+//
+// in one pass over the cache, with a reference m that follows the largest logit.  A code is exact in bf16 and in
+// fp16, so keys are multiplied as they are with queries as they are, and a block's scale (a power of two) goes
+// onto its logits; value codes times their scale are exact in bf16.  Probabilities are rounded, to two bf16 limbs
+// (2^-17), each a matrix product of its own: with one, 2^-9 a token would add to the output's own rounding.
+//
+// A workgroup takes RT tiles of 16 rows (row = new token * g + query head of the group) of one kv head and a range of
+// pages; of a page each of its four waves takes a step of 32 tokens, so that four kilobytes of keys and four of values
+// lie between a wave's loads and their use.  S^T = K Q^T: a lane gets logits of 8 tokens of one row, and these are, as
+// they stand, its part of the operand of O^T = V^T P^T.  No LDS until the waves' sums are joined at the end.
+#include <algorithm>
+
+#include "oscar_q8.h"
+
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float NO_REF = -1e30f;   // reference of a row that has seen no token
+// A reference moves when a logit passes it by this much (in powers of two): probabilities stay below 2^8, and a wave
+// seldom has to multiply its sums.
+constexpr float REF_SLACK = 8.0f;
+
+struct AttnParams {
+  Q8Cache c;
+  Q8Rows r;
+  const uint16_t* q;
+  int64_t q_stride;
+  void* out;
+  float* ws;          // [sequence][new token][query head][split][130]: sums of values, sum and reference
+  float scale_log2;   // of logits, in powers of two
+  int hq, g, splits, row_blocks, out_f32;
+};
+
+__device__ __forceinline__ bf16x8 bf16_operand(u32x2 codes, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[0], scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[0], scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[1], scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[1], scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ f16x8 f16_operand(u32x2 codes) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[0], 1.0f, false);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[0], 1.0f, true);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[1], 1.0f, false);
+  const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[1], 1.0f, true);
+  return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Queries and keys are of the io type, everything else of the product is bf16.
+template <bool F16> struct Io;
+template <> struct Io<false> {
+  using Op = bf16x8;
+  static __device__ __forceinline__ Op keys(u32x2 codes) { return bf16_operand(codes, 1.0f); }
+  static __device__ __forceinline__ f32x4 mul(Op a, Op b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Io<true> {
+  using Op = f16x8;
+  static __device__ __forceinline__ Op keys(u32x2 codes) { return f16_operand(codes); }
+  static __device__ __forceinline__ f32x4 mul(Op a, Op b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+
+__device__ __forceinline__ f32x4 mul_bf16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// A wave's rows: queries, sums of values (transposed: 8 tiles of 16 channels), sum and reference.
+template <bool F16, int RT> struct Rows {
+  typename Io<F16>::Op q[RT][4];
+  f32x4 o[RT][8];
+  float sum[RT], ref[RT];
+  int pos[RT];          // the lane's row's position, -1: no row
+  int min_pos, max_pos; // of the rows there are
+};
+
+// Probabilities of a step's 8 logits of the lane's row: two limbs of the operand.
+struct Limbs {
+  bf16x8 hi, lo;
+};
+template <bool F16, int RT>
+__device__ __forceinline__ Limbs probabilities(Rows<F16, RT>& w, int r, f32x4 s0, f32x4 s1, float scale, int t0, bool edge, int q4, int limit) {
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = s0[i] * scale, x[4 + i] = s1[i] * scale;
+  if (edge) {
+    const int last = min(w.pos[r], limit - 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = t0 + 4 * q4 + i <= last ? x[i] : -INFINITY;
+      x[4 + i] = t0 + 16 + 4 * q4 + i <= last ? x[4 + i] : -INFINITY;
+    }
+  }
+  float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+  if (__any(top > w.ref[r] + REF_SLACK)) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float ref = fmaxf(w.ref[r], top);
+    const float f = __builtin_amdgcn_exp2f(w.ref[r] - ref);
+    w.ref[r] = ref;
+    w.sum[r] *= f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) w.o[r][c] *= f;
+  }
+  Limbs p;
+  float part = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float e = __builtin_amdgcn_exp2f(x[i] - w.ref[r]);
+    part += e;
+    p.hi[i] = (__bf16)e;
+    p.lo[i] = (__bf16)(e - (float)p.hi[i]);
+  }
+  w.sum[r] += part;
+  return p;
+}
+
+// F16: the io type; RT: tiles of 16 rows a workgroup.
+template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : RT == 2 ? 2 : 1) void oscar_q8_attn_kernel(AttnParams P) {
+  using Op = typename Io<F16>::Op;
+  __shared__ float s_sum[4][16 * RT], s_ref[4][16 * RT];
+  __shared__ __align__(16) float s_o[4][16 * 128];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, q4 = lane >> 4;
+  // row blocks of one range of pages lie on one die of eight, next to each other
+  uint32_t id = blockIdx.x;
+  int rb = 0;
+  if (P.row_blocks > 1) {
+    const uint32_t group = id / (8 * P.row_blocks), in = id % (8 * P.row_blocks);
+    rb = P.row_blocks - 1 - in / 8;   // (the last rows see the most)
+    id = group * 8 + in % 8;
+  }
+  const int split = id % P.splits;
+  id /= P.splits;
+  const int h = id % P.c.heads, b = id / P.c.heads;
+  if (b >= P.c.batch) return;
+  const Q8Seq s = q8_seq(P.r, b);
+  const int rows = s.n * P.g;
+  if (rb * 16 * RT >= rows) return;
+
+  Rows<F16, RT> w;
+  w.min_pos = s.old + rb * 16 * RT / P.g;
+  w.max_pos = s.old + (min((rb + 1) * 16 * RT, rows) - 1) / P.g;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int row = (rb * RT + r) * 16 + n, t = row / P.g;
+    const int64_t at = s.row + t;
+    const bool is = row < rows && at >= 0 && at < P.r.n_rows;
+    w.pos[r] = is ? s.old + t : -1;
+    const uint16_t* q = P.q + at * P.q_stride + (h * P.g + row % P.g) * D + 16 * q4;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      u32x4 x = {};
+      if (is) x = *reinterpret_cast<const u32x4*>(q + 64 * (kk / 2) + 8 * (kk % 2));
+      w.q[r][kk] = __builtin_bit_cast(Op, x);
+    }
+    w.sum[r] = 0.0f;
+    w.ref[r] = NO_REF;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) w.o[r][c] = f32x4{};
+  }
+
+  // pages of whole blocks, and the window behind them
+  const int coded = s.len / P.c.block * P.c.block;
+  const int end = min(coded, w.max_pos + 1);                 // tokens of pages that some row sees
+  const int pages = min(max(end + R - 1, 0) / R, P.c.max_pages);
+  const int per = (pages + P.splits - 1) / P.splits;
+  const int p0 = min(split * per, pages), p1 = min(p0 + per, pages);
+  const int per_page = R / P.c.block;
+  const int32_t* table = P.c.table + (int64_t)b * P.c.max_pages;
+
+  u32x4 k[4], v[4];
+  float ks = 0.0f, vs = 0.0f;
+  const auto valid = [&](int p) { return p < p1 && p * R + wave * Q8_STEP_TOKENS < end; };
+  const auto page_of = [&](int p) -> int {
+    if (!valid(p)) return -1;
+    const int page = table[p];
+    return (uint32_t)page < (uint32_t)P.c.num_pages ? page : -1;
+  };
+  const auto at_of = [&](int page) { return (int64_t)page * P.c.heads + h; };
+  const auto load_k = [&](int page) {
+    const uint8_t* in = P.c.k_codes + at_of(page) * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES + lane * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = *reinterpret_cast<const u32x4*>(in + i * 1024);
+    ks = P.c.k_scales[at_of(page) * per_page + wave * Q8_STEP_TOKENS / P.c.block];
+  };
+  const auto load_v = [&](int page) {
+    const uint8_t* in = P.c.v_codes + at_of(page) * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES + lane * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const u32x4*>(in + i * 1024);
+    vs = P.c.v_scales[at_of(page) * per_page + wave * Q8_STEP_TOKENS / P.c.block];
+  };
+
+  int page = page_of(p0), next = page_of(p0 + 1);
+  if (page >= 0) load_k(page), load_v(page);
+  for (int p = p0; p < p1; ++p) {
+    const int after = page_of(p + 2);
+    const int t0 = p * R + wave * Q8_STEP_TOKENS;
+    if (page >= 0) {
+      f32x4 st[RT][2];
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile) {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const u32x4 x = k[2 * tile + kk / 2];
+          const Op key = Io<F16>::keys(u32x2{x[2 * (kk % 2)], x[2 * (kk % 2) + 1]});
+#pragma unroll
+          for (int r = 0; r < RT; ++r) st[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : st[r][tile]);
+        }
+      }
+      const float scale = ks * P.scale_log2;
+      if (next >= 0) load_k(next);
+      const bool edge = t0 + Q8_STEP_TOKENS - 1 > w.min_pos;
+      Limbs pr[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) pr[r] = probabilities<F16, RT>(w, r, st[r][0], st[r][1], scale, t0, edge, q4, end);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const u32x4 x = v[c / 2];
+        const bf16x8 val = bf16_operand(u32x2{x[2 * (c % 2)], x[2 * (c % 2) + 1]}, vs);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) w.o[r][c] = mul_bf16(val, pr[r].lo, mul_bf16(val, pr[r].hi, w.o[r][c]));
+      }
+      if (next >= 0) load_v(next);
+    } else if (next >= 0) {
+      load_k(next), load_v(next);
+    }
+    page = next;
+    next = after;
+  }
+
+  // the window: its steps by the last split's waves
+  if (split == P.splits - 1) {
+    const uint16_t* wk = P.c.win_k + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
+    const uint16_t* wv = P.c.win_v + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
+    const int stop = min(s.len, w.max_pos + 1);
+    for (int t0 = coded + wave * Q8_STEP_TOKENS; t0 < stop; t0 += 4 * Q8_STEP_TOKENS) {
+      const int slot = t0 % (2 * P.c.block);   // (a step does not wrap)
+      f32x4 st[RT][2];
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile) {
+        const uint16_t* row = wk + (slot + 16 * tile + n) * D + 16 * q4;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const Op key = __builtin_bit_cast(Op, *reinterpret_cast<const u32x4*>(row + 64 * (kk / 2) + 8 * (kk % 2)));
+#pragma unroll
+          for (int r = 0; r < RT; ++r) st[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : st[r][tile]);
+        }
+      }
+      Limbs pr[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) pr[r] = probabilities<F16, RT>(w, r, st[r][0], st[r][1], P.scale_log2, t0, true, q4, stop);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        bf16x8 val, rest;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int t = 16 * (i / 4) + 4 * q4 + i % 4;
+          // what no token owns counts as zero: it need not be a number
+          uint32_t x = wv[(slot + t) * D + 16 * c + n];
+          x = t0 + t < stop ? x : 0;
+          if constexpr (F16) {   // 11 bits in two limbs
+            const float f = (float)__builtin_bit_cast(_Float16, (uint16_t)x);
+            val[i] = (__bf16)f;
+            rest[i] = (__bf16)(f - (float)val[i]);
+          } else {
+            val[i] = __builtin_bit_cast(__bf16, (uint16_t)x);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          w.o[r][c] = mul_bf16(val, pr[r].lo, mul_bf16(val, pr[r].hi, w.o[r][c]));
+          if constexpr (F16) w.o[r][c] = mul_bf16(rest, pr[r].hi, w.o[r][c]);
+        }
+      }
+    }
+  }
+
+  // the four waves' sums
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    w.sum[r] += __shfl_xor(w.sum[r], 16);
+    w.sum[r] += __shfl_xor(w.sum[r], 32);
+    if (q4 == 0) s_sum[wave][16 * r + n] = w.sum[r], s_ref[wave][16 * r + n] = w.ref[r];
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    if (r > 0) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4*>(&s_o[wave][n * 128 + 16 * c + 4 * q4]) = w.o[r][c];
+    __syncthreads();
+    const int j = tid >> 4, row = (rb * RT + r) * 16 + j, t = row / P.g;
+    const int64_t at = s.row + t;
+    if (row < rows && at >= 0 && at < P.r.n_rows) {
+      float ref = NO_REF, sum = 0.0f, f[4], x[8] = {};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ref = fmaxf(ref, s_ref[i][16 * r + j]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[i] = __builtin_amdgcn_exp2f(s_ref[i][16 * r + j] - ref);
+        sum += f[i] * s_sum[i][16 * r + j];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += f[i] * s_o[i][j * 128 + (tid & 15) * 8 + e];
+      }
+      const int head = h * P.g + row % P.g, c0 = (tid & 15) * 8;
+      if (P.splits == 1) {
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= inv;
+        const int64_t to = (at * P.hq + head) * D + c0;
+        if (P.out_f32) {
+          float* out = reinterpret_cast<float*>(P.out) + to;
+          *reinterpret_cast<f32x4*>(out) = f32x4{x[0], x[1], x[2], x[3]};
+          *reinterpret_cast<f32x4*>(out + 4) = f32x4{x[4], x[5], x[6], x[7]};
+        } else {
+          Op y;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = x[e];
+          *reinterpret_cast<Op*>(reinterpret_cast<uint16_t*>(P.out) + to) = y;
+        }
+      } else {
+        float* ws = P.ws + ((((int64_t)b * P.r.T + t) * P.hq + head) * P.splits + split) * 130;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) *reinterpret_cast<float2*>(ws + c0 + e) = make_float2(x[e], x[e + 1]);
+        if (c0 == 0) *reinterpret_cast<float2*>(ws + 128) = make_float2(sum, ref);
+      }
+    }
+  }
+}
+
+// Joins the splits of a row: a wave a row and query head.
+template <bool F16> __global__ __launch_bounds__(256) void oscar_q8_join_kernel(AttnParams P) {
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);   // [sequence][new token][head]
+  const int head = unit % P.hq, t = unit / P.hq % P.r.T;
+  const int64_t b = unit / P.hq / P.r.T;
+  if (b >= P.c.batch) return;
+  const Q8Seq s = q8_seq(P.r, b);
+  const int64_t at = s.row + t;
+  if (t >= s.n || at < 0 || at >= P.r.n_rows) return;
+  const float* ws = P.ws + unit * P.splits * 130;
+  float ref = NO_REF;
+  for (int i = lane; i < P.splits; i += 64) ref = fmaxf(ref, ws[i * 130 + 129]);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) ref = fmaxf(ref, __shfl_xor(ref, d));
+  float sum = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll 8
+  for (int i = 0; i < P.splits; ++i) {
+    const float f = __builtin_amdgcn_exp2f(ws[i * 130 + 129] - ref);
+    const float2 o = *reinterpret_cast<const float2*>(ws + i * 130 + 2 * lane);
+    sum += f * ws[i * 130 + 128];
+    x += f * o.x;
+    y += f * o.y;
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  x *= inv, y *= inv;
+  const int64_t to = (at * P.hq + head) * D + 2 * lane;
+  if (P.out_f32) {
+    *reinterpret_cast<float2*>(reinterpret_cast<float*>(P.out) + to) = make_float2(x, y);
+  } else if constexpr (F16) {
+    *reinterpret_cast<f16x2*>(reinterpret_cast<uint16_t*>(P.out) + to) = f16x2{(_Float16)x, (_Float16)y};
+  } else {
+    *reinterpret_cast<bf16x2*>(reinterpret_cast<uint16_t*>(P.out) + to) = bf16x2{(__bf16)x, (__bf16)y};
+  }
+}
+
+// Tiles of 16 rows a workgroup.
+int row_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+
+template <bool F16> void launch(const AttnParams& P, int rt, uint32_t grid, hipStream_t st) {
+  if (rt == 1)
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 1>), dim3(grid), dim3(256), 0, st, P);
+  else if (rt == 2)
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 2>), dim3(grid), dim3(256), 0, st, P);
+  else
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 4>), dim3(grid), dim3(256), 0, st, P);
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool heads_fit(const oscar_q8_cache* c, int32_t hq) {
+  return hq >= 1 && hq % c->n_kv_heads == 0 && hq / c->n_kv_heads <= OSCAR_Q8_MAX_GROUP;
+}
+
+}  // namespace
+
+extern "C" int32_t oscar_q8_auto_splits(const oscar_q8_cache* cache, int32_t n_q_heads, int32_t T, int32_t max_seq_len) {
+  if (oscar_check_q8_sizes(cache) != OSCAR_OK || !heads_fit(cache, n_q_heads) || T < 1 || max_seq_len < 1) return 1;
+  const int64_t rows = (int64_t)T * (n_q_heads / cache->n_kv_heads);
+  const int rt = row_tiles(rows);
+  const int64_t units = (int64_t)cache->batch * cache->n_kv_heads * ((rows + 16 * rt - 1) / (16 * rt));
+  const int64_t pages = (max_seq_len + OSCAR_R - 1) / OSCAR_R;
+  // two workgroups a compute unit, two pages each at least
+  const int64_t splits = (2 * (int64_t)oscar_compute_units() + units - 1) / units;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({splits, (pages + 1) / 2, 512}));
+}
+
+extern "C" size_t oscar_q8_workspace_bytes(const oscar_q8_cache* cache, int32_t n_q_heads, int32_t T, int32_t num_splits) {
+  if (oscar_check_q8_sizes(cache) != OSCAR_OK || !heads_fit(cache, n_q_heads) || T < 1 || num_splits <= 1) return 0;
+  return (size_t)cache->batch * T * n_q_heads * num_splits * 130 * sizeof(float);
+}
+
+extern "C" int oscar_q8_attn(const void* q, int64_t q_stride, int64_t n_rows, int32_t n_q_heads, int32_t T,
+                             const int32_t* row_starts, const int32_t* new_lens, const int32_t* lens,
+                             const oscar_q8_cache* cache, void* out, int32_t out_dtype, float softmax_scale,
+                             int32_t max_seq_len_hint, int32_t num_splits, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  const int rc = oscar_check_q8_cache(cache);
+  if (rc != OSCAR_OK) return rc;
+  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0) return OSCAR_ERR_INVALID_ARG;
+  if (!heads_fit(cache, n_q_heads)) return OSCAR_ERR_UNSUPPORTED;
+  if (out_dtype != OSCAR_F32 && out_dtype != cache->io_dtype) return OSCAR_ERR_INVALID_ARG;
+  if (T < 0 || n_rows < 0 || max_seq_len_hint < 0 || num_splits < 0 || num_splits > 512) return OSCAR_ERR_INVALID_ARG;
+  if (T == 0 || n_rows == 0) return OSCAR_OK;
+  if (!q || !lens || !out || !aligned16(q) || !aligned16(out)) return OSCAR_ERR_INVALID_ARG;
+  if (q_stride < (int64_t)n_q_heads * OSCAR_D || q_stride % 8 != 0) return OSCAR_ERR_INVALID_ARG;
+  const int splits = num_splits ? num_splits : oscar_q8_auto_splits(cache, n_q_heads, T, max_seq_len_hint);
+  const int g = n_q_heads / cache->n_kv_heads;
+  const int64_t rows = (int64_t)T * g;
+  if (rows > INT32_MAX / 2) return OSCAR_ERR_INVALID_ARG;
+  const int rt = row_tiles(rows);
+  const int64_t row_blocks = (rows + 16 * rt - 1) / (16 * rt), units = (int64_t)cache->batch * cache->n_kv_heads * splits;
+  const int64_t grid = row_blocks == 1 ? units : (units + 7) / 8 * 8 * row_blocks;
+  const int64_t join = ((int64_t)cache->batch * T * n_q_heads + 3) / 4;
+  // a grid's threads are counted in 32 bits
+  if (row_blocks > INT32_MAX / 8 || grid * 256 > UINT32_MAX || (splits > 1 && join * 256 > UINT32_MAX)) return OSCAR_ERR_INVALID_ARG;
+  if (splits > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < oscar_q8_workspace_bytes(cache, n_q_heads, T, splits)))
+    return OSCAR_ERR_WORKSPACE;
+  AttnParams P = {};
+  P.c = q8_device_view(cache);
+  P.r = {row_starts, new_lens, lens, T, n_rows};
+  P.q = reinterpret_cast<const uint16_t*>(q);
+  P.q_stride = q_stride;
+  P.out = out;
+  P.ws = reinterpret_cast<float*>(workspace);
+  P.scale_log2 = (softmax_scale > 0.0f ? softmax_scale : 0.08838834764831845f) * 1.4426950408889634f;
+  P.hq = n_q_heads;
+  P.g = g;
+  P.splits = splits;
+  P.row_blocks = (int)row_blocks;
+  P.out_f32 = out_dtype == OSCAR_F32;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const bool f16 = cache->io_dtype == OSCAR_F16;
+  f16 ? launch<true>(P, rt, (uint32_t)grid, st) : launch<false>(P, rt, (uint32_t)grid, st);
+  if (splits > 1) {
+    if (f16)
+      hipLaunchKernelGGL((oscar_q8_join_kernel<true>), dim3((uint32_t)join), dim3(256), 0, st, P);
+    else
+      hipLaunchKernelGGL((oscar_q8_join_kernel<false>), dim3((uint32_t)join), dim3(256), 0, st, P);
+  }
+  if (hipGetLastError() != hipSuccess) return OSCAR_ERR_HIP;
+  return OSCAR_OK;
+}
