@@ -622,10 +622,15 @@ int oscar_q8_read(const oscar_q8_cache *cache, const int32_t *lens, const int32_
  *   tokens : device int32 [batch]
  *   probs  : device fp32 [batch][vocab], or NULL: what each token was drawn with (0 for those that do not
  *            stay), as oscar_verify_drafts takes it
- * Weights and sums are in 64 bits.  vocab <= OSCAR_VERIFY_MAX_VOCAB.  One launch. */
+ *   workspace : at least oscar_sample_workspace_bytes(...), 16-byte aligned; its contents do not matter.  Calls
+ *            that share one must be ordered
+ * Weights and sums are in 64 bits; the same call gives the same bits every time.  batch <= 65535, vocab <=
+ * OSCAR_VERIFY_MAX_VOCAB.  Two launches, one more with filters and one more with probs. */
+size_t oscar_sample_workspace_bytes(int32_t batch, int32_t vocab);
 int oscar_sample(const void *logits, int64_t row_stride, int32_t batch, int32_t vocab, int32_t dtype,
                  const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
-                 const float *u, int32_t *tokens, float *probs, void *stream);
+                 const float *u, int32_t *tokens, float *probs, void *workspace, size_t workspace_bytes,
+                 void *stream);
 
 /* Test/debug: copy sequence b, kv head h back to the HOST in a layout-free
  * form (one code per byte). Synchronizes `stream`. Host outputs, each may be

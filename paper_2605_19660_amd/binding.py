@@ -36,7 +36,7 @@ EXPORTS = ("oscar_version", "oscar_status_string", "oscar_cache_sizes",
            "oscar_draft_auto_splits", "oscar_draft_workspace_bytes", "oscar_draft_attn",
            "oscar_verify_workspace_bytes", "oscar_verify_drafts", "oscar_plan_step", "oscar_q8_sizes",
            "oscar_q8_append", "oscar_q8_auto_splits", "oscar_q8_workspace_bytes", "oscar_q8_attn",
-           "oscar_q8_read", "oscar_sample")
+           "oscar_q8_read", "oscar_sample_workspace_bytes", "oscar_sample")
 
 
 class OscarError(RuntimeError):
@@ -164,7 +164,9 @@ def lib():
     L.oscar_q8_read.restype = C.c_int
     L.oscar_q8_read.argtypes = [q8, vp, vp, i32, vp, vp, i32, vp]
     L.oscar_sample.restype = C.c_int
-    L.oscar_sample.argtypes = [vp, i64, i32, i32, i32] + [vp] * 8
+    L.oscar_sample.argtypes = [vp, i64, i32, i32, i32] + [vp] * 8 + [sz, vp]
+    L.oscar_sample_workspace_bytes.restype = sz
+    L.oscar_sample_workspace_bytes.argtypes = [i32, i32]
     _lib = L
     return L
 
@@ -935,26 +937,35 @@ def _f32_ptr(t, n: int):
     return t.data_ptr()
 
 
-def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=False, stream=None):
+def sample_workspace_bytes(batch: int, vocab: int) -> int:
+    return int(lib().oscar_sample_workspace_bytes(batch, vocab))
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=False, workspace=None, stream=None):
     """oscar_sample: logits [batch, vocab] of any distance between rows; u, temperature, top_p, min_p fp32 [batch], top_k
     int32 [batch].  Returns (tokens int32 [batch], probabilities fp32 [batch, vocab] or None): probs is True, False or
     the tensor that takes them."""
     import torch
     if stream is not None:
         with torch.cuda.stream(stream):
-            return sample(logits, u, temperature, top_k, top_p, min_p, tokens, probs)
+            return sample(logits, u, temperature, top_k, top_p, min_p, tokens, probs, workspace)
     batch, vocab = logits.shape
     if probs is True:
         probs = torch.empty((batch, vocab), dtype=torch.float32, device=logits.device)
     elif probs is False:
         probs = None
-    _here(logits, u, temperature, top_k, top_p, min_p, tokens, probs)
-    assert vocab == 0 or logits.stride(1) == 1 or vocab == 1
+    _here(logits, u, temperature, top_k, top_p, min_p, tokens, probs, workspace)
+    assert logits.stride(1) == 1 or vocab == 1
+    L = lib()
     if tokens is None:
         tokens = torch.empty(batch, dtype=torch.int32, device=logits.device)
-    rc = lib().oscar_sample(logits.data_ptr(), logits.stride(0), batch, vocab, dtype_code(logits.dtype),
+    if workspace is None:
+        workspace = torch.empty(L.oscar_sample_workspace_bytes(batch, vocab), dtype=torch.uint8, device=logits.device)
+    assert workspace.is_contiguous()
+    rc = L.oscar_sample(logits.data_ptr(), logits.stride(0), batch, vocab, dtype_code(logits.dtype),
                             _f32_ptr(temperature, batch), _int32_ptr(top_k, batch), _f32_ptr(top_p, batch), _f32_ptr(min_p, batch),
-                            _f32_ptr(u, batch), _int32_ptr(tokens, batch), _f32_ptr(probs, batch * vocab), _stream_ptr(None))
+                            _f32_ptr(u, batch), _int32_ptr(tokens, batch), _f32_ptr(probs, batch * vocab), workspace.data_ptr(),
+                            workspace.numel() * workspace.element_size(), _stream_ptr(None))
     if rc != OK:
         _check(rc, "oscar_sample")
     return tokens, probs

@@ -6,16 +6,23 @@
 //
 // Every filter keeps a prefix of that order, so that what stays is everything from one pair (logit, index) on: the pair
 // is held as one 64-bit number, (logit as an ordered integer, ~index), and the search is for that number, the cut.
-// Weights are worked out in 64 bits.  Where many are added by atomics they count as multiples of 2^-(62 - log2 of
-// the vocabulary): whole numbers, so that no order of additions changes a bit.
+// Weights are worked out in 64 bits.  Where many are added by atomics they count as whole multiples of a power of two
+// (2^-48 of a chunk's largest and less), so that no order of additions changes a bit.
 //
-// A workgroup of 16 waves takes a row.
-//  - top_k up to 1024: each thread knows the largest of its logits, and the k-th largest of the 1024 is no larger
-//    than the k-th largest of all.  What lies above it (some more than k) goes to LDS and is sorted there.
-//  - else the cut is searched by a histogram over the distance to the largest logit (equal steps, which spreads
-//    a row over the bins, as the bits of the numbers would not); the bin that holds the cut goes to LDS and is sorted.
-//    A bin that does not fit is split by the bits of its numbers until it does or holds one number only.
-// What bounds it: the 64-bit exponentials of one CU where no top_k spares them, else latency.
+// A row is taken in chunks, so that few rows still fill the chip, and logits lie in bins of equal steps (at most
+// temperature * 45 / 1024), counted from 0 so that chunks' bins lie on one grid:
+//   1. every chunk: its largest logit, and the running sums (of tokens for top_k, else of weights, in 64 bits) over
+//      the 1024 bins below it;
+//   2. every chunk: adds up the row's running sums, each chunk's shifted by whole bins and scaled by one factor, finds the
+//      bins in which the cuts lie, and puts its logits in those (with top_k: in those and above) on the row's list;
+//   3. a workgroup a row: sorts the list, finds the cut in it, what stays of every chunk (running sums above the list,
+//      the list's members one by one), the chunk the token is in, and in it the token;
+//   4. with probs, every chunk: its probabilities.
+// A row whose list does not fit (thousands of equal logits at the cut) or with a top_k past 1024 is searched by
+// one workgroup, which splits bins until they fit or hold one number.
+//
+// What bounds it: latency of three or four launches; for many long rows reading them two or three times (the second
+// time out of the caches) and the exponentials.
 #include "oscar_common.h"
 
 namespace {
@@ -24,15 +31,33 @@ constexpr int THREADS = 1024, WAVES = 16;
 constexpr int BINS = 1024;
 constexpr int CAP = 4096;                  // numbers sorted in LDS
 constexpr uint32_t DEAD = 0x007fffffu;     // key of -inf
+constexpr int CHUNK_BITS = 48;             // binary places of a weight in a chunk's sums (2^14 of them at most)
+constexpr int LIST_BITS = 50;              // of a member of the list (2^12)
+
+// What the second and third launch leave of a row.
+struct RowState {
+  uint32_t n;         // members of the list
+  int lo, hi;         // bins on the list
+  int kind;           // of what stays: see the third launch
+  double above, total;   // weights above the list, and of all
+  uint64_t cut;
+  double sum;         // weights of what stays
+};
+enum { ONE_TOKEN, NO_TOKEN, BY_CUT, DONE };
 
 struct SampleParams {
   const void* logits;
   int64_t stride;
-  int V, fixed;        // vocabulary; binary places of a weight that is added by atomics
+  int V, fixed;        // vocabulary; binary places of a weight in sums over a row
+  int chunks, chunk;   // of a row, and their size
   const float *temperature, *top_p, *min_p, *u;
   const int32_t* top_k;
   int32_t* tokens;
   float* probs;
+  uint64_t* best;      // [batch][chunks]: place of the largest logit
+  uint64_t* cum;       // [batch][chunks][BINS]: running sums
+  RowState* rows;      // [batch]
+  uint64_t* list;      // [batch][CAP]
 };
 
 // Ordered integers: equal for equal numbers (both zeros are one), DEAD for -inf and NaN.
@@ -45,6 +70,28 @@ __device__ __forceinline__ float number_of(uint32_t key) {
   return __uint_as_float(key ^ (key >> 31 ? 0x80000000u : 0xffffffffu));
 }
 __device__ __forceinline__ uint64_t place_of(uint32_t key, int i) { return (uint64_t)key << 32 | (uint32_t)~i; }
+
+// exp(y), y <= 0 or a little above, to 2^-51 of itself: 2^n 2^f with |f| <= 1/2, the series of 2^f = exp(f ln 2) up to
+// f^13 (the next term is below 2^-57).
+__device__ __forceinline__ double exp64(double y) {
+  const double z = fmax(y * 1.4426950408889634, -1200.0);
+  const double n = __builtin_rint(z), x = (z - n) * 0.6931471805599453;
+  double s = 1.0 / 6227020800.0;
+  s = fma(s, x, 1.0 / 479001600.0);
+  s = fma(s, x, 1.0 / 39916800.0);
+  s = fma(s, x, 1.0 / 3628800.0);
+  s = fma(s, x, 1.0 / 362880.0);
+  s = fma(s, x, 1.0 / 40320.0);
+  s = fma(s, x, 1.0 / 5040.0);
+  s = fma(s, x, 1.0 / 720.0);
+  s = fma(s, x, 1.0 / 120.0);
+  s = fma(s, x, 1.0 / 24.0);
+  s = fma(s, x, 1.0 / 6.0);
+  s = fma(s, x, 0.5);
+  s = fma(s, x, 1.0);
+  s = fma(s, x, 1.0);
+  return __builtin_amdgcn_ldexp(s, (int)n);
+}
 
 template <typename T> __device__ __forceinline__ T shfl_up_any(T v, int d) {
   const uint64_t bits = __builtin_bit_cast(uint64_t, v);
@@ -130,7 +177,7 @@ template <typename E> struct Row {
   double top, inv_t;
   int fixed;
   __device__ __forceinline__ uint32_t key(int i) const { return key_of(to_f32<E>(x[i])); }
-  __device__ __forceinline__ double weight(uint32_t k) const { return exp(((double)number_of(k) - top) * inv_t); }
+  __device__ __forceinline__ double weight(uint32_t k) const { return exp64(((double)number_of(k) - top) * inv_t); }
   __device__ __forceinline__ uint64_t whole(double w) const { return (uint64_t)(w * (double)(1ull << fixed) + 0.5); }
 };
 
@@ -303,94 +350,16 @@ __device__ void search_cut(Shared& S, const Row<E>& row, Search& q, double share
   __syncthreads();
 }
 
-template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_kernel(SampleParams P) {
-  __shared__ Shared S;
-  const int b = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6, V = P.V;
-  Row<E> row;
-  row.x = reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride;
-  row.V = V;
-  row.fixed = P.fixed;
+// A row by one workgroup, whatever its list would be.
+template <typename E> __device__ void whole_row(Shared& S, const SampleParams& P, const Row<E>& row, int b, int k, float p, float m, double from0) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, V = P.V;
   float* probs = P.probs ? P.probs + (int64_t)b * V : nullptr;
-
-  // the largest logit, every thread's largest, and the lowest above -inf
-  uint64_t best = 0;
   uint32_t least = 0xffffffffu;
 #pragma unroll 8
   for (int i = t; i < V; i += THREADS) {
     const uint32_t key = row.key(i);
-    const uint64_t at = place_of(key, i);
-    best = at > best ? at : best;
     least = key > DEAD ? min(least, key) : least;
   }
-  const uint32_t mine = (uint32_t)(best >> 32);
-  best = group_max(best, S.wave64);
-  const uint32_t top_key = (uint32_t)(best >> 32);
-  const bool any = top_key > DEAD;
-  const float temp = P.temperature ? P.temperature[b] : 1.0f;
-  const float p = P.top_p ? P.top_p[b] : 1.0f, m = P.min_p ? P.min_p[b] : 0.0f;
-  const int k = P.top_k ? P.top_k[b] : 0;
-  const float u = P.u[b];
-  if (!any || !(temp > 0.0f) || k == 1 || m > 1.0f || p <= 0.0f) {   // one token, or none
-    const int token = any ? (int)~(uint32_t)best : 0;
-    if (probs)
-      for (int i = t; i < V; i += THREADS) probs[i] = any && i == token ? 1.0f : 0.0f;
-    if (t == 0) P.tokens[b] = token;
-    return;
-  }
-  row.top = (double)number_of(top_key);
-  row.inv_t = 1.0 / (double)temp;
-  const double from0 = u > 0.0f ? (double)u : 0.0;
-
-  bool few = k > 0 && k <= THREADS;   // (of what can stay)
-  if (few) {
-    uint32_t bound = 0;   // the k-th largest of the threads' largest
-#pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t next = bound | 1u << bit;
-      if (__syncthreads_count(mine >= next) >= k) bound = next;
-    }
-    bound = max(bound, DEAD + 1);
-    if (t == 0) S.n = 0;
-    __syncthreads();
-#pragma unroll 8
-    for (int i = t; i < V; i += THREADS) {
-      const uint32_t key = row.key(i);
-      if (key >= bound) {
-        const uint32_t at = atomicAdd(&S.n, 1u);
-        if (at < CAP) S.list[at] = place_of(key, i);
-      }
-    }
-    if (probs)
-      for (int i = t; i < V; i += THREADS) probs[i] = 0.0f;
-    __syncthreads();
-    few = S.n <= CAP;
-  }
-  if (few) {
-    int n = (int)S.n;
-    sort_list(S.list, n);
-    n = min(n, k);   // (up to 1024: a token a thread)
-    const uint64_t at = t < n ? S.list[t] : 0;
-    const double w = t < n ? row.weight((uint32_t)(at >> 32)) : 0.0;
-    double sum;
-    const double before = group_scan(w, S.wave_f, &sum) - w;
-    const bool stays = t < n && (t == 0 || ((!(p < 1.0f) || before < (double)p * sum) && !(w < (double)m)));
-    n = __syncthreads_count(stays);
-    // in order of the index
-    if (t < n) S.list[t] = ~((uint64_t)(uint32_t)~(uint32_t)at << 32 | (uint32_t)(at >> 32));
-    __syncthreads();
-    sort_list(S.list, n);
-    const uint64_t x = t < n ? ~S.list[t] : 0;
-    const double y = t < n ? row.weight((uint32_t)x) : 0.0;
-    const double upto = group_scan(y, S.wave_f, &sum);
-    if (t == 0) S.found = n - 1;
-    __syncthreads();
-    if (t < n && upto > from0 * sum) atomicMin(&S.found, t);
-    __syncthreads();
-    if (t == S.found) P.tokens[b] = (int)(x >> 32);
-    if (probs && t < n) probs[x >> 32] = (float)(y / sum);
-    return;
-  }
-
   Search q = {false, 0.0, (uint64_t)(DEAD + 1) << 32};
   const float lowest = number_of(~(uint32_t)group_max((uint32_t)~least, S.wave64));
   if (k > 0 && k < V) {
@@ -452,27 +421,423 @@ template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_ke
     for (int i = t; i < V; i += THREADS) probs[i] = (float)(weight_at(i) / sum);
 }
 
+// How a row is drawn.
+struct Settings {
+  float temp, p, m;
+  int k;
+  double u;
+  bool one;       // the largest logit
+  bool by_count;  // top_k that fits the list: bins count tokens
+  bool whole;     // top_k that does not: one workgroup
+  bool cuts;      // else: whether top_p or min_p cut
+  float grid;     // bins a unit
+};
+__device__ __forceinline__ Settings settings(const SampleParams& P, int b) {
+  Settings s;
+  s.temp = P.temperature ? P.temperature[b] : 1.0f;
+  s.p = P.top_p ? P.top_p[b] : 1.0f;
+  s.m = P.min_p ? P.min_p[b] : 0.0f;
+  s.k = P.top_k ? P.top_k[b] : 0;
+  const float u = P.u[b];
+  s.u = u > 0.0f ? (double)u : 0.0;
+  s.one = !(s.temp > 0.0f) || s.k == 1 || s.m > 1.0f || s.p <= 0.0f;
+  s.by_count = s.k > 0 && s.k <= THREADS;
+  s.whole = !s.by_count && s.k > 0 && s.k < P.V;
+  s.cuts = s.p < 1.0f || s.m > 0.0f;
+  // weights fall to 2^-64 over the bins, or logits by 64, whichever is less: a high temperature spreads weights over
+  // few of the former
+  s.grid = BINS / fminf(fmaxf(45.0f * s.temp, 1e-25f), 64.0f);
+  return s;
+}
+// The grid's cell of a logit; cells fall with it.
+__device__ __forceinline__ int cell_of(float x, float grid) { return -(int)floorf(__builtin_amdgcn_fmed3f(x * grid, -0x1p30f, 0x1p30f)); }
+// Cells are narrower than a float's steps from 2^24 on.  A row whose largest logit is past ROW_GRID is searched by one
+// workgroup; a chunk whose largest is past CHUNK_GRID has everything in its last bin (far below such a row's bins).
+constexpr float ROW_GRID = 0x1p21f, CHUNK_GRID = 0x1p22f;
+__device__ __forceinline__ bool on_grid(float top, float grid, float end) { return fabsf(top * grid) < end; }
+// What a chunk's weights are relative to: no less than its largest logit, but for rounding, and one number for a cell.
+__device__ __forceinline__ double reference_of(float top, float grid) {
+  return on_grid(top, grid, CHUNK_GRID) ? (double)(1 - cell_of(top, grid)) / (double)grid : (double)top;
+}
+
+// A chunk's logits, a thread's 1024 apart; 0 behind the row's end.
+template <typename E, int PER> __device__ __forceinline__ void load_keys(const SampleParams& P, int b, int c, uint32_t* key) {
+  const E* x = reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride;
+  const int i0 = c * (PER * THREADS) + threadIdx.x;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) key[e] = i0 + e * THREADS < P.V ? key_of(to_f32<E>(x[i0 + e * THREADS])) : 0;
+}
+
+template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_sample_bins_kernel(SampleParams P) {
+  __shared__ uint64_t s_bin[BINS], s_wave[WAVES];
+  const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
+  uint32_t key[PER];
+  load_keys<E, PER>(P, b, c, key);
+  uint64_t best = 0;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    const uint64_t at = place_of(key[e], c * (PER * THREADS) + e * THREADS + t);
+    best = at > best ? at : best;
+  }
+  s_bin[t] = 0;
+  best = group_max(best, s_wave);
+  const int64_t chunk = (int64_t)b * P.chunks + c;
+  if (t == 0) {
+    P.best[chunk] = best;
+    if (c == 0) P.rows[b].n = 0;
+  }
+  const Settings s = settings(P, b);
+  const float top = number_of((uint32_t)(best >> 32));
+  if (s.one || s.whole || (uint32_t)(best >> 32) <= DEAD) return;
+  const int first = on_grid(top, s.grid, CHUNK_GRID) ? cell_of(top, s.grid) : -(1 << 30) - BINS;
+  uint64_t mine = 0;   // the last bin's, and without cuts everything
+  if (s.by_count) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      if (key[e] <= DEAD) continue;
+      const int bin = min(cell_of(number_of(key[e]), s.grid) - first, BINS - 1);
+      if (bin == BINS - 1) ++mine; else atomicAdd(reinterpret_cast<uint32_t*>(&s_bin[bin]), 1u);
+    }
+  } else {
+    const double ref = reference_of(top, s.grid), inv_t = 1.0 / (double)s.temp;
+#pragma unroll 4
+    for (int e = 0; e < PER; ++e) {
+      if (key[e] <= DEAD) continue;
+      const float x = number_of(key[e]);
+      const uint64_t w = (uint64_t)(exp64(((double)x - ref) * inv_t) * (double)(1ull << CHUNK_BITS) + 0.5);
+      const int bin = s.cuts ? min(cell_of(x, s.grid) - first, BINS - 1) : BINS - 1;
+      if (bin == BINS - 1) mine += w; else atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[bin]), (unsigned long long)w);
+    }
+  }
+  if (mine) atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[BINS - 1]), (unsigned long long)mine);
+  __syncthreads();
+  uint64_t all;
+  P.cum[chunk * BINS + t] = group_scan(s_bin[t], s_wave, &all);
+}
+
+// A row's chunks on one grid: every chunk's first bin in the row's, and what its sums are multiplied by.
+struct Chunks {
+  int shift[THREADS];      // -1: the chunk has no logit above -inf
+  double scale[THREADS];
+};
+// The row's largest logit (its place), by the workgroup; fills G.
+__device__ __forceinline__ uint64_t row_top(const SampleParams& P, int b, uint64_t* s_wave) {
+  const int t = threadIdx.x;
+  return group_max(t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0, s_wave);
+}
+__device__ __forceinline__ void place_chunks(const SampleParams& P, const Settings& s, int b, float top, Chunks& G) {
+  const int t = threadIdx.x;
+  if (t < P.chunks) {
+    const uint32_t key = (uint32_t)(P.best[(int64_t)b * P.chunks + t] >> 32);
+    const int first = cell_of(number_of(key), s.grid);
+    G.shift[t] = key > DEAD ? first - cell_of(top, s.grid) : -1;
+    G.scale[t] = s.by_count ? 1.0 : exp64((reference_of(number_of(key), s.grid) - (double)top) / (double)s.temp) / (double)(1ull << CHUNK_BITS);
+  }
+  __syncthreads();
+}
+// A chunk's running sum up to the row's bin.
+__device__ __forceinline__ double chunk_upto(const SampleParams& P, const Chunks& G, int64_t row_chunk, int c, int bin) {
+  const int own = bin - G.shift[c];
+  if (G.shift[c] < 0 || (own < 0 && bin != BINS - 1)) return 0.0;
+  return (double)P.cum[(row_chunk + c) * BINS + (bin == BINS - 1 ? BINS - 1 : own)] * G.scale[c];
+}
+
+template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_sample_list_kernel(SampleParams P) {
+  __shared__ Chunks G;
+  __shared__ uint64_t s_wave[WAVES];
+  __shared__ double s_cum[BINS];
+  __shared__ int s_bin;
+  __shared__ uint32_t s_base;
+  const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
+  const Settings s = settings(P, b);
+  if (s.one || s.whole || (!s.by_count && !s.cuts)) return;
+  const uint32_t top_key = (uint32_t)(row_top(P, b, s_wave) >> 32);
+  const float top = number_of(top_key);
+  if (top_key <= DEAD || !on_grid(top, s.grid, ROW_GRID)) return;
+  place_chunks(P, s, b, top, G);
+  double upto = 0.0;
+#pragma unroll 8
+  for (int q = 0; q < P.chunks; ++q) upto += chunk_upto(P, G, (int64_t)b * P.chunks, q, t);
+  s_cum[t] = upto;
+  if (t == 0) s_bin = BINS - 1;
+  __syncthreads();
+  const double total = s_cum[BINS - 1];
+  int lo = BINS, hi = -1;
+  if (s.by_count || s.p < 1.0f) {
+    const double target = s.by_count ? fmin((double)s.k, total) : (double)s.p * total;
+    if (upto >= target) atomicMin(&s_bin, t);
+    __syncthreads();
+    hi = s_bin;
+    lo = s.by_count ? 0 : hi;
+  }
+  if (!s.by_count && s.m > 0.0f) {
+    // the bins in which weights pass min_p, a little more on either side
+    const double x = (double)top + (double)s.temp * log((double)s.m), off = 1e-6 * (fabs((double)top) + fabs(x) + (double)s.temp);
+    const int first = cell_of(top, s.grid);
+    int from = 0, to = BINS - 1;
+    if (fabs(x) < 3e38) {   // (not at a temperature without end)
+      from = max(min(cell_of((float)(x + off), s.grid) - first, BINS - 1), 0);
+      to = max(min(cell_of((float)(x - off), s.grid) - first, BINS - 1), 0);
+    }
+    if (to < lo)
+      lo = from, hi = to;      // min_p cuts before top_p does
+    else if (from <= hi)
+      lo = min(lo, from), hi = max(hi, to);
+  }
+  if (c == 0 && t == 0) {
+    RowState& r = P.rows[b];
+    r.lo = lo;
+    r.hi = hi;
+    r.above = lo > 0 ? s_cum[lo - 1] : 0.0;
+    r.total = total;
+  }
+
+  uint32_t key[PER];
+  load_keys<E, PER>(P, b, c, key);
+  const int first = cell_of(top, s.grid);
+  uint32_t on = 0;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    const int bin = min(cell_of(number_of(key[e]), s.grid) - first, BINS - 1);
+    on |= (key[e] > DEAD && bin >= lo && bin <= hi ? 1u : 0u) << e;
+  }
+  uint64_t all;
+  const uint64_t mine = __popc(on);
+  uint32_t at = (uint32_t)(group_scan(mine, s_wave, &all) - mine);
+  if (t == 0 && all) s_base = atomicAdd(&P.rows[b].n, (uint32_t)all);
+  __syncthreads();
+  if (!all) return;
+  at += s_base;
+#pragma unroll
+  for (int e = 0; e < PER; ++e)
+    if (on >> e & 1) {
+      if (at < CAP) P.list[(int64_t)b * CAP + at] = place_of(key[e], c * (PER * THREADS) + e * THREADS + t);
+      ++at;
+    }
+}
+
+template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_pick_kernel(SampleParams P) {
+  __shared__ Shared S;
+  __shared__ Chunks G;
+  const int b = blockIdx.x, t = threadIdx.x, V = P.V;
+  const Settings s = settings(P, b);
+  const uint64_t best = row_top(P, b, S.wave64);
+  const uint32_t top_key = (uint32_t)(best >> 32);
+  RowState& R = P.rows[b];
+  if (top_key <= DEAD || s.one) {
+    if (t == 0) {
+      P.tokens[b] = top_key <= DEAD ? 0 : (int)~(uint32_t)best;
+      R.kind = top_key <= DEAD ? NO_TOKEN : ONE_TOKEN;
+    }
+    return;
+  }
+  const float top = number_of(top_key);
+  Row<E> row = {reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride, V, (double)top, 1.0 / (double)s.temp, P.fixed};
+  const bool listed = s.by_count || s.cuts;
+  const int n = listed ? (int)min(R.n, (uint32_t)CAP + 1) : 0;
+  if (s.whole || !on_grid(top, s.grid, ROW_GRID) || n > CAP) {
+    if (t == 0) R.kind = DONE;
+    whole_row<E>(S, P, row, b, s.k, s.p, s.m, s.u);
+    return;
+  }
+
+  // the cut
+  uint64_t cut = (uint64_t)(DEAD + 1) << 32;
+  if (listed) {
+    for (int i = t; i < n; i += THREADS) S.list[i] = P.list[(int64_t)b * CAP + i];
+    __syncthreads();
+    sort_list(S.list, n);
+  }
+  if (s.by_count) {
+    const int few = min(n, s.k);   // (up to 1024: a token a thread)
+    const uint64_t at = t < few ? S.list[t] : 0;
+    const double w = t < few ? row.weight((uint32_t)(at >> 32)) : 0.0;
+    double sum;
+    const double before = group_scan(w, S.wave_f, &sum) - w;
+    const bool stays = t < few && (t == 0 || ((!(s.p < 1.0f) || before < (double)s.p * sum) && !(w < (double)s.m)));
+    const int left = __syncthreads_count(stays);
+    cut = S.list[left - 1];
+    __syncthreads();
+    // in order of the index
+    if (t < left) S.list[t] = ~((uint64_t)(uint32_t)~(uint32_t)at << 32 | (uint32_t)(at >> 32));
+    __syncthreads();
+    sort_list(S.list, left);
+    const uint64_t x = t < left ? ~S.list[t] : 0;
+    const double y = t < left ? row.weight((uint32_t)x) : 0.0;
+    const double upto = group_scan(y, S.wave_f, &sum);
+    if (t == 0) S.found = left - 1;
+    __syncthreads();
+    if (t < left && upto > s.u * sum) atomicMin(&S.found, t);
+    __syncthreads();
+    if (t == S.found) P.tokens[b] = (int)(x >> 32);
+    if (t == 0) R.kind = BY_CUT, R.cut = cut, R.sum = sum;
+    return;
+  }
+
+  place_chunks(P, s, b, top, G);
+  const int lo = listed ? R.lo : BINS;
+  S.mass[t] = 0;   // the list's share of every chunk
+  __syncthreads();
+  if (listed) {
+    double above = R.above;
+    const double target = (double)s.p * R.total;
+    cut = n > 0 ? S.list[0] + 1 : cut;   // (none of the list)
+    for (int i0 = 0; i0 < n; i0 += THREADS) {
+      const int i = i0 + t;
+      const uint64_t at = i < n ? S.list[i] : 0;
+      const double w = i < n ? row.weight((uint32_t)(at >> 32)) : 0.0;
+      double here;
+      const double before = above + group_scan(w, S.wave_f, &here) - w;
+      const bool stays = i < n && ((lo == 0 && i == 0) || ((!(s.p < 1.0f) || before < target) && !(w < (double)s.m)));
+      const uint64_t last = group_max(stays ? ~at : 0, S.wave64);   // the lowest place that stays
+      if (last) cut = ~last;
+      if (stays)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[(int)~(uint32_t)at / P.chunk]),
+                  (unsigned long long)(w * (double)(1ull << LIST_BITS) + 0.5));
+      above += here;
+    }
+    __syncthreads();
+  }
+  // the chunk
+  const double share = t >= P.chunks ? 0.0
+                       : (lo == 0 ? 0.0 : chunk_upto(P, G, (int64_t)b * P.chunks, t, lo - 1)) +
+                             (double)S.mass[t] / (double)(1ull << LIST_BITS);
+  double sum;
+  const double upto = group_scan(share, S.wave_f, &sum);
+  const double target = s.u * sum;
+  if (t == 0) S.found = P.chunks, S.n = 0;
+  __syncthreads();
+  if (share > 0.0) {
+    if (upto > target) atomicMin(&S.found, t);
+    atomicMax(&S.n, (uint32_t)t);
+  }
+  __syncthreads();
+  const int c = S.found < P.chunks ? S.found : (int)S.n;   // (if rounding lets none pass: the last with any weight)
+  if (t == c) S.hit = __builtin_bit_cast(uint64_t, upto - share);
+  if (t == 0) R.kind = BY_CUT, R.cut = cut, R.sum = sum, S.n = 0;
+  __syncthreads();
+  // the token, a thread's part of the chunk in one piece
+  const int per = P.chunk / THREADS, i0 = c * P.chunk + t * per;
+  const auto weight_at = [&](int i) {
+    const uint32_t key = i < V ? row.key(i) : 0;
+    if (key <= DEAD || place_of(key, i) < cut) return 0.0;
+    const double w = row.weight(key);
+    return w < (double)s.m ? 0.0 : w;   // (an empty list has no cut)
+  };
+  double part = 0.0;
+  for (int e = 0; e < per; ++e) part += weight_at(i0 + e);
+  double all;
+  double before = __builtin_bit_cast(double, S.hit) + (group_scan(part, S.wave_f, &all) - part);
+  if (t == 0) S.found = THREADS;
+  __syncthreads();
+  if (part > 0.0) {
+    if (before + part > target) atomicMin(&S.found, t);
+    atomicMax(&S.n, (uint32_t)t);
+  }
+  __syncthreads();
+  const bool passed = S.found < THREADS;
+  if (t == (passed ? S.found : (int)S.n)) {
+    int token = 0;
+    for (int e = 0; e < per; ++e) {
+      const double w = weight_at(i0 + e);
+      if (!(w > 0.0)) continue;
+      token = i0 + e;
+      before += w;
+      if (passed && before > target) break;
+    }
+    P.tokens[b] = token;
+  }
+}
+
+template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_sample_probs_kernel(SampleParams P) {
+  __shared__ uint64_t s_wave[WAVES];
+  const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
+  const RowState& R = P.rows[b];
+  const int kind = R.kind;
+  if (kind == DONE) return;
+  const uint64_t best = row_top(P, b, s_wave);
+  const Settings s = settings(P, b);
+  const double top = (double)number_of((uint32_t)(best >> 32)), inv_t = 1.0 / (double)s.temp;
+  const uint64_t cut = kind == BY_CUT ? R.cut : kind == ONE_TOKEN ? best : ~0ull;
+  const double sum = kind == BY_CUT ? R.sum : 1.0;
+  uint32_t key[PER];
+  load_keys<E, PER>(P, b, c, key);
+  float* out = P.probs + (int64_t)b * P.V;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    const int i = c * (PER * THREADS) + e * THREADS + t;
+    if (i >= P.V) break;
+    float y = 0.0f;
+    if (key[e] > DEAD && place_of(key[e], i) >= cut) {
+      const double w = exp64(((double)number_of(key[e]) - top) * inv_t);
+      y = kind == ONE_TOKEN ? 1.0f : w < (double)s.m ? 0.0f : (float)(w / sum);
+    }
+    out[i] = y;
+  }
+}
+
+// Logits of a chunk: 16384, or 4096 where that leaves the chip half empty (one row of 32000: 8 workgroups, not 2).
+int chunk_of(int32_t batch, int32_t vocab) {
+  return (int64_t)batch * ((vocab + 4095) / 4096) <= 1024 && vocab <= 4096 * THREADS ? 4096 : 16384;
+}
+
+template <typename E, int PER> void launch(const SampleParams& P, int batch, hipStream_t st) {
+  const dim3 grid(P.chunks, batch);
+  hipLaunchKernelGGL((oscar_sample_bins_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
+  if (P.top_k || P.top_p || P.min_p) hipLaunchKernelGGL((oscar_sample_list_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
+  hipLaunchKernelGGL((oscar_sample_pick_kernel<E>), dim3(batch), dim3(THREADS), 0, st, P);
+  if (P.probs) hipLaunchKernelGGL((oscar_sample_probs_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
+}
+template <typename E> void launch(const SampleParams& P, int batch, hipStream_t st) {
+  P.chunk == 4096 ? launch<E, 4>(P, batch, st) : launch<E, 16>(P, batch, st);
+}
+
 }  // namespace
+
+extern "C" size_t oscar_sample_workspace_bytes(int32_t batch, int32_t vocab) {
+  if (batch < 1 || batch > 65535 || vocab < 1 || vocab > OSCAR_VERIFY_MAX_VOCAB) return 0;
+  const size_t chunk = chunk_of(batch, vocab), chunks = (vocab + chunk - 1) / chunk;
+  return batch * (chunks * (BINS + 1) * sizeof(uint64_t) + sizeof(RowState) + CAP * sizeof(uint64_t));
+}
 
 extern "C" int oscar_sample(const void* logits, int64_t row_stride, int32_t batch, int32_t vocab, int32_t dtype,
                             const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
-                            const float* u, int32_t* tokens, float* probs, void* stream) {
+                            const float* u, int32_t* tokens, float* probs, void* workspace, size_t workspace_bytes,
+                            void* stream) {
   if (dtype != OSCAR_F32 && dtype != OSCAR_BF16 && dtype != OSCAR_F16) return OSCAR_ERR_INVALID_ARG;
-  if (batch < 0 || vocab < 1 || vocab > OSCAR_VERIFY_MAX_VOCAB || (batch > 1 && row_stride < vocab)) return OSCAR_ERR_INVALID_ARG;
-  if ((int64_t)batch * THREADS > UINT32_MAX) return OSCAR_ERR_INVALID_ARG;   // (a grid's threads are counted in 32 bits)
+  if (batch < 0 || batch > 65535 || vocab < 1 || vocab > OSCAR_VERIFY_MAX_VOCAB || (batch > 1 && row_stride < vocab))
+    return OSCAR_ERR_INVALID_ARG;
   if (batch == 0) return OSCAR_OK;
   if (!logits || !u || !tokens) return OSCAR_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == OSCAR_F32 ? 4 : 2) != 0) return OSCAR_ERR_INVALID_ARG;
-  SampleParams P = {logits, row_stride, vocab, 0, temperature, top_p, min_p, u, top_k, tokens, probs};
+  if (!workspace || workspace_bytes < oscar_sample_workspace_bytes(batch, vocab) || (reinterpret_cast<uintptr_t>(workspace) & 15) != 0)
+    return OSCAR_ERR_WORKSPACE;
+  SampleParams P = {};
+  P.logits = logits;
+  P.stride = row_stride;
+  P.V = vocab;
   P.fixed = 62;
   while ((int64_t)1 << (62 - P.fixed) < vocab) --P.fixed;
+  P.chunk = chunk_of(batch, vocab);
+  P.chunks = (vocab + P.chunk - 1) / P.chunk;
+  P.temperature = temperature;
+  P.top_p = top_p;
+  P.min_p = min_p;
+  P.u = u;
+  P.top_k = top_k;
+  P.tokens = tokens;
+  P.probs = probs;
+  P.best = reinterpret_cast<uint64_t*>(workspace);
+  P.cum = P.best + (size_t)batch * P.chunks;
+  P.list = P.cum + (size_t)batch * P.chunks * BINS;
+  P.rows = reinterpret_cast<RowState*>(P.list + (size_t)batch * CAP);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (dtype == OSCAR_F32)
-    hipLaunchKernelGGL((oscar_sample_kernel<float>), dim3(batch), dim3(THREADS), 0, st, P);
+    launch<float>(P, batch, st);
   else if (dtype == OSCAR_BF16)
-    hipLaunchKernelGGL((oscar_sample_kernel<__hip_bfloat16>), dim3(batch), dim3(THREADS), 0, st, P);
+    launch<__hip_bfloat16>(P, batch, st);
   else
-    hipLaunchKernelGGL((oscar_sample_kernel<__half>), dim3(batch), dim3(THREADS), 0, st, P);
+    launch<__half>(P, batch, st);
   if (hipGetLastError() != hipSuccess) return OSCAR_ERR_HIP;
   return OSCAR_OK;
 }

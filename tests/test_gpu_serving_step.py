@@ -29,6 +29,7 @@ class Server:
         self.k_top += torch.tensor([0, 40, 1, 0, 2000], dtype=torch.int32, device="cuda")
         self.tokens, self.probs = e(B), e(B, V, dtype=torch.float32)
         self.ws = e(ob.q8_workspace_bytes(self.layers[0], HQ, MAX_NEW, 2), dtype=torch.uint8)
+        self.sample_ws = e(ob.sample_workspace_bytes(B, V), dtype=torch.uint8)
         self.reset(torch)
 
     def reset(self, torch):
@@ -50,7 +51,8 @@ class Server:
             ob.q8_append(c, self.k[l], v, p.lens, new_lens=p.new_lens, row_starts=p.row_starts, max_new=MAX_NEW)
             ob.q8_attn(c, self.q[l], p.lens, new_lens=p.new_lens, row_starts=p.row_starts, max_new=MAX_NEW, out=self.o[l], num_splits=2,
                        workspace=self.ws)
-        ob.sample(self.logits, self.u, top_k=self.k_top, top_p=self.p_top, tokens=self.tokens, probs=self.probs)
+        ob.sample(self.logits, self.u, top_k=self.k_top, top_p=self.p_top, tokens=self.tokens, probs=self.probs,
+                  workspace=self.sample_ws)
 
 
 def wishes(rng, lens, i):

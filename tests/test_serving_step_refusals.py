@@ -121,14 +121,20 @@ def test_split_count():
         assert 1 <= s <= min(512, (n + 127) // 128)
 
 
-def sample(x=P, stride=1000, batch=2, vocab=1000, dt=ob.F32, temp=None, k=None, p=None, m=None, u=P, tokens=P, probs=None):
-    return ob.lib().oscar_sample(x, stride, batch, vocab, dt, temp, k, p, m, u, tokens, probs, None)
+def sample(x=P, stride=1000, batch=2, vocab=1000, dt=ob.F32, temp=None, k=None, p=None, m=None, u=P, tokens=P, probs=None,
+           ws=P, wb=None):
+    wb = ob.sample_workspace_bytes(batch, vocab) if wb is None else wb
+    return ob.lib().oscar_sample(x, stride, batch, vocab, dt, temp, k, p, m, u, tokens, probs, ws, wb, None)
 
 
 def test_sample_refuses():
     for kw in (dict(x=None), dict(u=None), dict(tokens=None), dict(batch=-1), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(dt=3), dict(dt=-1),
-               dict(stride=999), dict(x=P + 2), dict(x=P + 1, dt=ob.BF16), dict(batch=1 << 23)):
+               dict(stride=999), dict(x=P + 2), dict(x=P + 1, dt=ob.BF16), dict(batch=65536)):
         assert sample(**kw) == ob.ERR_INVALID_ARG, kw
+    need = ob.sample_workspace_bytes(2, 1000)
+    assert need > 0 and ob.sample_workspace_bytes(0, 5) == 0 and ob.sample_workspace_bytes(1, 0) == 0
+    for kw in (dict(ws=None), dict(ws=P + 8), dict(wb=need - 1)):
+        assert sample(**kw) == ob.ERR_WORKSPACE, kw
     assert sample(batch=0, x=None) == ob.OK
 
 
