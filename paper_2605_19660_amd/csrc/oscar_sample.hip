@@ -71,43 +71,60 @@ __device__ __forceinline__ float number_of(uint32_t key) {
 }
 __device__ __forceinline__ uint64_t place_of(uint32_t key, int i) { return (uint64_t)key << 32 | (uint32_t)~i; }
 
-// exp(y), y <= 0 or a little above, to 2^-51 of itself: 2^n 2^f with |f| <= 1/2, the series of 2^f = exp(f ln 2) up to
-// f^13 (the next term is below 2^-57).
-__device__ __forceinline__ double exp64(double y) {
-  const double z = fmax(y * 1.4426950408889634, -1200.0);
-  const double n = __builtin_rint(z), x = (z - n) * 0.6931471805599453;
-  double s = 1.0 / 6227020800.0;
-  s = fma(s, x, 1.0 / 479001600.0);
-  s = fma(s, x, 1.0 / 39916800.0);
-  s = fma(s, x, 1.0 / 3628800.0);
-  s = fma(s, x, 1.0 / 362880.0);
-  s = fma(s, x, 1.0 / 40320.0);
-  s = fma(s, x, 1.0 / 5040.0);
-  s = fma(s, x, 1.0 / 720.0);
-  s = fma(s, x, 1.0 / 120.0);
-  s = fma(s, x, 1.0 / 24.0);
-  s = fma(s, x, 1.0 / 6.0);
-  s = fma(s, x, 0.5);
-  s = fma(s, x, 1.0);
-  s = fma(s, x, 1.0);
-  return __builtin_amdgcn_ldexp(s, (int)n);
+// 2^z 2^PLACES, z <= 0 or a little above, to 2^-51 of itself: 2^n 2^f with |f| <= 1/2, the series of 2^f up to f^13
+// ((ln 2)^k / k!; the next term is below 2^-57).
+template <int PLACES = 0> __device__ __forceinline__ double power_of_2(double z) {
+  z = fmax(z, -1200.0);
+  const double n = __builtin_rint(z), f = z - n;
+  double s = 0x1.816193166d0f9p-40;
+  s = fma(s, f, 0x1.c3bd650fc2986p-36);
+  s = fma(s, f, 0x1.e8cac7351bb25p-32);
+  s = fma(s, f, 0x1.e4cf5158b8ecap-28);
+  s = fma(s, f, 0x1.b5253d395e7c4p-24);
+  s = fma(s, f, 0x1.62c0223a5c824p-20);
+  s = fma(s, f, 0x1.ffcbfc588b0c7p-17);
+  s = fma(s, f, 0x1.430912f86c787p-13);
+  s = fma(s, f, 0x1.5d87fe78a6731p-10);
+  s = fma(s, f, 0x1.3b2ab6fba4e77p-7);
+  s = fma(s, f, 0x1.c6b08d704a0c0p-5);
+  s = fma(s, f, 0x1.ebfbdff82c58fp-3);
+  s = fma(s, f, 0x1.62e42fefa39efp-1);
+  s = fma(s, f, 0x1.0000000000000p+0);
+  return __builtin_amdgcn_ldexp(s, (int)n + PLACES);
+}
+__device__ __forceinline__ double exp64(double y) { return power_of_2(y * 1.4426950408889634); }
+// A number below 2^51, rounded to a whole one.
+__device__ __forceinline__ uint64_t whole_of(double x) {
+  return __builtin_bit_cast(uint64_t, x + 0x1p52) & ((1ull << 52) - 1);
 }
 
-template <typename T> __device__ __forceinline__ T shfl_up_any(T v, int d) {
-  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __shfl_up((uint32_t)bits, d), hi = __shfl_up((uint32_t)(bits >> 32), d);
-  return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+// The lanes' numbers moved up within a wave, 0 where none comes from; four steps inside rows of 16 lanes and two that carry
+// a row's last lane on (as permutations through LDS a scan waits for them six times).
+template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t moved(uint64_t bits) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(bits >> 32), CTRL, ROWS, 0xf, false);
+  return (uint64_t)hi << 32 | lo;
+}
+template <int CTRL, int ROWS, typename T, typename F> __device__ __forceinline__ T step(T v, F f) {
+  return f(v, __builtin_bit_cast(T, moved<CTRL, ROWS>(__builtin_bit_cast(uint64_t, v))));
+}
+template <typename T, typename F> __device__ __forceinline__ T wave_prefix(T v, F f) {   // f(x, 0) = x
+  v = step<0x111, 0xf>(v, f);   // row_shr:1, 2, 4, 8
+  v = step<0x112, 0xf>(v, f);
+  v = step<0x114, 0xf>(v, f);
+  v = step<0x118, 0xf>(v, f);
+  v = step<0x142, 0xa>(v, f);   // row_bcast:15 into rows 1 and 3
+  return step<0x143, 0xc>(v, f);   // row_bcast:31 into rows 2 and 3
 }
 template <typename T> __device__ __forceinline__ T wave_scan(T v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const T o = shfl_up_any(v, d);
-    v += lane >= d ? o : T(0);
-  }
-  return v;
+  return wave_prefix(v, [](T a, T b) { return a + b; });
 }
-// Sum over the threads up to this one; all: over all.  s: WAVES numbers.
+__device__ __forceinline__ double of_last_lane(double v) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)bits, 63), hi = __builtin_amdgcn_readlane((int)(bits >> 32), 63);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Sum over the threads up to this one; all: over all; s[w] is then the wave's sum.  s: WAVES numbers.
 template <typename T> __device__ __forceinline__ T group_scan(T v, T* s, T* all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   v = wave_scan(v);
@@ -123,23 +140,30 @@ template <typename T> __device__ __forceinline__ T group_scan(T v, T* s, T* all)
   *all = sum;
   return v + before;
 }
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int d) {
-  const uint32_t lo = __shfl_xor((uint32_t)v, d), hi = __shfl_xor((uint32_t)(v >> 32), d);
-  return (uint64_t)hi << 32 | lo;
-}
 __device__ __forceinline__ uint64_t group_max(uint64_t v, uint64_t* s) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint64_t o = shfl_xor64(v, d);
-    v = o > v ? o : v;
-  }
+  v = wave_prefix(v, [](uint64_t a, uint64_t b) { return b > a ? b : a; });
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 63) s[threadIdx.x >> 6] = v;
   __syncthreads();
   v = s[0];
 #pragma unroll
   for (int w = 1; w < WAVES; ++w) v = s[w] > v ? s[w] : v;
   return v;
+}
+
+// One addition in LDS a wave, one minimum a wave (of 1024 threads at one address each waits for all before it: 3 us).
+__device__ __forceinline__ void add_from_wave(uint64_t* to, uint64_t v) {
+  v = wave_scan(v);
+  if ((threadIdx.x & 63) == 63 && v) atomicAdd(reinterpret_cast<unsigned long long*>(to), (unsigned long long)v);
+}
+// The lowest thread for which `is`.
+__device__ __forceinline__ void first_thread(int* to, bool is) {
+  const uint64_t those = __ballot(is);
+  if ((threadIdx.x & 63) == 0 && those) atomicMin(to, (int)threadIdx.x + __builtin_ctzll(those));
+}
+__device__ __forceinline__ void last_thread(uint32_t* to, bool is) {
+  const uint64_t those = __ballot(is);
+  if ((threadIdx.x & 63) == 0 && those) atomicMax(to, threadIdx.x + 63 - __builtin_clzll(those));
 }
 
 struct Shared {
@@ -154,8 +178,21 @@ struct Shared {
   uint64_t hit;
 };
 
-// Falling order of list[0 .. n), by the workgroup; returns with the list in place for all.
+// Falling order of list[0 .. n), by the workgroup; returns with the list in place for all.  Up to 512 numbers (all
+// different) each counts those above it; more are sorted by exchanges, a barrier a step (2048: 18 us; 50: 2.8 us, counted 0.7).
 __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
+  if (n <= THREADS / 2) {
+    const uint64_t mine = threadIdx.x < n ? list[threadIdx.x] : 0;
+    int above = 0;
+    if (threadIdx.x < n) {
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) above += list[i] > mine ? 1 : 0;
+    }
+    __syncthreads();
+    if (threadIdx.x < n) list[above] = mine;
+    __syncthreads();
+    return;
+  }
   int size = 2;
   while (size < n) size *= 2;
   for (int i = n + threadIdx.x; i < size; i += THREADS) list[i] = 0;
@@ -174,10 +211,10 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
 template <typename E> struct Row {
   const E* x;
   int V;
-  double top, inv_t;
+  double top, scale;   // scale: log2(e) / temperature
   int fixed;
   __device__ __forceinline__ uint32_t key(int i) const { return key_of(to_f32<E>(x[i])); }
-  __device__ __forceinline__ double weight(uint32_t k) const { return exp64(((double)number_of(k) - top) * inv_t); }
+  __device__ __forceinline__ double weight(uint32_t k) const { return power_of_2(((double)number_of(k) - top) * scale); }
   __device__ __forceinline__ uint64_t whole(double w) const { return (uint64_t)(w * (double)(1ull << fixed) + 0.5); }
 };
 
@@ -197,7 +234,7 @@ __device__ __forceinline__ int find_bin(Shared& S, const Search& q, uint64_t& ab
   const uint64_t upto = above + group_scan(v, S.wave64, &all);
   if (t == 0) S.found = BINS - 1;
   __syncthreads();
-  if ((double)upto >= q.target && S.count[t] > 0) atomicMin(&S.found, t);
+  first_thread(&S.found, (double)upto >= q.target && S.count[t] > 0);
   __syncthreads();
   const int bin = S.found;
   if (t == bin) S.hit = upto - v;
@@ -215,7 +252,7 @@ __device__ void search_cut(Shared& S, const Row<E>& row, Search& q, double share
   const int t = threadIdx.x;
   const float top = (float)row.top;
   float range = top - lowest;
-  if (q.by_weight) range = fminf(range, (float)(45.0 / row.inv_t));   // (less is less than 2^-64 of the largest)
+  if (q.by_weight) range = fminf(range, (float)(65.0 / row.scale));   // (less is less than 2^-64 of the largest)
   const float steps = range > 0.0f ? BINS / range : 0.0f;
   const auto bin_of = [&](uint32_t key) { return (int)fminf((top - number_of(key)) * steps, (float)(BINS - 1)); };
   S.mass[t] = 0, S.count[t] = 0;
@@ -237,10 +274,9 @@ __device__ void search_cut(Shared& S, const Row<E>& row, Search& q, double share
       atomicAdd(&S.count[bin], 1u);
     }
   }
-  if (far_count) {
-    atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[BINS - 1]), (unsigned long long)far_mass);
-    atomicAdd(&S.count[BINS - 1], far_count);
-  }
+  add_from_wave(&S.mass[BINS - 1], far_mass);
+  far_count = (uint32_t)wave_scan((uint64_t)far_count);
+  if ((t & 63) == 63 && far_count) atomicAdd(&S.count[BINS - 1], far_count);
   __syncthreads();
   uint64_t all;
   group_scan(q.by_weight ? S.mass[t] : (uint64_t)S.count[t], S.wave64, &all);
@@ -393,10 +429,8 @@ template <typename E> __device__ void whole_row(Shared& S, const SampleParams& P
   const double target = from0 * sum;
   if (t == 0) S.found = pieces, S.n = 0;
   __syncthreads();
-  if (t < pieces && S.part[t] > 0.0) {
-    if (upto > target) atomicMin(&S.found, t);
-    atomicMax(&S.n, (uint32_t)t);
-  }
+  first_thread(&S.found, t < pieces && S.part[t] > 0.0 && upto > target);
+  last_thread(&S.n, t < pieces && S.part[t] > 0.0);
   __syncthreads();
   const bool passed = S.found < pieces;
   const int c = passed ? S.found : (int)S.n;   // (if rounding lets none pass: the last with any weight)
@@ -412,8 +446,7 @@ template <typename E> __device__ void whole_row(Shared& S, const SampleParams& P
       const uint64_t past = __ballot(w > 0.0 && before + here > target), some = __ballot(w > 0.0);
       if (some) last = c * piece + j + 63 - __builtin_clzll(some);
       if (past) token = c * piece + j + __builtin_ctzll(past);
-      before += __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(__builtin_bit_cast(uint64_t, here) >> 32), 63) << 32 |
-                                               (uint32_t)__builtin_amdgcn_readlane((int)__builtin_bit_cast(uint64_t, here), 63));
+      before += of_last_lane(here);
     }
     if (lane == 0) P.tokens[b] = token < 0 ? last : token;
   }
@@ -468,7 +501,7 @@ template <typename E, int PER> __device__ __forceinline__ void load_keys(const S
   for (int e = 0; e < PER; ++e) key[e] = i0 + e * THREADS < P.V ? key_of(to_f32<E>(x[i0 + e * THREADS])) : 0;
 }
 
-template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_sample_bins_kernel(SampleParams P) {
+template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_bins_kernel(SampleParams P) {
   __shared__ uint64_t s_bin[BINS], s_wave[WAVES];
   const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
   uint32_t key[PER];
@@ -479,6 +512,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     const uint64_t at = place_of(key[e], c * (PER * THREADS) + e * THREADS + t);
     best = at > best ? at : best;
   }
+  const Settings s = settings(P, b);
   s_bin[t] = 0;
   best = group_max(best, s_wave);
   const int64_t chunk = (int64_t)b * P.chunks + c;
@@ -486,7 +520,6 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     P.best[chunk] = best;
     if (c == 0) P.rows[b].n = 0;
   }
-  const Settings s = settings(P, b);
   const float top = number_of((uint32_t)(best >> 32));
   if (s.one || s.whole || (uint32_t)(best >> 32) <= DEAD) return;
   const int first = on_grid(top, s.grid, CHUNK_GRID) ? cell_of(top, s.grid) : -(1 << 30) - BINS;
@@ -499,17 +532,17 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
       if (bin == BINS - 1) ++mine; else atomicAdd(reinterpret_cast<uint32_t*>(&s_bin[bin]), 1u);
     }
   } else {
-    const double ref = reference_of(top, s.grid), inv_t = 1.0 / (double)s.temp;
+    const double ref = reference_of(top, s.grid), scale = 1.4426950408889634 / (double)s.temp;
 #pragma unroll 4
     for (int e = 0; e < PER; ++e) {
       if (key[e] <= DEAD) continue;
       const float x = number_of(key[e]);
-      const uint64_t w = (uint64_t)(exp64(((double)x - ref) * inv_t) * (double)(1ull << CHUNK_BITS) + 0.5);
+      const uint64_t w = whole_of(power_of_2<CHUNK_BITS>(((double)x - ref) * scale));
       const int bin = s.cuts ? min(cell_of(x, s.grid) - first, BINS - 1) : BINS - 1;
       if (bin == BINS - 1) mine += w; else atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[bin]), (unsigned long long)w);
     }
   }
-  if (mine) atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[BINS - 1]), (unsigned long long)mine);
+  add_from_wave(&s_bin[BINS - 1], mine);
   __syncthreads();
   uint64_t all;
   P.cum[chunk * BINS + t] = group_scan(s_bin[t], s_wave, &all);
@@ -520,41 +553,41 @@ struct Chunks {
   int shift[THREADS];      // -1: the chunk has no logit above -inf
   double scale[THREADS];
 };
-// The row's largest logit (its place), by the workgroup; fills G.
-__device__ __forceinline__ uint64_t row_top(const SampleParams& P, int b, uint64_t* s_wave) {
+// best: the largest logit (its place) of the chunk with the thread's number.
+__device__ __forceinline__ void place_chunk(const Settings& s, uint64_t best, float top, bool is, Chunks& G) {
   const int t = threadIdx.x;
-  return group_max(t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0, s_wave);
-}
-__device__ __forceinline__ void place_chunks(const SampleParams& P, const Settings& s, int b, float top, Chunks& G) {
-  const int t = threadIdx.x;
-  if (t < P.chunks) {
-    const uint32_t key = (uint32_t)(P.best[(int64_t)b * P.chunks + t] >> 32);
+  if (is) {
+    const uint32_t key = (uint32_t)(best >> 32);
     const int first = cell_of(number_of(key), s.grid);
     G.shift[t] = key > DEAD ? first - cell_of(top, s.grid) : -1;
     G.scale[t] = s.by_count ? 1.0 : exp64((reference_of(number_of(key), s.grid) - (double)top) / (double)s.temp) / (double)(1ull << CHUNK_BITS);
   }
   __syncthreads();
 }
-// A chunk's running sum up to the row's bin.
+// A chunk's running sum up to the row's bin.  (The load does not wait for whether it counts.)
 __device__ __forceinline__ double chunk_upto(const SampleParams& P, const Chunks& G, int64_t row_chunk, int c, int bin) {
-  const int own = bin - G.shift[c];
-  if (G.shift[c] < 0 || (own < 0 && bin != BINS - 1)) return 0.0;
-  return (double)P.cum[(row_chunk + c) * BINS + (bin == BINS - 1 ? BINS - 1 : own)] * G.scale[c];
+  const int shift = G.shift[c], own = bin == BINS - 1 ? bin : bin - shift;
+  const double sum = (double)P.cum[(row_chunk + c) * BINS + max(own, 0)] * G.scale[c];
+  return shift < 0 || own < 0 ? 0.0 : sum;
 }
 
-template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_sample_list_kernel(SampleParams P) {
+template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_list_kernel(SampleParams P) {
   __shared__ Chunks G;
   __shared__ uint64_t s_wave[WAVES];
   __shared__ double s_cum[BINS];
   __shared__ int s_bin;
   __shared__ uint32_t s_base;
   const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
+  // (what the launch waits for is asked for at once)
+  const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
   const Settings s = settings(P, b);
+  uint32_t key[PER];
+  load_keys<E, PER>(P, b, c, key);
   if (s.one || s.whole || (!s.by_count && !s.cuts)) return;
-  const uint32_t top_key = (uint32_t)(row_top(P, b, s_wave) >> 32);
+  const uint32_t top_key = (uint32_t)(group_max(chunk_best, s_wave) >> 32);
   const float top = number_of(top_key);
   if (top_key <= DEAD || !on_grid(top, s.grid, ROW_GRID)) return;
-  place_chunks(P, s, b, top, G);
+  place_chunk(s, chunk_best, top, t < P.chunks, G);
   double upto = 0.0;
 #pragma unroll 8
   for (int q = 0; q < P.chunks; ++q) upto += chunk_upto(P, G, (int64_t)b * P.chunks, q, t);
@@ -565,7 +598,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
   int lo = BINS, hi = -1;
   if (s.by_count || s.p < 1.0f) {
     const double target = s.by_count ? fmin((double)s.k, total) : (double)s.p * total;
-    if (upto >= target) atomicMin(&s_bin, t);
+    first_thread(&s_bin, upto >= target);
     __syncthreads();
     hi = s_bin;
     lo = s.by_count ? 0 : hi;
@@ -592,8 +625,6 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     r.total = total;
   }
 
-  uint32_t key[PER];
-  load_keys<E, PER>(P, b, c, key);
   const int first = cell_of(top, s.grid);
   uint32_t on = 0;
 #pragma unroll
@@ -616,14 +647,23 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     }
 }
 
-template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_pick_kernel(SampleParams P) {
+template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_sample_pick_kernel(SampleParams P) {
   __shared__ Shared S;
   __shared__ Chunks G;
   const int b = blockIdx.x, t = threadIdx.x, V = P.V;
+  const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
   const Settings s = settings(P, b);
-  const uint64_t best = row_top(P, b, S.wave64);
-  const uint32_t top_key = (uint32_t)(best >> 32);
   RowState& R = P.rows[b];
+  const RowState r = R;
+  uint64_t member[CAP / THREADS];
+#pragma unroll
+  for (int i = 0; i < CAP / THREADS; ++i) {
+    // (what lies behind the list's end is not used)
+    const int at = i * THREADS + t;
+    member[i] = at < (int)min(r.n, (uint32_t)CAP) ? P.list[(int64_t)b * CAP + at] : 0;
+  }
+  const uint64_t best = group_max(chunk_best, S.wave64);
+  const uint32_t top_key = (uint32_t)(best >> 32);
   if (top_key <= DEAD || s.one) {
     if (t == 0) {
       P.tokens[b] = top_key <= DEAD ? 0 : (int)~(uint32_t)best;
@@ -632,9 +672,9 @@ template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_pi
     return;
   }
   const float top = number_of(top_key);
-  Row<E> row = {reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride, V, (double)top, 1.0 / (double)s.temp, P.fixed};
+  Row<E> row = {reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride, V, (double)top, 1.4426950408889634 / (double)s.temp, P.fixed};
   const bool listed = s.by_count || s.cuts;
-  const int n = listed ? (int)min(R.n, (uint32_t)CAP + 1) : 0;
+  int n = listed ? (int)min(r.n, (uint32_t)CAP + 1) : 0;
   if (s.whole || !on_grid(top, s.grid, ROW_GRID) || n > CAP) {
     if (t == 0) R.kind = DONE;
     whole_row<E>(S, P, row, b, s.k, s.p, s.m, s.u);
@@ -644,9 +684,13 @@ template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_pi
   // the cut
   uint64_t cut = (uint64_t)(DEAD + 1) << 32;
   if (listed) {
-    for (int i = t; i < n; i += THREADS) S.list[i] = P.list[(int64_t)b * CAP + i];
-    __syncthreads();
-    sort_list(S.list, n);
+    if (s.by_count || n <= THREADS / 4 || !(s.p < 1.0f)) {
+#pragma unroll
+      for (int i = 0; i < CAP / THREADS; ++i)
+        if (i * THREADS + t < n) S.list[i * THREADS + t] = member[i];
+      __syncthreads();
+      sort_list(S.list, n);
+    }
   }
   if (s.by_count) {
     const int few = min(n, s.k);   // (up to 1024: a token a thread)
@@ -667,20 +711,65 @@ template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_pi
     const double upto = group_scan(y, S.wave_f, &sum);
     if (t == 0) S.found = left - 1;
     __syncthreads();
-    if (t < left && upto > s.u * sum) atomicMin(&S.found, t);
+    first_thread(&S.found, t < left && upto > s.u * sum);
     __syncthreads();
     if (t == S.found) P.tokens[b] = (int)(x >> 32);
     if (t == 0) R.kind = BY_CUT, R.cut = cut, R.sum = sum;
     return;
   }
 
-  place_chunks(P, s, b, top, G);
-  const int lo = listed ? R.lo : BINS;
+  place_chunk(s, chunk_best, top, t < P.chunks, G);
+  const int lo = listed ? r.lo : BINS;
   S.mass[t] = 0;   // the list's share of every chunk
   __syncthreads();
   if (listed) {
-    double above = R.above;
-    const double target = (double)s.p * R.total;
+    double above = r.above;
+    const double target = (double)s.p * r.total;
+    bool from_top = lo == 0;
+    if (n > THREADS / 4 && s.p < 1.0f) {
+      // a long list: once more in bins, of its numbers' bits, and only the bin with the cut is sorted
+      uint64_t* bins = reinterpret_cast<uint64_t*>(S.part);
+      uint32_t most = 0, least = 0xffffffffu;
+#pragma unroll
+      for (int i = 0; i < CAP / THREADS; ++i)
+        if (i * THREADS + t < n) most = max(most, (uint32_t)(member[i] >> 32)), least = min(least, (uint32_t)(member[i] >> 32));
+      bins[t] = 0;
+      most = (uint32_t)group_max(most, S.wave64);
+      least = ~(uint32_t)group_max((uint32_t)~least, S.wave64);
+      const int shift = max(32 - __builtin_clz((most - least) | 1) - 10, 0);   // (1024 bins)
+      if (t == 0) S.n = 0, S.found = (most - least) >> shift;   // (if rounding lets none reach the target: the last)
+      uint64_t w[CAP / THREADS];
+#pragma unroll
+      for (int i = 0; i < CAP / THREADS; ++i) {
+        w[i] = 0;
+        if (i * THREADS + t >= n) continue;
+        const uint32_t key = (uint32_t)(member[i] >> 32);
+        w[i] = whole_of(row.weight(key) * (double)(1ull << LIST_BITS));
+        atomicAdd(reinterpret_cast<unsigned long long*>(&bins[(most - key) >> shift]), (unsigned long long)w[i]);
+      }
+      __syncthreads();
+      uint64_t all;
+      const uint64_t here = bins[t], upto = group_scan(here, S.wave64, &all);
+      first_thread(&S.found, here > 0 && above + (double)upto / (double)(1ull << LIST_BITS) >= target);
+      __syncthreads();
+      const int bin = S.found;
+      if (t == bin) S.hit = upto - here;
+#pragma unroll
+      for (int i = 0; i < CAP / THREADS; ++i) {
+        if (i * THREADS + t >= n) continue;
+        const uint32_t key = (uint32_t)(member[i] >> 32);
+        const int at = (most - key) >> shift;
+        if (at == bin)
+          S.list[atomicAdd(&S.n, 1u)] = member[i];
+        else if (at < bin && !(row.weight(key) < (double)s.m))
+          atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[(int)~(uint32_t)member[i] / P.chunk]), (unsigned long long)w[i]);
+      }
+      __syncthreads();
+      above += (double)S.hit / (double)(1ull << LIST_BITS);
+      from_top = from_top && bin == 0;
+      n = (int)S.n;
+      sort_list(S.list, n);
+    }
     cut = n > 0 ? S.list[0] + 1 : cut;   // (none of the list)
     for (int i0 = 0; i0 < n; i0 += THREADS) {
       const int i = i0 + t;
@@ -688,12 +777,12 @@ template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_pi
       const double w = i < n ? row.weight((uint32_t)(at >> 32)) : 0.0;
       double here;
       const double before = above + group_scan(w, S.wave_f, &here) - w;
-      const bool stays = i < n && ((lo == 0 && i == 0) || ((!(s.p < 1.0f) || before < target) && !(w < (double)s.m)));
+      const bool stays = i < n && ((from_top && i == 0) || ((!(s.p < 1.0f) || before < target) && !(w < (double)s.m)));
       const uint64_t last = group_max(stays ? ~at : 0, S.wave64);   // the lowest place that stays
       if (last) cut = ~last;
       if (stays)
         atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[(int)~(uint32_t)at / P.chunk]),
-                  (unsigned long long)(w * (double)(1ull << LIST_BITS) + 0.5));
+                  (unsigned long long)whole_of(w * (double)(1ull << LIST_BITS)));
       above += here;
     }
     __syncthreads();
@@ -707,61 +796,66 @@ template <typename E> __global__ __launch_bounds__(THREADS) void oscar_sample_pi
   const double target = s.u * sum;
   if (t == 0) S.found = P.chunks, S.n = 0;
   __syncthreads();
-  if (share > 0.0) {
-    if (upto > target) atomicMin(&S.found, t);
-    atomicMax(&S.n, (uint32_t)t);
-  }
+  first_thread(&S.found, share > 0.0 && upto > target);
+  last_thread(&S.n, share > 0.0);
   __syncthreads();
   const int c = S.found < P.chunks ? S.found : (int)S.n;   // (if rounding lets none pass: the last with any weight)
   if (t == c) S.hit = __builtin_bit_cast(uint64_t, upto - share);
   if (t == 0) R.kind = BY_CUT, R.cut = cut, R.sum = sum, S.n = 0;
   __syncthreads();
-  // the token, a thread's part of the chunk in one piece
-  const int per = P.chunk / THREADS, i0 = c * P.chunk + t * per;
-  const auto weight_at = [&](int i) {
-    const uint32_t key = i < V ? row.key(i) : 0;
-    if (key <= DEAD || place_of(key, i) < cut) return 0.0;
-    const double w = row.weight(key);
-    return w < (double)s.m ? 0.0 : w;   // (an empty list has no cut)
-  };
-  double part = 0.0;
-  for (int e = 0; e < per; ++e) part += weight_at(i0 + e);
-  double all;
-  double before = __builtin_bit_cast(double, S.hit) + (group_scan(part, S.wave_f, &all) - part);
-  if (t == 0) S.found = THREADS;
-  __syncthreads();
-  if (part > 0.0) {
-    if (before + part > target) atomicMin(&S.found, t);
-    atomicMax(&S.n, (uint32_t)t);
-  }
-  __syncthreads();
-  const bool passed = S.found < THREADS;
-  if (t == (passed ? S.found : (int)S.n)) {
-    int token = 0;
-    for (int e = 0; e < per; ++e) {
-      const double w = weight_at(i0 + e);
-      if (!(w > 0.0)) continue;
-      token = i0 + e;
-      before += w;
-      if (passed && before > target) break;
+  // the token: a wave takes a part of the chunk in one piece, 64 logits at a time
+  const int lane = t & 63, wave = t >> 6, i0 = c * (PER * THREADS) + wave * (PER * 64) + lane;
+  uint32_t key[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) key[e] = i0 + e * 64 < V ? row.key(i0 + e * 64) : 0;
+  double w[PER], part = 0.0;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    w[e] = 0.0;
+    if (key[e] > DEAD && place_of(key[e], i0 + e * 64) >= cut) {
+      w[e] = row.weight(key[e]);
+      if (w[e] < (double)s.m) w[e] = 0.0;   // (an empty list has no cut)
     }
-    P.tokens[b] = token;
+    part += w[e];
   }
+  double all;
+  group_scan(part, S.wave_f, &all);
+  double before = __builtin_bit_cast(double, S.hit);
+  int in = -1, some = -1;   // the wave the token is in; the last with any weight
+  for (int v = 0; v < WAVES; ++v) {
+    if (!(S.wave_f[v] > 0.0)) continue;
+    some = v;
+    if (in < 0 && before + S.wave_f[v] > target) in = v;
+    if (in < 0) before += S.wave_f[v];
+  }
+  const bool passed = in >= 0;
+  if (wave != (passed ? in : some)) return;
+  int token = -1, last = 0;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    const double here = wave_scan(w[e]);
+    const uint64_t past = __ballot(passed && w[e] > 0.0 && before + here > target), any = __ballot(w[e] > 0.0);
+    if (any) last = i0 - lane + e * 64 + 63 - __builtin_clzll(any);
+    if (past && token < 0) token = i0 - lane + e * 64 + __builtin_ctzll(past);
+    before += of_last_lane(here);
+  }
+  if (lane == 0) P.tokens[b] = token < 0 ? last : token;
 }
 
-template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_sample_probs_kernel(SampleParams P) {
+template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_probs_kernel(SampleParams P) {
   __shared__ uint64_t s_wave[WAVES];
   const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
-  const RowState& R = P.rows[b];
-  const int kind = R.kind;
-  if (kind == DONE) return;
-  const uint64_t best = row_top(P, b, s_wave);
-  const Settings s = settings(P, b);
-  const double top = (double)number_of((uint32_t)(best >> 32)), inv_t = 1.0 / (double)s.temp;
-  const uint64_t cut = kind == BY_CUT ? R.cut : kind == ONE_TOKEN ? best : ~0ull;
-  const double sum = kind == BY_CUT ? R.sum : 1.0;
   uint32_t key[PER];
   load_keys<E, PER>(P, b, c, key);
+  const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
+  const Settings s = settings(P, b);
+  const RowState R = P.rows[b];
+  const int kind = R.kind;
+  if (kind == DONE) return;
+  const uint64_t best = group_max(chunk_best, s_wave);
+  const double top = (double)number_of((uint32_t)(best >> 32)), scale = 1.4426950408889634 / (double)s.temp;
+  const uint64_t cut = kind == BY_CUT ? R.cut : kind == ONE_TOKEN ? best : ~0ull;
+  const double inv_sum = kind == BY_CUT ? 1.0 / R.sum : 1.0;
   float* out = P.probs + (int64_t)b * P.V;
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
@@ -769,8 +863,8 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     if (i >= P.V) break;
     float y = 0.0f;
     if (key[e] > DEAD && place_of(key[e], i) >= cut) {
-      const double w = exp64(((double)number_of(key[e]) - top) * inv_t);
-      y = kind == ONE_TOKEN ? 1.0f : w < (double)s.m ? 0.0f : (float)(w / sum);
+      const double w = power_of_2(((double)number_of(key[e]) - top) * scale);
+      y = kind == ONE_TOKEN ? 1.0f : w < (double)s.m ? 0.0f : (float)(w * inv_sum);
     }
     out[i] = y;
   }
@@ -785,7 +879,7 @@ template <typename E, int PER> void launch(const SampleParams& P, int batch, hip
   const dim3 grid(P.chunks, batch);
   hipLaunchKernelGGL((oscar_sample_bins_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
   if (P.top_k || P.top_p || P.min_p) hipLaunchKernelGGL((oscar_sample_list_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
-  hipLaunchKernelGGL((oscar_sample_pick_kernel<E>), dim3(batch), dim3(THREADS), 0, st, P);
+  hipLaunchKernelGGL((oscar_sample_pick_kernel<E, PER>), dim3(batch), dim3(THREADS), 0, st, P);
   if (P.probs) hipLaunchKernelGGL((oscar_sample_probs_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
 }
 template <typename E> void launch(const SampleParams& P, int batch, hipStream_t st) {
