@@ -77,10 +77,12 @@ __device__ __forceinline__ u32x2 turn_quarters(u32x2 d) {
 template <typename E, int TILES> __global__ __launch_bounds__(256) void oscar_q8_append_kernel(AppendParams P) {
   constexpr int BLOCK = 16 * TILES;
   __shared__ float s_max[4];
-  const int b = blockIdx.z, h = blockIdx.y, side = blockIdx.x & 1, tid = threadIdx.x;
+  // (heads next to each other: a row's are)
+  const uint32_t unit = blockIdx.x / P.c.heads;
+  const int b = blockIdx.y, h = blockIdx.x % P.c.heads, side = unit & 1, tid = threadIdx.x;
   const Q8Seq s = q8_seq(P.r, b);
   if (s.n == 0) return;
-  const int first = max(s.old, 0) / BLOCK, j = first + (blockIdx.x >> 1);   // (the block's number in its sequence)
+  const int first = max(s.old, 0) / BLOCK, j = first + (int)(unit >> 1);   // (the block's number in its sequence)
   if ((int64_t)j * BLOCK >= s.len) return;
   const uint16_t* in = (side ? P.v : P.k) + h * D;
   const int64_t stride = side ? P.v_stride : P.k_stride;
@@ -194,14 +196,13 @@ struct ReadParams {
 
 constexpr int ROW_PITCH = D + 16;   // bytes of a row in LDS: 16-byte pieces of four rows on different banks
 
-// 8 numbers of a row, out.
-template <typename O> __device__ __forceinline__ void put8(O* to, const float* x) {
-  if constexpr (sizeof(O) == 4) {
+// What a lane writes at a time: 16 bytes, so that a wave's lie next to each other.
+template <typename O> constexpr int LANE_NUMBERS = 16 / sizeof(O);
+template <typename O> __device__ __forceinline__ void put(O* to, const float* x) {
+  if constexpr (sizeof(O) == 4)
     *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4*>(to + 4) = make_float4(x[4], x[5], x[6], x[7]);
-  } else {
+  else
     *reinterpret_cast<u32x4*>(to) = narrow8<O>(x);
-  }
 }
 
 // Lane quads: byte i of the result is byte (lane % 4) of lane i's dword.
@@ -227,7 +228,6 @@ template <typename E, typename O> __global__ __launch_bounds__(256) void oscar_q
   const int64_t t0 = step * Q8_STEP_TOKENS;
   if (unit / P.c.heads >= P.steps || t0 >= to) return;   // (no barriers below: a wave is by itself)
   const bool coded = t0 < len / P.c.block * P.c.block;
-  const int c8 = lane & 15;
   uint8_t* rows = s_rows[wave];
   float scale = 1.0f;
   const uint16_t* win = nullptr;
@@ -260,28 +260,35 @@ template <typename E, typename O> __global__ __launch_bounds__(256) void oscar_q
   } else {
     win = (side ? P.c.win_v : P.c.win_k) + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
   }
+  constexpr int N = LANE_NUMBERS<O>, LANES = D / N;   // of a row
+  const int c = lane % LANES * N;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int t = 4 * i + (lane >> 4);
+  for (int i = 0; i < Q8_STEP_TOKENS * LANES / 64; ++i) {
+    const int t = 64 / LANES * i + lane / LANES;
     const int64_t pos = t0 + t;
     if (pos < from || pos >= to) continue;
     float x[8];
     if (coded) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(rows + t * ROW_PITCH + c8 * 8);
 #pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[d], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[d], true);
+      for (int d = 0; d < N / 4; ++d) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(rows + t * ROW_PITCH + c + 4 * d);
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
         x[4 * d] = lo[0] * scale, x[4 * d + 1] = lo[1] * scale, x[4 * d + 2] = hi[0] * scale, x[4 * d + 3] = hi[1] * scale;
       }
     } else {
-      widen8<E>(*reinterpret_cast<const u32x4*>(win + (pos % (2 * P.c.block)) * D + c8 * 8), x);
+#pragma unroll
+      for (int d = 0; d < N / 4; ++d) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(win + (pos % (2 * P.c.block)) * D + c + 4 * d);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) x[4 * d + 2 * j] = widen<E>(w[j] & 0xffff), x[4 * d + 2 * j + 1] = widen<E>(w[j] >> 16);
+      }
     }
-    put8<O>(out + (((int64_t)b * P.T + (pos - start)) * P.c.heads + h) * D + c8 * 8, x);
+    put<O>(out + (((int64_t)b * P.T + (pos - start)) * P.c.heads + h) * D + c, x);
   }
 }
 
 template <typename E> void launch_append(const AppendParams& P, hipStream_t st) {
-  const dim3 grid(2 * P.blocks, P.c.heads, P.c.batch);
+  const dim3 grid(2 * P.blocks * P.c.heads, P.c.batch);
   if (P.c.block == 32)
     hipLaunchKernelGGL((oscar_q8_append_kernel<E, 2>), grid, dim3(256), 0, st, P);
   else if (P.c.block == 64)
@@ -354,7 +361,7 @@ extern "C" int oscar_q8_append(const void* k, const void* v, int64_t k_stride, i
   // T tokens from the last place of a block on
   P.blocks = (int)(((int64_t)T + 2 * cache->block - 2) / cache->block);
   // a grid's threads are counted in 32 bits
-  if ((int64_t)P.blocks * 2 * 256 > UINT32_MAX) return OSCAR_ERR_INVALID_ARG;
+  if ((int64_t)P.blocks * 2 * cache->n_kv_heads * 256 > UINT32_MAX) return OSCAR_ERR_INVALID_ARG;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (cache->io_dtype == OSCAR_BF16)
     launch_append<__hip_bfloat16>(P, st);

@@ -25,6 +25,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
+constexpr int O_PITCH = 132;       // of a row of sums in LDS: 16 rows' pieces on different banks
 constexpr float NO_REF = -1e30f;   // reference of a row that has seen no token
 // A reference moves when a logit passes it by this much (in powers of two): probabilities stay below 2^8, and a wave
 // seldom has to multiply its sums.
@@ -77,83 +78,92 @@ __device__ __forceinline__ f32x4 mul_bf16(bf16x8 a, bf16x8 b, f32x4 c) {
 template <bool F16, int RT> struct Rows {
   typename Io<F16>::Op q[RT][4];
   f32x4 o[RT][8];
-  float sum[RT], ref[RT];
+  f32x4 sum[RT];        // four times the same: probabilities are added up by the matrix cores too
+  float ref[RT];
   int pos[RT];          // the lane's row's position, -1: no row
   int min_pos, max_pos; // of the rows there are
 };
+
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }
 
 // Probabilities of a step's 8 logits of the lane's row: two limbs of the operand.
 struct Limbs {
   bf16x8 hi, lo;
 };
-template <bool F16, int RT>
-__device__ __forceinline__ Limbs probabilities(Rows<F16, RT>& w, int r, f32x4 s0, f32x4 s1, float scale, int t0, bool edge, int q4, int limit) {
-  float x[8];
+// Logits of tokens that a row does not see, of a step from t0 on: from `limit` on, or behind the row's own.
+template <bool F16, int RT> __device__ __forceinline__ void hide(const Rows<F16, RT>& w, int r, f32x4* s, int t0, int q4, int limit) {
+  const int last = min(w.pos[r], limit - 1);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = s0[i] * scale, x[4 + i] = s1[i] * scale;
-  if (edge) {
-    const int last = min(w.pos[r], limit - 1);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = t0 + 4 * q4 + i <= last ? x[i] : -INFINITY;
-      x[4 + i] = t0 + 16 + 4 * q4 + i <= last ? x[4 + i] : -INFINITY;
-    }
+  for (int i = 0; i < 4; ++i) {
+    s[0][i] = t0 + 4 * q4 + i <= last ? s[0][i] : -INFINITY;
+    s[1][i] = t0 + 16 + 4 * q4 + i <= last ? s[1][i] : -INFINITY;
   }
-  float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-  if (__any(top > w.ref[r] + REF_SLACK)) {
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float ref = fmaxf(w.ref[r], top);
+}
+// The reference follows the step's largest logit, all sums with it.
+template <bool F16, int RT> __device__ __forceinline__ void move_reference(Rows<F16, RT>& w, const f32x4 (*s)[2], float scale) {
+  float top[RT];
+  bool past = false;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    top[r] = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])),
+                   fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3]))) * scale;
+    past |= top[r] > w.ref[r] + REF_SLACK;
+  }
+  if (!__any(past)) return;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    top[r] = fmaxf(top[r], __shfl_xor(top[r], 16));
+    top[r] = fmaxf(top[r], __shfl_xor(top[r], 32));
+    const float ref = fmaxf(w.ref[r], top[r]);
     const float f = __builtin_amdgcn_exp2f(w.ref[r] - ref);
     w.ref[r] = ref;
     w.sum[r] *= f;
 #pragma unroll
     for (int c = 0; c < 8; ++c) w.o[r][c] *= f;
   }
+}
+// Probabilities, two limbs of the operand.
+template <bool F16, int RT> __device__ __forceinline__ Limbs probabilities(const Rows<F16, RT>& w, int r, const f32x4* s, float scale) {
   Limbs p;
-  float part = 0.0f;
+  u32x4 hi, lo;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float e = __builtin_amdgcn_exp2f(x[i] - w.ref[r]);
-    part += e;
-    p.hi[i] = (__bf16)e;
-    p.lo[i] = (__bf16)(e - (float)p.hi[i]);
+  for (int i = 0; i < 4; ++i) {   // (two at a time: the conversion takes two)
+    const float a = __builtin_amdgcn_exp2f(fmaf(s[i / 2][2 * (i & 1)], scale, -w.ref[r]));
+    const float b = __builtin_amdgcn_exp2f(fmaf(s[i / 2][2 * (i & 1) + 1], scale, -w.ref[r]));
+    hi[i] = two_bf16(a, b);
+    lo[i] = two_bf16(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xffff0000u));
   }
-  w.sum[r] += part;
+  p.hi = __builtin_bit_cast(bf16x8, hi);
+  p.lo = __builtin_bit_cast(bf16x8, lo);
   return p;
 }
+template <bool F16, int RT> __device__ __forceinline__ void add_up(Rows<F16, RT>& w, int r, const Limbs& p) {
+  const __bf16 one = (__bf16)1.0f;
+  const bf16x8 ones = {one, one, one, one, one, one, one, one};
+  w.sum[r] = mul_bf16(ones, p.lo, mul_bf16(ones, p.hi, w.sum[r]));
+}
 
-// F16: the io type; RT: tiles of 16 rows a workgroup.
-template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : RT == 2 ? 2 : 1) void oscar_q8_attn_kernel(AttnParams P) {
+// Where the waves' sums meet.
+template <int RT> struct __align__(16) Joined {
+  float o[4][16 * O_PITCH];
+  float sum[4][16 * RT], ref[4][16 * RT];
+};
+
+// The rows from row0 on (of a sequence and kv head) over the pages of a split, by a workgroup.
+template <bool F16, int RT>
+__device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, int b, int h, int split, int row0, Joined<RT>& J) {
   using Op = typename Io<F16>::Op;
-  __shared__ float s_sum[4][16 * RT], s_ref[4][16 * RT];
-  __shared__ __align__(16) float s_o[4][16 * 128];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, q4 = lane >> 4;
-  // row blocks of one range of pages lie on one die of eight, next to each other
-  uint32_t id = blockIdx.x;
-  int rb = 0;
-  if (P.row_blocks > 1) {
-    const uint32_t group = id / (8 * P.row_blocks), in = id % (8 * P.row_blocks);
-    rb = P.row_blocks - 1 - in / 8;   // (the last rows see the most)
-    id = group * 8 + in % 8;
-  }
-  const int split = id % P.splits;
-  id /= P.splits;
-  const int h = id % P.c.heads, b = id / P.c.heads;
-  if (b >= P.c.batch) return;
-  const Q8Seq s = q8_seq(P.r, b);
-  const int rows = s.n * P.g;
-  if (rb * 16 * RT >= rows) return;
-
+  const int rows = seq.n * P.g;
   Rows<F16, RT> w;
-  w.min_pos = s.old + rb * 16 * RT / P.g;
-  w.max_pos = s.old + (min((rb + 1) * 16 * RT, rows) - 1) / P.g;
+  w.min_pos = seq.old + row0 / P.g;
+  w.max_pos = seq.old + (min(row0 + 16 * RT, rows) - 1) / P.g;
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const int row = (rb * RT + r) * 16 + n, t = row / P.g;
-    const int64_t at = s.row + t;
+    const int row = row0 + r * 16 + n, t = row / P.g;
+    const int64_t at = seq.row + t;
     const bool is = row < rows && at >= 0 && at < P.r.n_rows;
-    w.pos[r] = is ? s.old + t : -1;
+    w.pos[r] = is ? seq.old + t : -1;
     const uint16_t* q = P.q + at * P.q_stride + (h * P.g + row % P.g) * D + 16 * q4;
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
@@ -161,14 +171,14 @@ template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : RT =
       if (is) x = *reinterpret_cast<const u32x4*>(q + 64 * (kk / 2) + 8 * (kk % 2));
       w.q[r][kk] = __builtin_bit_cast(Op, x);
     }
-    w.sum[r] = 0.0f;
+    w.sum[r] = f32x4{};
     w.ref[r] = NO_REF;
 #pragma unroll
     for (int c = 0; c < 8; ++c) w.o[r][c] = f32x4{};
   }
 
   // pages of whole blocks, and the window behind them
-  const int coded = s.len / P.c.block * P.c.block;
+  const int coded = seq.len / P.c.block * P.c.block;
   const int end = min(coded, w.max_pos + 1);                 // tokens of pages that some row sees
   const int pages = min(max(end + R - 1, 0) / R, P.c.max_pages);
   const int per = (pages + P.splits - 1) / P.splits;
@@ -176,62 +186,91 @@ template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : RT =
   const int per_page = R / P.c.block;
   const int32_t* table = P.c.table + (int64_t)b * P.c.max_pages;
 
+  // What is loaded lies one step ahead of its use, and logits are worked out a step ahead of their probabilities, so
+  // that the matrix cores have products to do while exponentials and limbs are made, and the other way round.
   u32x4 k[4], v[4];
   float ks = 0.0f, vs = 0.0f;
-  const auto valid = [&](int p) { return p < p1 && p * R + wave * Q8_STEP_TOKENS < end; };
   const auto page_of = [&](int p) -> int {
-    if (!valid(p)) return -1;
-    const int page = table[p];
+    if (p >= p1 || p * R + wave * Q8_STEP_TOKENS >= end) return -1;
+    const int page = __builtin_amdgcn_readfirstlane(table[p]);
     return (uint32_t)page < (uint32_t)P.c.num_pages ? page : -1;
   };
-  const auto at_of = [&](int page) { return (int64_t)page * P.c.heads + h; };
-  const auto load_k = [&](int page) {
-    const uint8_t* in = P.c.k_codes + at_of(page) * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES + lane * 16;
+  const auto load = [&](int page, const uint8_t* codes, const float* scales, u32x4* x, float& scale) {
+    scale = 1.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) k[i] = *reinterpret_cast<const u32x4*>(in + i * 1024);
-    ks = P.c.k_scales[at_of(page) * per_page + wave * Q8_STEP_TOKENS / P.c.block];
+    for (int i = 0; i < 4; ++i) x[i] = u32x4{};   // (a page that is none: what stands for it must be numbers)
+    if (page < 0) return;
+    const int64_t at = (int64_t)page * P.c.heads + h;
+    const uint8_t* in = codes + at * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES + lane * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(in + i * 1024);
+    scale = scales[at * per_page + wave * Q8_STEP_TOKENS / P.c.block];
   };
-  const auto load_v = [&](int page) {
-    const uint8_t* in = P.c.v_codes + at_of(page) * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES + lane * 16;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const u32x4*>(in + i * 1024);
-    vs = P.c.v_scales[at_of(page) * per_page + wave * Q8_STEP_TOKENS / P.c.block];
+  const auto key_operand = [&](int tile, int kk) {
+    const u32x4 x = k[2 * tile + kk / 2];
+    return Io<F16>::keys(u32x2{x[2 * (kk % 2)], x[2 * (kk % 2) + 1]});
   };
 
   int page = page_of(p0), next = page_of(p0 + 1);
-  if (page >= 0) load_k(page), load_v(page);
+  f32x4 s[RT][2];
+  if (p0 < p1) {
+    load(page, P.c.k_codes, P.c.k_scales, k, ks);
+    load(page, P.c.v_codes, P.c.v_scales, v, vs);
+#pragma unroll
+    for (int tile = 0; tile < 2; ++tile)
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const Op key = key_operand(tile, kk);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) s[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : s[r][tile]);
+      }
+  }
+  float scale = ks * P.scale_log2;
+  if (p0 < p1) load(next, P.c.k_codes, P.c.k_scales, k, ks);
   for (int p = p0; p < p1; ++p) {
     const int after = page_of(p + 2);
     const int t0 = p * R + wave * Q8_STEP_TOKENS;
-    if (page >= 0) {
-      f32x4 st[RT][2];
+    if (page < 0 || t0 + Q8_STEP_TOKENS - 1 > w.min_pos)
 #pragma unroll
-      for (int tile = 0; tile < 2; ++tile) {
+      for (int r = 0; r < RT; ++r) hide<F16, RT>(w, r, s[r], t0, q4, page < 0 ? 0 : end);
+    move_reference<F16, RT>(w, s, scale);
+    f32x4 later[RT][2];
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const u32x4 x = k[2 * tile + kk / 2];
-          const Op key = Io<F16>::keys(u32x2{x[2 * (kk % 2)], x[2 * (kk % 2) + 1]});
+    for (int tile = 0; tile < 2; ++tile)
 #pragma unroll
-          for (int r = 0; r < RT; ++r) st[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : st[r][tile]);
-        }
+      for (int kk = 0; kk < 4; ++kk) {
+        const Op key = key_operand(tile, kk);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) later[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : later[r][tile]);
       }
-      const float scale = ks * P.scale_log2;
-      if (next >= 0) load_k(next);
-      const bool edge = t0 + Q8_STEP_TOKENS - 1 > w.min_pos;
-      Limbs pr[RT];
+    const float later_scale = ks * P.scale_log2;
+    bf16x8 val[8];
 #pragma unroll
-      for (int r = 0; r < RT; ++r) pr[r] = probabilities<F16, RT>(w, r, st[r][0], st[r][1], scale, t0, edge, q4, end);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        const u32x4 x = v[c / 2];
-        const bf16x8 val = bf16_operand(u32x2{x[2 * (c % 2)], x[2 * (c % 2) + 1]}, vs);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) w.o[r][c] = mul_bf16(val, pr[r].lo, mul_bf16(val, pr[r].hi, w.o[r][c]));
-      }
-      if (next >= 0) load_v(next);
-    } else if (next >= 0) {
-      load_k(next), load_v(next);
+    for (int c = 0; c < 8; ++c) {
+      const u32x4 x = v[c / 2];
+      val[c] = bf16_operand(u32x2{x[2 * (c % 2)], x[2 * (c % 2) + 1]}, vs);
     }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const Limbs pr = probabilities<F16, RT>(w, r, s[r], scale);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) w.o[r][c] = mul_bf16(val[c], pr.hi, w.o[r][c]);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) w.o[r][c] = mul_bf16(val[c], pr.lo, w.o[r][c]);
+      add_up<F16, RT>(w, r, pr);
+    }
+#ifdef SGB
+#pragma unroll
+    for (int i = 0; i < 26 * RT; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, SGB, 0);
+    }
+#endif
+    load(after, P.c.k_codes, P.c.k_scales, k, ks);
+    load(next, P.c.v_codes, P.c.v_scales, v, vs);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) s[r][0] = later[r][0], s[r][1] = later[r][1];
+    scale = later_scale;
     page = next;
     next = after;
   }
@@ -240,7 +279,7 @@ template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : RT =
   if (split == P.splits - 1) {
     const uint16_t* wk = P.c.win_k + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
     const uint16_t* wv = P.c.win_v + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
-    const int stop = min(s.len, w.max_pos + 1);
+    const int stop = min(seq.len, w.max_pos + 1);
     for (int t0 = coded + wave * Q8_STEP_TOKENS; t0 < stop; t0 += 4 * Q8_STEP_TOKENS) {
       const int slot = t0 % (2 * P.c.block);   // (a step does not wrap)
       f32x4 st[RT][2];
@@ -254,9 +293,15 @@ template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : RT =
           for (int r = 0; r < RT; ++r) st[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : st[r][tile]);
         }
       }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) hide<F16, RT>(w, r, st[r], t0, q4, stop);
+      move_reference<F16, RT>(w, st, P.scale_log2);
       Limbs pr[RT];
 #pragma unroll
-      for (int r = 0; r < RT; ++r) pr[r] = probabilities<F16, RT>(w, r, st[r][0], st[r][1], P.scale_log2, t0, true, q4, stop);
+      for (int r = 0; r < RT; ++r) {
+        pr[r] = probabilities<F16, RT>(w, r, st[r], P.scale_log2);
+        add_up<F16, RT>(w, r, pr[r]);
+      }
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         bf16x8 val, rest;
@@ -286,28 +331,27 @@ template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : RT =
   // the four waves' sums
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    w.sum[r] += __shfl_xor(w.sum[r], 16);
-    w.sum[r] += __shfl_xor(w.sum[r], 32);
-    if (q4 == 0) s_sum[wave][16 * r + n] = w.sum[r], s_ref[wave][16 * r + n] = w.ref[r];
+    if (q4 == 0) J.sum[wave][16 * r + n] = w.sum[r][0], J.ref[wave][16 * r + n] = w.ref[r];
   }
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     if (r > 0) __syncthreads();
 #pragma unroll
-    for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4*>(&s_o[wave][n * 128 + 16 * c + 4 * q4]) = w.o[r][c];
+    for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4*>(&J.o[wave][n * O_PITCH + 16 * c + 4 * q4]) = w.o[r][c];
     __syncthreads();
-    const int j = tid >> 4, row = (rb * RT + r) * 16 + j, t = row / P.g;
-    const int64_t at = s.row + t;
+    const int j = tid >> 4, row = row0 + r * 16 + j, t = row / P.g;
+    const int64_t at = seq.row + t;
     if (row < rows && at >= 0 && at < P.r.n_rows) {
       float ref = NO_REF, sum = 0.0f, f[4], x[8] = {};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) ref = fmaxf(ref, s_ref[i][16 * r + j]);
+      for (int i = 0; i < 4; ++i) ref = fmaxf(ref, J.ref[i][16 * r + j]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        f[i] = __builtin_amdgcn_exp2f(s_ref[i][16 * r + j] - ref);
-        sum += f[i] * s_sum[i][16 * r + j];
+        f[i] = __builtin_amdgcn_exp2f(J.ref[i][16 * r + j] - ref);
+        sum += f[i] * J.sum[i][16 * r + j];
+        const f32x4 *o = reinterpret_cast<const f32x4*>(&J.o[i][j * O_PITCH + (tid & 15) * 8]), lo = o[0], hi = o[1];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += f[i] * s_o[i][j * 128 + (tid & 15) * 8 + e];
+        for (int e = 0; e < 4; ++e) x[e] += f[i] * lo[e], x[4 + e] += f[i] * hi[e];
       }
       const int head = h * P.g + row % P.g, c0 = (tid & 15) * 8;
       if (P.splits == 1) {
@@ -335,29 +379,83 @@ template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : RT =
   }
 }
 
-// Joins the splits of a row: a wave a row and query head.
+// F16: the io type; RT: tiles of 16 rows a workgroup.
+template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void oscar_q8_attn_kernel(AttnParams P) {
+  __shared__ Joined<RT> J;
+  // row blocks of one range of pages lie on one die of eight, next to each other
+  uint32_t id = blockIdx.x;
+  int rb = 0;
+  if (P.row_blocks > 1) {
+    const uint32_t group = id / (8 * P.row_blocks), in = id % (8 * P.row_blocks);
+    rb = P.row_blocks - 1 - in / 8;   // (the last rows see the most)
+    id = group * 8 + in % 8;
+  }
+  const int split = id % P.splits;
+  id /= P.splits;
+  const int h = id % P.c.heads, b = id / P.c.heads;
+  if (b >= P.c.batch) return;
+  const Q8Seq seq = q8_seq(P.r, b);
+  const int row0 = rb * 16 * RT, left = seq.n * P.g - row0;
+  if (left <= 0) return;
+  if (RT > 1 && left <= 16)   // (a block's last rows)
+    attend<F16, 1>(P, seq, b, h, split, row0, reinterpret_cast<Joined<1>&>(J));
+  else
+    attend<F16, RT>(P, seq, b, h, split, row0, J);
+}
+
+// Joins the splits of a row and query head: a workgroup, each wave a quarter of the splits.
 template <bool F16> __global__ __launch_bounds__(256) void oscar_q8_join_kernel(AttnParams P) {
-  const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);   // [sequence][new token][head]
+  __shared__ float2 s_o[4][64];
+  __shared__ float s_ref[4], s_sum[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t unit = blockIdx.x;   // [sequence][new token][head]
   const int head = unit % P.hq, t = unit / P.hq % P.r.T;
   const int64_t b = unit / P.hq / P.r.T;
-  if (b >= P.c.batch) return;
   const Q8Seq s = q8_seq(P.r, b);
   const int64_t at = s.row + t;
   if (t >= s.n || at < 0 || at >= P.r.n_rows) return;
+  const int per = (P.splits + 3) / 4, i0 = wave * per, i1 = min(i0 + per, P.splits);
   const float* ws = P.ws + unit * P.splits * 130;
-  float ref = NO_REF;
-  for (int i = lane; i < P.splits; i += 64) ref = fmaxf(ref, ws[i * 130 + 129]);
+  // statistics of up to 64 splits a round, then their sums
+  float ref = NO_REF, sum = 0.0f, x = 0.0f, y = 0.0f;
+  for (int c0 = i0; c0 < i1; c0 += 64) {
+    const float2 st = c0 + lane < i1 ? *reinterpret_cast<const float2*>(ws + (c0 + lane) * 130 + 128) : make_float2(0.0f, NO_REF);
+    float top = st.y;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) ref = fmaxf(ref, __shfl_xor(ref, d));
-  float sum = 0.0f, x = 0.0f, y = 0.0f;
-#pragma unroll 8
-  for (int i = 0; i < P.splits; ++i) {
-    const float f = __builtin_amdgcn_exp2f(ws[i * 130 + 129] - ref);
-    const float2 o = *reinterpret_cast<const float2*>(ws + i * 130 + 2 * lane);
-    sum += f * ws[i * 130 + 128];
-    x += f * o.x;
-    y += f * o.y;
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    top = fmaxf(top, ref);
+    const float back = __builtin_amdgcn_exp2f(ref - top), f = __builtin_amdgcn_exp2f(st.y - top);
+    ref = top;
+    float part = f * st.x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) part += __shfl_xor(part, d);
+    sum = sum * back + part;
+    x *= back, y *= back;
+    const int n = min(i1 - c0, 64);
+    for (int j = 0; j < n; j += 16) {   // (16 loads on the way at a time; what is past the end weighs nothing)
+      float2 o[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] = *reinterpret_cast<const float2*>(ws + (c0 + min(j + i, n - 1)) * 130 + 2 * lane);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float g = j + i < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), j + i)) : 0.0f;
+        x += g * o[i].x;
+        y += g * o[i].y;
+      }
+    }
+  }
+  s_o[wave][lane] = make_float2(x, y);
+  if (lane == 0) s_ref[wave] = ref, s_sum[wave] = sum;
+  __syncthreads();
+  if (wave > 0) return;
+  ref = fmaxf(fmaxf(s_ref[0], s_ref[1]), fmaxf(s_ref[2], s_ref[3]));
+  sum = x = y = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(s_ref[w] - ref);
+    sum += f * s_sum[w];
+    x += f * s_o[w][lane].x;
+    y += f * s_o[w][lane].y;
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
   x *= inv, y *= inv;
@@ -372,15 +470,16 @@ template <bool F16> __global__ __launch_bounds__(256) void oscar_q8_join_kernel(
 }
 
 // Tiles of 16 rows a workgroup.
-int row_tiles(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+#ifndef MAXRT
+#define MAXRT 2
+#endif
+int row_tiles(int64_t rows) { return std::min<int64_t>((rows + 15) / 16, MAXRT); }
 
 template <bool F16> void launch(const AttnParams& P, int rt, uint32_t grid, hipStream_t st) {
   if (rt == 1)
     hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 1>), dim3(grid), dim3(256), 0, st, P);
-  else if (rt == 2)
-    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 2>), dim3(grid), dim3(256), 0, st, P);
   else
-    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 4>), dim3(grid), dim3(256), 0, st, P);
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 2>), dim3(grid), dim3(256), 0, st, P);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -396,9 +495,13 @@ extern "C" int32_t oscar_q8_auto_splits(const oscar_q8_cache* cache, int32_t n_q
   const int rt = row_tiles(rows);
   const int64_t units = (int64_t)cache->batch * cache->n_kv_heads * ((rows + 16 * rt - 1) / (16 * rt));
   const int64_t pages = (max_seq_len + OSCAR_R - 1) / OSCAR_R;
-  // two workgroups a compute unit, two pages each at least
-  const int64_t splits = (2 * (int64_t)oscar_compute_units() + units - 1) / units;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({splits, (pages + 1) / 2, 512}));
+  // One workgroup a compute unit streams as fast as two, which leave twice the partial sums (8 sequences of 32K, 4 / 8
+  // splits 93.8 / 98.5 us; 1 of 8K 32 / 64 splits 9.2 / 10.2).  With two tiles a workgroup computes, and two fill a
+  // unit better (35 rows over 128K, 32 / 64 splits 45.6 / 37.9); but rows by the hundred have more partial sums
+  // than they save (200 rows over 2048, 1 / 2 splits 22.9 / 35.1).
+  const int64_t cus = oscar_compute_units();
+  const int64_t splits = rt == 1 ? cus / units : 2 * units <= cus ? 2 * cus / units : 1;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({splits, pages, 512}));
 }
 
 extern "C" size_t oscar_q8_workspace_bytes(const oscar_q8_cache* cache, int32_t n_q_heads, int32_t T, int32_t num_splits) {
@@ -427,7 +530,7 @@ extern "C" int oscar_q8_attn(const void* q, int64_t q_stride, int64_t n_rows, in
   const int rt = row_tiles(rows);
   const int64_t row_blocks = (rows + 16 * rt - 1) / (16 * rt), units = (int64_t)cache->batch * cache->n_kv_heads * splits;
   const int64_t grid = row_blocks == 1 ? units : (units + 7) / 8 * 8 * row_blocks;
-  const int64_t join = ((int64_t)cache->batch * T * n_q_heads + 3) / 4;
+  const int64_t join = (int64_t)cache->batch * T * n_q_heads;
   // a grid's threads are counted in 32 bits
   if (row_blocks > INT32_MAX / 8 || grid * 256 > UINT32_MAX || (splits > 1 && join * 256 > UINT32_MAX)) return OSCAR_ERR_INVALID_ARG;
   if (splits > 1 && (!workspace || !aligned16(workspace) || workspace_bytes < oscar_q8_workspace_bytes(cache, n_q_heads, T, splits)))
