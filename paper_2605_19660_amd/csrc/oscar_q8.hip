@@ -21,6 +21,10 @@ namespace {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t s16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 template <typename E> __device__ __forceinline__ float widen(uint32_t bits16);
 template <> __device__ __forceinline__ float widen<__hip_bfloat16>(uint32_t b) { return bf16_bits_to_f32(b); }
@@ -31,20 +35,41 @@ template <typename E> __device__ __forceinline__ uint32_t narrow(float x) {
   return __builtin_bit_cast(uint16_t, from_f32<E>(x));
 }
 
-// What counts for a number: NaN as 0, large ones as the largest the cache takes.
-template <typename E> __device__ __forceinline__ float counted(float x) {
-  constexpr float most = sizeof(E) == 2 && __is_same(E, __half) ? 65504.0f : 0x1p60f;
-  x = x == x ? x : 0.0f;
-  return __builtin_amdgcn_fmed3f(x, -most, most);
+// What the cache takes at most, as a number's bits without its sign (an infinity and a NaN have more).
+template <typename E> constexpr uint16_t MOST_BITS = __is_same(E, __half) ? 0x7bff : (127 + 60) << 7;
+__device__ __forceinline__ u16x2 most_bits(u16x2 most, u32x4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[i] & 0x7fff7fffu));
+  return most;
 }
-
-// The 8 numbers of a 16-byte piece of a row, made to count.
-template <typename E> __device__ __forceinline__ void widen8(u32x4 v, float* x) {
+// What counts for the numbers of a piece: NaN as 0, large ones as the largest.
+template <typename E> __device__ __forceinline__ u32x4 counted(u32x4 v) {
+  constexpr uint32_t nan = __is_same(E, __half) ? 0x7c00 : 0x7f80;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    x[2 * i] = counted<E>(widen<E>(v[i] & 0xffff));
-    x[2 * i + 1] = counted<E>(widen<E>(v[i] >> 16));
+    uint32_t out = 0;
+#pragma unroll
+    for (int s = 0; s < 32; s += 16) {
+      const uint32_t bits = v[i] >> s & 0x7fff, sign = v[i] >> s & 0x8000;
+      out |= (bits > nan ? 0 : sign | min(bits, (uint32_t)MOST_BITS<E>)) << s;
+    }
+    v[i] = out;
   }
+  return v;
+}
+// Two numbers divided by a power of two, to the nearest e4m3 numbers.
+template <typename E> __device__ __forceinline__ uint32_t two_codes(uint32_t old, uint32_t two, float scale, bool upper);
+template <> __device__ __forceinline__ uint32_t two_codes<__hip_bfloat16>(uint32_t old, uint32_t two, float scale, bool upper) {
+  const bf16x2 x = __builtin_bit_cast(bf16x2, two);
+  const s16x2 o = __builtin_bit_cast(s16x2, old);
+  return __builtin_bit_cast(uint32_t, upper ? __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(o, x, scale, true)
+                                            : __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(o, x, scale, false));
+}
+template <> __device__ __forceinline__ uint32_t two_codes<__half>(uint32_t old, uint32_t two, float scale, bool upper) {
+  const f16x2 x = __builtin_bit_cast(f16x2, two);
+  const s16x2 o = __builtin_bit_cast(s16x2, old);
+  return __builtin_bit_cast(uint32_t, upper ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(o, x, scale, true)
+                                            : __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(o, x, scale, false));
 }
 template <typename E> __device__ __forceinline__ u32x4 narrow8(const float* x) {
   u32x4 v;
@@ -73,10 +98,13 @@ __device__ __forceinline__ u32x2 turn_quarters(u32x2 d) {
   return u32x2{__builtin_amdgcn_perm(b[1], b[0], 0x06020400), __builtin_amdgcn_perm(b[1], b[0], 0x07030501)};
 }
 
+// What the lane two further in its quad gives.
+__device__ __forceinline__ uint32_t across_pairs(uint32_t d) { return __builtin_amdgcn_update_dpp(0, (int)d, 0x4E, 0xf, 0xf, true); }
+
 // E: the rows' type; TILES: 16-token tiles of a block.
-template <typename E, int TILES> __global__ __launch_bounds__(256) void oscar_q8_append_kernel(AppendParams P) {
+template <typename E, int TILES> __global__ __launch_bounds__(256, TILES == 8 ? 5 : 8) void oscar_q8_append_kernel(AppendParams P) {
   constexpr int BLOCK = 16 * TILES;
-  __shared__ float s_max[4];
+  __shared__ uint32_t s_max[4];
   // (heads next to each other: a row's are)
   const uint32_t unit = blockIdx.x / P.c.heads;
   const int b = blockIdx.y, h = blockIdx.x % P.c.heads, side = unit & 1, tid = threadIdx.x;
@@ -89,6 +117,7 @@ template <typename E, int TILES> __global__ __launch_bounds__(256) void oscar_q8
   uint16_t* win = (side ? P.c.win_v : P.c.win_k) + ((int64_t)b * P.c.heads + h) * (2 * BLOCK * D);
   const int m = tid >> 4, c8 = tid & 15;   // token of a tile, piece of 8 channels
 
+  const int page = q8_page(P.c, b, (int)((int64_t)j * BLOCK / R));   // (asked for ahead of the rows)
   const auto new_row = [&](int64_t pos) -> u32x4 {   // of a new token (zeros where there is no such row)
     const int64_t row = s.row + (pos - s.old);
     if (row < 0 || row >= P.r.n_rows) return u32x4{};
@@ -104,14 +133,14 @@ template <typename E, int TILES> __global__ __launch_bounds__(256) void oscar_q8
                             : *reinterpret_cast<const u32x4*>(win + (pos % (2 * BLOCK)) * D + c8 * 8);
   }
   const bool whole = ((int64_t)j + 1) * BLOCK <= s.len;
-  float top = 0.0f;
+  // the largest, by the numbers' bits; one that counts for another (rare) is replaced first
+  u16x2 most = {};
 #pragma unroll
-  for (int i = 0; i < TILES; ++i) {
-    float x[8];
-    widen8<E>(raw[i], x);
+  for (int i = 0; i < TILES; ++i) most = most_bits(most, raw[i]);
+  if (__any(max(most[0], most[1]) > MOST_BITS<E>)) {
+    most = u16x2{};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
-    raw[i] = narrow8<E>(x);
+    for (int i = 0; i < TILES; ++i) most = most_bits(most, raw[i] = counted<E>(raw[i]));
   }
   // The window takes the tokens from the last whole block on.  It has two places a token: a block j + 2, j + 4, ..
   // goes where this one, if it is the first, has just been read; so the first block's workgroup writes it, behind
@@ -126,49 +155,46 @@ template <typename E, int TILES> __global__ __launch_bounds__(256) void oscar_q8
   }
   if (!whole) return;
 
+  uint32_t bits = max(most[0], most[1]);
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  if ((tid & 63) == 0) s_max[tid >> 6] = top;
+  for (int d = 1; d < 64; d *= 2) bits = max(bits, (uint32_t)__shfl_xor((int)bits, d));
+  if ((tid & 63) == 0) s_max[tid >> 6] = bits;
   __syncthreads();
-  top = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+  const float top = widen<E>(max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3])));
   int e = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) - 9 + (__builtin_amdgcn_frexp_mantf(top) > 0.875f) : 0;
   e = max(e, -100);
-  const float inverse = __uint_as_float((uint32_t)(127 - e) << 23);
+  const float scale = __uint_as_float((uint32_t)(127 + e) << 23);
 
-  const int page = q8_page(P.c, b, (int)((int64_t)j * BLOCK / R));
   if (page >= 0) {
     const int t0 = (int)((int64_t)j * BLOCK % R);   // of the page
     uint8_t* out = (side ? P.c.v_codes : P.c.k_codes) + ((int64_t)page * P.c.heads + h) * Q8_PAGE_BYTES + t0 * D;
     u32x2 codes[TILES];
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
-      float x[8];
-      widen8<E>(raw[i], x);
 #pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        int w = 0;
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * d] * inverse, x[4 * d + 1] * inverse, w, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * d + 2] * inverse, x[4 * d + 3] * inverse, w, true);
-        codes[i][d] = w;
-      }
+      for (int d = 0; d < 2; ++d)
+        codes[i][d] = two_codes<E>(two_codes<E>(0, raw[i][2 * d], scale, false), raw[i][2 * d + 1], scale, true);
     }
     if (side == 0) {
 #pragma unroll
       for (int i = 0; i < TILES; ++i)
         *reinterpret_cast<u32x2*>(out + i * 2048 + (c8 / 8) * 1024 + (c8 % 8 / 2) * 256 + m * 16 + (c8 % 2) * 8) = codes[i];
     } else {
-      const int q4 = m / 4, c = c8 * 8 + (m % 4) * 2;   // afterwards: channels c and c + 1, tokens 4 q4 ..
+      // afterwards a lane has channels c and c + 1 of tokens 4 q4 ..; the lane two further on c + 16 and c + 17: they
+      // change so that one has c and c + 16, which lie next to each other, the other c + 1 and c + 17
+      const int q4 = m / 4, c = c8 * 8 + (m % 4) * 2;
+      const bool upper = c8 & 2;
+      uint8_t* to = out + (c / 32) * 1024 + q4 * 256 + (c % 16 + upper) * 16;
 #pragma unroll
       for (int i = 0; i < TILES; i += 2) {
         const u32x2 a = turn_quarters(codes[i]), z = turn_quarters(codes[i + 1]);
-        uint8_t* to = out + (i / 2) * Q8_STEP_BYTES + (c / 32) * 1024 + q4 * 256 + (c % 16) * 16 + (c % 32 / 16) * 8;
-        *reinterpret_cast<u32x2*>(to) = u32x2{a[0], z[0]};
-        *reinterpret_cast<u32x2*>(to + 16) = u32x2{a[1], z[1]};
+        const uint32_t a_in = across_pairs(upper ? a[0] : a[1]), z_in = across_pairs(upper ? z[0] : z[1]);
+        *reinterpret_cast<u32x4*>(to + (i / 2) * Q8_STEP_BYTES) =
+            upper ? u32x4{a_in, z_in, a[1], z[1]} : u32x4{a[0], z[0], a_in, z_in};
       }
     }
     if (tid == 0)
-      (side ? P.c.v_scales : P.c.k_scales)[((int64_t)page * P.c.heads + h) * (R / BLOCK) + t0 / BLOCK] =
-          __uint_as_float((uint32_t)(127 + e) << 23);
+      (side ? P.c.v_scales : P.c.k_scales)[((int64_t)page * P.c.heads + h) * (R / BLOCK) + t0 / BLOCK] = scale;
   }
 
   // the later block of this half of the window
@@ -179,9 +205,7 @@ template <typename E, int TILES> __global__ __launch_bounds__(256) void oscar_q8
   for (int i = 0; i < TILES; ++i) {
     const int64_t pos = (int64_t)late * BLOCK + 16 * i + m;
     if (pos < s.old || pos >= s.len) continue;
-    float x[8];
-    widen8<E>(new_row(pos), x);
-    *reinterpret_cast<u32x4*>(win + (pos % (2 * BLOCK)) * D + c8 * 8) = narrow8<E>(x);
+    *reinterpret_cast<u32x4*>(win + (pos % (2 * BLOCK)) * D + c8 * 8) = counted<E>(new_row(pos));
   }
 }
 
@@ -211,7 +235,7 @@ __device__ __forceinline__ uint32_t turn_quad(uint32_t d, int lane) {
   // even lanes: bytes 0 and 2 of both; odd lanes: bytes 1 and 3
   d = lane & 1 ? __builtin_amdgcn_perm(d, other, 0x07030501) : __builtin_amdgcn_perm(other, d, 0x06020400);
   // bytes: (own pair's first lane, second lane) for byte lane % 2, then the same for byte lane % 2 + 2
-  const uint32_t far = __builtin_amdgcn_update_dpp(0, (int)d, 0x4E, 0xf, 0xf, true);     // lanes 2 3 0 1
+  const uint32_t far = across_pairs(d);
   return lane & 2 ? __builtin_amdgcn_perm(d, far, 0x07060302) : __builtin_amdgcn_perm(far, d, 0x05040100);
 }
 
