@@ -26,6 +26,8 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int O_PITCH = 132;       // of a row of sums in LDS: 16 rows' pieces on different banks
+constexpr int V_PITCH = 264;       // bytes of a window row in LDS (a wave's 32 rows take the place of its 16 rows of sums)
+static_assert(32 * V_PITCH <= 16 * O_PITCH * 4, "a wave's window rows fit its sums' place");
 constexpr float NO_REF = -1e30f;   // reference of a row that has seen no token
 // A reference moves when a logit passes it by this much (in powers of two): probabilities stay below 2^8, and a wave
 // seldom has to multiply its sums.
@@ -216,6 +218,75 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
   if (p0 < p1) {
     load(page, P.c.k_codes, P.c.k_scales, k, ks);
     load(page, P.c.v_codes, P.c.v_scales, v, vs);
+  }
+  // the window, its steps by the last split's waves, while the first pages are on their way
+  if (split == P.splits - 1) {
+    const uint16_t* wk = P.c.win_k + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
+    const uint16_t* wv = P.c.win_v + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
+    const int stop = min(seq.len, w.max_pos + 1);
+    for (int t0 = coded + wave * Q8_STEP_TOKENS; t0 < stop; t0 += 4 * Q8_STEP_TOKENS) {
+      const int slot = t0 % (2 * P.c.block);   // (a step does not wrap)
+      // values go through LDS, because an operand wants 8 tokens of a channel in a lane; what no token owns becomes zero
+      u32x4 rows_v[8];
+      uint8_t* tile_v = reinterpret_cast<uint8_t*>(J.o[wave]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rows_v[i] = *reinterpret_cast<const u32x4*>(wv + (slot + 4 * i + q4) * D + 8 * n);
+      f32x4 st[RT][2];
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile) {
+        const uint16_t* row = wk + (slot + 16 * tile + n) * D + 16 * q4;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const Op key = __builtin_bit_cast(Op, *reinterpret_cast<const u32x4*>(row + 64 * (kk / 2) + 8 * (kk % 2)));
+#pragma unroll
+          for (int r = 0; r < RT; ++r) st[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : st[r][tile]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const u32x4 x = t0 + 4 * i + q4 < stop ? rows_v[i] : u32x4{};
+        u32x2* to = reinterpret_cast<u32x2*>(tile_v + (4 * i + q4) * V_PITCH + 16 * n);
+        to[0] = u32x2{x[0], x[1]};
+        to[1] = u32x2{x[2], x[3]};
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+      for (int r = 0; r < RT; ++r) hide<F16, RT>(w, r, st[r], t0, q4, stop);
+      move_reference<F16, RT>(w, st, P.scale_log2);
+      Limbs pr[RT];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        pr[r] = probabilities<F16, RT>(w, r, st[r], P.scale_log2);
+        add_up<F16, RT>(w, r, pr[r]);
+      }
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        bf16x8 val, rest;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint16_t x = *reinterpret_cast<const uint16_t*>(tile_v + (16 * (i / 4) + 4 * q4 + i % 4) * V_PITCH + 2 * (16 * c + n));
+          if constexpr (F16) {   // 11 bits in two limbs
+            const float f = (float)__builtin_bit_cast(_Float16, x);
+            val[i] = (__bf16)f;
+            rest[i] = (__bf16)(f - (float)val[i]);
+          } else {
+            val[i] = __builtin_bit_cast(__bf16, x);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          w.o[r][c] = mul_bf16(val, pr[r].lo, mul_bf16(val, pr[r].hi, w.o[r][c]));
+          if constexpr (F16) w.o[r][c] = mul_bf16(rest, pr[r].hi, w.o[r][c]);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+  }
+  if (p0 < p1) {
 #pragma unroll
     for (int tile = 0; tile < 2; ++tile)
 #pragma unroll
@@ -273,59 +344,6 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
     scale = later_scale;
     page = next;
     next = after;
-  }
-
-  // the window: its steps by the last split's waves
-  if (split == P.splits - 1) {
-    const uint16_t* wk = P.c.win_k + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
-    const uint16_t* wv = P.c.win_v + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
-    const int stop = min(seq.len, w.max_pos + 1);
-    for (int t0 = coded + wave * Q8_STEP_TOKENS; t0 < stop; t0 += 4 * Q8_STEP_TOKENS) {
-      const int slot = t0 % (2 * P.c.block);   // (a step does not wrap)
-      f32x4 st[RT][2];
-#pragma unroll
-      for (int tile = 0; tile < 2; ++tile) {
-        const uint16_t* row = wk + (slot + 16 * tile + n) * D + 16 * q4;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const Op key = __builtin_bit_cast(Op, *reinterpret_cast<const u32x4*>(row + 64 * (kk / 2) + 8 * (kk % 2)));
-#pragma unroll
-          for (int r = 0; r < RT; ++r) st[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : st[r][tile]);
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < RT; ++r) hide<F16, RT>(w, r, st[r], t0, q4, stop);
-      move_reference<F16, RT>(w, st, P.scale_log2);
-      Limbs pr[RT];
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        pr[r] = probabilities<F16, RT>(w, r, st[r], P.scale_log2);
-        add_up<F16, RT>(w, r, pr[r]);
-      }
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        bf16x8 val, rest;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int t = 16 * (i / 4) + 4 * q4 + i % 4;
-          // what no token owns counts as zero: it need not be a number
-          uint32_t x = wv[(slot + t) * D + 16 * c + n];
-          x = t0 + t < stop ? x : 0;
-          if constexpr (F16) {   // 11 bits in two limbs
-            const float f = (float)__builtin_bit_cast(_Float16, (uint16_t)x);
-            val[i] = (__bf16)f;
-            rest[i] = (__bf16)(f - (float)val[i]);
-          } else {
-            val[i] = __builtin_bit_cast(__bf16, (uint16_t)x);
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          w.o[r][c] = mul_bf16(val, pr[r].lo, mul_bf16(val, pr[r].hi, w.o[r][c]));
-          if constexpr (F16) w.o[r][c] = mul_bf16(rest, pr[r].hi, w.o[r][c]);
-        }
-      }
-    }
   }
 
   // the four waves' sums
