@@ -7,10 +7,20 @@
 // onto its logits; value codes times their scale are exact in bf16.  Probabilities are rounded, to two bf16 limbs
 // (2^-17), each a matrix product of its own: with one, 2^-9 a token would add to the output's own rounding.
 //
-// A workgroup takes RT tiles of 16 rows (row = new token * g + query head of the group) of one kv head and a range of
-// pages; of a page each of its four waves takes a step of 32 tokens, so that four kilobytes of keys and four of values
-// lie between a wave's loads and their use.  S^T = K Q^T: a lane gets logits of 8 tokens of one row, and these are, as
-// they stand, its part of the operand of O^T = V^T P^T.  No LDS until the waves' sums are joined at the end.
+// A workgroup takes 16 or 32 rows (row = new token * g + query head of the group) of one kv head and a range of
+// pages; of a page each of its four waves takes a step of 32 tokens.  S^T = K Q^T: a lane gets logits of tokens of
+// one row, and these are, as they stand, its part of the operand of O^T = V^T P^T.  What is loaded lies one step
+// ahead of its use, and logits are worked out a step ahead of their probabilities.  No barrier until the waves' sums
+// are joined at the end.
+//
+// Up to 16 rows (a decoding step) take products of 16 x 16 x 32: the cache's bytes bound it (8 sequences of 32K: 94 us,
+// 5.7 TB/s with the start, the end and the joining launch; a plain read of as many bytes takes 80).  More rows take products of
+// 32 x 32 x 16 and are bound by issue: 220 vector instructions a step of 32 x 32 (64 conversions, 48 for limbs, 16
+// exponentials, 24 exchanges) beside 24 products of 32 clocks; vector issue is busy 69 % of the time, the matrix cores 43 %
+// (8192 rows of a kv head over themselves: 232 us).  A product keeps vector instructions out for 8 clocks whatever
+// its size (measured, of two waves side by side), which speaks for the larger one; two tiles of 16 x 16 x 32 took 1 .. 5 % more.
+// Three waves a SIMD instead of two (queries in LDS) spill: 261 us; four tiles of 16 rows leave one wave: 303.
+
 #include <algorithm>
 
 #include "oscar_q8.h"
@@ -20,6 +30,7 @@ namespace {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -65,118 +76,240 @@ template <> struct Io<false> {
   using Op = bf16x8;
   static __device__ __forceinline__ Op keys(u32x2 codes) { return bf16_operand(codes, 1.0f); }
   static __device__ __forceinline__ f32x4 mul(Op a, Op b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x16 mul32(Op a, Op b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Io<true> {
   using Op = f16x8;
   static __device__ __forceinline__ Op keys(u32x2 codes) { return f16_operand(codes); }
   static __device__ __forceinline__ f32x4 mul(Op a, Op b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x16 mul32(Op a, Op b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
 __device__ __forceinline__ f32x4 mul_bf16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// A wave's rows: queries, sums of values (transposed: 8 tiles of 16 channels), sum and reference.
-template <bool F16, int RT> struct Rows {
-  typename Io<F16>::Op q[RT][4];
-  f32x4 o[RT][8];
-  f32x4 sum[RT];        // four times the same: probabilities are added up by the matrix cores too
-  float ref[RT];
-  int pos[RT];          // the lane's row's position, -1: no row
-  int min_pos, max_pos; // of the rows there are
-};
-
+__device__ __forceinline__ f32x16 mul32_bf16(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
 __device__ __forceinline__ uint32_t two_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }
 
-// Probabilities of a step's 8 logits of the lane's row: two limbs of the operand.
-struct Limbs {
-  bf16x8 hi, lo;
-};
-// Logits of tokens that a row does not see, of a step from t0 on: from `limit` on, or behind the row's own.
-template <bool F16, int RT> __device__ __forceinline__ void hide(const Rows<F16, RT>& w, int r, f32x4* s, int t0, int q4, int limit) {
-  const int last = min(w.pos[r], limit - 1);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    s[0][i] = t0 + 4 * q4 + i <= last ? s[0][i] : -INFINITY;
-    s[1][i] = t0 + 16 + 4 * q4 + i <= last ? s[1][i] : -INFINITY;
+// What a wave does with a step of 32 tokens, by the shape of its products.  LOGITS: of a lane; pairs of its
+// probabilities make OPERANDS operands of the value products.  keys / values: raw pages' bytes as Q8_STEP_BYTES has
+// them; window_keys: 16-bit keys at `row0`.
+//
+// 16 rows: lane 16 * q4 + n has row n and tokens 16 * (i / 4) + 4 * q4 + i % 4.
+template <bool F16> struct Rows16 {
+  using Op = typename Io<F16>::Op;
+  using Acc = f32x4;
+  using Logits = float[8];
+  static constexpr int ROWS = 16, LOGITS = 8, KEYS = 4, TILES = 8, OPERANDS = 1;
+  static __device__ __forceinline__ int row(int lane) { return lane & 15; }
+  static __device__ __forceinline__ int token(int lane, int i) { return 16 * (i / 4) + 4 * (lane >> 4) + i % 4; }
+  static __device__ __forceinline__ int channel(int lane, int tile, int i) { return 16 * tile + 4 * (lane >> 4) + i; }
+  static __device__ __forceinline__ int query_channel(int lane, int kk) { return 64 * (kk / 2) + 16 * (lane >> 4) + 8 * (kk % 2); }
+  static __device__ __forceinline__ float over_lanes(float x) {   // the largest of the lanes that share a row
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
   }
+  static __device__ __forceinline__ float sum_lanes(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+  }
+  static __device__ __forceinline__ void put(Logits& s, int tile, f32x4 x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[4 * tile + i] = x[i];
+  }
+  static __device__ __forceinline__ void keys(const u32x4* k, const Op* q, Logits& s) {
+#pragma unroll
+    for (int tile = 0; tile < 2; ++tile) {
+      f32x4 x = {};
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const u32x4 c = k[2 * tile + kk / 2];
+        x = Io<F16>::mul(Io<F16>::keys(u32x2{c[2 * (kk % 2)], c[2 * (kk % 2) + 1]}), q[kk], x);
+      }
+      put(s, tile, x);
+    }
+  }
+  static __device__ __forceinline__ void window_keys(const uint16_t* row0, int lane, const Op* q, Logits& s) {
+#pragma unroll
+    for (int tile = 0; tile < 2; ++tile) {
+      const uint16_t* in = row0 + (16 * tile + (lane & 15)) * D;
+      f32x4 x = {};
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        x = Io<F16>::mul(__builtin_bit_cast(Op, *reinterpret_cast<const u32x4*>(in + query_channel(lane, kk))), q[kk], x);
+      put(s, tile, x);
+    }
+  }
+  static __device__ __forceinline__ bf16x8 operand(const uint32_t* pairs, int) {
+    return __builtin_bit_cast(bf16x8, u32x4{pairs[0], pairs[1], pairs[2], pairs[3]});
+  }
+  static __device__ __forceinline__ void values(const u32x4* v, float scale, const bf16x8* hi, const bf16x8* lo, Acc* o) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const u32x4 x = v[c / 2];
+      const bf16x8 val = bf16_operand(u32x2{x[2 * (c % 2)], x[2 * (c % 2) + 1]}, scale);
+      o[c] = mul_bf16(val, lo[0], mul_bf16(val, hi[0], o[c]));
+    }
+  }
+  static __device__ __forceinline__ Acc mul(bf16x8 a, bf16x8 b, Acc c) { return mul_bf16(a, b, c); }
+  static __device__ __forceinline__ int value_channel(int lane, int tile) { return 16 * tile + (lane & 15); }
+  static __device__ __forceinline__ int value_token(int lane, int, int i) { return token(lane, i); }
+};
+
+// 32 rows: lane 32 * g + n has row n and tokens 8 * (i / 4) + 4 * g + i % 4.  Rows of 16 lanes of the bytes change places
+// so that 32 tokens (32 channels) lie side by side: a page's lane 16 * q4 + n has token n of either tile, channels of
+// q4 (channel n of either half, tokens of q4).  In place: bytes that are not loaded anew would be copied else.
+template <bool F16> struct Rows32 {
+  using Op = typename Io<F16>::Op;
+  using Acc = f32x16;
+  using Logits = f32x16;
+  static constexpr int ROWS = 32, LOGITS = 16, KEYS = 8, TILES = 4, OPERANDS = 2;
+  static __device__ __forceinline__ int row(int lane) { return lane & 31; }
+  static __device__ __forceinline__ int token(int lane, int i) { return 8 * (i / 4) + 4 * (lane >> 5) + i % 4; }
+  static __device__ __forceinline__ int channel(int lane, int tile, int i) { return 32 * tile + 8 * (i / 4) + 4 * (lane >> 5) + i % 4; }
+  // product kk: half of the channels kk / 4, even or odd sixteens of it kk / 2 % 2, eight of those kk % 2
+  static __device__ __forceinline__ int query_channel(int lane, int kk) {
+    return 64 * (kk / 4) + 16 * (2 * (lane >> 5) + kk / 2 % 2) + 8 * (kk % 2);
+  }
+  static __device__ __forceinline__ float over_lanes(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
+  static __device__ __forceinline__ float sum_lanes(float x) { return x + __shfl_xor(x, 32); }
+  static __device__ __forceinline__ void keys(u32x4* k, const Op* q, Logits& s) {
+    f32x16 x = {};
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const auto two = __builtin_amdgcn_permlane16_swap(k[half][d], k[2 + half][d], false, false);
+        k[half][d] = two[0], k[2 + half][d] = two[1];   // even and odd sixteens of channels
+      }
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        const u32x4 c = k[half + kk / 2 * 2];
+        x = Io<F16>::mul32(Io<F16>::keys(u32x2{c[2 * (kk % 2)], c[2 * (kk % 2) + 1]}), q[4 * half + kk], x);
+      }
+    }
+    s = x;
+  }
+  static __device__ __forceinline__ void window_keys(const uint16_t* row0, int lane, const Op* q, Logits& s) {
+    const uint16_t* in = row0 + (lane & 31) * D;
+    f32x16 x = {};
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+      x = Io<F16>::mul32(__builtin_bit_cast(Op, *reinterpret_cast<const u32x4*>(in + query_channel(lane, kk))), q[kk], x);
+    s = x;
+  }
+  // product j of the values takes the tokens of quarters g (j = 0) and 2 + g (j = 1) of a page's step
+  static __device__ __forceinline__ bf16x8 operand(const uint32_t* pairs, int j) {
+    return __builtin_bit_cast(bf16x8, u32x4{pairs[2 * j], pairs[2 * j + 1], pairs[4 + 2 * j], pairs[5 + 2 * j]});
+  }
+  static __device__ __forceinline__ void values(u32x4* v, float scale, const bf16x8* hi, const bf16x8* lo, Acc* o) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const auto two = __builtin_amdgcn_permlane16_swap(v[c][t], v[c][2 + t], false, false);
+        const auto four = __builtin_amdgcn_permlane32_swap(two[0], two[1], false, false);
+        v[c][t] = four[0], v[c][2 + t] = four[1];
+      }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {   // (a sum's products lie four apart)
+      bf16x8 val[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = mul32_bf16(val[c] = bf16_operand(u32x2{v[c][2 * j], v[c][2 * j + 1]}, scale), hi[j], o[c]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = mul32_bf16(val[c], lo[j], o[c]);
+    }
+  }
+  static __device__ __forceinline__ Acc mul(bf16x8 a, bf16x8 b, Acc c) { return mul32_bf16(a, b, c); }
+  static __device__ __forceinline__ int value_channel(int lane, int tile) { return 32 * tile + (lane & 31); }
+  static __device__ __forceinline__ int value_token(int lane, int j, int i) { return token(lane, 4 * j + i + (i / 4) * 4); }
+};
+
+// A wave's rows: queries, sums of values (transposed), sum and reference.
+template <class S> struct State {
+  typename S::Op q[S::KEYS];
+  typename S::Acc o[S::TILES];
+  float sum, ref;        // sum: of the lane's own tokens
+  int pos;               // the lane's row's position, -1: no row
+  int min_pos, max_pos;  // of the rows there are
+};
+
+// Logits of tokens that a row does not see, of a step from t0 on: from `limit` on, or behind the row's own.
+template <class S> __device__ __forceinline__ void hide(const State<S>& w, typename S::Logits& s, int t0, int lane, int limit) {
+  const int last = min(w.pos, limit - 1) - t0;
+#pragma unroll
+  for (int i = 0; i < S::LOGITS; ++i) s[i] = S::token(lane, i) <= last ? s[i] : -INFINITY;
 }
 // The reference follows the step's largest logit, all sums with it.
-template <bool F16, int RT> __device__ __forceinline__ void move_reference(Rows<F16, RT>& w, const f32x4 (*s)[2], float scale) {
-  float top[RT];
-  bool past = false;
+template <class S> __device__ __forceinline__ void move_reference(State<S>& w, const typename S::Logits& s, float scale) {
+  float top = s[0];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    top[r] = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])),
-                   fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3]))) * scale;
-    past |= top[r] > w.ref[r] + REF_SLACK;
-  }
-  if (!__any(past)) return;
+  for (int i = 1; i < S::LOGITS; ++i) top = fmaxf(top, s[i]);
+  top *= scale;
+  if (!__any(top > w.ref + REF_SLACK)) return;
+  const float ref = fmaxf(w.ref, S::over_lanes(top));
+  const float f = __builtin_amdgcn_exp2f(w.ref - ref);
+  w.ref = ref;
+  w.sum *= f;
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    top[r] = fmaxf(top[r], __shfl_xor(top[r], 16));
-    top[r] = fmaxf(top[r], __shfl_xor(top[r], 32));
-    const float ref = fmaxf(w.ref[r], top[r]);
-    const float f = __builtin_amdgcn_exp2f(w.ref[r] - ref);
-    w.ref[r] = ref;
-    w.sum[r] *= f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) w.o[r][c] *= f;
-  }
+  for (int c = 0; c < S::TILES; ++c) w.o[c] *= f;
 }
-// Probabilities, two limbs of the operand.
-template <bool F16, int RT> __device__ __forceinline__ Limbs probabilities(const Rows<F16, RT>& w, int r, const f32x4* s, float scale) {
-  Limbs p;
-  u32x4 hi, lo;
+// Probabilities, two limbs of the operands.
+template <class S> __device__ __forceinline__ void probabilities(State<S>& w, const typename S::Logits& s, float scale, bf16x8* hi, bf16x8* lo) {
+  uint32_t h[S::LOGITS / 2], l[S::LOGITS / 2];
+  float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {   // (two at a time: the conversion takes two)
-    const float a = __builtin_amdgcn_exp2f(fmaf(s[i / 2][2 * (i & 1)], scale, -w.ref[r]));
-    const float b = __builtin_amdgcn_exp2f(fmaf(s[i / 2][2 * (i & 1) + 1], scale, -w.ref[r]));
-    hi[i] = two_bf16(a, b);
-    lo[i] = two_bf16(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xffff0000u));
+  for (int i = 0; i < S::LOGITS / 2; ++i) {   // (two at a time: the conversion takes two)
+    const float a = __builtin_amdgcn_exp2f(fmaf(s[2 * i], scale, -w.ref)), b = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], scale, -w.ref));
+    sum += a + b;
+    h[i] = two_bf16(a, b);
+    l[i] = two_bf16(a - __uint_as_float(h[i] << 16), b - __uint_as_float(h[i] & 0xffff0000u));
   }
-  p.hi = __builtin_bit_cast(bf16x8, hi);
-  p.lo = __builtin_bit_cast(bf16x8, lo);
-  return p;
-}
-template <bool F16, int RT> __device__ __forceinline__ void add_up(Rows<F16, RT>& w, int r, const Limbs& p) {
-  const __bf16 one = (__bf16)1.0f;
-  const bf16x8 ones = {one, one, one, one, one, one, one, one};
-  w.sum[r] = mul_bf16(ones, p.lo, mul_bf16(ones, p.hi, w.sum[r]));
+  w.sum += sum;
+#pragma unroll
+  for (int j = 0; j < S::OPERANDS; ++j) hi[j] = S::operand(h, j), lo[j] = S::operand(l, j);
 }
 
-// Where the waves' sums meet.
-template <int RT> struct __align__(16) Joined {
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Where the waves' sums meet, 16 rows at a time.
+struct __align__(16) Joined {
   float o[4][16 * O_PITCH];
-  float sum[4][16 * RT], ref[4][16 * RT];
+  float sum[4][32], ref[4][32];
 };
 
 // The rows from row0 on (of a sequence and kv head) over the pages of a split, by a workgroup.
-template <bool F16, int RT>
-__device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, int b, int h, int split, int row0, Joined<RT>& J) {
-  using Op = typename Io<F16>::Op;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, q4 = lane >> 4;
+template <bool F16, class S>
+__device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, int b, int h, int split, int row0, Joined& J) {
+  using Op = typename S::Op;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rows = seq.n * P.g;
-  Rows<F16, RT> w;
+  State<S> w;
   w.min_pos = seq.old + row0 / P.g;
-  w.max_pos = seq.old + (min(row0 + 16 * RT, rows) - 1) / P.g;
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int row = row0 + r * 16 + n, t = row / P.g;
+  w.max_pos = seq.old + (min(row0 + S::ROWS, rows) - 1) / P.g;
+  {
+    const int row = row0 + S::row(lane), t = row / P.g;
     const int64_t at = seq.row + t;
     const bool is = row < rows && at >= 0 && at < P.r.n_rows;
-    w.pos[r] = is ? seq.old + t : -1;
-    const uint16_t* q = P.q + at * P.q_stride + (h * P.g + row % P.g) * D + 16 * q4;
+    w.pos = is ? seq.old + t : -1;
+    const uint16_t* q = P.q + at * P.q_stride + (h * P.g + row % P.g) * D;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
+    for (int kk = 0; kk < S::KEYS; ++kk) {
       u32x4 x = {};
-      if (is) x = *reinterpret_cast<const u32x4*>(q + 64 * (kk / 2) + 8 * (kk % 2));
-      w.q[r][kk] = __builtin_bit_cast(Op, x);
+      if (is) x = *reinterpret_cast<const u32x4*>(q + S::query_channel(lane, kk));
+      w.q[kk] = __builtin_bit_cast(Op, x);
     }
-    w.sum[r] = f32x4{};
-    w.ref[r] = NO_REF;
+    w.sum = 0.0f;
+    w.ref = NO_REF;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) w.o[r][c] = f32x4{};
+    for (int c = 0; c < S::TILES; ++c) w.o[c] = typename S::Acc{};
   }
 
   // pages of whole blocks, and the window behind them
@@ -188,19 +321,14 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
   const int per_page = R / P.c.block;
   const int32_t* table = P.c.table + (int64_t)b * P.c.max_pages;
 
-  // What is loaded lies one step ahead of its use, and logits are worked out a step ahead of their probabilities, so
-  // that the matrix cores have products to do while exponentials and limbs are made, and the other way round.
-  u32x4 k[4], v[4];
-  float ks = 0.0f, vs = 0.0f;
+  u32x4 k[4] = {}, v[4] = {};
+  float ks = 1.0f, vs = 1.0f;
   const auto page_of = [&](int p) -> int {
     if (p >= p1 || p * R + wave * Q8_STEP_TOKENS >= end) return -1;
     const int page = __builtin_amdgcn_readfirstlane(table[p]);
     return (uint32_t)page < (uint32_t)P.c.num_pages ? page : -1;
   };
   const auto load = [&](int page, const uint8_t* codes, const float* scales, u32x4* x, float& scale) {
-    scale = 1.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = u32x4{};   // (a page that is none: what stands for it must be numbers)
     if (page < 0) return;
     const int64_t at = (int64_t)page * P.c.heads + h;
     const uint8_t* in = codes + at * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES + lane * 16;
@@ -208,168 +336,116 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
     for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(in + i * 1024);
     scale = scales[at * per_page + wave * Q8_STEP_TOKENS / P.c.block];
   };
-  const auto key_operand = [&](int tile, int kk) {
-    const u32x4 x = k[2 * tile + kk / 2];
-    return Io<F16>::keys(u32x2{x[2 * (kk % 2)], x[2 * (kk % 2) + 1]});
-  };
 
   int page = page_of(p0), next = page_of(p0 + 1);
-  f32x4 s[RT][2];
   if (p0 < p1) {
     load(page, P.c.k_codes, P.c.k_scales, k, ks);
     load(page, P.c.v_codes, P.c.v_scales, v, vs);
   }
+
   // the window, its steps by the last split's waves, while the first pages are on their way
   if (split == P.splits - 1) {
-    const uint16_t* wk = P.c.win_k + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
-    const uint16_t* wv = P.c.win_v + ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
+    const int64_t win = ((int64_t)b * P.c.heads + h) * (2 * P.c.block * D);
     const int stop = min(seq.len, w.max_pos + 1);
     for (int t0 = coded + wave * Q8_STEP_TOKENS; t0 < stop; t0 += 4 * Q8_STEP_TOKENS) {
       const int slot = t0 % (2 * P.c.block);   // (a step does not wrap)
       // values go through LDS, because an operand wants 8 tokens of a channel in a lane; what no token owns becomes zero
       u32x4 rows_v[8];
       uint8_t* tile_v = reinterpret_cast<uint8_t*>(J.o[wave]);
+      const int tr = lane >> 4, tc = lane & 15;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rows_v[i] = *reinterpret_cast<const u32x4*>(wv + (slot + 4 * i + q4) * D + 8 * n);
-      f32x4 st[RT][2];
-#pragma unroll
-      for (int tile = 0; tile < 2; ++tile) {
-        const uint16_t* row = wk + (slot + 16 * tile + n) * D + 16 * q4;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const Op key = __builtin_bit_cast(Op, *reinterpret_cast<const u32x4*>(row + 64 * (kk / 2) + 8 * (kk % 2)));
-#pragma unroll
-          for (int r = 0; r < RT; ++r) st[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : st[r][tile]);
-        }
-      }
+      for (int i = 0; i < 8; ++i) rows_v[i] = *reinterpret_cast<const u32x4*>(P.c.win_v + win + (slot + 4 * i + tr) * D + 8 * tc);
+      typename S::Logits s;
+      S::window_keys(P.c.win_k + win + slot * D, lane, w.q, s);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const u32x4 x = t0 + 4 * i + q4 < stop ? rows_v[i] : u32x4{};
-        u32x2* to = reinterpret_cast<u32x2*>(tile_v + (4 * i + q4) * V_PITCH + 16 * n);
+        const u32x4 x = t0 + 4 * i + tr < stop ? rows_v[i] : u32x4{};
+        u32x2* to = reinterpret_cast<u32x2*>(tile_v + (4 * i + tr) * V_PITCH + 16 * tc);
         to[0] = u32x2{x[0], x[1]};
         to[1] = u32x2{x[2], x[3]};
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      wave_fence();
+      hide(w, s, t0, lane, stop);
+      move_reference(w, s, P.scale_log2);
+      bf16x8 hi[S::OPERANDS], lo[S::OPERANDS];
+      probabilities(w, s, P.scale_log2, hi, lo);
 #pragma unroll
-      for (int r = 0; r < RT; ++r) hide<F16, RT>(w, r, st[r], t0, q4, stop);
-      move_reference<F16, RT>(w, st, P.scale_log2);
-      Limbs pr[RT];
+      for (int c = 0; c < S::TILES; ++c)
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        pr[r] = probabilities<F16, RT>(w, r, st[r], P.scale_log2);
-        add_up<F16, RT>(w, r, pr[r]);
-      }
+        for (int j = 0; j < S::OPERANDS; ++j) {
+          bf16x8 val, rest;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        bf16x8 val, rest;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint16_t x = *reinterpret_cast<const uint16_t*>(tile_v + (16 * (i / 4) + 4 * q4 + i % 4) * V_PITCH + 2 * (16 * c + n));
-          if constexpr (F16) {   // 11 bits in two limbs
-            const float f = (float)__builtin_bit_cast(_Float16, x);
-            val[i] = (__bf16)f;
-            rest[i] = (__bf16)(f - (float)val[i]);
-          } else {
-            val[i] = __builtin_bit_cast(__bf16, x);
+          for (int i = 0; i < 8; ++i) {
+            const uint16_t x = *reinterpret_cast<const uint16_t*>(tile_v + S::value_token(lane, j, i) * V_PITCH + 2 * S::value_channel(lane, c));
+            if constexpr (F16) {   // 11 bits in two limbs
+              const float f = (float)__builtin_bit_cast(_Float16, x);
+              val[i] = (__bf16)f;
+              rest[i] = (__bf16)(f - (float)val[i]);
+            } else {
+              val[i] = __builtin_bit_cast(__bf16, x);
+            }
           }
+          w.o[c] = S::mul(val, lo[j], S::mul(val, hi[j], w.o[c]));
+          if constexpr (F16) w.o[c] = S::mul(rest, hi[j], w.o[c]);
         }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          w.o[r][c] = mul_bf16(val, pr[r].lo, mul_bf16(val, pr[r].hi, w.o[r][c]));
-          if constexpr (F16) w.o[r][c] = mul_bf16(rest, pr[r].hi, w.o[r][c]);
-        }
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      wave_fence();
     }
   }
-  if (p0 < p1) {
-#pragma unroll
-    for (int tile = 0; tile < 2; ++tile)
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        const Op key = key_operand(tile, kk);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) s[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : s[r][tile]);
-      }
-  }
+
+  typename S::Logits s = {};
+  if (p0 < p1) S::keys(k, w.q, s);
   float scale = ks * P.scale_log2;
-  if (p0 < p1) load(next, P.c.k_codes, P.c.k_scales, k, ks);
+  load(next, P.c.k_codes, P.c.k_scales, k, ks);
   for (int p = p0; p < p1; ++p) {
     const int after = page_of(p + 2);
     const int t0 = p * R + wave * Q8_STEP_TOKENS;
-    if (page < 0 || t0 + Q8_STEP_TOKENS - 1 > w.min_pos)
+    if (page < 0 || t0 + Q8_STEP_TOKENS - 1 > w.min_pos) {
+      hide(w, s, t0, lane, page < 0 ? 0 : end);
+      if (page < 0)   // (what stands for a page's values must be numbers)
 #pragma unroll
-      for (int r = 0; r < RT; ++r) hide<F16, RT>(w, r, s[r], t0, q4, page < 0 ? 0 : end);
-    move_reference<F16, RT>(w, s, scale);
-    f32x4 later[RT][2];
-#pragma unroll
-    for (int tile = 0; tile < 2; ++tile)
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        const Op key = key_operand(tile, kk);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) later[r][tile] = Io<F16>::mul(key, w.q[r][kk], kk == 0 ? f32x4{} : later[r][tile]);
-      }
-    const float later_scale = ks * P.scale_log2;
-    bf16x8 val[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const u32x4 x = v[c / 2];
-      val[c] = bf16_operand(u32x2{x[2 * (c % 2)], x[2 * (c % 2) + 1]}, vs);
+        for (int i = 0; i < 4; ++i) v[i] = u32x4{};
     }
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const Limbs pr = probabilities<F16, RT>(w, r, s[r], scale);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) w.o[r][c] = mul_bf16(val[c], pr.hi, w.o[r][c]);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) w.o[r][c] = mul_bf16(val[c], pr.lo, w.o[r][c]);
-      add_up<F16, RT>(w, r, pr);
-    }
-#ifdef SGB
-#pragma unroll
-    for (int i = 0; i < 26 * RT; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, SGB, 0);
-    }
-#endif
+    move_reference(w, s, scale);
+    bf16x8 hi[S::OPERANDS], lo[S::OPERANDS];
+    probabilities(w, s, scale, hi, lo);
+    S::keys(k, w.q, s);
+    scale = ks * P.scale_log2;
+    S::values(v, vs, hi, lo, w.o);
     load(after, P.c.k_codes, P.c.k_scales, k, ks);
     load(next, P.c.v_codes, P.c.v_scales, v, vs);
-#pragma unroll
-    for (int r = 0; r < RT; ++r) s[r][0] = later[r][0], s[r][1] = later[r][1];
-    scale = later_scale;
     page = next;
     next = after;
   }
 
   // the four waves' sums
+  w.sum = S::sum_lanes(w.sum);
+  if (lane < S::ROWS) J.sum[wave][lane] = w.sum, J.ref[wave][lane] = w.ref;
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    if (q4 == 0) J.sum[wave][16 * r + n] = w.sum[r][0], J.ref[wave][16 * r + n] = w.ref[r];
-  }
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
+  for (int r = 0; r < S::ROWS; r += 16) {
     if (r > 0) __syncthreads();
+    if (S::ROWS == 16 || (S::row(lane) & 16) == r) {
+      constexpr int NUMBERS = sizeof(typename S::Acc) / 4;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4*>(&J.o[wave][n * O_PITCH + 16 * c + 4 * q4]) = w.o[r][c];
+      for (int c = 0; c < S::TILES; ++c)
+#pragma unroll
+        for (int i = 0; i < NUMBERS; i += 4)
+          *reinterpret_cast<f32x4*>(&J.o[wave][(S::row(lane) & 15) * O_PITCH + S::channel(lane, c, i)]) =
+              f32x4{w.o[c][i], w.o[c][i + 1], w.o[c][i + 2], w.o[c][i + 3]};
+    }
     __syncthreads();
-    const int j = tid >> 4, row = row0 + r * 16 + j, t = row / P.g;
+    const int j = tid >> 4, row = row0 + r + j, t = row / P.g;
     const int64_t at = seq.row + t;
     if (row < rows && at >= 0 && at < P.r.n_rows) {
-      float ref = NO_REF, sum = 0.0f, f[4], x[8] = {};
+      float ref = NO_REF, sum = 0.0f, x[8] = {};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) ref = fmaxf(ref, J.ref[i][16 * r + j]);
+      for (int i = 0; i < 4; ++i) ref = fmaxf(ref, J.ref[i][r + j]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        f[i] = __builtin_amdgcn_exp2f(J.ref[i][16 * r + j] - ref);
-        sum += f[i] * J.sum[i][16 * r + j];
-        const f32x4 *o = reinterpret_cast<const f32x4*>(&J.o[i][j * O_PITCH + (tid & 15) * 8]), lo = o[0], hi = o[1];
+        const float f = __builtin_amdgcn_exp2f(J.ref[i][r + j] - ref);
+        sum += f * J.sum[i][r + j];
+        const f32x4 *o = reinterpret_cast<const f32x4*>(&J.o[i][j * O_PITCH + (tid & 15) * 8]), first = o[0], last = o[1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += f[i] * lo[e], x[4 + e] += f[i] * hi[e];
+        for (int e = 0; e < 4; ++e) x[e] += f * first[e], x[4 + e] += f * last[e];
       }
       const int head = h * P.g + row % P.g, c0 = (tid & 15) * 8;
       if (P.splits == 1) {
@@ -397,9 +473,9 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
   }
 }
 
-// F16: the io type; RT: tiles of 16 rows a workgroup.
-template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) void oscar_q8_attn_kernel(AttnParams P) {
-  __shared__ Joined<RT> J;
+// F16: the io type; ROWS: of a workgroup.
+template <bool F16, int ROWS> __global__ __launch_bounds__(256, ROWS == 16 ? 3 : 2) void oscar_q8_attn_kernel(AttnParams P) {
+  __shared__ Joined J;
   // row blocks of one range of pages lie on one die of eight, next to each other
   uint32_t id = blockIdx.x;
   int rb = 0;
@@ -413,12 +489,12 @@ template <bool F16, int RT> __global__ __launch_bounds__(256, RT == 1 ? 3 : 2) v
   const int h = id % P.c.heads, b = id / P.c.heads;
   if (b >= P.c.batch) return;
   const Q8Seq seq = q8_seq(P.r, b);
-  const int row0 = rb * 16 * RT, left = seq.n * P.g - row0;
+  const int row0 = rb * ROWS, left = seq.n * P.g - row0;
   if (left <= 0) return;
-  if (RT > 1 && left <= 16)   // (a block's last rows)
-    attend<F16, 1>(P, seq, b, h, split, row0, reinterpret_cast<Joined<1>&>(J));
-  else
-    attend<F16, RT>(P, seq, b, h, split, row0, J);
+  if (left <= 16)   // (all, or a sequence's last rows)
+    attend<F16, Rows16<F16>>(P, seq, b, h, split, row0, J);
+  else if constexpr (ROWS == 32)
+    attend<F16, Rows32<F16>>(P, seq, b, h, split, row0, J);
 }
 
 // Joins the splits of a row and query head: a workgroup, each wave a quarter of the splits.
@@ -487,17 +563,14 @@ template <bool F16> __global__ __launch_bounds__(256) void oscar_q8_join_kernel(
   }
 }
 
-// Tiles of 16 rows a workgroup.
-#ifndef MAXRT
-#define MAXRT 2
-#endif
-int row_tiles(int64_t rows) { return std::min<int64_t>((rows + 15) / 16, MAXRT); }
+// Rows of a workgroup.
+int rows_of(int64_t rows) { return rows <= 16 ? 16 : 32; }
 
-template <bool F16> void launch(const AttnParams& P, int rt, uint32_t grid, hipStream_t st) {
-  if (rt == 1)
-    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 1>), dim3(grid), dim3(256), 0, st, P);
+template <bool F16> void launch(const AttnParams& P, int block_rows, uint32_t grid, hipStream_t st) {
+  if (block_rows == 16)
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 16>), dim3(grid), dim3(256), 0, st, P);
   else
-    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 2>), dim3(grid), dim3(256), 0, st, P);
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 32>), dim3(grid), dim3(256), 0, st, P);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -510,15 +583,15 @@ bool heads_fit(const oscar_q8_cache* c, int32_t hq) {
 extern "C" int32_t oscar_q8_auto_splits(const oscar_q8_cache* cache, int32_t n_q_heads, int32_t T, int32_t max_seq_len) {
   if (oscar_check_q8_sizes(cache) != OSCAR_OK || !heads_fit(cache, n_q_heads) || T < 1 || max_seq_len < 1) return 1;
   const int64_t rows = (int64_t)T * (n_q_heads / cache->n_kv_heads);
-  const int rt = row_tiles(rows);
-  const int64_t units = (int64_t)cache->batch * cache->n_kv_heads * ((rows + 16 * rt - 1) / (16 * rt));
+  const int block = rows_of(rows);
+  const int64_t units = (int64_t)cache->batch * cache->n_kv_heads * ((rows + block - 1) / block);
   const int64_t pages = (max_seq_len + OSCAR_R - 1) / OSCAR_R;
   // One workgroup a compute unit streams as fast as two, which leave twice the partial sums (8 sequences of 32K, 4 / 8
-  // splits 93.8 / 98.5 us; 1 of 8K 32 / 64 splits 9.2 / 10.2).  With two tiles a workgroup computes, and two fill a
+  // splits 93.8 / 98.5 us; 1 of 8K 32 / 64 splits 9.2 / 10.2).  With 32 rows a workgroup computes, and two fill a
   // unit better (35 rows over 128K, 32 / 64 splits 45.6 / 37.9); but rows by the hundred have more partial sums
   // than they save (200 rows over 2048, 1 / 2 splits 22.9 / 35.1).
   const int64_t cus = oscar_compute_units();
-  const int64_t splits = rt == 1 ? cus / units : 2 * units <= cus ? 2 * cus / units : 1;
+  const int64_t splits = block == 16 ? cus / units : 2 * units <= cus ? 2 * cus / units : 1;
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>({splits, pages, 512}));
 }
 
@@ -545,8 +618,8 @@ extern "C" int oscar_q8_attn(const void* q, int64_t q_stride, int64_t n_rows, in
   const int g = n_q_heads / cache->n_kv_heads;
   const int64_t rows = (int64_t)T * g;
   if (rows > INT32_MAX / 2) return OSCAR_ERR_INVALID_ARG;
-  const int rt = row_tiles(rows);
-  const int64_t row_blocks = (rows + 16 * rt - 1) / (16 * rt), units = (int64_t)cache->batch * cache->n_kv_heads * splits;
+  const int block = rows_of(rows);
+  const int64_t row_blocks = (rows + block - 1) / block, units = (int64_t)cache->batch * cache->n_kv_heads * splits;
   const int64_t grid = row_blocks == 1 ? units : (units + 7) / 8 * 8 * row_blocks;
   const int64_t join = (int64_t)cache->batch * T * n_q_heads;
   // a grid's threads are counted in 32 bits
@@ -568,7 +641,7 @@ extern "C" int oscar_q8_attn(const void* q, int64_t q_stride, int64_t n_rows, in
   P.out_f32 = out_dtype == OSCAR_F32;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const bool f16 = cache->io_dtype == OSCAR_F16;
-  f16 ? launch<true>(P, rt, (uint32_t)grid, st) : launch<false>(P, rt, (uint32_t)grid, st);
+  f16 ? launch<true>(P, block, (uint32_t)grid, st) : launch<false>(P, block, (uint32_t)grid, st);
   if (splits > 1) {
     if (f16)
       hipLaunchKernelGGL((oscar_q8_join_kernel<true>), dim3((uint32_t)join), dim3(256), 0, st, P);
