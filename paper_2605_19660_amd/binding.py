@@ -588,8 +588,12 @@ def rope_axes(sections, interleaved: bool = False) -> bytes:
 
 def _token_stride(x) -> int:
     """Elements between the tokens of a [..., heads, 128] tensor, whose tokens must lie evenly apart."""
-    shape, stride = x.shape, x.stride()
+    shape = x.shape
     heads = shape[-2]
+    if x.is_contiguous():
+        assert shape[-1] == 128
+        return heads * 128
+    stride = x.stride()
     assert shape[-1] == 128 and stride[-1] == 1 and (heads == 1 or stride[-2] == 128)
     if len(shape) == 3:
         return stride[0] if shape[0] != 1 else heads * 128
@@ -605,12 +609,21 @@ def _token_stride(x) -> int:
     return heads * 128 if step is None else step
 
 
+_int32 = _float32 = None   # torch's types, once it is there (an import statement a call costs 0.3 us)
+
+
+def _number_types():
+    global _int32, _float32
+    import torch
+    _int32, _float32 = torch.int32, torch.float32
+    return _int32
+
+
 def _int32_ptr(t, n: int):
     """Address of an int32 device tensor of n numbers, or None."""
     if t is None:
         return None
-    import torch
-    assert t.dtype == torch.int32 and t.numel() == n and t.is_contiguous()
+    assert t.dtype is (_int32 or _number_types()) and t.numel() == n and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -778,25 +791,36 @@ def plan_step(lens, want, block_table, free_pages, n_free, n_rows: int, keep=Non
     """oscar_plan_step: lens, want, keep int32 [batch]; block_table int32 [batch, max_pages] and free_pages int32
     [num_pages] are changed in place, n_free int32 [1] is the stack's height.  The outputs are made where they are not
     given (lens_out=lens, new_lens=want, n_free_out=n_free: in place)."""
-    import torch
     if stream is not None:
+        import torch
         with torch.cuda.stream(stream):
             return plan_step(lens, want, block_table, free_pages, n_free, n_rows, keep, page_size, lens_out, new_lens,
                              n_free_out, row_starts, positions, row_seq, slots)
     _here(lens, want, keep, block_table, free_pages, n_free, lens_out, new_lens, n_free_out, row_starts, positions, row_seq, slots)
     batch, max_pages = block_table.shape
-    new = lambda t, n: torch.empty(n, dtype=torch.int32, device=lens.device) if t is None else t
-    p = StepPlan(new(lens_out, batch), new(new_lens, batch), new(n_free_out, 1), new(row_starts, batch + 1),
-                 new(positions, n_rows), new(row_seq, n_rows), new(slots, n_rows))
-    rc = lib().oscar_plan_step(_int32_ptr(lens, batch), _int32_ptr(keep, batch), _int32_ptr(want, batch), batch,
-                               _int32_ptr(block_table, batch * max_pages), max_pages, free_pages.numel(), page_size,
-                               _int32_ptr(free_pages, free_pages.numel()), _int32_ptr(n_free, 1), n_rows,
-                               _int32_ptr(p.lens, batch), _int32_ptr(p.new_lens, batch), _int32_ptr(p.n_free, 1),
-                               _int32_ptr(p.row_starts, batch + 1), _int32_ptr(p.positions, n_rows),
-                               _int32_ptr(p.row_seq, n_rows), _int32_ptr(p.slots, n_rows), _stream_ptr(None))
+    new = lambda n: lens.new_empty(n)
+    if lens_out is None:
+        lens_out = new(batch)
+    if new_lens is None:
+        new_lens = new(batch)
+    if n_free_out is None:
+        n_free_out = new(1)
+    if row_starts is None:
+        row_starts = new(batch + 1)
+    if positions is None:
+        positions = new(n_rows)
+    if row_seq is None:
+        row_seq = new(n_rows)
+    if slots is None:
+        slots = new(n_rows)
+    pages, ptr = free_pages.numel(), _int32_ptr
+    rc = lib().oscar_plan_step(ptr(lens, batch), ptr(keep, batch), ptr(want, batch), batch, ptr(block_table, batch * max_pages),
+                               max_pages, pages, page_size, ptr(free_pages, pages), ptr(n_free, 1), n_rows, ptr(lens_out, batch),
+                               ptr(new_lens, batch), ptr(n_free_out, 1), ptr(row_starts, batch + 1), ptr(positions, n_rows),
+                               ptr(row_seq, n_rows), ptr(slots, n_rows), _stream_ptr(None))
     if rc != OK:
         _check(rc, "oscar_plan_step")
-    return p
+    return StepPlan(lens_out, new_lens, n_free_out, row_starts, positions, row_seq, slots)
 
 
 class Q8Cache:
@@ -932,8 +956,9 @@ def _f32_ptr(t, n: int):
     """Address of an fp32 device tensor of n numbers, or None."""
     if t is None:
         return None
-    import torch
-    assert t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()
+    if _float32 is None:
+        _number_types()
+    assert t.dtype is _float32 and t.numel() == n and t.is_contiguous()
     return t.data_ptr()
 
 
