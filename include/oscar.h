@@ -625,7 +625,8 @@ int oscar_q8_read(const oscar_q8_cache *cache, const int32_t *lens, const int32_
  *   workspace : at least oscar_sample_workspace_bytes(...), 16-byte aligned; its contents do not matter.  Calls
  *            that share one must be ordered
  * Weights and sums are in 64 bits; the same call gives the same bits every time.  batch <= 65535, vocab <=
- * OSCAR_VERIFY_MAX_VOCAB.  Two launches, one more with filters and one more with probs. */
+ * OSCAR_SAMPLE_MAX_VOCAB.  Two launches, one or two more with filters and one more with probs. */
+#define OSCAR_SAMPLE_MAX_VOCAB (1 << 22)
 size_t oscar_sample_workspace_bytes(int32_t batch, int32_t vocab);
 int oscar_sample(const void *logits, int64_t row_stride, int32_t batch, int32_t vocab, int32_t dtype,
                  const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,

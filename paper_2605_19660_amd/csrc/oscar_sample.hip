@@ -31,14 +31,15 @@ constexpr int THREADS = 1024, WAVES = 16;
 constexpr int BINS = 1024;
 constexpr int CAP = 4096;                  // numbers sorted in LDS
 constexpr uint32_t DEAD = 0x007fffffu;     // key of -inf
-constexpr int CHUNK_BITS = 48;             // binary places of a weight in a chunk's sums (2^14 of them at most)
+constexpr int CHUNK_BITS = 49;             // binary places of a weight in a chunk's sums (2^13 of them at most)
 constexpr int LIST_BITS = 50;              // of a member of the list (2^12)
 
-// What the second and third launch leave of a row.
+// What the launches leave of a row.
 struct RowState {
   uint32_t n;         // members of the list
   int lo, hi;         // bins on the list
-  int kind;           // of what stays: see the third launch
+  int kind;           // of what stays: see the launch that draws
+  int first;          // cell of the row's largest logit
   double above, total;   // weights above the list, and of all
   uint64_t cut;
   double sum;         // weights of what stays
@@ -567,41 +568,41 @@ __device__ __forceinline__ void place_chunk(const Settings& s, uint64_t best, fl
 // A chunk's running sum up to the row's bin.  (The load does not wait for whether it counts.)
 __device__ __forceinline__ double chunk_upto(const SampleParams& P, const Chunks& G, int64_t row_chunk, int c, int bin) {
   const int shift = G.shift[c], own = bin == BINS - 1 ? bin : bin - shift;
-  const double sum = (double)P.cum[(row_chunk + c) * BINS + max(own, 0)] * G.scale[c];
-  return shift < 0 || own < 0 ? 0.0 : sum;
+  const uint64_t sum = P.cum[(row_chunk + c) * BINS + max(own, 0)];
+  return (double)(shift < 0 || own < 0 ? 0 : sum) * (shift < 0 ? 0.0 : G.scale[c]);
 }
 
-template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_list_kernel(SampleParams P) {
-  __shared__ Chunks G;
-  __shared__ uint64_t s_wave[WAVES];
-  __shared__ double s_cum[BINS];
-  __shared__ int s_bin;
-  __shared__ uint32_t s_base;
-  const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
-  // (what the launch waits for is asked for at once)
-  const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
-  const Settings s = settings(P, b);
-  uint32_t key[PER];
-  load_keys<E, PER>(P, b, c, key);
-  if (s.one || s.whole || (!s.by_count && !s.cuts)) return;
-  const uint32_t top_key = (uint32_t)(group_max(chunk_best, s_wave) >> 32);
-  const float top = number_of(top_key);
-  if (top_key <= DEAD || !on_grid(top, s.grid, ROW_GRID)) return;
-  place_chunk(s, chunk_best, top, t < P.chunks, G);
+// The bins that hold the cuts, by a workgroup with a thread a bin.
+struct Found {
+  int lo, hi;
+  double above, total;   // weights above bin lo, and of all
+};
+struct FindShared {
+  Chunks G;
+  double cum[BINS];
+  int bin;
+};
+__device__ __forceinline__ Found find_bins(const SampleParams& P, const Settings& s, int b, uint64_t chunk_best, float top, FindShared& F) {
+  const int t = threadIdx.x;
+  place_chunk(s, chunk_best, top, t < P.chunks, F.G);
   double upto = 0.0;
-#pragma unroll 8
-  for (int q = 0; q < P.chunks; ++q) upto += chunk_upto(P, G, (int64_t)b * P.chunks, q, t);
-  s_cum[t] = upto;
-  if (t == 0) s_bin = BINS - 1;
+  for (int q = 0; q < P.chunks; q += 8) {   // (8 on the way at a time)
+    double part[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[i] = chunk_upto(P, F.G, (int64_t)b * P.chunks, min(q + i, P.chunks - 1), t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) upto += q + i < P.chunks ? part[i] : 0.0;
+  }
+  F.cum[t] = upto;
+  if (t == 0) F.bin = BINS - 1;
   __syncthreads();
-  const double total = s_cum[BINS - 1];
-  int lo = BINS, hi = -1;
+  Found f = {BINS, -1, 0.0, F.cum[BINS - 1]};
   if (s.by_count || s.p < 1.0f) {
-    const double target = s.by_count ? fmin((double)s.k, total) : (double)s.p * total;
-    first_thread(&s_bin, upto >= target);
+    const double target = s.by_count ? fmin((double)s.k, f.total) : (double)s.p * f.total;
+    first_thread(&F.bin, upto >= target);
     __syncthreads();
-    hi = s_bin;
-    lo = s.by_count ? 0 : hi;
+    f.hi = F.bin;
+    f.lo = s.by_count ? 0 : f.hi;
   }
   if (!s.by_count && s.m > 0.0f) {
     // the bins in which weights pass min_p, a little more on either side
@@ -612,33 +613,69 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void osc
       from = max(min(cell_of((float)(x + off), s.grid) - first, BINS - 1), 0);
       to = max(min(cell_of((float)(x - off), s.grid) - first, BINS - 1), 0);
     }
-    if (to < lo)
-      lo = from, hi = to;      // min_p cuts before top_p does
-    else if (from <= hi)
-      lo = min(lo, from), hi = max(hi, to);
+    if (to < f.lo)
+      f.lo = from, f.hi = to;      // min_p cuts before top_p does
+    else if (from <= f.hi)
+      f.lo = min(f.lo, from), f.hi = max(f.hi, to);
   }
-  if (c == 0 && t == 0) {
-    RowState& r = P.rows[b];
-    r.lo = lo;
-    r.hi = hi;
-    r.above = lo > 0 ? s_cum[lo - 1] : 0.0;
-    r.total = total;
-  }
+  f.above = f.lo > 0 ? F.cum[f.lo - 1] : 0.0;
+  return f;
+}
+__device__ __forceinline__ bool has_list(const Settings& s) { return !s.one && !s.whole && (s.by_count || s.cuts); }
 
-  const int first = cell_of(top, s.grid);
+__global__ __launch_bounds__(THREADS) void oscar_sample_find_kernel(SampleParams P) {
+  __shared__ FindShared F;
+  __shared__ uint64_t s_wave[WAVES];
+  const int b = blockIdx.x, t = threadIdx.x;
+  const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
+  const Settings s = settings(P, b);
+  const uint32_t top_key = (uint32_t)(group_max(chunk_best, s_wave) >> 32);
+  const float top = number_of(top_key);
+  RowState& r = P.rows[b];
+  Found f = {0, -1, 0.0, 0.0};   // (no list)
+  if (has_list(s) && top_key > DEAD && on_grid(top, s.grid, ROW_GRID)) f = find_bins(P, s, b, chunk_best, top, F);
+  if (t == 0) r.lo = f.lo, r.hi = f.hi, r.above = f.above, r.total = f.total, r.first = cell_of(top, s.grid);
+}
+
+// FIND: the chunks look for the bins themselves (a launch less; but every chunk reads the sums of all the row's).
+template <typename E, int PER, bool FIND> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_list_kernel(SampleParams P) {
+  const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x, lane = t & 63;
+  // (what the launch waits for is asked for at once)
+  const Settings s = settings(P, b);
+  uint32_t key[PER];
+  int lo, hi, first;
+  if constexpr (FIND) {
+    __shared__ FindShared F;
+    __shared__ uint64_t s_wave[WAVES];
+    const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
+    load_keys<E, PER>(P, b, c, key);
+    if (!has_list(s)) return;
+    const uint32_t top_key = (uint32_t)(group_max(chunk_best, s_wave) >> 32);
+    const float top = number_of(top_key);
+    if (top_key <= DEAD || !on_grid(top, s.grid, ROW_GRID)) return;
+    const Found f = find_bins(P, s, b, chunk_best, top, F);
+    lo = f.lo, hi = f.hi, first = cell_of(top, s.grid);
+    if (c == 0 && t == 0) {
+      RowState& r = P.rows[b];
+      r.lo = lo, r.hi = hi, r.above = f.above, r.total = f.total;
+    }
+  } else {
+    const RowState& r = P.rows[b];
+    lo = r.lo, hi = r.hi, first = r.first;
+    if (hi < 0) return;
+    load_keys<E, PER>(P, b, c, key);
+  }
   uint32_t on = 0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
     const int bin = min(cell_of(number_of(key[e]), s.grid) - first, BINS - 1);
     on |= (key[e] > DEAD && bin >= lo && bin <= hi ? 1u : 0u) << e;
   }
-  uint64_t all;
-  const uint64_t mine = __popc(on);
-  uint32_t at = (uint32_t)(group_scan(mine, s_wave, &all) - mine);
-  if (t == 0 && all) s_base = atomicAdd(&P.rows[b].n, (uint32_t)all);
-  __syncthreads();
-  if (!all) return;
-  at += s_base;
+  // a place on the list, a wave at a time
+  const uint64_t mine = __popc(on), upto = wave_scan(mine);
+  uint32_t at = 0;
+  if (lane == 63 && upto) at = atomicAdd(&P.rows[b].n, (uint32_t)upto);
+  at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + (uint32_t)(upto - mine);
 #pragma unroll
   for (int e = 0; e < PER; ++e)
     if (on >> e & 1) {
@@ -870,26 +907,32 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void osc
   }
 }
 
-// Logits of a chunk: 16384, or 4096 where that leaves the chip half empty (one row of 32000: 8 workgroups, not 2).
-int chunk_of(int32_t batch, int32_t vocab) {
-  return (int64_t)batch * ((vocab + 4095) / 4096) <= 1024 && vocab <= 4096 * THREADS ? 4096 : 16384;
-}
+// Logits of a chunk: 8192, or 4096 where that leaves the chip half empty (one row of 32000: 8 workgroups, not 4).
+int chunk_of(int32_t batch, int32_t vocab) { return (int64_t)batch * ((vocab + 4095) / 4096) <= 512 ? 4096 : 8192; }
 
 template <typename E, int PER> void launch(const SampleParams& P, int batch, hipStream_t st) {
   const dim3 grid(P.chunks, batch);
   hipLaunchKernelGGL((oscar_sample_bins_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
-  if (P.top_k || P.top_p || P.min_p) hipLaunchKernelGGL((oscar_sample_list_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
+  if (P.top_k || P.top_p || P.min_p) {
+    // one row of 32000: a launch for the bins 5 us, every chunk for itself 3; 64 of 128003: 5 and 16
+    if ((int64_t)P.chunks * batch <= 64) {
+      hipLaunchKernelGGL((oscar_sample_list_kernel<E, PER, true>), grid, dim3(THREADS), 0, st, P);
+    } else {
+      hipLaunchKernelGGL(oscar_sample_find_kernel, dim3(batch), dim3(THREADS), 0, st, P);
+      hipLaunchKernelGGL((oscar_sample_list_kernel<E, PER, false>), grid, dim3(THREADS), 0, st, P);
+    }
+  }
   hipLaunchKernelGGL((oscar_sample_pick_kernel<E, PER>), dim3(batch), dim3(THREADS), 0, st, P);
   if (P.probs) hipLaunchKernelGGL((oscar_sample_probs_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
 }
 template <typename E> void launch(const SampleParams& P, int batch, hipStream_t st) {
-  P.chunk == 4096 ? launch<E, 4>(P, batch, st) : launch<E, 16>(P, batch, st);
+  P.chunk == 4096 ? launch<E, 4>(P, batch, st) : launch<E, 8>(P, batch, st);
 }
 
 }  // namespace
 
 extern "C" size_t oscar_sample_workspace_bytes(int32_t batch, int32_t vocab) {
-  if (batch < 1 || batch > 65535 || vocab < 1 || vocab > OSCAR_VERIFY_MAX_VOCAB) return 0;
+  if (batch < 1 || batch > 65535 || vocab < 1 || vocab > OSCAR_SAMPLE_MAX_VOCAB) return 0;
   const size_t chunk = chunk_of(batch, vocab), chunks = (vocab + chunk - 1) / chunk;
   return batch * (chunks * (BINS + 1) * sizeof(uint64_t) + sizeof(RowState) + CAP * sizeof(uint64_t));
 }
@@ -899,7 +942,7 @@ extern "C" int oscar_sample(const void* logits, int64_t row_stride, int32_t batc
                             const float* u, int32_t* tokens, float* probs, void* workspace, size_t workspace_bytes,
                             void* stream) {
   if (dtype != OSCAR_F32 && dtype != OSCAR_BF16 && dtype != OSCAR_F16) return OSCAR_ERR_INVALID_ARG;
-  if (batch < 0 || batch > 65535 || vocab < 1 || vocab > OSCAR_VERIFY_MAX_VOCAB || (batch > 1 && row_stride < vocab))
+  if (batch < 0 || batch > 65535 || vocab < 1 || vocab > OSCAR_SAMPLE_MAX_VOCAB || (batch > 1 && row_stride < vocab))
     return OSCAR_ERR_INVALID_ARG;
   if (batch == 0) return OSCAR_OK;
   if (!logits || !u || !tokens) return OSCAR_ERR_INVALID_ARG;

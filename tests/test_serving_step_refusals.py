@@ -128,7 +128,7 @@ def sample(x=P, stride=1000, batch=2, vocab=1000, dt=ob.F32, temp=None, k=None, 
 
 
 def test_sample_refuses():
-    for kw in (dict(x=None), dict(u=None), dict(tokens=None), dict(batch=-1), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(dt=3), dict(dt=-1),
+    for kw in (dict(x=None), dict(u=None), dict(tokens=None), dict(batch=-1), dict(vocab=0), dict(vocab=(1 << 22) + 1, stride=1 << 23), dict(dt=3), dict(dt=-1),
                dict(stride=999), dict(x=P + 2), dict(x=P + 1, dt=ob.BF16), dict(batch=65536)):
         assert sample(**kw) == ob.ERR_INVALID_ARG, kw
     need = ob.sample_workspace_bytes(2, 1000)
