@@ -93,8 +93,23 @@ template <int PLACES = 0> __device__ __forceinline__ double power_of_2(double z)
   s = fma(s, f, 0x1.0000000000000p+0);
   return __builtin_amdgcn_ldexp(s, (int)n + PLACES);
 }
-__device__ __forceinline__ double exp64(double y) { return power_of_2(y * 1.4426950408889634); }
-// A number below 2^51, rounded to a whole one.
+// The same, to 2^-45, by a table of 2^(i / 32), i < 32: |f| <= 1/64 of a power is left, the series ends with f^5.
+__device__ __forceinline__ void fill_powers(double* table) {
+  if (threadIdx.x < 32) table[threadIdx.x] = power_of_2((double)threadIdx.x * 0.03125);
+}
+template <int PLACES> __device__ __forceinline__ double power_of_2(double z, const double* table) {
+  z = fmax(z * 32.0, -38400.0);
+  const double n = __builtin_rint(z), f = z - n;
+  const int i = (int)n;
+  const double t = table[i & 31];
+  double s = 0x1.5d87fe78a6731p-35;
+  s = fma(s, f, 0x1.3b2ab6fba4e77p-27);
+  s = fma(s, f, 0x1.c6b08d704a0c0p-20);
+  s = fma(s, f, 0x1.ebfbdff82c58fp-13);
+  s = fma(s, f, 0x1.62e42fefa39efp-6);
+  return __builtin_amdgcn_ldexp(fma(s * f, t, t), (i >> 5) + PLACES);
+}
+// A number below 2^52, rounded to a whole one.
 __device__ __forceinline__ uint64_t whole_of(double x) {
   return __builtin_bit_cast(uint64_t, x + 0x1p52) & ((1ull << 52) - 1);
 }
@@ -464,7 +479,7 @@ struct Settings {
   bool by_count;  // top_k that fits the list: bins count tokens
   bool whole;     // top_k that does not: one workgroup
   bool cuts;      // else: whether top_p or min_p cut
-  float grid;     // bins a unit
+  float width, grid;   // of a bin, and bins a unit
 };
 __device__ __forceinline__ Settings settings(const SampleParams& P, int b) {
   Settings s;
@@ -480,7 +495,8 @@ __device__ __forceinline__ Settings settings(const SampleParams& P, int b) {
   s.cuts = s.p < 1.0f || s.m > 0.0f;
   // weights fall to 2^-64 over the bins, or logits by 64, whichever is less: a high temperature spreads weights over
   // few of the former
-  s.grid = BINS / fminf(fmaxf(45.0f * s.temp, 1e-25f), 64.0f);
+  s.width = fminf(fmaxf(45.0f * s.temp, 1e-25f), 64.0f) * (1.0f / BINS);
+  s.grid = 1.0f / s.width;
   return s;
 }
 // The grid's cell of a logit; cells fall with it.
@@ -489,11 +505,6 @@ __device__ __forceinline__ int cell_of(float x, float grid) { return -(int)floor
 // workgroup; a chunk whose largest is past CHUNK_GRID has everything in its last bin (far below such a row's bins).
 constexpr float ROW_GRID = 0x1p21f, CHUNK_GRID = 0x1p22f;
 __device__ __forceinline__ bool on_grid(float top, float grid, float end) { return fabsf(top * grid) < end; }
-// What a chunk's weights are relative to: no less than its largest logit, but for rounding, and one number for a cell.
-__device__ __forceinline__ double reference_of(float top, float grid) {
-  return on_grid(top, grid, CHUNK_GRID) ? (double)(1 - cell_of(top, grid)) / (double)grid : (double)top;
-}
-
 // A chunk's logits, a thread's 1024 apart; 0 behind the row's end.
 template <typename E, int PER> __device__ __forceinline__ void load_keys(const SampleParams& P, int b, int c, uint32_t* key) {
   const E* x = reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride;
@@ -504,6 +515,7 @@ template <typename E, int PER> __device__ __forceinline__ void load_keys(const S
 
 template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_bins_kernel(SampleParams P) {
   __shared__ uint64_t s_bin[BINS], s_wave[WAVES];
+  __shared__ double s_power[32];
   const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
   uint32_t key[PER];
   load_keys<E, PER>(P, b, c, key);
@@ -515,6 +527,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void osc
   }
   const Settings s = settings(P, b);
   s_bin[t] = 0;
+  fill_powers(s_power);
   best = group_max(best, s_wave);
   const int64_t chunk = (int64_t)b * P.chunks + c;
   if (t == 0) {
@@ -533,18 +546,22 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void osc
       if (bin == BINS - 1) ++mine; else atomicAdd(reinterpret_cast<uint32_t*>(&s_bin[bin]), 1u);
     }
   } else {
-    const double ref = reference_of(top, s.grid), scale = 1.4426950408889634 / (double)s.temp;
+    const double ref = (double)top, scale = 1.4426950408889634 / (double)s.temp;
 #pragma unroll 4
     for (int e = 0; e < PER; ++e) {
       if (key[e] <= DEAD) continue;
       const float x = number_of(key[e]);
-      const uint64_t w = whole_of(power_of_2<CHUNK_BITS>(((double)x - ref) * scale));
+      const uint64_t w = whole_of(power_of_2<CHUNK_BITS>(((double)x - ref) * scale, s_power));
       const int bin = s.cuts ? min(cell_of(x, s.grid) - first, BINS - 1) : BINS - 1;
       if (bin == BINS - 1) mine += w; else atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[bin]), (unsigned long long)w);
     }
   }
   add_from_wave(&s_bin[BINS - 1], mine);
   __syncthreads();
+  if (!s.by_count && !s.cuts) {   // (nothing is looked up but their sum)
+    if (t == 0) P.cum[chunk * BINS + BINS - 1] = s_bin[BINS - 1];
+    return;
+  }
   uint64_t all;
   P.cum[chunk * BINS + t] = group_scan(s_bin[t], s_wave, &all);
 }
@@ -561,7 +578,7 @@ __device__ __forceinline__ void place_chunk(const Settings& s, uint64_t best, fl
     const uint32_t key = (uint32_t)(best >> 32);
     const int first = cell_of(number_of(key), s.grid);
     G.shift[t] = key > DEAD ? first - cell_of(top, s.grid) : -1;
-    G.scale[t] = s.by_count ? 1.0 : exp64((reference_of(number_of(key), s.grid) - (double)top) / (double)s.temp) / (double)(1ull << CHUNK_BITS);
+    G.scale[t] = s.by_count ? 1.0 : power_of_2<-CHUNK_BITS>(((double)number_of(key) - (double)top) * (1.4426950408889634 / (double)s.temp));
   }
   __syncthreads();
 }
