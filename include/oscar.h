@@ -584,8 +584,8 @@ int oscar_q8_append(const void *k, const void *v, int64_t k_stride, int64_t v_st
  *   num_splits  : (<= 512), 0 = oscar_q8_auto_splits; workspace: oscar_q8_workspace_bytes(...), 16-byte
  *         aligned, NULL where that is 0.  Calls that share one must be ordered
  * Rows that belong to no sequence are left as they were; a row that sees no token gets zeros; tokens in a page
- * that is no page are left out.  Queries and logits are finite.  Keys and values enter as they are, queries too;
- * probabilities are carried in two bf16 limbs (16 bits), sums and statistics are fp32.  The same call gives the same
+ * that is no page are left out.  Queries are finite, scaled logits below 2^30 in size.  Keys and values enter as they are,
+ * queries too; probabilities are carried in two bf16 limbs (16 bits), sums and statistics are fp32.  The same call gives the same
  * bits every time.  One launch, two with several splits. */
 #define OSCAR_Q8_MAX_GROUP 64 /* n_q_heads / n_kv_heads */
 int32_t oscar_q8_auto_splits(const oscar_q8_cache *cache, int32_t n_q_heads, int32_t T, int32_t max_seq_len);

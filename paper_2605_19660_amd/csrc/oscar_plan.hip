@@ -20,9 +20,7 @@
 
 namespace {
 
-constexpr int THREADS = 1024;
-// rows that the deciding workgroup writes itself; more go to a launch of their own
-constexpr int INLINE_ROWS = 8192;
+constexpr int MOST_THREADS = 1024;
 
 struct PlanParams {
   const int32_t *lens, *keep, *want;
@@ -33,19 +31,21 @@ struct PlanParams {
   int rows_here;   // whether this launch writes the rows
 };
 
-__device__ __forceinline__ int64_t shfl_up64(int64_t v, int d) {
-  const int lo = __shfl_up((int)(uint32_t)v, d), hi = __shfl_up((int)(v >> 32), d);
-  return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+// Moved up within a wave, 0 where no lane gives (as permutations through LDS a scan waits for them six times).
+template <int CTRL, int ROWS> __device__ __forceinline__ int64_t moved(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (int64_t)((uint64_t)hi << 32 | lo);
 }
-
-// Sum over the threads up to this one, of the workgroup; s_wave: 16 numbers that no one else uses meanwhile.
-__device__ __forceinline__ int64_t group_scan(int64_t v, int64_t* s_wave) {
+// Sum over the threads up to this one, of the workgroup; s_wave: a number a wave that no one else uses meanwhile.
+template <int THREADS> __device__ __forceinline__ int64_t group_scan(int64_t v, int64_t* s_wave) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t u = shfl_up64(v, d);
-    v += lane >= d ? u : 0;
-  }
+  v += moved<0x111, 0xf>(v);   // row_shr:1, 2, 4, 8
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);   // row_bcast:15 into rows 1 and 3
+  v += moved<0x143, 0xc>(v);   // row_bcast:31 into rows 2 and 3
   __syncthreads();
   if (lane == 63) s_wave[wave] = v;
   __syncthreads();
@@ -89,21 +89,24 @@ __device__ __forceinline__ void put_row(const PlanParams& P, int64_t row, int b,
   }
 }
 
-__global__ __launch_bounds__(THREADS) void oscar_plan_kernel(PlanParams P) {
+// THREADS: of the deciding workgroup; a chunk of so many sequences is decided at a time.
+template <int THREADS> __global__ __launch_bounds__(THREADS) void oscar_plan_kernel(PlanParams P) {
   __shared__ int64_t s_wave[THREADS / 64], s_sum[THREADS];
   __shared__ int s_kept[THREADS];
   __shared__ int64_t s_most[2];   // rows and pages of the last one that takes part
   const int tid = threadIdx.x;
   const int64_t have = min(max((int64_t)P.n_free[0], (int64_t)0), (int64_t)P.num_pages);
+  Seq mine = {};   // of the first chunk
+  if (tid < P.batch) mine = load_seq(P, tid);
 
   // pages that come back
   int64_t avail = have;
   if (P.keep) {
     for (int b0 = 0; b0 < P.batch; b0 += THREADS) {
       const int b = b0 + tid, n = min(P.batch - b0, THREADS);
-      Seq s = {};
-      if (tid < n) s = load_seq(P, b);
-      const int64_t upto = group_scan(s.held - s.kept, s_wave);
+      Seq s = mine;
+      if (b0 > 0) s = tid < n ? load_seq(P, b) : Seq{};
+      const int64_t upto = group_scan<THREADS>(s.held - s.kept, s_wave);
       s_sum[tid] = upto;
       s_kept[tid] = (int)s.kept;
       __syncthreads();
@@ -122,13 +125,13 @@ __global__ __launch_bounds__(THREADS) void oscar_plan_kernel(PlanParams P) {
   int64_t pages_asked = 0, rows_asked = 0, pages_given = 0, rows_given = 0;
   for (int b0 = 0; b0 < P.batch; b0 += THREADS) {
     const int b = b0 + tid, n = min(P.batch - b0, THREADS);
-    Seq s = {};
-    if (tid < n) s = load_seq(P, b);
+    Seq s = mine;
+    if (b0 > 0) s = tid < n ? load_seq(P, b) : Seq{};
     const bool fits = s.want > 0 && s.k + s.want <= (int64_t)P.max_pages * P.ps;
     const int64_t need = fits ? (s.k + s.want + P.ps - 1) / P.ps - s.kept : 0;
-    const int64_t pages_upto = pages_asked + group_scan(need, s_wave);
+    const int64_t pages_upto = pages_asked + group_scan<THREADS>(need, s_wave);
     const bool paged = fits && (need == 0 || pages_upto <= avail);
-    const int64_t rows_upto = rows_asked + group_scan(paged ? s.want : 0, s_wave);
+    const int64_t rows_upto = rows_asked + group_scan<THREADS>(paged ? s.want : 0, s_wave);
     const bool on = paged && rows_upto <= P.n_rows;
     if (tid == 0) s_most[0] = rows_given, s_most[1] = pages_given;
     s_sum[tid] = rows_upto;
@@ -210,9 +213,14 @@ extern "C" int oscar_plan_step(const int32_t* lens, const int32_t* keep, const i
   PlanParams P = {lens, keep, want, batch, max_pages_per_seq, num_pages, page_size, n_rows, block_table, free_pages, n_free,
                   lens_out, new_lens, n_free_out, row_starts, positions, row_seq, slots, 0};
   const bool maps = n_rows > 0 && (positions || row_seq || slots);
-  P.rows_here = maps && n_rows <= INLINE_ROWS && batch <= THREADS;
+  // one workgroup writes some rows a thread beside what else it does; more go to a launch of their own
+  const bool small = batch <= 256 && n_rows <= 2048;
+  P.rows_here = maps && (small || (n_rows <= 8192 && batch <= MOST_THREADS));
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(oscar_plan_kernel, dim3(1), dim3(THREADS), 0, st, P);
+  if (small)
+    hipLaunchKernelGGL(oscar_plan_kernel<256>, dim3(1), dim3(256), 0, st, P);
+  else
+    hipLaunchKernelGGL(oscar_plan_kernel<MOST_THREADS>, dim3(1), dim3(MOST_THREADS), 0, st, P);
   if (maps && !P.rows_here)
     hipLaunchKernelGGL(oscar_plan_rows_kernel, dim3((uint32_t)(((int64_t)n_rows + 255) / 256)), dim3(256), 0, st, P);
   if (hipGetLastError() != hipSuccess) return OSCAR_ERR_HIP;

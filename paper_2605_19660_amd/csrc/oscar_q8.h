@@ -44,7 +44,7 @@ struct Q8Seq {
 __device__ __forceinline__ Q8Seq q8_seq(const Q8Rows& r, int b) {
   Q8Seq s;
   s.n = r.new_lens ? min(max(r.new_lens[b], 0), r.T) : r.T;
-  s.len = max(r.lens[b], 0);
+  s.len = min(max(r.lens[b], 0), INT32_MAX - 4096);   // (a step or two past it is still a number)
   s.old = s.len - s.n;
   s.row = r.row_starts ? r.row_starts[b] : (int64_t)b * r.T;
   return s;

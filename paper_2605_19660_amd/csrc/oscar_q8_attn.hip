@@ -39,7 +39,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int O_PITCH = 132;       // of a row of sums in LDS: 16 rows' pieces on different banks
 constexpr int V_PITCH = 264;       // bytes of a window row in LDS (a wave's 32 rows take the place of its 16 rows of sums)
 static_assert(32 * V_PITCH <= 16 * O_PITCH * 4, "a wave's window rows fit its sums' place");
-constexpr float NO_REF = -1e30f;   // reference of a row that has seen no token
+constexpr float NO_REF = -3e38f;   // reference of a row that has seen no token
 // A reference moves when a logit passes it by this much (in powers of two): probabilities stay below 2^8, and a wave
 // seldom has to multiply its sums.
 constexpr float REF_SLACK = 8.0f;
@@ -257,7 +257,8 @@ template <class S> __device__ __forceinline__ void move_reference(State<S>& w, c
 #pragma unroll
   for (int c = 0; c < S::TILES; ++c) w.o[c] *= f;
 }
-// Probabilities, two limbs of the operands.
+// Probabilities, two limbs of the operands.  (The product is not rounded before the reference, which was taken from a
+// rounded one, is subtracted: all powers of a row may be off by the same half step, which is less than 2^6 for logits below 2^30.)
 template <class S> __device__ __forceinline__ void probabilities(State<S>& w, const typename S::Logits& s, float scale, bf16x8* hi, bf16x8* lo) {
   uint32_t h[S::LOGITS / 2], l[S::LOGITS / 2];
   float sum = 0.0f;

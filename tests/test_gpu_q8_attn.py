@@ -275,3 +275,81 @@ def test_another_stream():
     out = ob.q8_attn(c, qd, n, max_seq_len_hint=600, num_splits=3, stream=s)
     s.synchronize()
     compare([out[b].double().cpu().numpy() for b in range(2)], attention(q, x, lens, [1, 1], 32, "bf16", "bf16"))
+
+
+def test_lengths_of_any_size_stay_inside_their_tensors():
+    """Lengths up to 2^31 - 1 and below 0: what no page or window holds is left out."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(16)
+    x = [tokens(rng, 5, 300, 1, "bf16") for _ in "kv"]
+    c = scattered_cache(ob, 1, 5, 2, 32, "bf16", rng, poison=False)
+    append(ob, c, x, [0] * 5, [300] * 5, "bf16")
+    lens = ints([2 ** 31 - 1, 2 ** 31 - 4097, -1, -2 ** 31, 300])
+    guard = torch.full((7, 3, 4, D), 7.0, device="cuda")
+    for splits in (1, 3):
+        out = guard[1:6]
+        out.fill_(7.0)
+        ob.q8_attn(c, dev(tokens(rng, 5, 3, 4, "bf16"), "bf16"), lens, out=out, num_splits=splits)
+        assert (guard[0] == 7.0).all() and (guard[6] == 7.0).all()
+        assert not out[2:4].any() and torch.isfinite(out).all() and out[4].any()
+    before = [y.clone() for y in (c.k_codes, c.v_codes, c.block_table)]
+    k = torch.full((5, 40, 1, D), 7.0, device="cuda")
+    ob.q8_read(c, lens, starts=ints([2 ** 31 - 30, 0, 0, 0, 280]), k=k)
+    assert (k[2:4] == 7.0).all()
+    rows = dev(tokens(rng, 5, 3, 1, "bf16"), "bf16")
+    ob.q8_append(c, rows, rows, lens)       # (past the table's end: the window only)
+    assert all(torch.equal(y, z) for y, z in zip(before, (c.k_codes, c.v_codes, c.block_table)))
+
+
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+def test_logits_of_any_size(sign):
+    """Scaled logits of 2^29 in size and their neighbours: whoever has the largest takes the row."""
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(17)
+    x = [tokens(rng, 1, 100, 1, "bf16") for _ in "kv"]
+    x[0][...] = 2.0 ** 12 * rng.choice([1.0, 1.0078125], size=x[0].shape)
+    x[0][0, 97] = 2.0 ** 12 * (1.0 if sign < 0 else 1.0078125)          # in the window: it is the largest
+    q = sign * 2.0 ** 13 * np.ones((1, 1, 1, D))
+    c = scattered_cache(ob, 1, 1, 1, 32, "bf16", rng)
+    append(ob, c, x, [0], [100], "bf16")
+    k = stands_for(x[0][0, :, 0], 32, "bf16")[0]
+    logits = k @ q[0, 0, 0] / np.sqrt(D)
+    best = np.nonzero(logits == logits.max())[0]
+    got = run(ob, c, q, [100], [1], "bf16", "f32")[0]
+    assert 2.0 ** 28 < abs(logits).max() < 2.0 ** 30
+    # (equal logits share the row; the next is thousands below)
+    want = stands_for(x[1][0, :, 0], 32, "bf16")[0][best].mean(0)
+    assert (np.abs(got[0, 0] - want) <= 2.0 ** -16 * np.abs(x[1][0, best, 0]).max(0) + 2.0 ** -24).all()
+
+
+def test_captured_and_replayed_over_growing_lengths():
+    """One graph of append and attention, replayed while the lengths on the device grow past block and page ends, with
+    eager work between; every replay is the eager call's bits."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(18)
+    B, H, HQ, first = 3, 2, 6, [120, 30, 250]
+    x = [tokens(rng, B, 400, H, "bf16") for _ in "kv"]
+    a, b = (scattered_cache(ob, H, B, 4, 32, "bf16", np.random.default_rng(0)) for _ in range(2))
+    for c in (a, b):
+        append(ob, c, x, [0] * B, first, "bf16")
+    k, v, q = (torch.zeros(B, 1, n, D, dtype=torch.bfloat16, device="cuda") for n in (H, H, HQ))
+    lens, out = ints(first), torch.zeros(B, 1, HQ, D, dtype=torch.bfloat16, device="cuda")
+    ws = torch.zeros(ob.q8_workspace_bytes(b, HQ, 1, 3), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ob.q8_append(b, k, v, lens)
+        ob.q8_attn(b, q, lens, out=out, num_splits=3, workspace=ws)
+    n = np.array(first)
+    for i in range(140):
+        n += 1
+        k.copy_(dev(np.stack([x[0][j, n[j] - 1] for j in range(B)])[:, None], "bf16"))
+        v.copy_(dev(np.stack([x[1][j, n[j] - 1] for j in range(B)])[:, None], "bf16"))
+        q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(i)))
+        lens.copy_(torch.from_numpy(n))
+        graph.replay()
+        ob.q8_append(a, k, v, lens)
+        want = ob.q8_attn(a, q, lens, num_splits=3)
+        assert torch.equal(out, want), i
+    compare([out[j].double().cpu().numpy() for j in range(B)], attention(q.double().cpu().numpy(), x, list(n), [1] * B, 32, "bf16", "bf16"))
