@@ -547,13 +547,20 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void osc
     }
   } else {
     const double ref = (double)top, scale = 1.4426950408889634 / (double)s.temp;
-#pragma unroll 4
+    uint64_t w[PER];   // (without branches: the exponentials' steps wait for each other, and side by side they do not)
+#pragma unroll
     for (int e = 0; e < PER; ++e) {
-      if (key[e] <= DEAD) continue;
-      const float x = number_of(key[e]);
-      const uint64_t w = whole_of(power_of_2<CHUNK_BITS>(((double)x - ref) * scale, s_power));
-      const int bin = s.cuts ? min(cell_of(x, s.grid) - first, BINS - 1) : BINS - 1;
-      if (bin == BINS - 1) mine += w; else atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[bin]), (unsigned long long)w);
+      const float x = number_of(max(key[e], DEAD + 1));
+      w[e] = whole_of(power_of_2<CHUNK_BITS>(((double)x - ref) * scale, s_power));
+      if (key[e] <= DEAD) w[e] = 0;
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int bin = s.cuts ? min(cell_of(number_of(key[e]), s.grid) - first, BINS - 1) : BINS - 1;
+      if (bin == BINS - 1)
+        mine += w[e];
+      else if (key[e] > DEAD)
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[bin]), (unsigned long long)w[e]);
     }
   }
   add_from_wave(&s_bin[BINS - 1], mine);
@@ -865,11 +872,9 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
   double w[PER], part = 0.0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
-    w[e] = 0.0;
-    if (key[e] > DEAD && place_of(key[e], i0 + e * 64) >= cut) {
-      w[e] = row.weight(key[e]);
-      if (w[e] < (double)s.m) w[e] = 0.0;   // (an empty list has no cut)
-    }
+    const bool stays = key[e] > DEAD && place_of(key[e], i0 + e * 64) >= cut;
+    w[e] = row.weight(max(key[e], DEAD + 1));
+    if (!stays || w[e] < (double)s.m) w[e] = 0.0;   // (min_p: an empty list has no cut)
     part += w[e];
   }
   double all;
