@@ -509,8 +509,13 @@ __device__ __forceinline__ bool on_grid(float top, float grid, float end) { retu
 template <typename E, int PER> __device__ __forceinline__ void load_keys(const SampleParams& P, int b, int c, uint32_t* key) {
   const E* x = reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride;
   const int i0 = c * (PER * THREADS) + threadIdx.x;
+  // (all on the way before the first is looked at: no branch around a load, 1.5 .. 3 us a launch.  As vectors of 16 bytes,
+  // at rows of odd lengths, the launches take 1 .. 2 us longer)
+  E raw[PER];
 #pragma unroll
-  for (int e = 0; e < PER; ++e) key[e] = i0 + e * THREADS < P.V ? key_of(to_f32<E>(x[i0 + e * THREADS])) : 0;
+  for (int e = 0; e < PER; ++e) raw[e] = x[min(i0 + e * THREADS, P.V - 1)];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) key[e] = i0 + e * THREADS < P.V ? key_of(to_f32<E>(raw[e])) : 0;
 }
 
 template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_bins_kernel(SampleParams P) {
@@ -868,7 +873,9 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
   const int lane = t & 63, wave = t >> 6, i0 = c * (PER * THREADS) + wave * (PER * 64) + lane;
   uint32_t key[PER];
 #pragma unroll
-  for (int e = 0; e < PER; ++e) key[e] = i0 + e * 64 < V ? row.key(i0 + e * 64) : 0;
+  for (int e = 0; e < PER; ++e) key[e] = row.key(min(i0 + e * 64, V - 1));
+#pragma unroll
+  for (int e = 0; e < PER; ++e) key[e] = i0 + e * 64 < V ? key[e] : 0;
   double w[PER], part = 0.0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
