@@ -10,10 +10,12 @@
 // Append: a workgroup takes one block of one kv head, keys or values: reads it once (a new token's 256 bytes
 // by 16 lanes, the tokens that were there from the window), finds the largest, converts in registers.  Four value
 // tokens lie in four rows of 16 lanes of a wave and change places by half and quarter swaps of registers, because
-// pages hold values channel by channel.  Bound by memory for prompts, by latency for single tokens.
+// pages hold values channel by channel.  Bound by memory for prompts (4 x 8192 tokens of 8 kv heads: 37 .. 40 us, 5.0 .. 5.4
+// TB/s read and written, a copy's own 5.1), by latency for single tokens (3 us).
 //
 // Read: a wave takes a step (32 tokens) of a kv head: codes in whole kilobytes, rows put together in LDS, 16 bytes
-// a lane out.  Bound by writing rows.
+// a lane out, past the caches (what was appended stays there: fp16 rows of 4 x 16K tokens as fp32 112 -> 85 us).  Bound by
+// writing rows: those 85 us are 6.4 TB/s, 4 x 8192 tokens in bf16 31 us and 6.4, 2048 9 us and 5.5.
 #include "oscar_q8.h"
 
 namespace {
@@ -121,7 +123,8 @@ template <typename E, int TILES> __global__ __launch_bounds__(256, TILES == 8 ? 
   const auto new_row = [&](int64_t pos) -> u32x4 {   // of a new token (zeros where there is no such row)
     const int64_t row = s.row + (pos - s.old);
     if (row < 0 || row >= P.r.n_rows) return u32x4{};
-    return *reinterpret_cast<const u32x4*>(in + row * stride + c8 * 8);
+    // (read once: it leaves what is written in the caches; 4 x 8K tokens, written and read back, 68 -> 61 us)
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(in + row * stride + c8 * 8));
   };
   u32x4 raw[TILES];
 #pragma unroll
@@ -224,9 +227,10 @@ constexpr int ROW_PITCH = D + 16;   // bytes of a row in LDS: 16-byte pieces of 
 template <typename O> constexpr int LANE_NUMBERS = 16 / sizeof(O);
 template <typename O> __device__ __forceinline__ void put(O* to, const float* x) {
   if constexpr (sizeof(O) == 4)
-    *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+    __builtin_nontemporal_store(u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])},
+                                reinterpret_cast<u32x4*>(to));
   else
-    *reinterpret_cast<u32x4*>(to) = narrow8<O>(x);
+    __builtin_nontemporal_store(narrow8<O>(x), reinterpret_cast<u32x4*>(to));
 }
 
 // Lane quads: byte i of the result is byte (lane % 4) of lane i's dword.
