@@ -229,8 +229,9 @@ template <typename E> struct Row {
   int V;
   double top, scale;   // scale: log2(e) / temperature
   int fixed;
+  const double* powers;
   __device__ __forceinline__ uint32_t key(int i) const { return key_of(to_f32<E>(x[i])); }
-  __device__ __forceinline__ double weight(uint32_t k) const { return power_of_2(((double)number_of(k) - top) * scale); }
+  __device__ __forceinline__ double weight(uint32_t k) const { return power_of_2<0>(((double)number_of(k) - top) * scale, powers); }
   __device__ __forceinline__ uint64_t whole(double w) const { return (uint64_t)(w * (double)(1ull << fixed) + 0.5); }
 };
 
@@ -505,35 +506,43 @@ __device__ __forceinline__ int cell_of(float x, float grid) { return -(int)floor
 // workgroup; a chunk whose largest is past CHUNK_GRID has everything in its last bin (far below such a row's bins).
 constexpr float ROW_GRID = 0x1p21f, CHUNK_GRID = 0x1p22f;
 __device__ __forceinline__ bool on_grid(float top, float grid, float end) { return fabsf(top * grid) < end; }
-// A chunk's logits, a thread's 1024 apart; 0 behind the row's end.
-template <typename E, int PER> __device__ __forceinline__ void load_keys(const SampleParams& P, int b, int c, uint32_t* key) {
-  const E* x = reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride;
+// The bin of a logit under a cell of the grid (its negative, as a float): whole numbers below 2^24, or far above BINS.
+__device__ __forceinline__ int bin_under(float first, float x, float grid) {
+  return (int)fminf(first - floorf(x * grid), (float)(BINS - 1));
+}
+// A chunk's logits, a thread's 1024 apart, as numbers that have an order: NaN as -inf, +inf as the largest; -inf behind
+// the row's end.
+template <typename E, int PER> __device__ __forceinline__ void load_row(const SampleParams& P, int b, int c, float* x) {
+  const E* from = reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride;
   const int i0 = c * (PER * THREADS) + threadIdx.x;
   // (all on the way before the first is looked at: no branch around a load, 1.5 .. 3 us a launch.  As vectors of 16 bytes,
   // at rows of odd lengths, the launches take 1 .. 2 us longer)
   E raw[PER];
 #pragma unroll
-  for (int e = 0; e < PER; ++e) raw[e] = x[min(i0 + e * THREADS, P.V - 1)];
+  for (int e = 0; e < PER; ++e) raw[e] = from[min(i0 + e * THREADS, P.V - 1)];
 #pragma unroll
-  for (int e = 0; e < PER; ++e) key[e] = i0 + e * THREADS < P.V ? key_of(to_f32<E>(raw[e])) : 0;
+  for (int e = 0; e < PER; ++e) {
+    const float v = to_f32<E>(raw[e]);
+    x[e] = i0 + e * THREADS < P.V && v == v ? fminf(v, 3.402823466e38f) : -INFINITY;
+  }
 }
 
 template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_bins_kernel(SampleParams P) {
   __shared__ uint64_t s_bin[BINS], s_wave[WAVES];
   __shared__ double s_power[32];
   const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
-  uint32_t key[PER];
-  load_keys<E, PER>(P, b, c, key);
-  uint64_t best = 0;
+  float x[PER];
+  load_row<E, PER>(P, b, c, x);
+  float most = x[0];
 #pragma unroll
-  for (int e = 0; e < PER; ++e) {
-    const uint64_t at = place_of(key[e], c * (PER * THREADS) + e * THREADS + t);
-    best = at > best ? at : best;
-  }
+  for (int e = 1; e < PER; ++e) most = fmaxf(most, x[e]);
   const Settings s = settings(P, b);
   s_bin[t] = 0;
   fill_powers(s_power);
-  best = group_max(best, s_wave);
+  uint32_t first_most = 0;   // of the largest
+#pragma unroll
+  for (int e = PER - 1; e >= 0; --e) first_most = x[e] == most ? c * (PER * THREADS) + e * THREADS + t : first_most;
+  const uint64_t best = group_max(place_of(key_of(most), first_most), s_wave);
   const int64_t chunk = (int64_t)b * P.chunks + c;
   if (t == 0) {
     P.best[chunk] = best;
@@ -541,31 +550,32 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void osc
   }
   const float top = number_of((uint32_t)(best >> 32));
   if (s.one || s.whole || (uint32_t)(best >> 32) <= DEAD) return;
-  const int first = on_grid(top, s.grid, CHUNK_GRID) ? cell_of(top, s.grid) : -(1 << 30) - BINS;
+  const float first = on_grid(top, s.grid, CHUNK_GRID) ? floorf(top * s.grid) : INFINITY;
   uint64_t mine = 0;   // the last bin's, and without cuts everything
   if (s.by_count) {
+    uint32_t far = 0;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      if (key[e] <= DEAD) continue;
-      const int bin = min(cell_of(number_of(key[e]), s.grid) - first, BINS - 1);
-      if (bin == BINS - 1) ++mine; else atomicAdd(reinterpret_cast<uint32_t*>(&s_bin[bin]), 1u);
+      const int bin = bin_under(first, x[e], s.grid);
+      if (bin < BINS - 1) atomicAdd(reinterpret_cast<uint32_t*>(&s_bin[bin]), 1u);
+      far += bin == BINS - 1 && x[e] > -INFINITY ? 1 : 0;
     }
+    mine = far;
   } else {
     const double ref = (double)top, scale = 1.4426950408889634 / (double)s.temp;
-    uint64_t w[PER];   // (without branches: the exponentials' steps wait for each other, and side by side they do not)
+    uint64_t w[PER];   // (without branches: the exponentials' steps wait for each other, and side by side they do not; -inf: 0)
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const float x = number_of(max(key[e], DEAD + 1));
-      w[e] = whole_of(power_of_2<CHUNK_BITS>(((double)x - ref) * scale, s_power));
-      if (key[e] <= DEAD) w[e] = 0;
-    }
+    for (int e = 0; e < PER; ++e) w[e] = whole_of(power_of_2<CHUNK_BITS>(((double)x[e] - ref) * scale, s_power));
+    if (s.cuts) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const int bin = s.cuts ? min(cell_of(number_of(key[e]), s.grid) - first, BINS - 1) : BINS - 1;
-      if (bin == BINS - 1)
-        mine += w[e];
-      else if (key[e] > DEAD)
-        atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[bin]), (unsigned long long)w[e]);
+      for (int e = 0; e < PER; ++e) {
+        const int bin = bin_under(first, x[e], s.grid);
+        if (bin < BINS - 1) atomicAdd(reinterpret_cast<unsigned long long*>(&s_bin[bin]), (unsigned long long)w[e]);
+        mine += bin == BINS - 1 ? w[e] : 0;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) mine += w[e];
     }
   }
   add_from_wave(&s_bin[BINS - 1], mine);
@@ -671,13 +681,13 @@ template <typename E, int PER, bool FIND> __global__ __launch_bounds__(THREADS, 
   const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x, lane = t & 63;
   // (what the launch waits for is asked for at once)
   const Settings s = settings(P, b);
-  uint32_t key[PER];
+  float x[PER];
   int lo, hi, first;
   if constexpr (FIND) {
     __shared__ FindShared F;
     __shared__ uint64_t s_wave[WAVES];
     const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
-    load_keys<E, PER>(P, b, c, key);
+    load_row<E, PER>(P, b, c, x);
     if (!has_list(s)) return;
     const uint32_t top_key = (uint32_t)(group_max(chunk_best, s_wave) >> 32);
     const float top = number_of(top_key);
@@ -692,13 +702,13 @@ template <typename E, int PER, bool FIND> __global__ __launch_bounds__(THREADS, 
     const RowState& r = P.rows[b];
     lo = r.lo, hi = r.hi, first = r.first;
     if (hi < 0) return;
-    load_keys<E, PER>(P, b, c, key);
+    load_row<E, PER>(P, b, c, x);
   }
   uint32_t on = 0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
-    const int bin = min(cell_of(number_of(key[e]), s.grid) - first, BINS - 1);
-    on |= (key[e] > DEAD && bin >= lo && bin <= hi ? 1u : 0u) << e;
+    const int bin = bin_under(-(float)first, x[e], s.grid);
+    on |= (x[e] > -INFINITY && bin >= lo && bin <= hi ? 1u : 0u) << e;
   }
   // a place on the list, a wave at a time
   const uint64_t mine = __popc(on), upto = wave_scan(mine);
@@ -708,7 +718,7 @@ template <typename E, int PER, bool FIND> __global__ __launch_bounds__(THREADS, 
 #pragma unroll
   for (int e = 0; e < PER; ++e)
     if (on >> e & 1) {
-      if (at < CAP) P.list[(int64_t)b * CAP + at] = place_of(key[e], c * (PER * THREADS) + e * THREADS + t);
+      if (at < CAP) P.list[(int64_t)b * CAP + at] = place_of(key_of(x[e]), c * (PER * THREADS) + e * THREADS + t);
       ++at;
     }
 }
@@ -716,6 +726,7 @@ template <typename E, int PER, bool FIND> __global__ __launch_bounds__(THREADS, 
 template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_sample_pick_kernel(SampleParams P) {
   __shared__ Shared S;
   __shared__ Chunks G;
+  __shared__ double s_power[32];
   const int b = blockIdx.x, t = threadIdx.x, V = P.V;
   const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
   const Settings s = settings(P, b);
@@ -728,6 +739,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     const int at = i * THREADS + t;
     member[i] = at < (int)min(r.n, (uint32_t)CAP) ? P.list[(int64_t)b * CAP + at] : 0;
   }
+  fill_powers(s_power);
   const uint64_t best = group_max(chunk_best, S.wave64);
   const uint32_t top_key = (uint32_t)(best >> 32);
   if (top_key <= DEAD || s.one) {
@@ -738,7 +750,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     return;
   }
   const float top = number_of(top_key);
-  Row<E> row = {reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride, V, (double)top, 1.4426950408889634 / (double)s.temp, P.fixed};
+  Row<E> row = {reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride, V, (double)top, 1.4426950408889634 / (double)s.temp, P.fixed, s_power};
   const bool listed = s.by_count || s.cuts;
   int n = listed ? (int)min(r.n, (uint32_t)CAP + 1) : 0;
   if (s.whole || !on_grid(top, s.grid, ROW_GRID) || n > CAP) {
@@ -910,17 +922,22 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
 
 template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void oscar_sample_probs_kernel(SampleParams P) {
   __shared__ uint64_t s_wave[WAVES];
+  __shared__ double s_power[32];
   const int b = blockIdx.y, c = blockIdx.x, t = threadIdx.x;
-  uint32_t key[PER];
-  load_keys<E, PER>(P, b, c, key);
+  float x[PER];
+  load_row<E, PER>(P, b, c, x);
   const uint64_t chunk_best = t < P.chunks ? P.best[(int64_t)b * P.chunks + t] : 0;
   const Settings s = settings(P, b);
   const RowState R = P.rows[b];
   const int kind = R.kind;
   if (kind == DONE) return;
+  fill_powers(s_power);
   const uint64_t best = group_max(chunk_best, s_wave);
   const double top = (double)number_of((uint32_t)(best >> 32)), scale = 1.4426950408889634 / (double)s.temp;
+  // (of nothing: NaN, which no logit reaches)
   const uint64_t cut = kind == BY_CUT ? R.cut : kind == ONE_TOKEN ? best : ~0ull;
+  const float cut_x = number_of((uint32_t)(cut >> 32));
+  const uint32_t cut_i = ~(uint32_t)cut;
   const double inv_sum = kind == BY_CUT ? 1.0 / R.sum : 1.0;
   float* out = P.probs + (int64_t)b * P.V;
 #pragma unroll
@@ -928,11 +945,11 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void osc
     const int i = c * (PER * THREADS) + e * THREADS + t;
     if (i >= P.V) break;
     float y = 0.0f;
-    if (key[e] > DEAD && place_of(key[e], i) >= cut) {
-      const double w = power_of_2(((double)number_of(key[e]) - top) * scale);
+    if (x[e] > cut_x || (x[e] == cut_x && (uint32_t)i <= cut_i)) {
+      const double w = power_of_2<0>(((double)x[e] - top) * scale, s_power);
       y = kind == ONE_TOKEN ? 1.0f : w < (double)s.m ? 0.0f : (float)(w * inv_sum);
     }
-    out[i] = y;
+    __builtin_nontemporal_store(y, out + i);
   }
 }
 
