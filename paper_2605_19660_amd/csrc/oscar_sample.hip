@@ -13,16 +13,20 @@
 // temperature * 45 / 1024), counted from 0 so that chunks' bins lie on one grid:
 //   1. every chunk: its largest logit, and the running sums (of tokens for top_k, else of weights, in 64 bits) over
 //      the 1024 bins below it;
-//   2. every chunk: adds up the row's running sums, each chunk's shifted by whole bins and scaled by one factor, finds the
-//      bins in which the cuts lie, and puts its logits in those (with top_k: in those and above) on the row's list;
-//   3. a workgroup a row: sorts the list, finds the cut in it, what stays of every chunk (running sums above the list,
+//   2. the row's running sums are added up, each chunk's shifted by whole bins and scaled by one factor, and the bins found
+//      in which the cuts lie: with few chunks by each of them, else by a workgroup a row in a launch of its own;
+//   3. every chunk puts its logits in those bins (with top_k: in those and above) on the row's list;
+//   4. a workgroup a row: sorts the list, finds the cut in it, what stays of every chunk (running sums above the list,
 //      the list's members one by one), the chunk the token is in, and in it the token;
-//   4. with probs, every chunk: its probabilities.
+//   5. with probs, every chunk: its probabilities.
 // A row whose list does not fit (thousands of equal logits at the cut) or with a top_k past 1024 is searched by
 // one workgroup, which splits bins until they fit or hold one number.
 //
-// What bounds it: latency of three or four launches; for many long rows reading them two or three times (the second
-// time out of the caches) and the exponentials.
+// What bounds it: one row of 32000 with top_p takes 23 us, a chain of dependent steps in three launches (7.5, 6 and 9.5):
+// loads that wait for the launch before, scans over a workgroup, a sort.  64 rows of 128003 with mixed settings and
+// probabilities take 72 us, 20.8 bins, 7.8 to find, 9.5 list, 17 draw, 16.4 probabilities: the rows are read three times
+// (8 us where nothing else is done, 5 TB/s; past the first time out of the caches), the bins are bound by vector instructions
+// (40 a logit, half of them its exponential), the draw by its longest list.
 #include "oscar_common.h"
 
 namespace {
@@ -195,7 +199,7 @@ struct Shared {
 };
 
 // Falling order of list[0 .. n), by the workgroup; returns with the list in place for all.  Up to 512 numbers (all
-// different) each counts those above it; more are sorted by exchanges, a barrier a step (2048: 18 us; 50: 2.8 us, counted 0.7).
+// different) each counts those above it; more are sorted by exchanges, a barrier a step (2048: some 18 us; 50: 2.8 us, counted 0.9).
 __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
   if (n <= THREADS / 2) {
     const uint64_t mine = threadIdx.x < n ? list[threadIdx.x] : 0;
@@ -953,15 +957,17 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS, 8) void osc
   }
 }
 
-// Logits of a chunk: 8192, or 4096 where that leaves the chip half empty (one row of 32000: 8 workgroups, not 4).
-int chunk_of(int32_t batch, int32_t vocab) { return (int64_t)batch * ((vocab + 4095) / 4096) <= 512 ? 4096 : 8192; }
+// Logits of a chunk: 4096 as long as a CU has no second one, else 8192 (top_p over 32 rows of 32000: 32.3 us in pieces of
+// 4096, 33.8 in pieces of 8192; 64: 36.6 and 34.7; 16 of 128003: 45 and 38; 64: 78 and 59).
+int chunk_of(int32_t batch, int32_t vocab) { return (int64_t)batch * ((vocab + 4095) / 4096) <= 256 ? 4096 : 8192; }
 
 template <typename E, int PER> void launch(const SampleParams& P, int batch, hipStream_t st) {
   const dim3 grid(P.chunks, batch);
   hipLaunchKernelGGL((oscar_sample_bins_kernel<E, PER>), grid, dim3(THREADS), 0, st, P);
   if (P.top_k || P.top_p || P.min_p) {
-    // one row of 32000: a launch for the bins 5 us, every chunk for itself 3; 64 of 128003: 5 and 16
-    if ((int64_t)P.chunks * batch <= 64) {
+    // Each chunk for itself, or a launch for the bins: a draw takes 23.1 and 24.6 us of one row of 32000, 30.2 and 31.3 of
+    // 16 (128 chunks), 32.7 and 32.3 of 32, 68 and 59 of 64 of 128003
+    if ((int64_t)P.chunks * batch <= 128) {
       hipLaunchKernelGGL((oscar_sample_list_kernel<E, PER, true>), grid, dim3(THREADS), 0, st, P);
     } else {
       hipLaunchKernelGGL(oscar_sample_find_kernel, dim3(batch), dim3(THREADS), 0, st, P);
