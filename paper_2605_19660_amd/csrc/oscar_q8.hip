@@ -14,8 +14,8 @@
 // TB/s read and written, a copy's own 5.1), by latency for single tokens (3 us).
 //
 // Read: a wave takes a step (32 tokens) of a kv head: codes in whole kilobytes, rows put together in LDS, 16 bytes
-// a lane out, past the caches (what was appended stays there: fp16 rows of 4 x 16K tokens as fp32 112 -> 85 us).  Bound by
-// writing rows: those 85 us are 6.4 TB/s, 4 x 8192 tokens in bf16 31 us and 6.4, 2048 9 us and 5.5.
+// a lane out.  Bound by writing rows: 4 x 16K tokens of fp16 as fp32 take 106 us, 5.1 TB/s read and written, a copy's own
+// rate (85 where the last-level cache holds the codes); 4 x 8192 in bf16, just appended, 32 us, 2048 12.
 #include "oscar_q8.h"
 
 namespace {
@@ -123,7 +123,7 @@ template <typename E, int TILES> __global__ __launch_bounds__(256, TILES == 8 ? 
   const auto new_row = [&](int64_t pos) -> u32x4 {   // of a new token (zeros where there is no such row)
     const int64_t row = s.row + (pos - s.old);
     if (row < 0 || row >= P.r.n_rows) return u32x4{};
-    // (read once: it leaves what is written in the caches; 4 x 8K tokens, written and read back, 68 -> 61 us)
+    // (read once: what is written stays in the caches; 4 x 8K tokens, written and read back, 68 -> 61 us)
     return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(in + row * stride + c8 * 8));
   };
   u32x4 raw[TILES];
@@ -225,12 +225,14 @@ constexpr int ROW_PITCH = D + 16;   // bytes of a row in LDS: 16-byte pieces of 
 
 // What a lane writes at a time: 16 bytes, so that a wave's lie next to each other.
 template <typename O> constexpr int LANE_NUMBERS = 16 / sizeof(O);
+// (32-bit rows past the caches: 65536 tokens of 8 kv heads read 130 -> 111 us, read and then added up 284 -> 263; 16-bit rows
+// gain as much alone and lose it again where the next launch uses them: 64 us, 65 past the caches)
 template <typename O> __device__ __forceinline__ void put(O* to, const float* x) {
   if constexpr (sizeof(O) == 4)
     __builtin_nontemporal_store(u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])},
                                 reinterpret_cast<u32x4*>(to));
   else
-    __builtin_nontemporal_store(narrow8<O>(x), reinterpret_cast<u32x4*>(to));
+    *reinterpret_cast<u32x4*>(to) = narrow8<O>(x);
 }
 
 // Lane quads: byte i of the result is byte (lane % 4) of lane i's dword.
