@@ -621,7 +621,7 @@ int oscar_q8_read(const oscar_q8_cache *cache, const int32_t *lens, const int32_
  *   u      : device fp32 [batch], in [0, 1)
  *   tokens : device int32 [batch]
  *   probs  : device fp32 [batch][vocab], or NULL: what each token was drawn with (0 for those that do not
- *            stay), as oscar_verify_drafts takes it
+ *            stay), as oscar_verify_drafts takes it; overlaps nothing else
  *   workspace : at least oscar_sample_workspace_bytes(...), 16-byte aligned; its contents do not matter.  Calls
  *            that share one must be ordered
  * Weights and sums are in 64 bits; the same call gives the same bits every time.  batch <= 65535, vocab <=
