@@ -967,8 +967,9 @@ template <typename E, int PER> void launch(const SampleParams& P, int batch, hip
   if (P.top_k || P.top_p || P.min_p) {
     // Each chunk for itself, or a launch for the bins: a draw takes 23.1 and 24.6 us of one row of 32000, 30.2 and 31.3 of
     // 16 (128 chunks), 32.7 and 32.3 of 32, 68 and 59 of 64 of 128003
-    if ((int64_t)P.chunks * batch <= 128) {
-      hipLaunchKernelGGL((oscar_sample_list_kernel<E, PER, true>), grid, dim3(THREADS), 0, st, P);
+    // (pieces of 8192 are 129 and more)
+    if (PER == 4 && (int64_t)P.chunks * batch <= 128) {
+      hipLaunchKernelGGL((oscar_sample_list_kernel<E, 4, true>), grid, dim3(THREADS), 0, st, P);
     } else {
       hipLaunchKernelGGL(oscar_sample_find_kernel, dim3(batch), dim3(THREADS), 0, st, P);
       hipLaunchKernelGGL((oscar_sample_list_kernel<E, PER, false>), grid, dim3(THREADS), 0, st, P);

@@ -95,6 +95,21 @@ def test_a_large_vocabulary_and_many_rows():
     check(x, k=[50, 0, 0, 1024, 1025, 100000] * 2, p=[0.95, 0.9, 1.0, 0.9, 0.7, 0.999] * 2, temp=[0.8, 1.2] * 6, m=[0.0] * 6 + [0.02] * 6)
 
 
+@pytest.mark.parametrize("B, V", [(1, 4096), (128, 4096), (129, 4096), (256, 4000), (257, 4097), (4, 128003), (6, 128003), (2, 524288), (1, 1 << 22)])
+def test_every_way_a_row_is_cut(B, V):
+    """Few and many rows of one and of many pieces; a piece that is masked whole, a row that is, one of equal numbers."""
+    rng = np.random.default_rng(B + V)
+    io = ("f32", "bf16", "f16")[B % 3]
+    x = logits(rng, B, V, io)
+    x[0, V // 4:V // 4 + V // 2] = -np.inf
+    if B > 3:
+        x[1] = -np.inf
+        x[2] = 0.25
+    among = lambda *a: np.array(a)[rng.integers(0, len(a), size=B)]
+    check(x, io, p=0.9)
+    check(x, io, temp=among(0.0, 0.7, 1.0, 1.3), k=among(0, 0, 1, 50, 1024), p=among(1.0, 0.5, 0.95), m=among(0.0, 0.0, 0.02))
+
+
 @pytest.mark.parametrize("V", [5, 1000, 6000, 40000])
 def test_equal_logits(V):
     """Ties go to the lowest index, in any number: rows of one value, of two, and of a few that repeat."""
