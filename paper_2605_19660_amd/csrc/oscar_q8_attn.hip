@@ -592,8 +592,18 @@ extern "C" int32_t oscar_q8_auto_splits(const oscar_q8_cache* cache, int32_t n_q
   // unit better (35 rows over 128K, 32 / 64 splits 45.6 / 37.9); but rows by the hundred have more partial sums
   // than they save (200 rows over 2048, 1 / 2 splits 22.9 / 35.1).
   const int64_t cus = oscar_compute_units();
-  const int64_t splits = block == 16 ? cus / units : 2 * units <= cus ? 2 * cus / units : 1;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>({splits, pages, 512}));
+  const int64_t most = std::min<int64_t>({block == 16 ? cus / units : 2 * units <= cus ? 2 * cus / units : 1, pages, 512});
+  // Of that many, half as many and so on the one that takes least: a page of a split 0.75 us (1 with 32 rows), the joining
+  // launch 5.5 (3.5 of them on the GPU), a row's sums of a split 0.5 ns.  One row over 1000, 8 / 1 splits: 10.1 / 10.9 us
+  // of graph, 12.4 / 10.9 of calls; 8 rows of 8 sequences over 1000, 8 / 1 splits 20.4 / 14.4, over 4000, 8 / 4 / 1 26 / 25 / 41.
+  const double page_us = block == 16 ? 0.75 : 1.0, row_us = 0.0005 * (double)cache->batch * T * n_q_heads;
+  int64_t best = 1;
+  double least = (double)pages * page_us;
+  for (int64_t s = most; s > 1; s /= 2) {
+    const double us = (double)((pages + s - 1) / s) * page_us + 5.5 + row_us * (double)s;
+    if (us < least) best = s, least = us;
+  }
+  return (int32_t)best;
 }
 
 extern "C" size_t oscar_q8_workspace_bytes(const oscar_q8_cache* cache, int32_t n_q_heads, int32_t T, int32_t num_splits) {
