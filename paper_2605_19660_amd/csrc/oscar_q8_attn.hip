@@ -477,13 +477,23 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
 // F16: the io type; ROWS: of a workgroup.
 template <bool F16, int ROWS> __global__ __launch_bounds__(256, ROWS == 16 ? 3 : 2) void oscar_q8_attn_kernel(AttnParams P) {
   __shared__ Joined J;
-  // row blocks of one range of pages lie on one die of eight, next to each other
+  // row blocks of one range of pages lie on one die of eight, next to each other; the ranges that are left over when every
+  // die has as many share the dies (300 rows x 2 kv heads over 30000: on two dies 549 us, on all 150)
   uint32_t id = blockIdx.x;
   int rb = 0;
   if (P.row_blocks > 1) {
-    const uint32_t group = id / (8 * P.row_blocks), in = id % (8 * P.row_blocks);
-    rb = P.row_blocks - 1 - in / 8;   // (the last rows see the most)
-    id = group * 8 + in % 8;
+    const uint32_t units = (uint32_t)P.c.batch * P.c.heads * P.splits, even = units / 8 * 8, blocks = P.row_blocks;
+    if (id < even * blocks) {
+      const uint32_t group = id / (8 * blocks), in = id % (8 * blocks);
+      rb = in / 8;
+      id = group * 8 + in % 8;
+    } else {
+      const uint32_t rest = (units - even) * blocks, in = id - even * blocks, at = in % 8 * ((rest + 7) / 8) + in / 8;
+      if (at >= rest) return;
+      rb = at % blocks;
+      id = even + at / blocks;
+    }
+    rb = P.row_blocks - 1 - rb;   // (the last rows see the most)
   }
   const int split = id % P.splits;
   id /= P.splits;
@@ -587,21 +597,21 @@ extern "C" int32_t oscar_q8_auto_splits(const oscar_q8_cache* cache, int32_t n_q
   const int block = rows_of(rows);
   const int64_t units = (int64_t)cache->batch * cache->n_kv_heads * ((rows + block - 1) / block);
   const int64_t pages = (max_seq_len + OSCAR_R - 1) / OSCAR_R;
-  // One workgroup a compute unit streams as fast as two, which leave twice the partial sums (8 sequences of 32K, 4 / 8
-  // splits 93.8 / 98.5 us; 1 of 8K 32 / 64 splits 9.2 / 10.2).  With 32 rows a workgroup computes, and two fill a
-  // unit better (35 rows over 128K, 32 / 64 splits 45.6 / 37.9); but rows by the hundred have more partial sums
-  // than they save (200 rows over 2048, 1 / 2 splits 22.9 / 35.1).
   const int64_t cus = oscar_compute_units();
-  const int64_t most = std::min<int64_t>({block == 16 ? cus / units : 2 * units <= cus ? 2 * cus / units : 1, pages, 512});
-  // Of that many, half as many and so on the one that takes least: a page of a split 0.75 us (1 with 32 rows), the joining
-  // launch 5.5 (3.5 of them on the GPU), a row's sums of a split 0.5 ns.  One row over 1000, 8 / 1 splits: 10.1 / 10.9 us
-  // of graph, 12.4 / 10.9 of calls; 8 rows of 8 sequences over 1000, 8 / 1 splits 20.4 / 14.4, over 4000, 8 / 4 / 1 26 / 25 / 41.
-  const double page_us = block == 16 ? 0.75 : 1.0, row_us = 0.0005 * (double)cache->batch * T * n_q_heads;
+  // The one that takes least.  16 rows read: a page of a split takes 0.75 us, and more workgroups than compute units do not
+  // read faster (8 sequences of 32K, 4 / 8 splits 93.8 / 98.5 us).  32 rows compute: a page takes 1.05 us, of each of two
+  // workgroups that share a unit 2 * 0.88.  The joining launch takes 5.5 us (3.5 of them on the GPU), a row's sums of a split
+  // 0.5 ns.  One row over 1000, 8 / 1 splits: 10.1 / 10.9 us of graph, 12.4 / 10.9 of calls; 8 rows of 8 sequences over 1000,
+  // 8 / 1 splits 20.4 / 14.4; 35 rows over 128K, 32 / 64 45.6 / 37.9; 700 of 2 sequences over 54539, 1 / 4 443 / 286.
+  const double row_us = 0.0005 * (double)cache->batch * T * n_q_heads;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({block == 16 ? cus / units : 4 * cus / units, pages, 512}));
   int64_t best = 1;
-  double least = (double)pages * page_us;
-  for (int64_t s = most; s > 1; s /= 2) {
-    const double us = (double)((pages + s - 1) / s) * page_us + 5.5 + row_us * (double)s;
-    if (us < least) best = s, least = us;
+  double least = 0.0;
+  for (int64_t s = 1; s <= most; ++s) {
+    const int64_t rounds = block == 16 ? 1 : (units * s + cus - 1) / cus, share = (pages + s - 1) / s;
+    double us = (double)(rounds * share) * (block == 16 ? 0.75 : rounds == 1 ? 1.05 : rounds == 2 ? 0.88 : 0.9);
+    if (s > 1) us = 1.07 * (us + 5.5 + row_us * (double)s);   // (one split unless several gain a little)
+    if (s == 1 || us < least) best = s, least = us;
   }
   return (int32_t)best;
 }
@@ -631,7 +641,7 @@ extern "C" int oscar_q8_attn(const void* q, int64_t q_stride, int64_t n_rows, in
   if (rows > INT32_MAX / 2) return OSCAR_ERR_INVALID_ARG;
   const int block = rows_of(rows);
   const int64_t row_blocks = (rows + block - 1) / block, units = (int64_t)cache->batch * cache->n_kv_heads * splits;
-  const int64_t grid = row_blocks == 1 ? units : (units + 7) / 8 * 8 * row_blocks;
+  const int64_t grid = row_blocks == 1 ? units : (units * row_blocks + 7) / 8 * 8;
   const int64_t join = (int64_t)cache->batch * T * n_q_heads;
   // a grid's threads are counted in 32 bits
   if (row_blocks > INT32_MAX / 8 || grid * 256 > UINT32_MAX || (splits > 1 && join * 256 > UINT32_MAX)) return OSCAR_ERR_INVALID_ARG;
