@@ -198,10 +198,13 @@ struct Shared {
   uint64_t hit;
 };
 
-// Falling order of list[0 .. n), by the workgroup; returns with the list in place for all.  Up to 512 numbers (all
-// different) each counts those above it; more are sorted by exchanges, a barrier a step (2048: some 18 us; 50: 2.8 us, counted 0.9).
-__device__ __forceinline__ void sort_list(uint64_t* list, int n) {
-  if (n <= THREADS / 2) {
+// Falling order of S.list[0 .. n), all different, by the workgroup; returns with the list in place for all.  Up to 256 numbers
+// each counts those above it; more are dealt into bins of equal steps (LOGITS: of the logits they are places of), where each
+// counts its own bin.  Where one bin gets many they are sorted by exchanges, a barrier a step.  (Two sorts a draw with top_k of
+// one row of 128003: top_k 1000, exchanged 56 us, by bins 39; 400, counted 40, by bins 36; 200 31 and 34; 50 25 and 33.)
+template <bool LOGITS> __device__ __forceinline__ void sort_list(Shared& S, int n) {
+  uint64_t* list = S.list;
+  if (n <= THREADS / 4) {
     const uint64_t mine = threadIdx.x < n ? list[threadIdx.x] : 0;
     int above = 0;
     if (threadIdx.x < n) {
@@ -212,6 +215,55 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
     if (threadIdx.x < n) list[above] = mine;
     __syncthreads();
     return;
+  }
+  {
+    const int t = threadIdx.x;
+    uint64_t x[CAP / THREADS], most = 0, least = ~0ull;
+#pragma unroll
+    for (int i = 0; i < CAP / THREADS; ++i) {
+      x[i] = i * THREADS + t < n ? list[i * THREADS + t] : 0;
+      if (i * THREADS + t < n) most = x[i] > most ? x[i] : most, least = x[i] < least ? x[i] : least;
+    }
+    S.count[t] = 0;
+    most = group_max(most, S.wave64);
+    least = ~group_max(~least, S.wave64);
+    const int shift = max(54 - __builtin_clzll((most - least) | 1), 0);   // (1024 bins)
+    const float top = number_of((uint32_t)(most >> 32)), range = top - number_of((uint32_t)(least >> 32));
+    const bool logits = LOGITS && range > 0.0f;
+    const auto bin_of = [&](uint64_t place) {
+      return logits ? (int)((top - number_of((uint32_t)(place >> 32))) / range * (BINS - 1)) : (int)((most - place) >> shift);
+    };
+    uint32_t at[CAP / THREADS];
+#pragma unroll
+    for (int i = 0; i < CAP / THREADS; ++i) at[i] = i * THREADS + t < n ? atomicAdd(&S.count[bin_of(x[i])], 1u) : 0;
+    __syncthreads();
+    const uint32_t here = S.count[t];
+    uint64_t all;
+    const uint32_t upto = (uint32_t)group_scan((uint64_t)here, S.wave64, &all);
+    S.count[t] = upto;
+    if (!__syncthreads_or(here > 32)) {
+      int from[CAP / THREADS], to[CAP / THREADS];
+#pragma unroll
+      for (int i = 0; i < CAP / THREADS; ++i) {
+        if (i * THREADS + t >= n) continue;
+        const int bin = bin_of(x[i]);
+        from[i] = bin ? S.count[bin - 1] : 0, to[i] = S.count[bin];
+        list[from[i] + at[i]] = x[i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < CAP / THREADS; ++i) {
+        if (i * THREADS + t >= n) continue;
+        at[i] = from[i];
+        for (int j = from[i]; j < to[i]; ++j) at[i] += list[j] > x[i] ? 1 : 0;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < CAP / THREADS; ++i)
+        if (i * THREADS + t < n) list[at[i]] = x[i];
+      __syncthreads();
+      return;
+    }
   }
   int size = 2;
   while (size < n) size *= 2;
@@ -390,7 +442,7 @@ __device__ void search_cut(Shared& S, const Row<E>& row, Search& q, double share
   }
   __syncthreads();
   const int n = min((int)S.n, CAP);
-  sort_list(S.list, n);
+  sort_list<true>(S, n);
   if (t == 0) S.hit = 0;
   uint64_t before = above;
   for (int i0 = 0; i0 < n; i0 += THREADS) {
@@ -771,7 +823,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
       for (int i = 0; i < CAP / THREADS; ++i)
         if (i * THREADS + t < n) S.list[i * THREADS + t] = member[i];
       __syncthreads();
-      sort_list(S.list, n);
+      sort_list<true>(S, n);
     }
   }
   if (s.by_count) {
@@ -787,7 +839,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     // in order of the index
     if (t < left) S.list[t] = ~((uint64_t)(uint32_t)~(uint32_t)at << 32 | (uint32_t)(at >> 32));
     __syncthreads();
-    sort_list(S.list, left);
+    sort_list<false>(S, left);
     const uint64_t x = t < left ? ~S.list[t] : 0;
     const double y = t < left ? row.weight((uint32_t)x) : 0.0;
     const double upto = group_scan(y, S.wave_f, &sum);
@@ -850,7 +902,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
       above += (double)S.hit / (double)(1ull << LIST_BITS);
       from_top = from_top && bin == 0;
       n = (int)S.n;
-      sort_list(S.list, n);
+      sort_list<true>(S, n);
     }
     cut = n > 0 ? S.list[0] + 1 : cut;   // (none of the list)
     for (int i0 = 0; i0 < n; i0 += THREADS) {

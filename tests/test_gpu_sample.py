@@ -207,3 +207,21 @@ def test_replays_and_other_streams():
         assert torch.equal(t, tokens) and torch.equal(q, probs)
         want, _ = rule(x.double().cpu().numpy(), np.ones(B), k.cpu().numpy(), p.double().cpu().numpy(), np.zeros(B), u.double().cpu().numpy())
         assert np.array_equal(tokens.cpu().numpy(), want)
+
+
+def test_long_lists_of_every_kind():
+    """Lists of hundreds to thousands of tokens that are sorted: spread, crowded on one side of zero or about it, beside one
+    far above, in a few values with many ties."""
+    rng = np.random.default_rng(7)
+    V = 20000
+    x = np.stack([rng.standard_normal(V), rng.random(V) * 1e-3, (rng.random(V) - 0.5) * 1e-35, rng.random(V) * 1e-4 - 30.0,
+                  rng.integers(0, 200, size=V) * 0.25, rng.integers(0, 3, size=V) - 1.0, -np.arange(V) * 1e-4, rng.standard_normal(V) ** 3])
+    x[3, 17] = 40.0
+    x = x.astype(np.float32).astype(np.float64)
+    for k in (255, 256, 257, 512, 513, 1000, 1024):
+        check(x, k=k)
+        check(x, k=k, p=0.8, temp=0.5)
+    check(x, k=1025)
+    check(x, k=5000, p=0.9)
+    check(x, p=0.02)
+    check(x, m=0.97, temp=2.0)
