@@ -287,7 +287,10 @@ struct __align__(16) Joined {
 };
 
 // The rows from row0 on (of a sequence and kv head) over the pages of a split, by a workgroup.
-template <bool F16, class S>
+// ONCE: no other workgroup reads these pages, and they are asked for past the caches (caches of 1 GB in all, one after the
+// other: 1 x 1000 tokens 15.1 -> 12.9 us, 8 x 4000 21.1 -> 18.7, 8 x 32K 95 -> 82, with 32 rows 115 -> 102; the same cache
+// again and again, 8 x 4000, 18.4 -> 19.0; pages that several blocks of rows read, 35 rows over 128K, 39 -> 44)
+template <bool F16, class S, bool ONCE>
 __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, int b, int h, int split, int row0, Joined& J) {
   using Op = typename S::Op;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -334,7 +337,10 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
     const int64_t at = (int64_t)page * P.c.heads + h;
     const uint8_t* in = codes + at * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES + lane * 16;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(in + i * 1024);
+    for (int i = 0; i < 4; ++i) {
+      const u32x4* from = reinterpret_cast<const u32x4*>(in + i * 1024);
+      x[i] = ONCE ? __builtin_nontemporal_load(from) : *from;
+    }
     scale = scales[at * per_page + wave * Q8_STEP_TOKENS / P.c.block];
   };
 
@@ -474,14 +480,14 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
   }
 }
 
-// F16: the io type; ROWS: of a workgroup.
-template <bool F16, int ROWS> __global__ __launch_bounds__(256, ROWS == 16 ? 3 : 2) void oscar_q8_attn_kernel(AttnParams P) {
+// F16: the io type; ROWS: of a workgroup; ONCE: one workgroup has all of a sequence's rows.
+template <bool F16, int ROWS, bool ONCE> __global__ __launch_bounds__(256, 2) void oscar_q8_attn_kernel(AttnParams P) {
   __shared__ Joined J;
   // row blocks of one range of pages lie on one die of eight, next to each other; the ranges that are left over when every
   // die has as many share the dies (300 rows x 2 kv heads over 30000: on two dies 549 us, on all 150)
   uint32_t id = blockIdx.x;
   int rb = 0;
-  if (P.row_blocks > 1) {
+  if (!ONCE) {
     const uint32_t units = (uint32_t)P.c.batch * P.c.heads * P.splits, even = units / 8 * 8, blocks = P.row_blocks;
     if (id < even * blocks) {
       const uint32_t group = id / (8 * blocks), in = id % (8 * blocks);
@@ -503,9 +509,9 @@ template <bool F16, int ROWS> __global__ __launch_bounds__(256, ROWS == 16 ? 3 :
   const int row0 = rb * ROWS, left = seq.n * P.g - row0;
   if (left <= 0) return;
   if (left <= 16)   // (all, or a sequence's last rows)
-    attend<F16, Rows16<F16>>(P, seq, b, h, split, row0, J);
+    attend<F16, Rows16<F16>, ONCE>(P, seq, b, h, split, row0, J);
   else if constexpr (ROWS == 32)
-    attend<F16, Rows32<F16>>(P, seq, b, h, split, row0, J);
+    attend<F16, Rows32<F16>, ONCE>(P, seq, b, h, split, row0, J);
 }
 
 // Joins the splits of a row and query head: a workgroup, each wave a quarter of the splits.
@@ -579,9 +585,11 @@ int rows_of(int64_t rows) { return rows <= 16 ? 16 : 32; }
 
 template <bool F16> void launch(const AttnParams& P, int block_rows, uint32_t grid, hipStream_t st) {
   if (block_rows == 16)
-    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 16>), dim3(grid), dim3(256), 0, st, P);
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 16, true>), dim3(grid), dim3(256), 0, st, P);
+  else if (P.row_blocks == 1)
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 32, true>), dim3(grid), dim3(256), 0, st, P);
   else
-    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 32>), dim3(grid), dim3(256), 0, st, P);
+    hipLaunchKernelGGL((oscar_q8_attn_kernel<F16, 32, false>), dim3(grid), dim3(256), 0, st, P);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
