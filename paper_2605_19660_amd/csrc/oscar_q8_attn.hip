@@ -13,8 +13,8 @@
 // ahead of its use, and logits are worked out a step ahead of their probabilities.  No barrier until the waves' sums
 // are joined at the end.
 //
-// Up to 16 rows (a decoding step) take products of 16 x 16 x 32: the cache's bytes bound it (8 sequences of 32K: 94 us,
-// 5.7 TB/s with the start, the end and the joining launch; a plain read of as many bytes takes 80).  More rows take products of
+// Up to 16 rows (a decoding step) take products of 16 x 16 x 32: the cache's bytes bound it (8 sequences of 32K: 82 us,
+// 6.6 TB/s with the start, the end and the joining launch; a plain read of as many bytes takes 80).  More rows take products of
 // 32 x 32 x 16 and are bound by issue: 220 vector instructions a step of 32 x 32 (64 conversions, 48 for limbs, 16
 // exponentials, 24 exchanges) beside 24 products of 32 clocks; vector issue is busy 69 % of the time, the matrix cores 43 %
 // (8192 rows of a kv head over themselves: 232 us).  A product keeps vector instructions out for 8 clocks whatever
@@ -607,7 +607,7 @@ extern "C" int32_t oscar_q8_auto_splits(const oscar_q8_cache* cache, int32_t n_q
   const int64_t pages = (max_seq_len + OSCAR_R - 1) / OSCAR_R;
   const int64_t cus = oscar_compute_units();
   // The one that takes least.  16 rows read: a page of a split takes 0.75 us, and more workgroups than compute units do not
-  // read faster (8 sequences of 32K, 4 / 8 splits 93.8 / 98.5 us).  32 rows compute: a page takes 1.05 us, of each of two
+  // read faster (8 sequences of 32K, 4 / 8 splits 82 / 86 us).  32 rows compute: a page takes 1.05 us, of each of two
   // workgroups that share a unit 2 * 0.88.  The joining launch takes 5.5 us (3.5 of them on the GPU), a row's sums of a split
   // 0.5 ns.  One row over 1000, 8 / 1 splits: 10.1 / 10.9 us of graph, 12.4 / 10.9 of calls; 8 rows of 8 sequences over 1000,
   // 8 / 1 splits 20.4 / 14.4; 35 rows over 128K, 32 / 64 45.6 / 37.9; 700 of 2 sequences over 54539, 1 / 4 443 / 286.
