@@ -170,6 +170,18 @@ __device__ __forceinline__ uint64_t group_max(uint64_t v, uint64_t* s) {
   for (int w = 1; w < WAVES; ++w) v = s[w] > v ? s[w] : v;
   return v;
 }
+// The largest of each half.
+__device__ __forceinline__ uint64_t group_max_halves(uint32_t upper, uint32_t lower, uint64_t* s) {
+  const auto most = [](uint64_t a, uint64_t b) { return (uint64_t)max((uint32_t)(a >> 32), (uint32_t)(b >> 32)) << 32 | max((uint32_t)a, (uint32_t)b); };
+  uint64_t v = wave_prefix((uint64_t)upper << 32 | lower, most);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) s[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = s[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) v = most(v, s[w]);
+  return v;
+}
 
 // One addition in LDS a wave, one minimum a wave (of 1024 threads at one address each waits for all before it: 3 us).
 __device__ __forceinline__ void add_from_wave(uint64_t* to, uint64_t v) {
@@ -791,9 +803,8 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
   uint64_t member[CAP / THREADS];
 #pragma unroll
   for (int i = 0; i < CAP / THREADS; ++i) {
-    // (what lies behind the list's end is not used)
-    const int at = i * THREADS + t;
-    member[i] = at < (int)min(r.n, (uint32_t)CAP) ? P.list[(int64_t)b * CAP + at] : 0;
+    // (what lies behind the list's end is not used; its length is still on its way)
+    member[i] = P.list[(int64_t)b * CAP + i * THREADS + t];
   }
   fill_powers(s_power);
   const uint64_t best = group_max(chunk_best, S.wave64);
@@ -868,8 +879,8 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
       for (int i = 0; i < CAP / THREADS; ++i)
         if (i * THREADS + t < n) most = max(most, (uint32_t)(member[i] >> 32)), least = min(least, (uint32_t)(member[i] >> 32));
       bins[t] = 0;
-      most = (uint32_t)group_max(most, S.wave64);
-      least = ~(uint32_t)group_max((uint32_t)~least, S.wave64);
+      const uint64_t ends = group_max_halves(most, ~least, S.wave64);
+      most = (uint32_t)(ends >> 32), least = ~(uint32_t)ends;
       const int shift = max(32 - __builtin_clz((most - least) | 1) - 10, 0);   // (1024 bins)
       if (t == 0) S.n = 0, S.found = (most - least) >> shift;   // (if rounding lets none reach the target: the last)
       uint64_t w[CAP / THREADS];
@@ -912,8 +923,8 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
       double here;
       const double before = above + group_scan(w, S.wave_f, &here) - w;
       const bool stays = i < n && ((from_top && i == 0) || ((!(s.p < 1.0f) || before < target) && !(w < (double)s.m)));
-      const uint64_t last = group_max(stays ? ~at : 0, S.wave64);   // the lowest place that stays
-      if (last) cut = ~last;
+      const int left = __syncthreads_count(stays);   // (the first so many: weights fall)
+      if (left) cut = S.list[i0 + left - 1];
       if (stays)
         atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[(int)~(uint32_t)at / P.chunk]),
                   (unsigned long long)whole_of(w * (double)(1ull << LIST_BITS)));
