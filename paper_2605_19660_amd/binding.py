@@ -902,7 +902,9 @@ def q8_attn(cache: Q8Cache, q, lens, new_lens=None, row_starts=None, max_new: in
             max_seq_len_hint: int = 0, num_splits: int = 0, workspace=None, stream=None):
     """oscar_q8_attn: q [batch, T, n_q_heads, 128] or, with row_starts, [n_rows, n_q_heads, 128] of any even distance
     between rows; the tokens they belong to are in the cache (q8_append) and in lens.  Returns `out`, of q's shape and
-    of its type or fp32; made here, rows that belong to no sequence are zeros, else they stay as they were."""
+    of its type or fp32; made here, rows that belong to no sequence are zeros, else they stay as they were.  Without
+    a max_seq_len_hint splits are counted for sequences as long as the block table has room for (one split would
+    leave most of the GPU idle over a long cache; too many cost a launch and a few microseconds)."""
     import torch
     if stream is not None:
         with torch.cuda.stream(stream):
@@ -916,7 +918,7 @@ def q8_attn(cache: Q8Cache, q, lens, new_lens=None, row_starts=None, max_new: in
         out = (torch.empty if new_lens is None and row_starts is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
     assert out.shape == q.shape and out.is_contiguous()
     if num_splits == 0:
-        num_splits = L.oscar_q8_auto_splits(c, heads, T, max_seq_len_hint)
+        num_splits = L.oscar_q8_auto_splits(c, heads, T, max_seq_len_hint or cache.max_pages_per_seq * 128)
     ws, ws_bytes = None, 0
     if workspace is not None:
         assert workspace.is_contiguous()
