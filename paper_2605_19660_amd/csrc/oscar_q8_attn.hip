@@ -94,6 +94,11 @@ __device__ __forceinline__ f32x16 mul32_bf16(bf16x8 a, bf16x8 b, f32x16 c) {
 }
 __device__ __forceinline__ uint32_t two_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }
 
+// ONCE: past the caches.
+template <bool ONCE, typename T> __device__ __forceinline__ T fetch(const uint8_t* p) {
+  return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const T*>(p)) : *reinterpret_cast<const T*>(p);
+}
+
 // What a wave does with a step of 32 tokens, by the shape of its products.  LOGITS: of a lane; pairs of its
 // probabilities make OPERANDS operands of the value products.  keys / values: raw pages' bytes as Q8_STEP_BYTES has
 // them; window_keys: 16-bit keys at `row0`.
@@ -119,6 +124,13 @@ template <bool F16> struct Rows16 {
   static __device__ __forceinline__ void put(Logits& s, int tile, f32x4 x) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[4 * tile + i] = x[i];
+  }
+  template <bool ONCE> static __device__ __forceinline__ void load_keys(const uint8_t* step, int lane, u32x4* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fetch<ONCE, u32x4>(step + i * 1024 + lane * 16);
+  }
+  template <bool ONCE> static __device__ __forceinline__ void load_values(const uint8_t* step, int lane, u32x4* x) {
+    load_keys<ONCE>(step, lane, x);
   }
   static __device__ __forceinline__ void keys(const u32x4* k, const Op* q, Logits& s) {
 #pragma unroll
@@ -159,9 +171,8 @@ template <bool F16> struct Rows16 {
   static __device__ __forceinline__ int value_token(int lane, int, int i) { return token(lane, i); }
 };
 
-// 32 rows: lane 32 * g + n has row n and tokens 8 * (i / 4) + 4 * g + i % 4.  Rows of 16 lanes of the bytes change places
-// so that 32 tokens (32 channels) lie side by side: a page's lane 16 * q4 + n has token n of either tile, channels of
-// q4 (channel n of either half, tokens of q4).  In place: bytes that are not loaded anew would be copied else.
+// 32 rows: lane 32 * g + n has row n and tokens 8 * (i / 4) + 4 * g + i % 4.  Lanes ask for the bytes of their own token (of
+// their own channel, 8 at a time), in stretches of 256 bytes; as they lie, 24 exchanges between lanes a step take 5 % of the time.
 template <bool F16> struct Rows32 {
   using Op = typename Io<F16>::Op;
   using Acc = f32x16;
@@ -176,15 +187,23 @@ template <bool F16> struct Rows32 {
   }
   static __device__ __forceinline__ float over_lanes(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
   static __device__ __forceinline__ float sum_lanes(float x) { return x + __shfl_xor(x, 32); }
-  static __device__ __forceinline__ void keys(u32x4* k, const Op* q, Logits& s) {
+  template <bool ONCE> static __device__ __forceinline__ void load_keys(const uint8_t* step, int lane, u32x4* x) {
+    const uint8_t* in = step + (lane >> 4 & 1) * 2048 + (lane >> 5) * 512 + (lane & 15) * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fetch<ONCE, u32x4>(in + (i & 1) * 1024 + (i >> 1) * 256);   // half i % 2 of the channels
+  }
+  template <bool ONCE> static __device__ __forceinline__ void load_values(const uint8_t* step, int lane, u32x4* x) {
+    const uint8_t* in = step + (lane >> 5) * 256 + (lane & 15) * 16 + (lane >> 4 & 1) * 8;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const u32x2 a = fetch<ONCE, u32x2>(in + c * 1024), b = fetch<ONCE, u32x2>(in + c * 1024 + 512);
+      x[c] = u32x4{a[0], a[1], b[0], b[1]};
+    }
+  }
+  static __device__ __forceinline__ void keys(const u32x4* k, const Op* q, Logits& s) {
     f32x16 x = {};
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const auto two = __builtin_amdgcn_permlane16_swap(k[half][d], k[2 + half][d], false, false);
-        k[half][d] = two[0], k[2 + half][d] = two[1];   // even and odd sixteens of channels
-      }
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         const u32x4 c = k[half + kk / 2 * 2];
@@ -205,15 +224,7 @@ template <bool F16> struct Rows32 {
   static __device__ __forceinline__ bf16x8 operand(const uint32_t* pairs, int j) {
     return __builtin_bit_cast(bf16x8, u32x4{pairs[2 * j], pairs[2 * j + 1], pairs[4 + 2 * j], pairs[5 + 2 * j]});
   }
-  static __device__ __forceinline__ void values(u32x4* v, float scale, const bf16x8* hi, const bf16x8* lo, Acc* o) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const auto two = __builtin_amdgcn_permlane16_swap(v[c][t], v[c][2 + t], false, false);
-        const auto four = __builtin_amdgcn_permlane32_swap(two[0], two[1], false, false);
-        v[c][t] = four[0], v[c][2 + t] = four[1];
-      }
+  static __device__ __forceinline__ void values(const u32x4* v, float scale, const bf16x8* hi, const bf16x8* lo, Acc* o) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {   // (a sum's products lie four apart)
       bf16x8 val[4];
@@ -332,22 +343,23 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
     const int page = __builtin_amdgcn_readfirstlane(table[p]);
     return (uint32_t)page < (uint32_t)P.c.num_pages ? page : -1;
   };
-  const auto load = [&](int page, const uint8_t* codes, const float* scales, u32x4* x, float& scale) {
+  const auto load_keys = [&](int page, u32x4* x, float& scale) {
     if (page < 0) return;
     const int64_t at = (int64_t)page * P.c.heads + h;
-    const uint8_t* in = codes + at * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES + lane * 16;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u32x4* from = reinterpret_cast<const u32x4*>(in + i * 1024);
-      x[i] = ONCE ? __builtin_nontemporal_load(from) : *from;
-    }
-    scale = scales[at * per_page + wave * Q8_STEP_TOKENS / P.c.block];
+    S::template load_keys<ONCE>(P.c.k_codes + at * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES, lane, x);
+    scale = P.c.k_scales[at * per_page + wave * Q8_STEP_TOKENS / P.c.block];
+  };
+  const auto load_values = [&](int page, u32x4* x, float& scale) {
+    if (page < 0) return;
+    const int64_t at = (int64_t)page * P.c.heads + h;
+    S::template load_values<ONCE>(P.c.v_codes + at * Q8_PAGE_BYTES + wave * Q8_STEP_BYTES, lane, x);
+    scale = P.c.v_scales[at * per_page + wave * Q8_STEP_TOKENS / P.c.block];
   };
 
   int page = page_of(p0), next = page_of(p0 + 1);
   if (p0 < p1) {
-    load(page, P.c.k_codes, P.c.k_scales, k, ks);
-    load(page, P.c.v_codes, P.c.v_scales, v, vs);
+    load_keys(page, k, ks);
+    load_values(page, v, vs);
   }
 
   // the window, its steps by the last split's waves, while the first pages are on their way
@@ -402,7 +414,7 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
   typename S::Logits s = {};
   if (p0 < p1) S::keys(k, w.q, s);
   float scale = ks * P.scale_log2;
-  load(next, P.c.k_codes, P.c.k_scales, k, ks);
+  load_keys(next, k, ks);
   for (int p = p0; p < p1; ++p) {
     const int after = page_of(p + 2);
     const int t0 = p * R + wave * Q8_STEP_TOKENS;
@@ -418,8 +430,8 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
     S::keys(k, w.q, s);
     scale = ks * P.scale_log2;
     S::values(v, vs, hi, lo, w.o);
-    load(after, P.c.k_codes, P.c.k_scales, k, ks);
-    load(next, P.c.v_codes, P.c.v_scales, v, vs);
+    load_keys(after, k, ks);
+    load_values(next, v, vs);
     page = next;
     next = after;
   }
