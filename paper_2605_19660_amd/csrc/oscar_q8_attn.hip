@@ -15,11 +15,13 @@
 //
 // Up to 16 rows (a decoding step) take products of 16 x 16 x 32: the cache's bytes bound it (8 sequences of 32K: 82 us,
 // 6.6 TB/s with the start, the end and the joining launch; a plain read of as many bytes takes 80).  More rows take products of
-// 32 x 32 x 16 and are bound by issue: 220 vector instructions a step of 32 x 32 (64 conversions, 48 for limbs, 16
-// exponentials, 24 exchanges) beside 24 products of 32 clocks; vector issue is busy 69 % of the time, the matrix cores 43 %
-// (8192 rows of a kv head over themselves: 232 us).  A product keeps vector instructions out for 8 clocks whatever
+// 32 x 32 x 16 and are bound by issue: 172 vector instructions a step of 32 x 32 (64 conversions, 48 for limbs, 16
+// exponentials) beside 24 products of 32 clocks, and the two hide little of each other: over pieces of up to 500 tokens the
+// matrix cores are busy 37 % of the time and other vector instructions issued 43 % (8 sequences of 4100, 32 heads:
+// 130 us, 565 TFLOP/s of the formula's products).  A product keeps vector instructions out for 8 clocks whatever
 // its size (measured, of two waves side by side), which speaks for the larger one; two tiles of 16 x 16 x 32 took 1 .. 5 % more.
-// Three waves a SIMD instead of two (queries in LDS) spill: 261 us; four tiles of 16 rows leave one wave: 303.
+// Three waves a SIMD instead of two (queries in LDS) spill, four tiles of 16 rows leave one wave: 261 and 303 us where this
+// takes 232.  Scales through the lanes instead of scalar loads take 5 .. 25 % more.
 
 #include <algorithm>
 
@@ -278,6 +280,7 @@ template <class S> __device__ __forceinline__ void probabilities(State<S>& w, co
     const float a = __builtin_amdgcn_exp2f(fmaf(s[2 * i], scale, -w.ref)), b = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], scale, -w.ref));
     sum += a + b;
     h[i] = two_bf16(a, b);
+    asm("" : "+v"(h[i]));   // (else what is taken from it is converted once more)
     l[i] = two_bf16(a - __uint_as_float(h[i] << 16), b - __uint_as_float(h[i] & 0xffff0000u));
   }
   w.sum += sum;
