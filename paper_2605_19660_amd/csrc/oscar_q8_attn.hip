@@ -20,8 +20,8 @@
 // matrix cores are busy 37 % of the time and other vector instructions issued 43 % (8 sequences of 4100, 32 heads:
 // 130 us, 565 TFLOP/s of the formula's products).  A product keeps vector instructions out for 8 clocks whatever
 // its size (measured, of two waves side by side), which speaks for the larger one; two tiles of 16 x 16 x 32 took 1 .. 5 % more.
-// Three waves a SIMD instead of two (queries in LDS) spill, four tiles of 16 rows leave one wave: 261 and 303 us where this
-// takes 232.  Scales through the lanes instead of scalar loads take 5 .. 25 % more.
+// Three waves a SIMD instead of two (queries in LDS) spill, four tiles of 16 rows leave one wave: 261 and 303 us where two
+// took 232.  Scales through the lanes instead of scalar loads take 5 .. 25 % more.
 
 #include <algorithm>
 

@@ -91,6 +91,10 @@ CASES = [
     ([90], [2], (64, 1), 32, "f16", "f16"),
     ([200, 100], [100, 100], (1, 1), 64, "f16", "f32"),
     ([2049], [1], (3, 3), 32, "bf16", "f32"),
+    # 17 .. 32 rows, a workgroup each
+    ([300, 17, 129, 6], [6, 6, 2, 6], (8, 2), 32, "f16", "f32"),
+    ([515, 260], [2, 2], (32, 2), 64, "f16", "f16"),
+    ([1030, 31], [9, 9], (9, 3), 128, "bf16", "bf16"),
 ]
 
 
