@@ -241,7 +241,7 @@ template <bool LOGITS> __device__ __forceinline__ void sort_list(Shared& S, int 
     least = ~group_max(~least, S.wave64);
     const int shift = max(54 - __builtin_clzll((most - least) | 1), 0);   // (1024 bins)
     const float top = number_of((uint32_t)(most >> 32)), range = top - number_of((uint32_t)(least >> 32));
-    const bool logits = LOGITS && range > 0.0f;
+    const bool logits = LOGITS && range > 0.0f && range < INFINITY;
     const auto bin_of = [&](uint64_t place) {
       return logits ? (int)((top - number_of((uint32_t)(place >> 32))) / range * (BINS - 1)) : (int)((most - place) >> shift);
     };
