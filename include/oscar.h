@@ -568,6 +568,8 @@ int oscar_q8_sizes(const oscar_q8_cache *cache, oscar_q8_pool_sizes *out);
  * absolute value, scale = 2^ceil(log2(a / 448)) (2^-100 at least, 1 for a block of zeros), code = x / scale
  * rounded to the nearest e4m3 number, ties to even.  What a token becomes depends on its block's tokens only, not on how they
  * were cut into calls.  A NaN counts as 0; numbers beyond +-65504 (F16) or +-2^60 (BF16), infinities among them, as those.
+ * In an F16 cache numbers from 63488 on round to a code that stands for 65536: what oscar_q8_read and oscar_q8_attn
+ * give out of it as F16 is +-65504 there, never an infinity.
  *   k, v : device, rows of n_kv_heads vectors of 128 channels of io_dtype, k_stride (v_stride) elements apart;
  *          16-byte aligned, strides multiples of 8
  * Tokens whose page is no page, or behind the table's end, are not kept.  One launch. */
@@ -600,7 +602,7 @@ int oscar_q8_attn(const void *q, int64_t q_stride, int64_t n_rows, int32_t n_q_h
  * rest from the window.
  *   lens   : device int32 [batch];  starts: device int32 [batch] or NULL = 0; may be negative
  *   k, v   : device, [batch][T][n_kv_heads][128] of out_dtype (any of the three), 16-byte aligned; either may
- *            be NULL
+ *            be NULL.  (Numbers of a BF16 cache beyond fp16's are infinities as F16.)
  * Rows of tokens that a sequence does not hold (before 0, from lens[b] on, in a page that is no page) are left
  * as they were.  One launch. */
 int oscar_q8_read(const oscar_q8_cache *cache, const int32_t *lens, const int32_t *starts, int32_t T, void *k,

@@ -227,7 +227,11 @@ constexpr int ROW_PITCH = D + 16;   // bytes of a row in LDS: 16-byte pieces of 
 template <typename O> constexpr int LANE_NUMBERS = 16 / sizeof(O);
 // (32-bit rows past the caches: 65536 tokens of 8 kv heads read 130 -> 111 us, read and then added up 284 -> 263; 16-bit rows
 // gain as much alone and lose it again where the next launch uses them: 64 us, 65 past the caches)
-template <typename O> __device__ __forceinline__ void put(O* to, const float* x) {
+// fp16 tokens from 63488 on are codes of 65536 (256 * 256): as fp16 they go out as its largest number, no infinity.
+template <typename E, typename O> __device__ __forceinline__ void put(O* to, float* x) {
+  if constexpr (__is_same(E, __half) && __is_same(O, __half))
+#pragma unroll
+    for (int i = 0; i < LANE_NUMBERS<O>; ++i) x[i] = __builtin_amdgcn_fmed3f(x[i], -65504.0f, 65504.0f);
   if constexpr (sizeof(O) == 4)
     __builtin_nontemporal_store(u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])},
                                 reinterpret_cast<u32x4*>(to));
@@ -313,7 +317,7 @@ template <typename E, typename O> __global__ __launch_bounds__(256) void oscar_q
         for (int j = 0; j < 2; ++j) x[4 * d + 2 * j] = widen<E>(w[j] & 0xffff), x[4 * d + 2 * j + 1] = widen<E>(w[j] >> 16);
       }
     }
-    put<O>(out + (((int64_t)b * P.T + (pos - start)) * P.c.heads + h) * D + c, x);
+    put<E>(out + (((int64_t)b * P.T + (pos - start)) * P.c.heads + h) * D + c, x);
   }
 }
 

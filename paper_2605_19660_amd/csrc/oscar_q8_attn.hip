@@ -94,6 +94,10 @@ __device__ __forceinline__ f32x4 mul_bf16(bf16x8 a, bf16x8 b, f32x4 c) {
 __device__ __forceinline__ f32x16 mul32_bf16(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+// An output as the io type holds it: values of an fp16 cache are up to 65536, which goes out as the largest fp16 number.
+template <bool F16> __device__ __forceinline__ float io_number(float x) {
+  return F16 ? __builtin_amdgcn_fmed3f(x, -65504.0f, 65504.0f) : x;
+}
 __device__ __forceinline__ uint32_t two_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }
 
 // ONCE: past the caches.
@@ -482,7 +486,7 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
         } else {
           Op y;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = x[e];
+          for (int e = 0; e < 8; ++e) y[e] = io_number<F16>(x[e]);
           *reinterpret_cast<Op*>(reinterpret_cast<uint16_t*>(P.out) + to) = y;
         }
       } else {
@@ -589,7 +593,7 @@ template <bool F16> __global__ __launch_bounds__(256) void oscar_q8_join_kernel(
   if (P.out_f32) {
     *reinterpret_cast<float2*>(reinterpret_cast<float*>(P.out) + to) = make_float2(x, y);
   } else if constexpr (F16) {
-    *reinterpret_cast<f16x2*>(reinterpret_cast<uint16_t*>(P.out) + to) = f16x2{(_Float16)x, (_Float16)y};
+    *reinterpret_cast<f16x2*>(reinterpret_cast<uint16_t*>(P.out) + to) = f16x2{(_Float16)io_number<F16>(x), (_Float16)io_number<F16>(y)};
   } else {
     *reinterpret_cast<bf16x2*>(reinterpret_cast<uint16_t*>(P.out) + to) = bf16x2{(__bf16)x, (__bf16)y};
   }

@@ -214,3 +214,30 @@ def test_a_pool_past_4_gib():
         for h in range(H):
             assert np.array_equal(got[0, :, h].double().cpu().numpy(), stands_for(y[0, :, h], 32, "bf16")[0])
     assert bool(c.k_codes[1:pages - 2].any()) is False and bool(c.v_codes[1:pages - 2].any()) is False
+
+
+def test_the_largest_fp16_numbers_come_back_finite():
+    """A block of an fp16 cache with numbers from 63488 on holds 65536 for them, which is no fp16 number: read as fp16 they are
+    65504, as bf16 and fp32 what the codes say; infinities the same way."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(21)
+    x = [tokens(rng, 2, 70, 2, "f16") for _ in "kv"]
+    for y in x:
+        y[0, :, 0, ::5] = rng.choice([65504.0, -65504.0, 63488.0, -63488.0, 63456.0, -63456.0, 61440.0], size=y[0, :, 0, ::5].shape)
+        y[1, [3, 40, 66], 1, 9], y[1, [4, 50, 67], 1, 10] = np.inf, -np.inf
+    c = scattered_cache(ob, 2, 2, 1, 32, "f16", rng)
+    append(ob, c, x, [0, 0], [70, 68], "f16")
+    check(ob, c, x, [70, 68], "f16")
+    for out in ("f16", "bf16", "f32"):
+        k, v = (torch.full((2, 70, 2, D), 3.0, dtype=torch_type(out), device="cuda") for _ in "kv")
+        ob.q8_read(c, ints([70, 68]), k=k, v=v)
+        for y, got in zip(x, (k, v)):
+            want = np.full((2, 70, 2, D), 3.0)
+            for b, n in enumerate([70, 68]):
+                for h in range(2):
+                    want[b, :n, h] = stands_for(y[b, :n, h], 32, "f16")[0]
+            assert (np.abs(want) == 65536.0).any() and (np.abs(want) == 65504.0).any()
+            if out == "f16":
+                want = np.clip(want, -65504.0, 65504.0)
+            assert torch.equal(got.cpu(), torch.from_numpy(want).to(torch_type(out))), out

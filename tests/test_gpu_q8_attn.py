@@ -357,3 +357,29 @@ def test_captured_and_replayed_over_growing_lengths():
         want = ob.q8_attn(a, q, lens, num_splits=3)
         assert torch.equal(out, want), i
     compare([out[j].double().cpu().numpy() for j in range(B)], attention(q.double().cpu().numpy(), x, list(n), [1] * B, 32, "bf16", "bf16"))
+
+
+@pytest.mark.parametrize("heads", [(2, 1), (20, 1)])
+def test_the_largest_fp16_numbers_stay_finite(heads):
+    """Values of an fp16 cache whose codes stand for 65536: an output that is one of them, or nearly, is 65504 as fp16."""
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(22)
+    lens, new = [64, 40, 33], [1, 2, 1]
+    x = [tokens(rng, 3, 64, 1, "f16") for _ in "kv"]
+    x[1][0, :, 0, :4] = [65504.0, -65504.0, 63488.0, np.inf]      # every token has it
+    x[1][1, 7, 0, :2] = 65504.0, -np.inf                          # one that takes the softmax
+    x[1][2, :, 0, :2] = 63488.0, -63488.0
+    q = tokens(rng, 3, 2, heads[0], "f16")
+    x[0][1, :, 0] = 0.01 * rng.integers(-3, 4, size=(64, D))
+    x[0][1, 7, 0] = 4.0 * np.sign(q[1, 0, 0])
+    q[1, :] = q[1, 0, 0]
+    x = [dev(y, "f16").double().cpu().numpy() for y in x]
+    c = scattered_cache(ob, 1, 3, 1, 32, "f16", rng)
+    append(ob, c, x, [0] * 3, lens, "f16")
+    for out in ("f16", "f32"):
+        want = attention(q, x, lens, new, 32, "f16", out)
+        assert max(np.abs(o).max() for o, _ in want) > 65520.0     # (what rounds to infinity)
+        if out == "f16":
+            want = [(np.clip(o, -65504.0, 65504.0), tol) for o, tol in want]
+        for splits in (1, 2):
+            compare(run(ob, c, q, lens, new, "f16", out, num_splits=splits), want)
