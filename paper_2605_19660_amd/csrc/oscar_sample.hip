@@ -53,7 +53,7 @@ enum { ONE_TOKEN, NO_TOKEN, BY_CUT, DONE };
 struct SampleParams {
   const void* logits;
   int64_t stride;
-  int V, fixed;        // vocabulary; binary places of a weight in sums over a row
+  int V;               // vocabulary
   int chunks, chunk;   // of a row, and their size
   const float *temperature, *top_p, *min_p, *u;
   const int32_t* top_k;
@@ -296,35 +296,55 @@ template <typename E> struct Row {
   const E* x;
   int V;
   double top, scale;   // scale: log2(e) / temperature
-  int fixed;
   const double* powers;
   __device__ __forceinline__ uint32_t key(int i) const { return key_of(to_f32<E>(x[i])); }
   __device__ __forceinline__ double weight(uint32_t k) const { return power_of_2<0>(((double)number_of(k) - top) * scale, powers); }
-  __device__ __forceinline__ uint64_t whole(double w) const { return (uint64_t)(w * (double)(1ull << fixed) + 0.5); }
 };
+
+// Weights of a whole row are added up in two whole numbers, of multiples of 2^-40 and of what is left in multiples of 2^-80
+// (2^22 of either stay below 2^63): millions of tokens of 2^-42 beside one of 1 are not lost.
+__device__ __forceinline__ void split_weight(double w, uint64_t& high, uint64_t& low) {
+  const double x = w * 0x1p40, whole = floor(x);
+  high = whole_of(whole), low = whole_of((x - whole) * 0x1p40);
+}
+__device__ __forceinline__ double joined_weight(uint64_t high, uint64_t low) { return (double)high * 0x1p-40 + (double)low * 0x1p-80; }
 
 // How far a search has come: the cut lies among the places from `from` on whose keys are within lo .. hi, and
 // `above` (tokens or weight) lies over them.
 struct Search {
   bool by_weight;
-  double target;      // tokens or (whole) weight to reach
+  double target;      // tokens or weight to reach
   uint64_t from;      // the cut so far
 };
 
+// What a search has in bin t: tokens, or their weight.  The weights' lower parts lie where the list is not yet.
+__device__ __forceinline__ double in_bin_of(const Shared& S, const Search& q, int t) {
+  return q.by_weight ? joined_weight(S.mass[t], S.list[t]) : (double)S.count[t];
+}
+__device__ __forceinline__ void clear_bins(Shared& S) {
+  S.mass[threadIdx.x] = 0, S.list[threadIdx.x] = 0, S.count[threadIdx.x] = 0;
+}
+__device__ __forceinline__ void add_to_bin(Shared& S, int bin, double w) {
+  uint64_t high, low;
+  split_weight(w, high, low);
+  atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[bin]), (unsigned long long)high);
+  atomicAdd(reinterpret_cast<unsigned long long*>(&S.list[bin]), (unsigned long long)low);
+}
+
 // The bin that holds the cut: the first whose running sum reaches the target; above: the sum before it.
-__device__ __forceinline__ int find_bin(Shared& S, const Search& q, uint64_t& above, uint32_t& in_bin) {
+__device__ __forceinline__ int find_bin(Shared& S, const Search& q, double& above, uint32_t& in_bin) {
   const int t = threadIdx.x;
-  const uint64_t v = q.by_weight ? S.mass[t] : S.count[t];
-  uint64_t all;
-  const uint64_t upto = above + group_scan(v, S.wave64, &all);
+  const double v = in_bin_of(S, q, t);
+  double all;
+  const double upto = above + group_scan(v, S.wave_f, &all);
   if (t == 0) S.found = BINS - 1;
   __syncthreads();
-  first_thread(&S.found, (double)upto >= q.target && S.count[t] > 0);
+  first_thread(&S.found, upto >= q.target && S.count[t] > 0);
   __syncthreads();
   const int bin = S.found;
-  if (t == bin) S.hit = upto - v;
+  if (t == bin) S.hit = __builtin_bit_cast(uint64_t, upto - v);
   __syncthreads();
-  above = S.hit;
+  above = __builtin_bit_cast(double, S.hit);
   in_bin = S.count[bin];
   __syncthreads();
   return bin;
@@ -340,34 +360,38 @@ __device__ void search_cut(Shared& S, const Row<E>& row, Search& q, double share
   if (q.by_weight) range = fminf(range, (float)(65.0 / row.scale));   // (less is less than 2^-64 of the largest)
   const float steps = range > 0.0f ? BINS / range : 0.0f;
   const auto bin_of = [&](uint32_t key) { return (int)fminf((top - number_of(key)) * steps, (float)(BINS - 1)); };
-  S.mass[t] = 0, S.count[t] = 0;
+  clear_bins(S);
   __syncthreads();
   // (the last bin holds all that is far below: it is added up in registers)
-  uint64_t far_mass = 0;
+  uint64_t far_high = 0, far_low = 0;
   uint32_t far_count = 0;
 #pragma unroll 4
   for (int i = t; i < row.V; i += THREADS) {
     const uint32_t key = row.key(i);
     if (key <= DEAD || place_of(key, i) < q.from) continue;
     const int bin = bin_of(key);
-    const uint64_t m = q.by_weight ? row.whole(row.weight(key)) : 0;
     if (bin == BINS - 1) {
-      far_mass += m;
+      if (q.by_weight) {
+        uint64_t high, low;
+        split_weight(row.weight(key), high, low);
+        far_high += high, far_low += low;
+      }
       ++far_count;
     } else {
-      if (q.by_weight) atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[bin]), (unsigned long long)m);
+      if (q.by_weight) add_to_bin(S, bin, row.weight(key));
       atomicAdd(&S.count[bin], 1u);
     }
   }
-  add_from_wave(&S.mass[BINS - 1], far_mass);
+  add_from_wave(&S.mass[BINS - 1], far_high);
+  add_from_wave(&S.list[BINS - 1], far_low);
   far_count = (uint32_t)wave_scan((uint64_t)far_count);
   if ((t & 63) == 63 && far_count) atomicAdd(&S.count[BINS - 1], far_count);
   __syncthreads();
-  uint64_t all;
-  group_scan(q.by_weight ? S.mass[t] : (uint64_t)S.count[t], S.wave64, &all);
-  if (q.by_weight) q.target = share * (double)all;
-  else if (q.target >= (double)all) return;   // (everything stays)
-  uint64_t above = 0;
+  double all;
+  group_scan(in_bin_of(S, q, t), S.wave_f, &all);
+  if (q.by_weight) q.target = share * all;
+  else if (q.target >= all) return;   // (everything stays)
+  double above = 0.0;
   uint32_t in_bin;
   const int bin = find_bin(S, q, above, in_bin);
 
@@ -390,13 +414,13 @@ __device__ void search_cut(Shared& S, const Row<E>& row, Search& q, double share
     int shift = 0;
     while ((hi - lo) >> shift >= BINS) ++shift;
     __syncthreads();
-    S.mass[t] = 0, S.count[t] = 0;
+    clear_bins(S);
     __syncthreads();
     for (int i = t; i < row.V; i += THREADS) {
       const uint32_t key = row.key(i);
       if (key < lo || key > hi || key <= DEAD || place_of(key, i) < q.from) continue;
       const int b = (hi - key) >> shift;
-      if (q.by_weight) atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[b]), (unsigned long long)row.whole(row.weight(key)));
+      if (q.by_weight) add_to_bin(S, b, row.weight(key));
       atomicAdd(&S.count[b], 1u);
     }
     __syncthreads();
@@ -409,8 +433,8 @@ __device__ void search_cut(Shared& S, const Row<E>& row, Search& q, double share
 
   if (in_bin > CAP) {
     // one number, many times: the cut is the r-th of them in order of their index
-    const uint64_t m = q.by_weight ? row.whole(row.weight(hi)) : 1;
-    const double r_exact = m ? ceil((q.target - (double)above) / (double)m) : (double)in_bin;
+    const double m = q.by_weight ? row.weight(hi) : 1.0;
+    const double r_exact = m > 0.0 ? ceil((q.target - above) / m) : (double)in_bin;
     const uint32_t r = (uint32_t)fmin(fmax(r_exact, 1.0), (double)in_bin);
     // in pieces of the row, one a wave at a time
     uint32_t before = 0;
@@ -456,14 +480,14 @@ __device__ void search_cut(Shared& S, const Row<E>& row, Search& q, double share
   const int n = min((int)S.n, CAP);
   sort_list<true>(S, n);
   if (t == 0) S.hit = 0;
-  uint64_t before = above;
+  double before = above;
   for (int i0 = 0; i0 < n; i0 += THREADS) {
     const int i = i0 + t;
-    const uint64_t m = i >= n ? 0 : q.by_weight ? row.whole(row.weight((uint32_t)(S.list[i] >> 32))) : 1;
-    uint64_t here;
-    const uint64_t upto = before + group_scan(m, S.wave64, &here);
+    const double m = i >= n ? 0.0 : q.by_weight ? row.weight((uint32_t)(S.list[i] >> 32)) : 1.0;
+    double here;
+    const double upto = before + group_scan(m, S.wave_f, &here);
     // stays if what is before it does not reach the target; the very first stays anyway
-    const bool stays = i < n && ((double)(upto - m) < q.target || (i == 0 && above == 0));
+    const bool stays = i < n && (upto - m < q.target || (i == 0 && above == 0.0));
     const uint64_t last = group_max(stays ? ~S.list[i] : 0, S.wave64);   // the lowest place that stays
     if (last) q.from = ~last;
     before += here;
@@ -817,7 +841,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
     return;
   }
   const float top = number_of(top_key);
-  Row<E> row = {reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride, V, (double)top, 1.4426950408889634 / (double)s.temp, P.fixed, s_power};
+  Row<E> row = {reinterpret_cast<const E*>(P.logits) + (int64_t)b * P.stride, V, (double)top, 1.4426950408889634 / (double)s.temp, s_power};
   const bool listed = s.by_count || s.cuts;
   int n = listed ? (int)min(r.n, (uint32_t)CAP + 1) : 0;
   if (s.whole || !on_grid(top, s.grid, ROW_GRID) || n > CAP) {
@@ -1069,8 +1093,6 @@ extern "C" int oscar_sample(const void* logits, int64_t row_stride, int32_t batc
   P.logits = logits;
   P.stride = row_stride;
   P.V = vocab;
-  P.fixed = 62;
-  while ((int64_t)1 << (62 - P.fixed) < vocab) --P.fixed;
   P.chunk = chunk_of(batch, vocab);
   P.chunks = (vocab + P.chunk - 1) / P.chunk;
   P.temperature = temperature;

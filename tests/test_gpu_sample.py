@@ -225,3 +225,32 @@ def test_long_lists_of_every_kind():
     check(x, k=5000, p=0.9)
     check(x, p=0.02)
     check(x, m=0.97, temp=2.0)
+
+
+@pytest.mark.parametrize("levels", [1, 1000, 3000])
+def test_many_small_weights_beside_a_large_one(levels):
+    """2^22 tokens of which all but one weigh 2.5e-13: a top_p that needs hundreds of thousands of them.  They are too many
+    for a list, and their sum is 1e-6 of the one that is large."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    V = 1 << 22
+    x = (-29.0 - (np.arange(V) * 7919 % levels) * np.spacing(np.float32(29))).astype(np.float32)
+    x[V - 1] = 0.0
+    p, u = np.float32(0.999999), np.float32(2e-8)
+    # sums of up to 2^22 numbers in 64 bits of mantissa: 2^-41 of the sum, 2 of the small ones
+    w = np.exp(x.astype(np.longdouble))
+    order = np.argsort(-x, kind="stable")
+    before = np.concatenate([[0], np.cumsum(w[order])[:-1]])
+    n = int((before < np.longdouble(p) * w.sum()).sum())
+    assert 100_000 < n < 400_000
+    token, probs = ob.sample(torch.from_numpy(x)[None].cuda(), torch.tensor([u]).cuda(), top_p=torch.tensor([p]).cuda(), probs=True)
+    stays = probs[0].cpu().numpy() > 0
+    assert abs(int(stays.sum()) - n) <= 4, (int(stays.sum()), n)
+    # the largest n, equal ones by index, whatever n came out as
+    mine = np.sort(order[:int(stays.sum())])
+    assert np.array_equal(np.nonzero(stays)[0], mine)
+    cum = np.cumsum(w[mine])
+    assert abs(int(np.searchsorted(mine, int(token))) - int((cum <= np.longdouble(u) * cum[-1]).sum())) <= 4
+    want = (w[mine] / cum[-1]).astype(np.float64)
+    got = probs[0].double().cpu().numpy()[mine]
+    assert (np.abs(got - want) <= want * (2.0 ** -24 + 1e-11)).all()
