@@ -620,7 +620,7 @@ int oscar_q8_read(const oscar_q8_cache *cache, const int32_t *lens, const int32_
  * never drawn; +inf as the largest fp32.  A row without a number above -inf gives token 0 and no probability.
  *   logits : device, rows of vocab numbers of dtype (F32|BF16|F16), row_stride elements apart
  *   temperature, top_p, min_p : device fp32 [batch] or NULL (1, 1, 0);  top_k: device int32 [batch] or NULL
- *   u      : device fp32 [batch], in [0, 1)
+ *   u      : device fp32 [batch], in [0, 1) (below 0 and a NaN count as 0; 1 and more draw the last token that stays)
  *   tokens : device int32 [batch]
  *   probs  : device fp32 [batch][vocab], or NULL: what each token was drawn with (0 for those that do not
  *            stay), as oscar_verify_drafts takes it; overlaps nothing else

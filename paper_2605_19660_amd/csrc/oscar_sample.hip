@@ -970,7 +970,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
   __syncthreads();
   const int c = S.found < P.chunks ? S.found : (int)S.n;   // (if rounding lets none pass: the last with any weight)
   if (t == c) S.hit = __builtin_bit_cast(uint64_t, upto - share);
-  if (t == 0) R.kind = BY_CUT, R.cut = cut, R.sum = sum, S.n = 0;
+  if (t == 0) R.kind = BY_CUT, R.cut = cut, R.sum = sum;
   __syncthreads();
   // the token: a wave takes a part of the chunk in one piece, 64 logits at a time
   const int lane = t & 63, wave = t >> 6, i0 = c * (PER * THREADS) + wave * (PER * 64) + lane;

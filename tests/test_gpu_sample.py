@@ -254,3 +254,23 @@ def test_many_small_weights_beside_a_large_one(levels):
     want = (w[mine] / cum[-1]).astype(np.float64)
     got = probs[0].double().cpu().numpy()[mine]
     assert (np.abs(got - want) <= want * (2.0 ** -24 + 1e-11)).all()
+
+
+def test_a_number_of_1_and_more_draws_the_last_that_stays():
+    """Every way a row is drawn: no filter, a list by tokens and by weights, rows that one workgroup searches."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(31)
+    for B, V in ((1, 50), (4, 9001), (3, 128003)):
+        x = logits(rng, B, V)
+        x[0, V - 3:] = -np.inf
+        for kw in (dict(), dict(k=40), dict(p=0.9), dict(m=0.02), dict(p=0.95, m=1e-3), dict(k=2000, p=0.9), dict(temp=1e-9, p=0.9)):
+            f = {n: np.broadcast_to(np.asarray(a, np.int32 if n == "k" else np.float32), (B,)) for n, a in kw.items()}
+            g = lambda n, none: f.get(n, np.full(B, none)).astype(np.float64)
+            _, probs = rule(x.astype(np.float32).astype(np.float64), g("temp", 1.0), f.get("k", np.zeros(B, int)), g("p", 1.0), g("m", 0.0), np.zeros(B))
+            want = [int(np.nonzero(r)[0][-1]) for r in probs]
+            names = dict(temp="temperature", k="top_k", p="top_p", m="min_p")
+            args = {names[n]: torch.from_numpy(a.copy()).cuda() for n, a in f.items()}
+            for u in (1.0, 2.5, np.inf):
+                token, _ = ob.sample(torch.from_numpy(x).float().cuda(), torch.full((B,), u, device="cuda"), **args)
+                assert token.tolist() == want, (B, V, kw, u)
