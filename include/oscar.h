@@ -504,6 +504,7 @@ int oscar_verify_drafts(const void *target, const void *draft, const int32_t *dr
  *     n_rows.  Otherwise it waits with what it keeps: nobody behind takes the pages it waits for
  *   - pages are handed out from the top of the stack, in order of sequence and page, into block_table
  *   lens, want  : device int32 [batch] (below 0 counts as 0); keep: the same, or NULL
+ *                 (how many tokens a cache can give up is the cache's matter: see oscar_q8_cache)
  *   block_table : device int32 [batch][max_pages_per_seq], changed in place
  *   free_pages  : device int32 [num_pages], the stack, changed in place; n_free: device int32 [1], its height.
  *                 Every page is in the stack or in one sequence's part of the table, once
@@ -536,8 +537,13 @@ int oscar_plan_step(const int32_t *lens, const int32_t *keep, const int32_t *wan
  *   window : [sequence][kv head][2 * block][128] of io_dtype, position p at p mod 2 * block
  * Of a sequence of n tokens the first n / block * block (whole blocks) are codes in pages, the rest are in the window.
  * The window also holds the 16-bit form of the last whole block (of those of its tokens that came through
- * oscar_q8_append): a length may be taken back by up to `block` tokens, to as little as n / block * block -
- * block, simply by saying so in the next call (drafted tokens that do not stand). */
+ * oscar_q8_append), so that a length may be taken back, simply by saying so in the next call (drafted tokens that do not
+ * stand).  How far: a place of the window is lost to the token 2 * block further on, so what counts is not the length
+ * at hand but the longest one.  With f = 0 to begin with, and after every append that ends at a length n
+ *   f = max(f, n / block * block - block),
+ * a length may go to f and anything above, as often as one likes.  Below f only to a multiple of block, whose tokens are all
+ * codes (in pages that are still the sequence's; 0: another sequence begins); f is then that length.  At any other length below f the
+ * window has later tokens in the places of the sequence's, and no call can see that. */
 typedef struct oscar_q8_cache {
   int32_t batch, max_pages_per_seq, num_pages;
   int32_t n_kv_heads;

@@ -790,7 +790,8 @@ def plan_step(lens, want, block_table, free_pages, n_free, n_rows: int, keep=Non
               new_lens=None, n_free_out=None, row_starts=None, positions=None, row_seq=None, slots=None, stream=None) -> StepPlan:
     """oscar_plan_step: lens, want, keep int32 [batch]; block_table int32 [batch, max_pages] and free_pages int32
     [num_pages] are changed in place, n_free int32 [1] is the stack's height.  The outputs are made where they are not
-    given (lens_out=lens, new_lens=want, n_free_out=n_free: in place)."""
+    given (lens_out=lens, new_lens=want, n_free_out=n_free: in place).  keep below lens gives up tokens: a Q8Cache says how many
+    it can."""
     if stream is not None:
         import torch
         with torch.cuda.stream(stream):
@@ -827,7 +828,9 @@ class Q8Cache:
     """Device pools of one paged 8-bit cache (oscar_q8_cache), allocated through torch.
 
     block_table defaults to sequence-major identity; pass a device int32 tensor [batch, max_pages_per_seq] to share one
-    between layers or with plan_step.  Lengths are the caller's: the calls take them."""
+    between layers or with plan_step.  Lengths are the caller's: the calls take them.  They may go back, to f and above: f is the
+    largest n // block * block - block of the lengths n that appends ended at; or to a multiple of block below, from which f counts
+    anew.  At other lengths the window would give later tokens for the sequence's own (see oscar_q8_cache)."""
 
     def __init__(self, n_kv_heads: int, batch: int, max_pages_per_seq: int, block: int = 32, io_dtype: int = BF16,
                  device="cuda", num_pages: int | None = None, block_table=None):

@@ -241,3 +241,42 @@ def test_the_largest_fp16_numbers_come_back_finite():
             if out == "f16":
                 want = np.clip(want, -65504.0, 65504.0)
             assert torch.equal(got.cpu(), torch.from_numpy(want).to(torch_type(out))), out
+
+
+@pytest.mark.parametrize("block", [32, 64, 128])
+def test_lengths_taken_back_again_and_again(block):
+    """Lengths that go back and forth as far as the cache allows: to f and above, f = n / block * block - block of the
+    longest append that ended at n, or to a multiple of block below, which f is then.  After every change what is read is
+    what a cache of that length holds."""
+    import torch
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(100 + block)
+    B, H, most = 6, 2, 7 * block
+    x = [tokens(rng, B, most, H, "bf16") for _ in "kv"]
+    c = scattered_cache(ob, H, B, most // 128 + 1, block, "bf16", rng)
+    n, f = np.zeros(B, int), np.zeros(B, int)
+
+    def holds():
+        k, v = (torch.zeros(B, most, H, D, device="cuda") for _ in "kv")
+        ob.q8_read(c, ints(n), k=k, v=v)
+        for y, got in zip(x, (k, v)):
+            got = got.double().cpu().numpy()
+            for b in range(B):
+                for h in range(H):
+                    assert np.array_equal(got[b, :n[b], h], stands_for(y[b, :n[b], h], block, "bf16")[0]), (b, n[b], f[b])
+
+    for i in range(60):
+        new = np.array([min(most - n[b], int(rng.choice([0, 1, 2, 7, block // 2, block, block + 3, 3 * block]))) for b in range(B)])
+        append(ob, c, x, n, new, "bf16", packed=i % 2 == 1)
+        n += new
+        f = np.maximum(f, np.where(new > 0, n // block * block - block, 0))
+        holds()
+        for b in range(B):
+            r = rng.random()
+            if r < 0.2:
+                n[b] = f[b] = int(rng.integers(0, f[b] // block + 1)) * block     # a multiple of block, below f or f
+            elif r < 0.7:
+                n[b] = int(rng.choice([f[b], rng.integers(f[b], n[b] + 1)]))
+            for y in x:                                                          # other tokens come instead
+                y[b, n[b]:] = tokens(rng, 1, most, H, "bf16")[0, n[b]:]
+        holds()
