@@ -403,7 +403,7 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const uint16_t x = *reinterpret_cast<const uint16_t*>(tile_v + S::value_token(lane, j, i) * V_PITCH + 2 * S::value_channel(lane, c));
-            if constexpr (F16) {   // 11 bits in two limbs
+            if constexpr (F16) {   // 11 bits in two limbs, each by both of the probabilities'
               const float f = (float)__builtin_bit_cast(_Float16, x);
               val[i] = (__bf16)f;
               rest[i] = (__bf16)(f - (float)val[i]);
@@ -412,7 +412,7 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
             }
           }
           w.o[c] = S::mul(val, lo[j], S::mul(val, hi[j], w.o[c]));
-          if constexpr (F16) w.o[c] = S::mul(rest, hi[j], w.o[c]);
+          if constexpr (F16) w.o[c] = S::mul(rest, lo[j], S::mul(rest, hi[j], w.o[c]));
         }
       wave_fence();
     }

@@ -383,3 +383,25 @@ def test_the_largest_fp16_numbers_stay_finite(heads):
             want = [(np.clip(o, -65504.0, 65504.0), tol) for o, tol in want]
         for splits in (1, 2):
             compare(run(ob, c, q, lens, new, "f16", out, num_splits=splits), want)
+
+
+@pytest.mark.parametrize("rows", [1, 20])
+def test_fp16_values_of_the_window_enter_as_they_are(rows):
+    """A token of logit 0 and 30 of one weight just above 1/2, with a value whose last three bits the products take apart.
+
+    The weight w = (1 + 2^-9 (1 - 2^-7)) / 2 is two bf16 limbs exactly, 1/2 and 2^-10 (1 - 2^-7); the computed one is within 2^-22 (the
+    exponential) and 2^-23 (scale and logit, each rounded) of it, less than half a step (2^-19) of the lower limb, so that the limbs are
+    the exact ones and only their sum is off by as much.  A product adds 32 numbers, 2^-24 each at worst; the sum of the
+    weights and the division take 12 steps.  Without the lower limbs' product with the value's last bits, 3 2^-10, the output is
+    too small by 2^-9 3 2^-10 = 2^-17.4 of itself."""
+    from paper_2605_19660_amd import binding as ob
+    w, value = (1.0 + 2.0 ** -9 * (1.0 - 2.0 ** -7)) / 2.0, 1.0 + 3.0 * 2.0 ** -10
+    x = [np.zeros((1, 31, 1, D)) for _ in "kv"]
+    x[0][0, 1:, 0, 0], x[1][0, 1:, 0] = -1.0, value
+    q = np.zeros((1, 1, rows, D))
+    q[..., 0] = 1.0
+    c = scattered_cache(ob, 1, 1, 1, 32, "f16", np.random.default_rng(0))
+    append(ob, c, x, [0], [31], "f16")
+    got = run(ob, c, q, [31], [1], "f16", "f32", scale=-np.log(w))[0][0]
+    off = np.abs(got / (30 * w * value / (30 * w + 1.0)) - 1.0)
+    assert (off <= (32 + 12) * 2.0 ** -24 + 1.5 * 2.0 ** -22).all(), float(off.max())
