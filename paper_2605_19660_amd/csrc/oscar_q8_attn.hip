@@ -345,6 +345,8 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
 
   u32x4 k[4] = {}, v[4] = {};
   float ks = 1.0f, vs = 1.0f;
+  // (no less than the smallest number: hidden logits times 0 are none)
+  const auto logit_scale = [&](float block) { return fmaxf(block * P.scale_log2, 0x1p-126f); };
   const auto page_of = [&](int p) -> int {
     if (p >= p1 || p * R + wave * Q8_STEP_TOKENS >= end) return -1;
     const int page = __builtin_amdgcn_readfirstlane(table[p]);
@@ -420,7 +422,7 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
 
   typename S::Logits s = {};
   if (p0 < p1) S::keys(k, w.q, s);
-  float scale = ks * P.scale_log2;
+  float scale = logit_scale(ks);
   load_keys(next, k, ks);
   for (int p = p0; p < p1; ++p) {
     const int after = page_of(p + 2);
@@ -435,7 +437,7 @@ __device__ __forceinline__ void attend(const AttnParams& P, const Q8Seq& seq, in
     bf16x8 hi[S::OPERANDS], lo[S::OPERANDS];
     probabilities(w, s, scale, hi, lo);
     S::keys(k, w.q, s);
-    scale = ks * P.scale_log2;
+    scale = logit_scale(ks);
     S::values(v, vs, hi, lo, w.o);
     load_keys(after, k, ks);
     load_values(next, v, vs);

@@ -405,3 +405,20 @@ def test_fp16_values_of_the_window_enter_as_they_are(rows):
     got = run(ob, c, q, [31], [1], "f16", "f32", scale=-np.log(w))[0][0]
     off = np.abs(got / (30 * w * value / (30 * w + 1.0)) - 1.0)
     assert (off <= (32 + 12) * 2.0 ** -24 + 1.5 * 2.0 ** -22).all(), float(off.max())
+
+
+def test_a_scale_below_the_smallest_number():
+    """Keys of 2^-105 in blocks of scale 2^-100, and a softmax_scale of 2^-70: the scale of their logits is below every fp32 number, and
+    all tokens weigh the same, those that a row does not see nothing."""
+    from paper_2605_19660_amd import binding as ob
+    rng = np.random.default_rng(23)
+    lens, new = [64, 200], [9, 33]
+    x = [tokens(rng, 2, 200, 1, "bf16") for _ in "kv"]
+    x[0][...] = 2.0 ** -105 * rng.choice([1.0, -1.0], size=x[0].shape)
+    q = tokens(rng, 2, 33, 2, "bf16")
+    c = scattered_cache(ob, 1, 2, 2, 32, "bf16", rng)
+    append(ob, c, x, [0, 0], lens, "bf16")
+    for scale in (2.0 ** -70, 1e-40):
+        want = attention(q, x, lens, new, 32, "bf16", "f32", scale=scale)
+        for splits in (1, 2):
+            compare(run(ob, c, q, lens, new, "bf16", "f32", num_splits=splits, scale=scale), want)
