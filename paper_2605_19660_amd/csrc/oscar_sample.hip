@@ -889,7 +889,12 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
 
   place_chunk(s, chunk_best, top, t < P.chunks, G);
   const int lo = listed ? r.lo : BINS;
-  S.mass[t] = 0;   // the list's share of every chunk
+  // The list's share of every chunk.  min_p alone lets tokens of any weight stay, and what they have below 2^-LIST_BITS is added up by
+  // itself, in multiples of 2^(-2 LIST_BITS) and no less than one; with top_p they weigh 2^-46 of the largest and more (one of less
+  // and all behind it would be less than 2^-24 of the row).
+  uint64_t* rest = reinterpret_cast<uint64_t*>(S.part);
+  const bool any_weight = !(s.p < 1.0f);
+  S.mass[t] = 0, rest[t] = 0;
   __syncthreads();
   if (listed) {
     double above = r.above;
@@ -949,9 +954,13 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
       const bool stays = i < n && ((from_top && i == 0) || ((!(s.p < 1.0f) || before < target) && !(w < (double)s.m)));
       const int left = __syncthreads_count(stays);   // (the first so many: weights fall)
       if (left) cut = S.list[i0 + left - 1];
-      if (stays)
-        atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[(int)~(uint32_t)at / P.chunk]),
-                  (unsigned long long)whole_of(w * (double)(1ull << LIST_BITS)));
+      if (stays) {
+        const int c = (int)~(uint32_t)at / P.chunk;
+        const double x = w * (double)(1ull << LIST_BITS), whole = any_weight ? floor(x) : x;
+        atomicAdd(reinterpret_cast<unsigned long long*>(&S.mass[c]), (unsigned long long)whole_of(whole));
+        if (any_weight)
+          atomicAdd(reinterpret_cast<unsigned long long*>(&rest[c]), (unsigned long long)whole_of(ceil((x - whole) * (double)(1ull << LIST_BITS))));
+      }
       above += here;
     }
     __syncthreads();
@@ -959,7 +968,7 @@ template <typename E, int PER> __global__ __launch_bounds__(THREADS) void oscar_
   // the chunk
   const double share = t >= P.chunks ? 0.0
                        : (lo == 0 ? 0.0 : chunk_upto(P, G, (int64_t)b * P.chunks, t, lo - 1)) +
-                             (double)S.mass[t] / (double)(1ull << LIST_BITS);
+                             ((double)S.mass[t] + (any_weight ? (double)rest[t] / (double)(1ull << LIST_BITS) : 0.0)) / (double)(1ull << LIST_BITS);
   double sum;
   const double upto = group_scan(share, S.wave_f, &sum);
   const double target = s.u * sum;

@@ -274,3 +274,17 @@ def test_a_number_of_1_and_more_draws_the_last_that_stays():
             for u in (1.0, 2.5, np.inf):
                 token, _ = ob.sample(torch.from_numpy(x).float().cuda(), torch.full((B,), u, device="cuda"), **args)
                 assert token.tolist() == want, (B, V, kw, u)
+
+
+@pytest.mark.parametrize("V", [5000, 70000])
+def test_tokens_of_hardly_any_weight(V):
+    """min_p lets tokens of e^-60 of the largest stay, which no sum of the row shows: a random number of 0 draws the first of them, a tiny one
+    the token it says."""
+    x = np.zeros((6, V))
+    x[:, :4096] = -np.inf
+    x[:, 10:110] = -60.0
+    x[4:, 10:110] = -69.0
+    x[5, 7] = -70.0                                             # (does not stay)
+    last = np.nextafter(np.float32(1), np.float32(0))
+    few = 8.756510762696521e-27 / (V - 4096)                    # e^-60 of the sum, nearly
+    check(x, m=1e-30, u=[0.0, 20.5 * few, 99.5 * few, 1e-20, 0.0, last])
