@@ -632,7 +632,8 @@ int oscar_q8_read(const oscar_q8_cache *cache, const int32_t *lens, const int32_
  *            stay), as oscar_verify_drafts takes it; overlaps nothing else
  *   workspace : at least oscar_sample_workspace_bytes(...), 16-byte aligned; its contents do not matter.  Calls
  *            that share one must be ordered
- * Weights and sums are in 64 bits; the same call gives the same bits every time.  batch <= 65535, vocab <=
+ * Weights are 64-bit floats, good to 2^-40 of themselves, and sums of them, running ones too, to 2^-36 of the row's sum;
+ * the same call gives the same bits every time.  batch <= 65535, vocab <=
  * OSCAR_SAMPLE_MAX_VOCAB.  Two launches, one or two more with filters and one more with probs. */
 #define OSCAR_SAMPLE_MAX_VOCAB (1 << 22)
 size_t oscar_sample_workspace_bytes(int32_t batch, int32_t vocab);
