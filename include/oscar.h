@@ -516,7 +516,8 @@ int oscar_verify_drafts(const void *target, const void *draft, const int32_t *dr
  *   positions, row_seq, slots : device int32 [n_rows] or NULL: every row's position in its sequence (for
  *                 oscar_rope), its sequence, and its place page * page_size + position % page_size in a
  *                 paged pool; -1 in rows behind the last sequence
- * The other outputs overlap nothing.  Works for any cache here (page_size 128).  batch <=
+ * The other outputs overlap nothing.  Made for the 8-bit cache below, whose calls take the lengths and rows as they come out
+ * (page_size 128).  A packed cache (oscar_cache) keeps its own lengths, gives no token back and takes no row_starts: not for it.  batch <=
  * OSCAR_PLAN_MAX_BATCH; num_pages * page_size and max_pages_per_seq * page_size below 2^31.  One launch, two for many rows. */
 #define OSCAR_PLAN_MAX_BATCH (1 << 20)
 int oscar_plan_step(const int32_t *lens, const int32_t *keep, const int32_t *want, int32_t batch,
