@@ -579,7 +579,8 @@ int oscar_q8_sizes(const oscar_q8_cache *cache, oscar_q8_pool_sizes *out);
  * give out of it as F16 is +-65504 there, never an infinity.
  *   k, v : device, rows of n_kv_heads vectors of 128 channels of io_dtype, k_stride (v_stride) elements apart;
  *          16-byte aligned, strides multiples of 8
- * Tokens whose page is no page, or behind the table's end, are not kept.  One launch. */
+ * Tokens whose page is no page, or behind the table's end, are not kept once their block is complete; until then they are
+ * in the window, which needs no page.  One launch. */
 int oscar_q8_append(const void *k, const void *v, int64_t k_stride, int64_t v_stride, int64_t n_rows, int32_t T,
                     const int32_t *row_starts, const int32_t *new_lens, const int32_t *lens,
                     const oscar_q8_cache *cache, void *stream);
@@ -592,8 +593,8 @@ int oscar_q8_append(const void *k, const void *v, int64_t k_stride, int64_t v_st
  *   softmax_scale <= 0 means 1 / sqrt(128); max_seq_len_hint: a bound on lens[], for the split count only
  *   num_splits  : (<= 512), 0 = oscar_q8_auto_splits; workspace: oscar_q8_workspace_bytes(...), 16-byte
  *         aligned, NULL where that is 0.  Calls that share one must be ordered
- * Rows that belong to no sequence are left as they were; a row that sees no token gets zeros; tokens in a page
- * that is no page are left out.  Queries are finite, scaled logits below 2^30 in size.  Keys and values enter as they are,
+ * Rows that belong to no sequence are left as they were; a row that sees no token gets zeros; tokens coded in a page
+ * that is no page are left out.  Queries are below 2^100 in size, scaled logits below 2^30.  Keys and values enter as they are,
  * queries too; probabilities are carried in two bf16 limbs (16 bits), sums and statistics are fp32.  The same call gives the same
  * bits every time.  One launch, two with several splits. */
 #define OSCAR_Q8_MAX_GROUP 64 /* n_q_heads / n_kv_heads */
@@ -610,7 +611,7 @@ int oscar_q8_attn(const void *q, int64_t q_stride, int64_t n_rows, int32_t n_q_h
  *   lens   : device int32 [batch];  starts: device int32 [batch] or NULL = 0; may be negative
  *   k, v   : device, [batch][T][n_kv_heads][128] of out_dtype (any of the three), 16-byte aligned; either may
  *            be NULL.  (Numbers of a BF16 cache beyond fp16's are infinities as F16.)
- * Rows of tokens that a sequence does not hold (before 0, from lens[b] on, in a page that is no page) are left
+ * Rows of tokens that a sequence does not hold (before 0, from lens[b] on, coded in a page that is no page) are left
  * as they were.  One launch. */
 int oscar_q8_read(const oscar_q8_cache *cache, const int32_t *lens, const int32_t *starts, int32_t T, void *k,
                   void *v, int32_t out_dtype, void *stream);
