@@ -625,7 +625,7 @@ extern "C" int32_t oscar_q8_auto_splits(const oscar_q8_cache* cache, int32_t n_q
   const int64_t rows = (int64_t)T * (n_q_heads / cache->n_kv_heads);
   const int block = rows_of(rows);
   const int64_t units = (int64_t)cache->batch * cache->n_kv_heads * ((rows + block - 1) / block);
-  const int64_t pages = (max_seq_len + OSCAR_R - 1) / OSCAR_R;
+  const int64_t pages = ((int64_t)max_seq_len + OSCAR_R - 1) / OSCAR_R;
   const int64_t cus = oscar_compute_units();
   // The one that takes least.  16 rows read: a page of a split takes 0.75 us, and more workgroups than compute units do not
   // read faster (8 sequences of 32K, 4 / 8 splits 82 / 86 us).  32 rows compute: a page takes 1.05 us, of each of two

@@ -121,6 +121,13 @@ def test_split_count():
         assert 1 <= s <= min(512, (n + 127) // 128)
 
 
+def test_split_count_of_the_longest_lengths():
+    """Bounds up to 2^31 - 1 count as many splits as bounds a page below."""
+    splits = lambda T, n: ob.lib().oscar_q8_auto_splits(C.byref(q8(batch=1, n_kv_heads=8)), 32, T, n)
+    for T in (1, 5, 40):
+        assert [splits(T, n) for n in (BIG, BIG - 126, BIG - 127)] == [splits(T, BIG - 255)] * 3 and splits(T, BIG) > 1
+
+
 def sample(x=P, stride=1000, batch=2, vocab=1000, dt=ob.F32, temp=None, k=None, p=None, m=None, u=P, tokens=P, probs=None,
            ws=P, wb=None):
     wb = ob.sample_workspace_bytes(batch, vocab) if wb is None else wb
