@@ -288,3 +288,23 @@ def test_tokens_of_hardly_any_weight(V):
     last = np.nextafter(np.float32(1), np.float32(0))
     few = 8.756510762696521e-27 / (V - 4096)                    # e^-60 of the sum, nearly
     check(x, m=1e-30, u=[0.0, 20.5 * few, 99.5 * few, 1e-20, 0.0, last])
+
+
+def test_lists_that_span_all_numbers():
+    """Hundreds of tokens about the largest fp32 numbers of both signs: the list's span is itself no number."""
+    rng = np.random.default_rng(41)
+    V = 3000
+    x = np.stack([rng.choice([-1.0, 1.0], size=V) * rng.uniform(1e38, 3.4e38, size=V), rng.uniform(-3.4e38, 3.4e38, size=V),
+                  np.where(rng.random(V) < 0.9, -3.4028234663852886e38, 3.4028234663852886e38)]).astype(np.float32).astype(np.float64)
+    x[0, 7], x[1, 9] = np.inf, -np.inf
+    for kw in (dict(k=1000), dict(k=300, p=0.5), dict(k=1024, temp=1e38), dict(k=700, temp=1e37, p=0.9), dict(k=2000, temp=np.inf), dict(temp=1e38, p=0.9)):
+        check(x, **kw)
+
+
+def test_a_count_past_the_bins_of_a_low_temperature():
+    """top_k whose last token lies further below the largest than the bins of a low temperature reach, over many tokens."""
+    rng = np.random.default_rng(42)
+    x = logits(rng, 4, 128003)
+    x[2:, 500] = x[2:].max() + 20.0
+    for kw in (dict(k=50, temp=0.05), dict(k=1000, temp=0.1), dict(k=50, temp=[0.1, 0.3, 0.1, 0.4], p=0.9), dict(k=[1000, 1024, 50, 1025], temp=0.2, p=0.999)):
+        check(x, **kw)
