@@ -591,7 +591,8 @@ int oscar_q8_append(const void *k, const void *v, int64_t k_stride, int64_t v_st
  *         aligned, the stride a multiple of 8; query head h reads kv head h / (n_q_heads / n_kv_heads)
  *   out : device, [n_rows][n_q_heads][128] of out_dtype (io_dtype or F32), 16-byte aligned
  *   softmax_scale <= 0 means 1 / sqrt(128); max_seq_len_hint: a bound on lens[], for the split count only
- *   num_splits  : (<= 512), 0 = oscar_q8_auto_splits; workspace: oscar_q8_workspace_bytes(...), 16-byte
+ *   num_splits  : (<= 512), 0 = oscar_q8_auto_splits, one count for all sequences, fewer for a larger T: long sequences
+ *         of single tokens beside pieces of prompts are better two calls, each with the others' new_lens 0; workspace: oscar_q8_workspace_bytes(...), 16-byte
  *         aligned, NULL where that is 0.  Calls that share one must be ordered
  * Rows that belong to no sequence are left as they were; a row that sees no token gets zeros; tokens coded in a page
  * that is no page are left out.  Queries are below 2^100 in size, scaled logits below 2^30.  Keys and values enter as they are,

@@ -907,7 +907,8 @@ def q8_attn(cache: Q8Cache, q, lens, new_lens=None, row_starts=None, max_new: in
     between rows; the tokens they belong to are in the cache (q8_append) and in lens.  Returns `out`, of q's shape and
     of its type or fp32; made here, rows that belong to no sequence are zeros, else they stay as they were.  Without
     a max_seq_len_hint splits are counted for sequences as long as the block table has room for (one split would
-    leave most of the GPU idle over a long cache; too many cost a launch and a few microseconds)."""
+    leave most of the GPU idle over a long cache; too many cost a launch and a few microseconds).  max_new is the step's own
+    bound; long sequences of single tokens beside pieces of prompts are better two calls, each with the others' new_lens 0."""
     import torch
     if stream is not None:
         with torch.cuda.stream(stream):
