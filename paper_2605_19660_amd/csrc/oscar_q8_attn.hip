@@ -5,7 +5,8 @@
 // in one pass over the cache, with a reference m that follows the largest logit.  A code is exact in bf16 and in
 // fp16, so keys are multiplied as they are with queries as they are, and a block's scale (a power of two) goes
 // onto its logits; value codes times their scale are exact in bf16.  Probabilities are rounded, to two bf16 limbs
-// (2^-17), each a matrix product of its own: with one, 2^-9 a token would add to the output's own rounding.
+// (2^-17), each a matrix product of its own: with one, 2^-9 a token would add to the output's own rounding.  With two, fp32 outputs over
+// 1000 tokens are 6 .. 12 parts in 10^7 off, 3 .. 6 with probabilities of 24 bits; of 4096 rounded to bf16 0 .. 4 differ by it.
 //
 // A workgroup takes 16 or 32 rows (row = new token * g + query head of the group) of one kv head and a range of
 // pages; of a page each of its four waves takes a step of 32 tokens.  S^T = K Q^T: a lane gets logits of tokens of

@@ -25,9 +25,9 @@
 // A row whose list does not fit (thousands of equal logits at the cut) or with a top_k past 1024 is searched by
 // one workgroup, which splits bins until they fit or hold one number.
 //
-// What bounds it: one row of 32000 with top_p takes 23 us, a chain of dependent steps in three launches (7.5, 6 and 9.5):
+// What bounds it: one row of 32000 with top_p takes 24 us, a chain of dependent steps in three launches (6.6, 7.1 and 9.6):
 // loads that wait for the launch before, scans over a workgroup, a sort.  64 rows of 128003 with mixed settings and
-// probabilities take 72 us, 20.8 bins, 7.8 to find, 9.5 list, 17 draw, 16.4 probabilities: the rows are read three times
+// probabilities take 71 us, 21.1 bins, 7.8 to find, 9.6 list, 15.7 draw, 16.8 probabilities: the rows are read three times
 // (8 us where nothing else is done, 5 TB/s; past the first time out of the caches), the bins are bound by vector instructions
 // (40 a logit, half of them its exponential), the draw by its longest list.
 #include "oscar_common.h"
